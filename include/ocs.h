@@ -423,6 +423,86 @@ ocs_status ocs_qconv(const void* X_codes, int a_signed, const float* a_scale, in
                      const float* bias, float* Y, int32_t* acc_out, const float* residual, int relu,
                      float* max_abs_out, void* ws, size_t ws_bytes, int* dev_status, void* stream);
 
+/* Element types of the calls below. */
+typedef enum {
+  OCS_F32 = 0,
+  OCS_F16 = 1,
+  OCS_BF16 = 2
+} ocs_dtype;
+
+/* ocs_quantize_rows -------------------------------------------------------------------------
+ * Linear quantization (Eq. 1, no clipping) with one grid per row: a row of activations is one token
+ * (grid chosen on that token alone), a row of split weights [O][C+S] is one output channel.
+ *     alpha_m = max_c |X[m][c]|, scales[m] = alpha_m / L, inv = L / alpha_m   (fp32, each rounded once)
+ *     codes[m][c] = clamp(rint(X[m][c] * inv), -L, L)      round-half-to-even; unsigned: [0, L_u]
+ *     codes[m][C+s] = codes[m][idx_map[C+s]], s < S        (the duplicated channels of a split layer)
+ * The duplicated channels of Eq. 3 are appended here, where the row is on chip anyway, so that the product
+ * below runs on C+S plain channels.  An all-zero row gives zero codes and scale 0.  A row whose alpha is
+ * below 2^-100 is multiplied by 2^64 first (exact), so that inv stays finite.
+ * X of type x_type [rows][C], row stride ldx >= C elements, aligned to its element; codes int8 (uint8 bit
+ * pattern when is_signed = 0) [rows][C+S], row stride ld_codes >= C+S bytes, bytes beyond C+S untouched;
+ * scales fp32 [rows]; idx_map int32 [C+S] as ocs_split writes it (NULL when S = 0).  bits in [2,8].
+ * rows = 0 is a no-op.  Limits: C + S < 2^30.  Device flags: NONFINITE (that row's outputs are
+ * unspecified), BAD_INDEX. */
+ocs_status ocs_quantize_rows(const void* X, ocs_dtype x_type, int64_t rows, int C, int64_t ldx, int S,
+                             const int32_t* idx_map, int bits, int is_signed, int8_t* codes, int64_t ld_codes,
+                             float* scales, int* dev_status, void* stream);
+
+/* ocs_qlinear_rows --------------------------------------------------------------------------
+ * The integer layer with a scale per token and per output channel:
+ *     acc[m][n] = sum_{k < K} A[m][k] * Wc[n][k]                                 (int32, exact)
+ *     Y[m][n]   = fmaf((float)acc[m][n], a_scales[m] * w_scales[n], bias[n])     (bias 0 if NULL)
+ * rounded once more to y_type.  A codes [M][K] (uint8 when a_signed = 0 else int8), row stride lda bytes;
+ * Wc int8 [N][K], row stride ldw bytes; both 16-byte aligned with strides that are multiples of 16;
+ * a_scales fp32 [M], w_scales fp32 [N], bias fp32 [N]; Y [M][N] of y_type, row stride ldy elements.
+ * M = 0 is a no-op.  Limits: K * 128 * (a_signed ? 128 : 255) must fit int32, M < 2^30.
+ * Device flag: TIMEOUT. */
+ocs_status ocs_qlinear_rows(const void* A_codes, int a_signed, const float* a_scales, int M, int K, int64_t lda,
+                            const int8_t* W_codes, const float* w_scales, int N, int64_t ldw, const float* bias,
+                            void* Y, ocs_dtype y_type, int64_t ldy, int* dev_status, void* stream);
+
+/* ocs_linear_rows ---------------------------------------------------------------------------
+ * ocs_quantize_rows on X followed by ocs_qlinear_rows on its codes (K = C + S), in one call: the codes and
+ * token scales live in the workspace and the product's launch overlaps the quantization.  Bit-identical to
+ * the two calls.  Workspace: ocs_linear_rows_workspace_bytes(M, C, S).  Arguments, limits and device flags
+ * of the two calls. */
+size_t ocs_linear_rows_workspace_bytes(int M, int C, int S);
+ocs_status ocs_linear_rows(const void* X, ocs_dtype x_type, int M, int C, int64_t ldx, int S, const int32_t* idx_map,
+                           int bits, int is_signed, const int8_t* W_codes, const float* w_scales, int N, int64_t ldw,
+                           const float* bias, void* Y, ocs_dtype y_type, int64_t ldy, void* ws, size_t ws_bytes,
+                           int* dev_status, void* stream);
+
+/* ocs_token_logprobs ------------------------------------------------------------------------
+ * What a language model's logits say about given tokens (Section 6 reports perplexity, the exponential of
+ * the mean of -logprob).  With z = inv_temperature * logits[t][:], p = softmax(z):
+ *     logprob[t] = ln p[targets[t]]                 entropy[t] = -sum_v p_v ln p_v
+ *     top_ids[t][0..top_k), top_logprob[t][0..top_k): the top_k largest logits, largest first, of equal
+ *     logits (-0 equals 0) the lowest index first, with their ln p.
+ * logits of `type` [rows][V], row stride ld >= V elements, aligned to its element; targets int32 [rows]
+ * (NULL: none; a negative entry: this row has no given token and logprob 0); top_k in [0, 64], at most V;
+ * logprob (with targets), entropy, top_ids int32 and top_logprob (with top_k > 0) and stats may each be
+ * NULL where they are not wanted.  stats fp32 [rows][4], kept for the gradient: max logit, ln of the sum of
+ * exp(z - max z), entropy, ln of the sum of exp(z).
+ * A logit of -infinity is a masked token: p = 0, no part in the entropy.  A row with nothing but
+ * -infinity has logprob and top_logprob -infinity, entropy 0.  A row with NaN or +infinity sets NONFINITE;
+ * its floats are NaN and its top_ids -1.  A target >= V sets BAD_INDEX and counts as none.
+ * Sums and statistics are fp32.  rows = 0 is a no-op.  inv_temperature > 0 and finite. */
+ocs_status ocs_token_logprobs(const void* logits, ocs_dtype type, int64_t rows, int V, int64_t ld,
+                              const int32_t* targets, float inv_temperature, int top_k, float* logprob, float* entropy,
+                              int32_t* top_ids, float* top_logprob, float* stats, int* dev_status, void* stream);
+
+/* ocs_token_logprobs_backward: the gradient of sum_t (g_logprob[t] * logprob[t] + g_entropy[t] * entropy[t])
+ * with respect to the logits (the alternatives carry none):
+ *     d[t][v] = inv_temperature * (g_logprob[t] * (1[v = targets[t]] - p_v) - g_entropy[t] * p_v * (ln p_v + entropy[t]))
+ * logits, targets and inv_temperature as in the forward call, stats from it; g_logprob, g_entropy fp32
+ * [rows], NULL counts as zero.  d_logits of the logits' type [rows][V], row stride ld_d; it may be the
+ * logits' own buffer (d_logits = logits and ld_d = ld).  A masked token (p = 0) takes part only as the given
+ * one; a row without any unmasked token gets zeros.  Device flag: BAD_INDEX. */
+ocs_status ocs_token_logprobs_backward(const void* logits, ocs_dtype type, int64_t rows, int V, int64_t ld,
+                                       const int32_t* targets, float inv_temperature, const float* stats,
+                                       const float* g_logprob, const float* g_entropy, void* d_logits, int64_t ld_d,
+                                       int* dev_status, void* stream);
+
 /* Steps between quantized layers ------------------------------------------------------------
  * The paper runs whole networks through the split and quantized layers (Section 5: ImageNet
  * CNNs; Section 6: a two-layer LSTM language model).  These calls are the float steps between

@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+from typing import NamedTuple
 
 import torch
 
@@ -34,8 +35,24 @@ EXPORTS = [
     "ocs_quantize_workspace_bytes", "ocs_quantize", "ocs_quantize_workspace_views", "ocs_quantize_noalloc",
     "ocs_qlinear_workspace_bytes", "ocs_qlinear", "ocs_transpose_codes", "ocs_selftest_force_gemm_plan",
     "ocs_conv_packed_k", "ocs_pack_conv_weights", "ocs_pack_conv_weights_batch", "ocs_qconv_workspace_bytes", "ocs_qconv",
+    "ocs_quantize_rows", "ocs_qlinear_rows", "ocs_linear_rows_workspace_bytes", "ocs_linear_rows",
+    "ocs_token_logprobs", "ocs_token_logprobs_backward",
     "ocs_add_relu", "ocs_maxpool3x3s2", "ocs_global_avgpool", "ocs_nchw_to_nhwc", "ocs_embedding", "ocs_lstm_cell",
 ]
+
+DTYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}   # ocs_dtype
+
+# Signatures of the calls a decoding loop makes once per layer and token: with them ctypes takes plain integers
+# and None, which costs the host a fraction of wrapping every argument.
+_P, _I, _L, _F = C.c_void_p, C.c_int, C.c_int64, C.c_float
+_ARGTYPES = {
+    "ocs_quantize_rows": [_P, _I, _L, _I, _L, _I, _P, _I, _I, _P, _L, _P, _P, _P],
+    "ocs_qlinear_rows": [_P, _I, _P, _I, _I, _L, _P, _P, _I, _L, _P, _P, _I, _L, _P, _P],
+    "ocs_linear_rows_workspace_bytes": [_I, _I, _I],
+    "ocs_linear_rows": [_P, _I, _I, _I, _L, _I, _P, _I, _I, _P, _P, _I, _L, _P, _P, _I, _L, _P, C.c_size_t, _P, _P],
+    "ocs_token_logprobs": [_P, _I, _L, _I, _L, _P, _F, _I, _P, _P, _P, _P, _P, _P, _P],
+    "ocs_token_logprobs_backward": [_P, _I, _L, _I, _L, _P, _F, _P, _P, _P, _P, _L, _P, _P],
+}
 
 _lib = None
 
@@ -61,6 +78,9 @@ def lib():
         L.ocs_quantize_workspace_views.restype = None
         L.ocs_kernel_launches.restype = C.c_longlong
         L.ocs_conv_packed_k.restype = C.c_int64
+        for name, types in _ARGTYPES.items():
+            getattr(L, name).argtypes = types
+        L.ocs_linear_rows_workspace_bytes.restype = C.c_size_t
         _lib = L
     return _lib
 
@@ -572,3 +592,165 @@ def ocs_pack_conv_weights_batch(jobs):
         outs.append(packed)
     _check(lib().ocs_pack_conv_weights_batch(descs, n, _stream()), "ocs_pack_conv_weights_batch")
     return outs
+
+
+# ------------------------------------------------------------------------- token and channel scales, logits
+def _addr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _raw_stream(t):
+    return torch._C._cuda_getCurrentRawStream(t.get_device())
+
+
+def _rows_of(t):
+    """Row stride of a 2-D tensor whose rows are contiguous and do not overlap.  A single row has no stride of its own:
+    it counts as padded to 16 elements, which no call reads or writes."""
+    assert t.dim() == 2
+    rows, cols = t.shape
+    if rows == 1:
+        assert cols <= 1 or t.stride(1) == 1
+        return (cols + 15) & ~15
+    ld = t.stride(0)
+    assert (cols <= 1 or t.stride(1) == 1) and (ld >= cols or rows == 0)
+    return max(ld, cols)
+
+
+def _check_idx(idx_map, Cn: int, S: int):
+    assert S >= 0
+    if S > 0:
+        assert idx_map is not None and idx_map.is_cuda and idx_map.dtype == torch.int32 and idx_map.is_contiguous()
+        assert idx_map.numel() >= Cn + S
+
+
+def _check_vec(t, n: int):
+    assert t is None or (t.is_cuda and t.dtype == torch.float32 and t.is_contiguous() and t.numel() >= n)
+
+
+def ocs_quantize_rows(x, bits: int = 8, is_signed: bool = True, idx_map=None, S: int = 0, ld_codes: int | None = None,
+                      dev_status=None, out=None):
+    """x fp32 / fp16 / bf16 [rows, C] (row stride = x.stride(0)) -> (codes int8 / uint8 [rows, ld_codes], scales fp32
+    [rows]): one grid per row, the S duplicated channels of idx_map appended at columns C..C+S-1.
+    `out` = (codes, scales)."""
+    assert x.is_cuda and x.dtype in DTYPES
+    ldx = _rows_of(x)
+    rows, Cn = x.shape
+    S = int(S)
+    _check_idx(idx_map, Cn, S)
+    if out is not None:
+        codes, scales = out
+        assert codes.is_cuda and codes.element_size() == 1 and codes.shape[0] == rows and codes.shape[1] >= Cn + S
+        _check_vec(scales, rows)
+    else:
+        codes = torch.empty((rows, round_up(Cn + S, 16) if ld_codes is None else ld_codes),
+                            dtype=torch.int8 if is_signed else torch.uint8, device=x.device)
+        scales = torch.empty(rows, dtype=torch.float32, device=x.device)
+    st = lib().ocs_quantize_rows(x.data_ptr(), DTYPES[x.dtype], rows, Cn, ldx, S, _addr(idx_map), int(bits),
+                                 1 if is_signed else 0, codes.data_ptr(), _rows_of(codes), scales.data_ptr(),
+                                 _addr(dev_status), _raw_stream(x))
+    _check(st, "ocs_quantize_rows")
+    return codes, scales
+
+
+def ocs_qlinear_rows(A_codes, a_scales, W_codes, w_scales, K: int | None = None, bias=None, out_dtype=torch.float32,
+                     out=None, dev_status=None):
+    """A_codes int8 / uint8 [M, lda >= K] with scales fp32 [M], W_codes int8 [N, ldw >= K] with scales fp32 [N]
+    -> Y [M, N] of out_dtype (fp32, fp16, bf16).  K: contraction length (default: the narrower of the two)."""
+    assert A_codes.is_cuda and A_codes.dtype in (torch.int8, torch.uint8) and W_codes.is_cuda and W_codes.dtype == torch.int8
+    M, N = A_codes.shape[0], W_codes.shape[0]
+    lda, ldw = _rows_of(A_codes), _rows_of(W_codes)
+    if K is None:
+        K = min(A_codes.shape[1], W_codes.shape[1])
+    assert 0 < K <= A_codes.shape[1] and K <= W_codes.shape[1]
+    assert a_scales is not None and w_scales is not None
+    _check_vec(a_scales, M), _check_vec(w_scales, N), _check_vec(bias, N)
+    if out is None:
+        out = torch.empty((M, N), dtype=out_dtype, device=A_codes.device)
+    assert out.is_cuda and out.dtype in DTYPES and out.shape == (M, N)
+    st = lib().ocs_qlinear_rows(A_codes.data_ptr(), 1 if A_codes.dtype == torch.int8 else 0, a_scales.data_ptr(), M, K, lda,
+                                W_codes.data_ptr(), w_scales.data_ptr(), N, ldw, _addr(bias), out.data_ptr(),
+                                DTYPES[out.dtype], _rows_of(out), _addr(dev_status), _raw_stream(A_codes))
+    _check(st, "ocs_qlinear_rows")
+    return out
+
+
+def ocs_linear_rows(x, W_codes, w_scales, idx_map=None, S: int = 0, bits: int = 8, is_signed: bool = True, bias=None,
+                    out_dtype=None, out=None, ws=None, dev_status=None):
+    """x fp32 / fp16 / bf16 [M, C], W_codes int8 [N, ldw >= C+S] with scales fp32 [N] -> Y [M, N] (of x's type, or
+    out_dtype): ocs_quantize_rows and ocs_qlinear_rows in one call."""
+    assert x.is_cuda and x.dtype in DTYPES and W_codes.is_cuda and W_codes.dtype == torch.int8
+    ldx, ldw = _rows_of(x), _rows_of(W_codes)
+    M, Cn = x.shape
+    N, S = W_codes.shape[0], int(S)
+    _check_idx(idx_map, Cn, S)
+    assert W_codes.shape[1] >= Cn + S and w_scales is not None
+    _check_vec(w_scales, N), _check_vec(bias, N)
+    if out is None:
+        out = torch.empty((M, N), dtype=x.dtype if out_dtype is None else out_dtype, device=x.device)
+    assert out.is_cuda and out.dtype in DTYPES and out.shape == (M, N)
+    L = lib()
+    if ws is None:
+        ws = torch.empty(L.ocs_linear_rows_workspace_bytes(M, Cn, S), dtype=torch.uint8, device=x.device)
+    st = L.ocs_linear_rows(x.data_ptr(), DTYPES[x.dtype], M, Cn, ldx, S, _addr(idx_map), int(bits), 1 if is_signed else 0,
+                           W_codes.data_ptr(), w_scales.data_ptr(), N, ldw, _addr(bias), out.data_ptr(), DTYPES[out.dtype],
+                           _rows_of(out), ws.data_ptr(), ws.numel(), _addr(dev_status), _raw_stream(x))
+    _check(st, "ocs_linear_rows")
+    return out
+
+
+class TokenLogprobs(NamedTuple):
+    """What ocs_token_logprobs returns; a part that was not asked for is None."""
+    logprob: torch.Tensor | None       # fp32 [rows]: ln p of the given tokens
+    entropy: torch.Tensor              # fp32 [rows]
+    top_ids: torch.Tensor | None       # int32 [rows, top_k], likeliest first
+    top_logprob: torch.Tensor | None   # fp32 [rows, top_k]
+    stats: torch.Tensor                # fp32 [rows, 4], for ocs_token_logprobs_backward
+
+
+def ocs_token_logprobs(logits, targets=None, top_k: int = 0, inv_temperature: float = 1.0, out: TokenLogprobs | None = None,
+                       dev_status=None) -> TokenLogprobs:
+    """logits fp32 / fp16 / bf16 [rows, V], targets int32 [rows] (negative: no given token) -> TokenLogprobs."""
+    assert logits.is_cuda and logits.dtype in DTYPES
+    ld = _rows_of(logits)
+    rows, V = logits.shape
+    assert targets is None or (targets.is_cuda and targets.dtype == torch.int32 and targets.is_contiguous()
+                               and targets.numel() >= rows)
+    k = int(top_k)
+    if out is None:
+        dev = logits.device
+        # one allocation for the floats: statistics first (16 bytes a row), then entropy, logprob, alternatives
+        buf = torch.empty(rows * (6 + max(k, 0)), dtype=torch.float32, device=dev)
+        out = TokenLogprobs(buf[5 * rows:6 * rows] if targets is not None else None, buf[4 * rows:5 * rows],
+                            torch.empty((rows, k), dtype=torch.int32, device=dev) if k > 0 else None,
+                            buf[6 * rows:].view(rows, k) if k > 0 else None, buf[:4 * rows].view(rows, 4))
+    else:
+        _check_vec(out.logprob, rows), _check_vec(out.entropy, rows), _check_vec(out.top_logprob, rows * k)
+        _check_vec(out.stats, 4 * rows)
+        assert out.top_ids is None or (out.top_ids.is_cuda and out.top_ids.dtype == torch.int32
+                                       and out.top_ids.is_contiguous() and out.top_ids.numel() >= rows * k)
+    st = lib().ocs_token_logprobs(logits.data_ptr(), DTYPES[logits.dtype], rows, V, ld, _addr(targets), inv_temperature, k,
+                                  _addr(out.logprob), _addr(out.entropy), _addr(out.top_ids), _addr(out.top_logprob),
+                                  _addr(out.stats), _addr(dev_status), _raw_stream(logits))
+    _check(st, "ocs_token_logprobs")
+    return out
+
+
+def ocs_token_logprobs_backward(logits, targets, stats, g_logprob=None, g_entropy=None, inv_temperature: float = 1.0,
+                                out=None, dev_status=None):
+    """Gradient of sum(g_logprob * logprob + g_entropy * entropy) with respect to the logits, in their type; stats from
+    ocs_token_logprobs with the same arguments.  `out` may be the logits themselves."""
+    assert logits.is_cuda and logits.dtype in DTYPES
+    ld = _rows_of(logits)
+    rows, V = logits.shape
+    assert targets is None or (targets.is_cuda and targets.dtype == torch.int32 and targets.is_contiguous()
+                               and targets.numel() >= rows)
+    assert stats is not None
+    _check_vec(stats, 4 * rows), _check_vec(g_logprob, rows), _check_vec(g_entropy, rows)
+    if out is None:
+        out = torch.empty((rows, V), dtype=logits.dtype, device=logits.device)
+    assert out.is_cuda and out.dtype == logits.dtype and out.shape == (rows, V)
+    st = lib().ocs_token_logprobs_backward(logits.data_ptr(), DTYPES[logits.dtype], rows, V, ld, _addr(targets),
+                                           inv_temperature, stats.data_ptr(), _addr(g_logprob), _addr(g_entropy),
+                                           out.data_ptr(), _rows_of(out), _addr(dev_status), _raw_stream(logits))
+    _check(st, "ocs_token_logprobs_backward")
+    return out

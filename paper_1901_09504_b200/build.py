@@ -9,7 +9,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 _ROOT = os.path.dirname(_HERE)
 CSRC = os.path.join(_HERE, "csrc")
 LIB = os.path.join(_HERE, "libocs_b200.so")
-SOURCES = ["split.cu", "actsel.cu", "quantize.cu", "gemm.cu", "glue.cu", "knapsack.cu", "api.cu"]
+SOURCES = ["split.cu", "actsel.cu", "quantize.cu", "gemm.cu", "glue.cu", "knapsack.cu", "rows.cu", "rowgemm.cu", "logprobs.cu", "api.cu"]
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
@@ -27,7 +27,7 @@ def needs_build() -> bool:
     if not os.path.exists(LIB):
         return True
     t = os.path.getmtime(LIB)
-    deps = _sources() + [os.path.join(CSRC, "common.cuh"), os.path.join(_ROOT, "include", "ocs.h"),
+    deps = _sources() + [os.path.join(CSRC, "common.cuh"), os.path.join(CSRC, "elem.cuh"), os.path.join(_ROOT, "include", "ocs.h"),
                          os.path.abspath(__file__)]
     return any(os.path.getmtime(d) > t for d in deps if os.path.exists(d))
 
