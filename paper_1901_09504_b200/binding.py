@@ -35,7 +35,7 @@ EXPORTS = [
     "ocs_quantize_workspace_bytes", "ocs_quantize", "ocs_quantize_workspace_views", "ocs_quantize_noalloc",
     "ocs_qlinear_workspace_bytes", "ocs_qlinear", "ocs_transpose_codes", "ocs_selftest_force_gemm_plan",
     "ocs_conv_packed_k", "ocs_pack_conv_weights", "ocs_pack_conv_weights_batch", "ocs_qconv_workspace_bytes", "ocs_qconv",
-    "ocs_quantize_rows", "ocs_qlinear_rows", "ocs_linear_rows_workspace_bytes", "ocs_linear_rows",
+    "ocs_quantize_rows", "ocs_qlinear_rows", "ocs_linear_rows_workspace_bytes", "ocs_linear_rows", "ocs_selftest_force_row_plan",
     "ocs_token_logprobs", "ocs_token_logprobs_backward",
     "ocs_add_relu", "ocs_maxpool3x3s2", "ocs_global_avgpool", "ocs_nchw_to_nhwc", "ocs_embedding", "ocs_lstm_cell",
 ]
@@ -696,6 +696,12 @@ def ocs_linear_rows(x, W_codes, w_scales, idx_map=None, S: int = 0, bits: int = 
                            _rows_of(out), ws.data_ptr(), ws.numel(), _addr(dev_status), _raw_stream(x))
     _check(st, "ocs_linear_rows")
     return out
+
+
+def ocs_selftest_force_row_plan(tn: int = 0, cg: int = 1, slices: int = 1):
+    """Fixes tokens per tile / CTAs per tile / K split of the following ocs_qlinear_rows / ocs_linear_rows calls (tn = 0:
+    planner)."""
+    _check(lib().ocs_selftest_force_row_plan(int(tn), int(cg), int(slices)), "ocs_selftest_force_row_plan")
 
 
 class TokenLogprobs(NamedTuple):

@@ -27,7 +27,7 @@ def needs_build() -> bool:
     if not os.path.exists(LIB):
         return True
     t = os.path.getmtime(LIB)
-    deps = _sources() + [os.path.join(CSRC, "common.cuh"), os.path.join(CSRC, "elem.cuh"), os.path.join(_ROOT, "include", "ocs.h"),
+    deps = _sources() + [os.path.join(CSRC, "common.cuh"), os.path.join(CSRC, "elem.cuh"), os.path.join(CSRC, "ptx.cuh"), os.path.join(_ROOT, "include", "ocs.h"),
                          os.path.abspath(__file__)]
     return any(os.path.getmtime(d) > t for d in deps if os.path.exists(d))
 

@@ -1,14 +1,411 @@
 // ocs_qlinear_rows / ocs_linear_rows: the int8 layer with a scale per token and per output channel.
+#include <atomic>
+
 #include "elem.cuh"
+#include "ptx.cuh"
 
 namespace ocs {
 namespace {
 
-constexpr int kTile = 64;       // tokens and channels of one CTA's tile
-constexpr int kStep = 64;       // contraction bytes staged at a time
+constexpr int TW = 128;        // channels (weight rows) of one CTA's tile: the lanes of tensor memory
+constexpr int KB = 128;        // contraction bytes of a K-block: one 128-byte swizzle span
+constexpr int UK = 32;         // contraction indices of one tcgen05.mma.kind::i8
+constexpr int kThreads = 320;  // copy warp, tensor-core warp, 8 epilogue warps
+constexpr int kEpiWarps = 8;
 
 struct RowGemm {
-  const uint8_t* A;
+  int M, N, num_kb, t_signed;
+  int n_tiles, m_tiles, total;   // channel tiles (TW * CG), token tiles (TN)
+  int slices;                    // CTAs (pairs) that share a tile and split its K-blocks
+  const float* a_scales;
+  const float* w_scales;
+  const float* bias;
+  long long ldy;
+  int* dev_status;
+};
+
+// TN tokens, CG CTAs per tensor-core tile
+template <int TN, int CG>
+struct RowSmem {
+  static constexpr int kTokens = TN / CG;                       // token rows this CTA stages
+  static constexpr int kWBytes = TW * KB, kTBytes = kTokens * KB;
+  static constexpr int kStageBytes = kWBytes + kTBytes;
+  static constexpr int kXBytes = TN == 256 ? 0 : TN * TW * 4;   // partial sums of this CTA's share (K split)
+  static constexpr int kWarpTokens = TN < 32 ? 16 : TN / 2;      // columns an epilogue warp finishes
+  static constexpr int kScaleBytes = kEpiWarps * kWarpTokens * 4;
+  static constexpr int kCtrlBytes = 512;
+  static constexpr int kBudget = 227 * 1024 - 1024 - kCtrlBytes - kScaleBytes;
+  static constexpr int kStagesFit = (kBudget - kXBytes) / kStageBytes;
+  static constexpr int kStages = kStagesFit < 12 ? kStagesFit : 12;
+  static constexpr int kDynBytes = 1024 + kStages * kStageBytes + kXBytes + kScaleBytes + kCtrlBytes;
+  static constexpr int kAccStride = TN < 32 ? 32 : TN;
+  static constexpr uint32_t kTmemCols = 2 * kAccStride;
+  static_assert(kStages >= 3 && kDynBytes <= 227 * 1024 && kTBytes % 1024 == 0, "tile does not fit");
+};
+
+__host__ __device__ constexpr uint32_t row_instr_desc(int m, int n, int b_signed) {
+  return (2u << 4)                               // accumulator S32
+         | (1u << 7)                             // A (weights): int8
+         | ((uint32_t)(b_signed ? 1 : 0) << 10)  // B (tokens): uint8 / int8
+         | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
+}
+
+// Tile t of the launch: token tiles in groups of eight, all channel tiles of a group before the next group, so that
+// the tiles in flight at one time share their operand panels in L2.
+__device__ __forceinline__ void tile_of(const RowGemm& p, int t, int* mt, int* nt) {
+  const int per_group = 8 * p.n_tiles;
+  const int g = t / per_group, in = t - g * per_group;
+  const int rows = min(8, p.m_tiles - 8 * g);
+  *nt = in / rows;
+  *mt = 8 * g + in - *nt * rows;
+}
+
+template <typename T> struct Pair;
+template <> struct Pair<__half> { static __device__ __forceinline__ uint32_t pack(float a, float b) { __half2 h = __floats2half2_rn(a, b); return *reinterpret_cast<uint32_t*>(&h); } };
+template <> struct Pair<__nv_bfloat16> { static __device__ __forceinline__ uint32_t pack(float a, float b) { __nv_bfloat162 h = __floats2bfloat162_rn(a, b); return *reinterpret_cast<uint32_t*>(&h); } };
+
+// CNT consecutive tokens of channel n: float(acc) * (a_scale * w_scale) + bias, rounded to T and stored.  The lanes of
+// the warp hold consecutive channels.
+template <typename T, int CNT>
+__device__ __forceinline__ void finish(const RowGemm& p, T* __restrict__ Y, const int* acc, const float* sc, int m0, int n,
+                                       float ws, float b, bool pairs) {
+  T* y = Y + (long long)m0 * p.ldy + n;
+  if (sizeof(T) == 2 && pairs) {
+    // neighbouring lanes swap halves, so that a lane stores two channels of one token in 32 bits
+    const int lane = threadIdx.x & 31, odd = lane & 1;
+#pragma unroll
+    for (int j = 0; j < CNT; j += 2) {
+      const float f0 = fmaf(__int2float_rn(acc[j]), __fmul_rn(sc[j], ws), b);
+      const float f1 = fmaf(__int2float_rn(acc[j + 1]), __fmul_rn(sc[j + 1], ws), b);
+      if constexpr (sizeof(T) == 2) {
+        const uint32_t mine = Pair<T>::pack(f0, f1);
+        const uint32_t other = __shfl_xor_sync(0xffffffffu, mine, 1);
+        const uint32_t out = odd ? __byte_perm(other, mine, 0x7632) : __byte_perm(mine, other, 0x5410);
+        // even lane: token j, channels n, n+1; odd lane: token j+1, channels n-1, n
+        if (m0 + j + odd < p.M && n - odd < p.N) *reinterpret_cast<uint32_t*>(y + (long long)(j + odd) * p.ldy - odd) = out;
+      }
+    }
+  } else if (n < p.N) {
+#pragma unroll
+    for (int j = 0; j < CNT; ++j) {
+      if (m0 + j < p.M)
+        y[(long long)j * p.ldy] = from_f32<T>(fmaf(__int2float_rn(acc[j]), __fmul_rn(sc[j], ws), b));
+    }
+  }
+}
+
+template <typename T, int TN, int CG>
+__global__ void __launch_bounds__(kThreads, 1)
+row_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtensorMap tm_t, const RowGemm p,
+                T* __restrict__ Y) {
+  using L = RowSmem<TN, CG>;
+  extern __shared__ unsigned char smem_dyn[];
+  const uint32_t raw = smem_u32(smem_dyn);
+  const uint32_t base = (raw + 1023u) & ~1023u;
+  unsigned char* tiles = smem_dyn + (base - raw);
+  unsigned char* xbuf = tiles + L::kStages * L::kStageBytes;
+  float* scale_buf = reinterpret_cast<float*>(xbuf + L::kXBytes);
+  uint64_t* bars = reinterpret_cast<uint64_t*>(xbuf + L::kXBytes + L::kScaleBytes);
+  auto full_bar = [&](int s) { return smem_u32(bars + s); };
+  auto empty_bar = [&](int s) { return smem_u32(bars + L::kStages + s); };
+  auto accfull_bar = [&](int a) { return smem_u32(bars + 2 * L::kStages + a); };
+  auto accempty_bar = [&](int a) { return smem_u32(bars + 2 * L::kStages + 2 + a); };
+  const uint32_t xfull_bar = smem_u32(bars + 2 * L::kStages + 4);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * L::kStages + 5);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  static_assert((2 * L::kStages + 5) * 8 + 8 <= L::kCtrlBytes, "control block");
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int CL = CG * p.slices;
+  const int rank = CL > 1 ? (int)cluster_rank() : 0;
+  const int half = rank % CG, slice = rank / CG;
+  const int cluster = blockIdx.x / CL, n_clusters = gridDim.x / CL;
+  const int my_kb = (p.num_kb - slice + p.slices - 1) / p.slices;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < L::kStages; ++s) {
+      mbar_init(full_bar(s), 1);     // the leader's producer announces the bytes of both CTAs
+      mbar_init(empty_bar(s), 1);    // commit of the MMAs that read the stage
+    }
+    for (int a = 0; a < 2; ++a) {
+      mbar_init(accfull_bar(a), 1);
+      mbar_init(accempty_bar(a), CG * kEpiWarps);
+    }
+    mbar_init(xfull_bar, 1);
+    *abort_flag = 0;
+    fence_barrier_init();
+    if (L::kXBytes && p.slices > 1) mbar_arrive_expect_tx(xfull_bar, (uint32_t)L::kXBytes);
+    prefetch_tmap(&tm_w);
+    prefetch_tmap(&tm_t);
+  }
+  if (warp == 1) {
+    if (CG == 2) tmem_alloc_pair(smem_u32(tmem_slot), L::kTmemCols);
+    else tmem_alloc(smem_u32(tmem_slot), L::kTmemCols);
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (CL > 1) cluster_sync_all();   // no peer touches our barriers before they are set up
+  tc_fence_after();
+  const uint32_t tmem_base = *tmem_slot;
+
+  if (warp == 0) {
+    // ---------------------------------------------------------------- copies
+    if (lane == 0) {
+      const uint32_t lead = CG == 2 ? (uint32_t)(rank & ~1) : 0;
+      int it = 0;
+      bool ok = true;
+      // weights do not depend on the kernel before: the first ring of them is requested before waiting for it
+      int ahead = 0;
+      int mt, nt;
+      auto load_w = [&](int s, int kb) {
+        if (CG == 2) tma_load_2d_pair(base + s * L::kStageBytes, &tm_w, peer_addr(full_bar(s), lead), kb * KB, (nt * CG + half) * TW);
+        else tma_load_2d(base + s * L::kStageBytes, &tm_w, full_bar(s), kb * KB, nt * TW);
+      };
+      auto load_t = [&](int s, int kb) {
+        const uint32_t dst = base + s * L::kStageBytes + L::kWBytes;
+        if (CG == 2) tma_load_2d_pair(dst, &tm_t, peer_addr(full_bar(s), lead), kb * KB, mt * TN + half * L::kTokens);
+        else tma_load_2d(dst, &tm_t, full_bar(s), kb * KB, mt * TN);
+      };
+      if (cluster < p.total) {
+        tile_of(p, cluster, &mt, &nt);
+        ahead = min(L::kStages, my_kb);
+        for (int i = 0; i < ahead; ++i) {
+          if (half == 0) mbar_arrive_expect_tx(full_bar(i), CG * L::kStageBytes);
+          load_w(i, slice + i * p.slices);
+        }
+      }
+      grid_wait_previous();
+      for (int t = cluster; ok && t < p.total; t += n_clusters) {
+        tile_of(p, t, &mt, &nt);
+        for (int i = 0; i < my_kb; ++i, ++it) {
+          const int s = it % L::kStages;
+          if (it >= ahead) {
+            if (!mbar_wait(empty_bar(s), (uint32_t)((it / L::kStages) & 1) ^ 1u, abort_flag)) { ok = false; break; }
+            if (half == 0) mbar_arrive_expect_tx(full_bar(s), CG * L::kStageBytes);
+            load_w(s, slice + i * p.slices);
+          }
+          load_t(s, slice + i * p.slices);
+        }
+      }
+      // every commit has arrived (also those the other CTA of a pair sends here) before the CTA may leave
+      for (int i = 0; ok && i < L::kStages; ++i, ++it)
+        ok = mbar_wait(empty_bar(it % L::kStages), (uint32_t)((it / L::kStages) & 1) ^ 1u, abort_flag);
+      if (*abort_flag)   // copies that are still in flight land before the CTA's shared memory is released
+        for (int i = 0; i < 2000; ++i) __nanosleep(100);
+    }
+  } else if (warp == 1) {
+    // ---------------------------------------------------------------- tensor cores
+    if (lane == 0 && half == 0) {
+      constexpr uint32_t kDescM = TW * CG;
+      const uint32_t idesc = row_instr_desc(kDescM, TN, p.t_signed);
+      const uint16_t mask = (uint16_t)(3u << (rank & ~1));
+      int it = 0, j = 0;
+      bool ok = true;
+      for (int t = cluster; ok && t < p.total; t += n_clusters, ++j) {
+        const int acc = j & 1;
+        if (!mbar_wait_cluster(accempty_bar(acc), (((uint32_t)j >> 1) & 1u) ^ 1u, abort_flag)) break;
+        tc_fence_after();
+        const uint32_t d = tmem_base + (uint32_t)(acc * L::kAccStride);
+        for (int i = 0; i < my_kb; ++i, ++it) {
+          const int s = it % L::kStages;
+          if (!mbar_wait(full_bar(s), (uint32_t)(it / L::kStages) & 1u, abort_flag)) { ok = false; break; }
+          tc_fence_after();
+          const uint32_t w = base + s * L::kStageBytes, x = w + L::kWBytes;
+#pragma unroll
+          for (int k = 0; k < KB / UK; ++k) {
+            const uint32_t more = (i > 0 || k > 0) ? 1u : 0u;
+            if (CG == 2) umma_i8_pair(d, smem_desc_sw128(w + k * UK), smem_desc_sw128(x + k * UK), idesc, more);
+            else umma_i8(d, smem_desc_sw128(w + k * UK), smem_desc_sw128(x + k * UK), idesc, more);
+          }
+          if (CG == 2) umma_commit_pair(empty_bar(s), mask);
+          else umma_commit(empty_bar(s));
+        }
+        if (!ok) break;
+        if (CG == 2) umma_commit_pair(accfull_bar(acc), mask);
+        else umma_commit(accfull_bar(acc));
+      }
+    }
+  } else {
+    // ---------------------------------------------------------------- epilogue
+    constexpr int EC = TN >= 64 ? 32 : 16;              // accumulator columns (tokens) moved at a time
+    const int ew = warp - 2, q = warp & 3, part = ew >> 2;   // lanes 32q.. of tensor memory; two warps share a quadrant
+    float* sc = scale_buf + ew * L::kWarpTokens;
+    const bool pairs = sizeof(T) == 2 && (p.ldy % 2 == 0) && (p.N % 2 == 0) && (reinterpret_cast<uintptr_t>(Y) & 3) == 0;
+    grid_wait_previous();
+    int j = 0;
+    for (int t = cluster; t < p.total; t += n_clusters, ++j) {
+      int mt, nt;
+      tile_of(p, t, &mt, &nt);
+      const int acc = j & 1;
+      const int n = (nt * CG + half) * TW + q * 32 + lane;
+      const float ws = n < p.N ? __ldg(p.w_scales + n) : 0.0f;
+      const float b = p.bias && n < p.N ? __ldg(p.bias + n) : 0.0f;
+      if (p.slices > 1) {
+        // K split: owner o of the tile's slices finishes tokens [o * own, (o + 1) * own).  Every CTA sends the columns
+        // another one owns into that one's buffer, cells of 16 bytes [sender][four tokens][channel], counted as
+        // transaction bytes on the owner's barrier.
+        if constexpr (L::kXBytes > 0) {
+          const int own = TN / p.slices, groups = own / 4;
+          if (!mbar_wait(accfull_bar(acc), ((uint32_t)j >> 1) & 1u, abort_flag)) break;
+          tc_fence_after();
+          for (int c = part * 16; c < TN; c += 32) {
+            uint32_t v[16];
+            __syncwarp();
+            tmem_ld16(tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(acc * L::kAccStride + c), v);
+#pragma unroll
+            for (int e = 0; e < 16; e += 4) {
+              const int owner = (c + e) / own, g = ((c + e) - owner * own) / 4;
+              const uint32_t cell = smem_u32(xbuf) + (uint32_t)((slice * groups + g) * TW + q * 32 + lane) * 16u;
+              const uint32_t peer = (uint32_t)(owner * CG + half);
+              st_async_v4(peer_addr(cell, peer), make_uint4(v[e], v[e + 1], v[e + 2], v[e + 3]), peer_addr(xfull_bar, peer));
+            }
+          }
+          if (!mbar_wait_cluster(xfull_bar, 0u, abort_flag)) break;
+          for (int g = part; g < groups; g += 2) {
+            const unsigned char* cell = xbuf + (size_t)(g * TW + q * 32 + lane) * 16;
+            int4 a = *reinterpret_cast<const int4*>(cell);
+            for (int sl = 1; sl < p.slices; ++sl) {
+              const int4 v = *reinterpret_cast<const int4*>(cell + (size_t)sl * groups * TW * 16);
+              a.x += v.x; a.y += v.y; a.z += v.z; a.w += v.w;
+            }
+            const int m0 = mt * TN + slice * own + g * 4;
+            const int av[4] = {a.x, a.y, a.z, a.w};
+            float s4[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s4[e] = m0 + e < p.M ? __ldcg(p.a_scales + m0 + e) : 0.0f;
+            finish<T, 4>(p, Y, av, s4, m0, n, ws, b, pairs);
+          }
+        }
+        break;   // a K split is used only where every cluster has one tile
+      }
+      // the token scales of this warp's columns: fetched while the main loop runs
+      __syncwarp();
+      for (int i = lane; i < L::kWarpTokens; i += 32) {
+        const int m = mt * TN + (i / EC) * 2 * EC + part * EC + i % EC;
+        sc[i] = m < p.M ? __ldcg(p.a_scales + m) : 0.0f;
+      }
+      __syncwarp();
+      if (!mbar_wait(accfull_bar(acc), ((uint32_t)j >> 1) & 1u, abort_flag)) break;
+      tc_fence_after();
+      for (int c = part * EC, i = 0; c < TN; c += 2 * EC, ++i) {
+        const int m0 = mt * TN + c;
+        if (m0 >= p.M) break;   // warp-uniform
+        uint32_t v[EC];
+        __syncwarp();
+        const uint32_t addr = tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(acc * L::kAccStride + c);
+        if constexpr (EC == 32) tmem_ld32(addr, v);
+        else tmem_ld16(addr, v);
+        float s[EC];
+#pragma unroll
+        for (int e = 0; e < EC; e += 4) {
+          const float4 f = *reinterpret_cast<const float4*>(sc + i * EC + e);
+          s[e] = f.x; s[e + 1] = f.y; s[e + 2] = f.z; s[e + 3] = f.w;
+        }
+        finish<T, EC>(p, Y, reinterpret_cast<const int*>(v), s, m0, n, ws, b, pairs);
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) {
+        if (CG == 2) mbar_arrive_peer(peer_addr(accempty_bar(acc), (uint32_t)(rank & ~1)));
+        else mbar_arrive(accempty_bar(acc));
+      }
+    }
+    tc_fence_before();
+  }
+
+  __syncthreads();
+  if (CL > 1) cluster_sync_all();   // no CTA leaves while a peer may still store into it or arrive on its barriers
+  if (warp == 1) {
+    __syncwarp();
+    tc_fence_after();
+    if (CG == 2) tmem_dealloc_pair(tmem_base, L::kTmemCols);
+    else tmem_dealloc(tmem_base, L::kTmemCols);
+  }
+  if (threadIdx.x == 0 && *abort_flag) flag(p.dev_status, OCS_DEV_TIMEOUT);
+}
+
+// ------------------------------------------------------------------------------------------------ host
+struct RowPlan {
+  int tn, cg, slices;
+};
+
+// Test hook (ocs_selftest_force_row_plan): the plan of the following calls where it is valid for the problem.
+std::atomic<int> g_force_tn{0}, g_force_cg{0}, g_force_slices{0};
+
+// CTAs resident at once, one per SM, for cluster sizes 1, 2, 4, 8 (a cluster lies inside one GPC)
+int cluster_capacity(int cl) { return cl <= 2 ? 148 : (cl == 4 ? 132 : 120); }
+
+bool split_fits(int tn, int cg, int slices, long long tiles, int num_kb) {
+  if (slices == 1) return true;
+  return cg * slices <= 8 && tn / slices >= 4 && tn < 256 && slices <= num_kb &&
+         tiles * cg * slices <= cluster_capacity(cg * slices);
+}
+
+RowPlan choose_plan(int M, int N, int num_kb) {
+  auto tiles = [&](int tn, int cg) { return (long long)((M + tn - 1) / tn) * ((N + TW * cg - 1) / (TW * cg)); };
+  const int ft = g_force_tn.load(), fc = g_force_cg.load(), fs = g_force_slices.load();
+  if (ft) {
+    RowPlan r{ft, ft >= 128 ? fc : 1, fs};
+    while (r.slices > 1 && !split_fits(r.tn, r.cg, r.slices, tiles(r.tn, r.cg), num_kb)) r.slices /= 2;
+    return r;
+  }
+  RowPlan r{M <= 16 ? 16 : M <= 32 ? 32 : M <= 64 ? 64 : M <= 128 ? 128 : 256, 1, 1};
+  if (r.tn == 256 && tiles(256, 2) >= 60) r.cg = 2;
+  for (int s = 2; s <= 8; s *= 2)
+    if (split_fits(r.tn, r.cg, s, tiles(r.tn, r.cg), num_kb) && num_kb >= 4 * s) r.slices = s;
+  return r;
+}
+
+template <typename T, int TN, int CG>
+ocs_status launch_tiles(RowGemm p, int slices, const void* A, long long lda, const int8_t* W, long long ldw, int K, T* Y,
+                        bool overlap, cudaStream_t stream) {
+  using L = RowSmem<TN, CG>;
+  static std::atomic<unsigned long long> ready{0};   // devices whose copy of the kernel has its attribute set
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return OCS_ERR_CUDA;
+  if (dev >= 64 || !(ready.load() >> dev & 1)) {
+    if (cudaFuncSetAttribute(row_gemm_kernel<T, TN, CG>, cudaFuncAttributeMaxDynamicSharedMemorySize, L::kDynBytes) != cudaSuccess)
+      return OCS_ERR_CUDA;
+    if (dev < 64) ready.fetch_or(1ull << dev);
+  }
+  p.n_tiles = (p.N + TW * CG - 1) / (TW * CG);
+  p.m_tiles = (p.M + TN - 1) / TN;
+  const long long total = (long long)p.n_tiles * p.m_tiles;
+  if (total > 0x3fffffff) return OCS_ERR_UNSUPPORTED;
+  p.total = (int)total;
+  p.slices = slices;
+  CUtensorMap tm_w, tm_t;
+  const cuuint64_t wd[2] = {(cuuint64_t)K, (cuuint64_t)p.N}, ws[1] = {(cuuint64_t)ldw};
+  const cuuint64_t td[2] = {(cuuint64_t)K, (cuuint64_t)p.M}, ts[1] = {(cuuint64_t)lda};
+  const cuuint32_t wb[2] = {KB, TW}, tb[2] = {KB, (cuuint32_t)L::kTokens};
+  if (!encode_u8(&tm_w, W, 2, wd, ws, wb) || !encode_u8(&tm_t, A, 2, td, ts, tb)) return OCS_ERR_CUDA;
+  const int cl = CG * slices;
+  const long long slots = cluster_capacity(cl) / cl;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)((total < slots ? total : slots) * cl), 1, 1);
+  cfg.blockDim = dim3(kThreads, 1, 1);
+  cfg.dynamicSmemBytes = L::kDynBytes;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[2];
+  int n_attr = 0;
+  if (cl > 1) {
+    attr[n_attr].id = cudaLaunchAttributeClusterDimension;
+    attr[n_attr].val.clusterDim.x = cl; attr[n_attr].val.clusterDim.y = 1; attr[n_attr].val.clusterDim.z = 1;
+    ++n_attr;
+  }
+  if (overlap) {
+    attr[n_attr].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[n_attr].val.programmaticStreamSerializationAllowed = 1;
+    ++n_attr;
+  }
+  cfg.attrs = attr; cfg.numAttrs = n_attr;
+  LaunchScope scope("row_gemm_kernel", stream);
+  if (cudaLaunchKernelEx(&cfg, row_gemm_kernel<T, TN, CG>, tm_w, tm_t, p, Y) != cudaSuccess) return OCS_ERR_CUDA;
+  return launch_status();
+}
+
+struct Product {
+  const void* A;
   const float* a_scales;
   const int8_t* W;
   const float* w_scales;
@@ -18,39 +415,29 @@ struct RowGemm {
   int* dev_status;
 };
 
-// 64 x 64 tile, 256 threads of 4 x 4 outputs, operands staged in shared memory, four products per instruction.
 template <typename T>
-__global__ void __launch_bounds__(256) row_gemm_kernel(const RowGemm p, T* __restrict__ Y) {
-  __shared__ uint32_t sa[kTile][kStep / 4 + 1], sw[kTile][kStep / 4 + 1];
-  const int m0 = blockIdx.y * kTile, n0 = blockIdx.x * kTile;
-  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  int acc[4][4] = {};
-  for (int k0 = 0; k0 < p.K; k0 += kStep) {
-    for (int i = threadIdx.x; i < kTile * kStep; i += 256) {
-      const int r = i / kStep, k = i - r * kStep;
-      const bool in = k0 + k < p.K;
-      reinterpret_cast<uint8_t*>(&sa[r][0])[k] = in && m0 + r < p.M ? p.A[(long long)(m0 + r) * p.lda + k0 + k] : 0;
-      reinterpret_cast<int8_t*>(&sw[r][0])[k] = in && n0 + r < p.N ? p.W[(long long)(n0 + r) * p.ldw + k0 + k] : 0;
-    }
-    __syncthreads();
-    for (int k = 0; k < kStep / 4; ++k)
-      for (int i = 0; i < 4; ++i)
-        for (int j = 0; j < 4; ++j) {
-          const int a = (int)sa[ty + 16 * i][k], w = (int)sw[tx + 16 * j][k];
-          if (p.a_signed) acc[i][j] = __dp4a(a, w, acc[i][j]);
-          else asm("dp4a.u32.s32 %0, %1, %2, %0;" : "+r"(acc[i][j]) : "r"(a), "r"(w));
-        }
-    __syncthreads();
+ocs_status launch_product(const Product& g, void* Y_, bool overlap, cudaStream_t stream) {
+  RowGemm p{};
+  p.M = g.M; p.N = g.N; p.num_kb = (g.K + KB - 1) / KB; p.t_signed = g.a_signed;
+  p.a_scales = g.a_scales; p.w_scales = g.w_scales; p.bias = g.bias; p.ldy = g.ldy; p.dev_status = g.dev_status;
+  const RowPlan plan = choose_plan(g.M, g.N, p.num_kb);
+  T* Y = static_cast<T*>(Y_);
+  switch (plan.tn * 2 + plan.cg - 1) {
+    case 32: return launch_tiles<T, 16, 1>(p, plan.slices, g.A, g.lda, g.W, g.ldw, g.K, Y, overlap, stream);
+    case 64: return launch_tiles<T, 32, 1>(p, plan.slices, g.A, g.lda, g.W, g.ldw, g.K, Y, overlap, stream);
+    case 128: return launch_tiles<T, 64, 1>(p, plan.slices, g.A, g.lda, g.W, g.ldw, g.K, Y, overlap, stream);
+    case 256: return launch_tiles<T, 128, 1>(p, plan.slices, g.A, g.lda, g.W, g.ldw, g.K, Y, overlap, stream);
+    case 257: return launch_tiles<T, 128, 2>(p, plan.slices, g.A, g.lda, g.W, g.ldw, g.K, Y, overlap, stream);
+    case 512: return launch_tiles<T, 256, 1>(p, plan.slices, g.A, g.lda, g.W, g.ldw, g.K, Y, overlap, stream);
+    default: return launch_tiles<T, 256, 2>(p, plan.slices, g.A, g.lda, g.W, g.ldw, g.K, Y, overlap, stream);
   }
-  for (int i = 0; i < 4; ++i) {
-    const int m = m0 + ty + 16 * i;
-    if (m >= p.M) continue;
-    for (int j = 0; j < 4; ++j) {
-      const int n = n0 + tx + 16 * j;
-      if (n >= p.N) continue;
-      const float sc = __fmul_rn(p.a_scales[m], p.w_scales[n]);
-      Y[(long long)m * p.ldy + n] = from_f32<T>(fmaf(__int2float_rn(acc[i][j]), sc, p.bias ? p.bias[n] : 0.0f));
-    }
+}
+
+ocs_status run_product(const Product& p, void* Y, ocs_dtype y_type, bool overlap, cudaStream_t stream) {
+  switch (y_type) {
+    case OCS_F16: return launch_product<__half>(p, Y, overlap, stream);
+    case OCS_BF16: return launch_product<__nv_bfloat16>(p, Y, overlap, stream);
+    default: return launch_product<float>(p, Y, overlap, stream);
   }
 }
 
@@ -62,23 +449,6 @@ ocs_status check_product(int a_signed, int M, int K, int64_t lda, const void* A,
   if (ldy < N || !aligned(Y, elem_bytes(y_type)) || !aligned(w_scales, 4) || (bias && !aligned(bias, 4))) return OCS_ERR_SHAPE;
   if ((int64_t)K * 128 * (a_signed ? 128 : 255) > 2147483647ll || M >= (1 << 30)) return OCS_ERR_UNSUPPORTED;
   return OCS_OK;
-}
-
-template <typename T>
-ocs_status launch_product(const RowGemm& p, void* Y, cudaStream_t stream) {
-  const long long gy = (p.M + kTile - 1) / kTile;
-  if (gy > 65535) return OCS_ERR_UNSUPPORTED;
-  LaunchScope ls("row_gemm_kernel", stream);
-  row_gemm_kernel<T><<<dim3((p.N + kTile - 1) / kTile, (unsigned)gy), 256, 0, stream>>>(p, static_cast<T*>(Y));
-  return launch_status();
-}
-
-ocs_status run_product(const RowGemm& p, void* Y, ocs_dtype y_type, cudaStream_t stream) {
-  switch (y_type) {
-    case OCS_F16: return launch_product<__half>(p, Y, stream);
-    case OCS_BF16: return launch_product<__nv_bfloat16>(p, Y, stream);
-    default: return launch_product<float>(p, Y, stream);
-  }
 }
 
 }  // namespace
@@ -99,9 +469,9 @@ extern "C" ocs_status ocs_qlinear_rows(const void* A_codes, int a_signed, const 
   if (st != OCS_OK) return st;
   if (!aligned(a_scales, 4)) return OCS_ERR_SHAPE;
   if ((st = check_device()) != OCS_OK) return st;
-  RowGemm p{static_cast<const uint8_t*>(A_codes), a_scales, W_codes, w_scales, bias, M, N, K, a_signed ? 1 : 0,
+  Product p{A_codes, a_scales, W_codes, w_scales, bias, M, N, K, a_signed ? 1 : 0,
             lda, ldw, ldy, dev_status};
-  return run_product(p, Y, y_type, stream);
+  return run_product(p, Y, y_type, false, stream);
 }
 
 extern "C" size_t ocs_linear_rows_workspace_bytes(int M, int C, int S) {
@@ -128,7 +498,17 @@ extern "C" ocs_status ocs_linear_rows(const void* X, ocs_dtype x_type, int M, in
   float* scales = reinterpret_cast<float*>(codes + align_up((size_t)M * lda, 256));
   st = ocs_quantize_rows(X, x_type, M, C, ldx, S, idx_map, bits, is_signed, codes, lda, scales, dev_status, stream_);
   if (st != OCS_OK) return st;
-  RowGemm p{reinterpret_cast<const uint8_t*>(codes), scales, W_codes, w_scales, bias, M, N, K, is_signed ? 1 : 0,
+  Product p{codes, scales, W_codes, w_scales, bias, M, N, K, is_signed ? 1 : 0,
             lda, ldw, ldy, dev_status};
-  return run_product(p, Y, y_type, stream);
+  return run_product(p, Y, y_type, true, stream);
+}
+
+// Test hook: the next ocs_qlinear_rows / ocs_linear_rows calls of this process use the given plan; tn = 0 gives the
+// choice back.
+extern "C" ocs_status ocs_selftest_force_row_plan(int tn, int cg, int slices) {
+  if (tn != 0 && ((tn != 16 && tn != 32 && tn != 64 && tn != 128 && tn != 256) || (cg != 1 && cg != 2) ||
+                  (slices != 1 && slices != 2 && slices != 4 && slices != 8)))
+    return OCS_ERR_INVALID_ARG;
+  g_force_tn.store(tn); g_force_cg.store(cg); g_force_slices.store(slices);
+  return OCS_OK;
 }

@@ -161,6 +161,27 @@ def test_qlinear_rows(M, K, N, signed):
         assert (rest == 7.0).all()                         # nothing is written beside Y
 
 
+@pytest.mark.parametrize("M,K,N", [(5, 4096, 300), (130, 2100, 520), (300, 1100, 777)])
+def test_qlinear_rows_does_not_depend_on_the_plan(M, K, N):
+    """Tokens per tile, pairs of CTAs and K splits: the same bits under every plan."""
+    A, W = _codes(1, M, K, True), _codes(2, N, K, True)
+    a_s, w_s = torch.rand(M, generator=_gen(1), device="cuda"), torch.rand(N, generator=_gen(2), device="cuda")
+    bias = torch.randn(N, generator=_gen(3), device="cuda")
+    st = ocs.new_status()
+    first = ocs.ocs_qlinear_rows(A, a_s, W, w_s, bias=bias, dev_status=st)
+    check_product(A, a_s, W, w_s, bias, first)
+    try:
+        for tn, cg, slices in [(16, 1, 1), (16, 1, 4), (32, 1, 1), (32, 1, 8), (64, 1, 1), (64, 1, 2), (64, 1, 8), (128, 1, 1),
+                               (128, 1, 2), (128, 1, 8), (128, 2, 1), (128, 2, 2), (128, 2, 4), (256, 1, 1), (256, 2, 1)]:
+            ocs.ocs_selftest_force_row_plan(tn, cg, slices)
+            for _ in range(2):
+                Y = ocs.ocs_qlinear_rows(A, a_s, W, w_s, bias=bias, dev_status=st)
+                assert ocs.ocs_poll_status(st) == 0, (tn, cg, slices)
+                assert torch.equal(Y, first), (tn, cg, slices)
+    finally:
+        ocs.ocs_selftest_force_row_plan(0)
+
+
 def test_qlinear_rows_extreme_codes():
     """Accumulators at the ends of the documented range, and values that leave fp16."""
     for signed, K, a in ((True, 131071, -128), (False, 65793, 255)):
