@@ -32,79 +32,106 @@ __device__ __forceinline__ float ex2(float x) {                // 2^x, relative 
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
   return r;
 }
-__device__ __forceinline__ unsigned long long add_f32x2(unsigned long long a, unsigned long long b) {
-  unsigned long long r;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-  return r;
-}
-__device__ __forceinline__ unsigned long long mul_f32x2(unsigned long long a, unsigned long long b) {
-  unsigned long long r;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-  return r;
-}
-
-// 16 bytes of a row
+// 32 bytes of a row
 template <typename T>
 struct Vec {
-  static constexpr int VE = 16 / (int)sizeof(T);
-  uint4 w;
-  __device__ __forceinline__ uint32_t word(int i) const { return i == 0 ? w.x : i == 1 ? w.y : i == 2 ? w.z : w.w; }
-  // elements 2i and 2i + 1 as a packed pair of fp32
-  __device__ __forceinline__ unsigned long long pair(int i) const;
-  __device__ __forceinline__ float max_all() const;   // NaN if any element is
+  static constexpr int VE = 32 / (int)sizeof(T);
+  uint32_t w[8];
+  __device__ __forceinline__ void load(const void* p) {   // 32-byte aligned
+    asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7]) : "l"(p));
+  }
+  __device__ __forceinline__ void floats(float* f) const;      // the elements as fp32
+  __device__ __forceinline__ void floored(float* f) const;     // ... none below lowest<T>()
+  __device__ __forceinline__ float max_all() const;            // the largest; NaN if any element is
 };
-template <> __device__ __forceinline__ unsigned long long Vec<float>::pair(int i) const {
-  return pack_f32x2(__uint_as_float(word(2 * i)), __uint_as_float(word(2 * i + 1)));
+// Stand-in for a masked token's -infinity in the sums: finite, so that 0 * d stays 0, and so low that 2^d is zero
+// (sums_hold() says when that is so).
+template <typename T> __device__ __forceinline__ constexpr float lowest() { return -0x1p100f; }
+template <> __device__ __forceinline__ constexpr float lowest<__half>() { return -65504.0f; }
+
+template <> __device__ __forceinline__ void Vec<float>::floats(float* f) const {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) f[i] = __uint_as_float(w[i]);
 }
-template <> __device__ __forceinline__ unsigned long long Vec<__nv_bfloat16>::pair(int i) const {
-  const uint32_t v = word(i);
-  return pack_f32x2(__uint_as_float(v << 16), __uint_as_float(v & 0xffff0000u));
-}
-template <> __device__ __forceinline__ unsigned long long Vec<__half>::pair(int i) const {
-  const uint32_t v = word(i);
-  const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&v));
-  return pack_f32x2(f.x, f.y);
+template <> __device__ __forceinline__ void Vec<float>::floored(float* f) const {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) f[i] = fmaxf(__uint_as_float(w[i]), lowest<float>());
 }
 template <> __device__ __forceinline__ float Vec<float>::max_all() const {
-  return max_nan(max_nan(__uint_as_float(w.x), __uint_as_float(w.y)), max_nan(__uint_as_float(w.z), __uint_as_float(w.w)));
+  float m[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) m[i] = max_nan(__uint_as_float(w[2 * i]), __uint_as_float(w[2 * i + 1]));
+  return max_nan(max_nan(m[0], m[1]), max_nan(m[2], m[3]));
 }
-template <> __device__ __forceinline__ float Vec<__nv_bfloat16>::max_all() const {
-  const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&w);
-  const __nv_bfloat162 m = __hmax2_nan(__hmax2_nan(h[0], h[1]), __hmax2_nan(h[2], h[3]));
-  return max_nan(__low2float(m), __high2float(m));
+__device__ __forceinline__ void widen(__nv_bfloat162 h, float* f) {
+  const uint32_t b = *reinterpret_cast<const uint32_t*>(&h);
+  f[0] = __uint_as_float(b << 16);
+  f[1] = __uint_as_float(b & 0xffff0000u);
 }
-template <> __device__ __forceinline__ float Vec<__half>::max_all() const {
-  const __half2* h = reinterpret_cast<const __half2*>(&w);
-  const __half2 m = __hmax2_nan(__hmax2_nan(h[0], h[1]), __hmax2_nan(h[2], h[3]));
-  return max_nan(__low2float(m), __high2float(m));
+__device__ __forceinline__ void widen(__half2 h, float* f) {
+  const float2 x = __half22float2(h);
+  f[0] = x.x;
+  f[1] = x.y;
 }
+template <typename H2> __device__ __forceinline__ H2 as_half2(uint32_t w) { return *reinterpret_cast<const H2*>(&w); }
+template <typename H2>
+__device__ __forceinline__ float packed_max(const uint32_t* w) {
+  H2 m[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) m[i] = __hmax2_nan(as_half2<H2>(w[2 * i]), as_half2<H2>(w[2 * i + 1]));
+  float f[2];
+  widen(__hmax2_nan(__hmax2_nan(m[0], m[1]), __hmax2_nan(m[2], m[3])), f);
+  return max_nan(f[0], f[1]);
+}
+template <> __device__ __forceinline__ void Vec<__nv_bfloat16>::floats(float* f) const {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) widen(as_half2<__nv_bfloat162>(w[i]), f + 2 * i);
+}
+template <> __device__ __forceinline__ void Vec<__nv_bfloat16>::floored(float* f) const {
+  const __nv_bfloat162 low = __float2bfloat162_rn(lowest<__nv_bfloat16>());
+#pragma unroll
+  for (int i = 0; i < 8; ++i) widen(__hmax2(as_half2<__nv_bfloat162>(w[i]), low), f + 2 * i);
+}
+template <> __device__ __forceinline__ float Vec<__nv_bfloat16>::max_all() const { return packed_max<__nv_bfloat162>(w); }
+template <> __device__ __forceinline__ void Vec<__half>::floats(float* f) const {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) widen(as_half2<__half2>(w[i]), f + 2 * i);
+}
+template <> __device__ __forceinline__ void Vec<__half>::floored(float* f) const {
+  const __half2 low = __float2half2_rn(lowest<__half>());
+#pragma unroll
+  for (int i = 0; i < 8; ++i) widen(__hmax2(as_half2<__half2>(w[i]), low), f + 2 * i);
+}
+template <> __device__ __forceinline__ float Vec<__half>::max_all() const { return packed_max<__half2>(w); }
 
 template <typename T> __device__ __forceinline__ T minus_infinity();
 template <> __device__ __forceinline__ float minus_infinity<float>() { return -INFINITY; }
 template <> __device__ __forceinline__ __half minus_infinity<__half>() { return __ushort_as_half(0xfc00); }
 template <> __device__ __forceinline__ __nv_bfloat16 minus_infinity<__nv_bfloat16>() { return __ushort_as_bfloat16(0xff80); }
 
-// A row as aligned vectors of 16 bytes: vector j holds elements j * VE - a .. j * VE - a + VE - 1, where a is how many
-// elements past a 16-byte boundary the row starts.  The first and the last one may hang over; what lies outside the row is
+// A row as aligned vectors of 32 bytes: vector j holds elements j * VE - a .. j * VE - a + VE - 1, where a is how many
+// elements past a 32-byte boundary the row starts.  The first and the last one may hang over; what lies outside the row is
 // never read and counts as -infinity.
 template <typename T>
 struct RowVectors {
   static constexpr int VE = Vec<T>::VE;
   const T* x;
-  int V, a, count;
+  int V, a, count, n_whole;    // vectors (a > 0) .. (a > 0) + n_whole - 1 lie inside the row
   __device__ __forceinline__ RowVectors(const T* row, int n) : x(row), V(n) {
-    a = (int)((reinterpret_cast<uintptr_t>(row) & 15) / sizeof(T));
+    a = (int)((reinterpret_cast<uintptr_t>(row) & 31) / sizeof(T));
     count = (V + a + VE - 1) / VE;
+    n_whole = (V + a) / VE - (a > 0);
   }
   __device__ __forceinline__ int first(int j) const { return j * VE - a; }
-  __device__ __forceinline__ bool whole(int j) const { return first(j) >= 0 && first(j) + VE <= V; }
+  __device__ __forceinline__ bool whole(int j) const { return j - (a > 0) >= 0 && j - (a > 0) < n_whole; }
   __device__ __forceinline__ Vec<T> load(int j) const {
     Vec<T> v;
     const int e0 = first(j);
     if (whole(j)) {
-      v.w = *reinterpret_cast<const uint4*>(x + e0);
+      v.load(x + e0);
     } else {
-      T* e = reinterpret_cast<T*>(&v.w);
+      T* e = reinterpret_cast<T*>(v.w);
 #pragma unroll
       for (int i = 0; i < VE; ++i) e[i] = (unsigned)(e0 + i) < (unsigned)V ? x[e0 + i] : minus_infinity<T>();
     }
@@ -117,22 +144,69 @@ struct RowVectors {
 struct Stats {
   float m, s, w;
 };
+__device__ __forceinline__ void shift(Stats& t, float d) {   // every term's exponent moves by d
+  t.w = __fmul_rn(fmaf(t.s, d, t.w), ex2(d));
+  t.s = __fmul_rn(t.s, ex2(d));
+}
 __device__ __forceinline__ void move_max(Stats& t, float m, float c) {   // the same sums relative to another maximum
-  const float d = fmaxf(__fmul_rn(__fsub_rn(t.m, m), c), kFloor);        // -infinity or NaN (nothing summed yet): s = w = 0
-  const float r = ex2(d);
-  t.w = __fmul_rn(fmaf(t.s, d, t.w), r);
-  t.s = __fmul_rn(t.s, r);
+  shift(t, fmaxf(__fmul_rn(__fsub_rn(t.m, m), c), kFloor));              // -infinity or NaN (nothing summed yet): s = w = 0
   t.m = m;
+}
+// The main loop takes d = fma(l, c, -M) with M = fl(m * c) instead of (l - m) * c: one instruction, one rounding.  That
+// holds while no product overflows and a masked token's stand-in is far enough below the maximum; otherwise (logits
+// around the type's lowest or largest value) the sums are taken once more in the other form.
+template <typename T>
+__device__ __forceinline__ bool sums_hold(float m, float c) {
+  return fabsf(m) < 0x1p90f && c < 0x1p20f && __fmul_rn(__fsub_rn(lowest<T>(), m), c) <= -160.0f;
 }
 __device__ __forceinline__ Stats warp_stats(Stats t, float c) {
   float m = t.m;
   for (int o = 16; o > 0; o >>= 1) m = max_nan(m, __shfl_xor_sync(0xffffffffu, m, o));
   move_max(t, m, c);
+#pragma unroll
   for (int o = 16; o > 0; o >>= 1) {
     t.s = __fadd_rn(t.s, __shfl_xor_sync(0xffffffffu, t.s, o));
     t.w = __fadd_rn(t.w, __shfl_xor_sync(0xffffffffu, t.w, o));
   }
   return t;
+}
+
+// One thread's share of a row: its largest element m, the first vector that holds it, and the sums relative to M (in
+// two chains each).  M is not the running maximum but follows it at a distance of up to kLag: it starts at the largest
+// first element of the warp's threads, so that almost no later vector has to scale the sums.
+constexpr float kLag = 8.0f;
+struct Running {
+  float m, M, s[2], w[2];
+  int pos;
+};
+template <typename T>
+__device__ __forceinline__ void take(Running& t, const Vec<T>& v, int j, float c) {
+  constexpr int VE = Vec<T>::VE;
+  const float mx = v.max_all();
+  if (mx > t.m) t.pos = j;
+  t.m = max_nan(t.m, mx);
+  const float to = __fmul_rn(fmaxf(mx, lowest<T>()), c);
+  if (to > __fadd_rn(t.M, kLag)) {
+    const float d = fmaxf(__fsub_rn(t.M, to), kFloor), r = ex2(d);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      t.w[i] = __fmul_rn(fmaf(t.s[i], d, t.w[i]), r);
+      t.s[i] = __fmul_rn(t.s[i], r);
+    }
+    t.M = to;
+  }
+  float f[VE];
+  v.floored(f);
+#pragma unroll
+  for (int i = 0; i < VE; ++i) {
+    const float d = fmaf(f[i], c, -t.M), e = ex2(d);
+    t.s[i & 1] = __fadd_rn(t.s[i & 1], e);
+    t.w[i & 1] = fmaf(e, d, t.w[i & 1]);
+  }
+}
+__device__ __forceinline__ float warp_max(float m) {   // NaN if any lane's is
+  for (int o = 16; o > 0; o >>= 1) m = max_nan(m, __shfl_xor_sync(0xffffffffu, m, o));
+  return m;
 }
 
 struct LogprobParams {
@@ -147,123 +221,123 @@ struct LogprobParams {
 
 struct LogprobSmem {
   Stats warp[kWarps];
-  Stats part[kMaxCluster];                       // of the CTAs that share the row
-  key_t sorted[kLpThreads];                      // every thread's largest element, descending within a warp
-  key_t cand[kCandidates];
-  key_t top[kMaxCluster * kMaxTop];              // each CTA's largest, then the row's
-  key_t best[kMaxTop];
-  key_t tau;
+  Stats part[kMaxCluster];                             // of the CTAs that share the row
+  __align__(16) key_t cand[kCandidates];
+  __align__(16) key_t top[kMaxCluster * kMaxTop];      // each CTA's largest, descending
+  key_t best[kMaxTop];                                 // the row's
+  key_t low[kWarps], high[kWarps];
   int hot[kLpThreads];
   int n_hot, n_cand;
-  key_t round[kWarps];
 };
 
-// The k largest of n keys in list, descending, to out (all threads; n may be less than k: zeros follow).
-__device__ __forceinline__ void rank_select(const key_t* list, int n, int k, key_t* out) {
-  for (int i = threadIdx.x; i < k; i += kLpThreads)
-    if (i >= n) out[i] = 0;
-  for (int i = threadIdx.x; i < n; i += kLpThreads) {
-    const key_t mine = list[i];
-    int r = 0;
-    for (int j = 0; j < n && r < k; ++j) r += list[j] > mine;
-    if (r < k && mine != 0) out[r] = mine;
+// How many of n keys are larger than v.
+__device__ __forceinline__ int count_larger(const key_t* list, int n, key_t v) {
+  const ulonglong2* two = reinterpret_cast<const ulonglong2*>(list);
+  int r = 0;
+#pragma unroll 4
+  for (int i = 0; i < n / 2; ++i) {
+    const ulonglong2 k = two[i];
+    r += (k.x > v) + (k.y > v);
   }
+  if (n & 1) r += list[n - 1] > v;
+  return r;
 }
 
-// The k largest elements of vectors [lo, hi) of the row, as keys in out, given every thread's largest element (its value,
-// and the vector that holds it first).
-//   1. tau = the k-th largest of the threads' keys, each lowered to the last index of its vector: k elements at least
-//      are not below it.  Only threads with a key not below tau (raised to the first index) can hold such an element:
-//      the vectors are disjoint, so these are k threads at most.
-//   2. A warp reads the elements of one of these threads again and collects what is not below tau.
+template <bool MAX>
+__device__ __forceinline__ key_t warp_reduce(key_t v) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    const key_t other = __shfl_xor_sync(0xffffffffu, v, o);
+    v = (other > v) == MAX ? other : v;
+  }
+  return v;
+}
+
+// The k largest elements of vectors [lo, hi) of the row, descending, as keys in out (zeros where there are fewer), given
+// every thread's largest element (its value, and the vector that holds it first).
+//   1. tau: a key that at least k of the threads' largest elements are not below, and not many more than k, by bisection
+//      (each step counts with one barrier).  The threads' keys are lowered to the last index of their vector, so at least
+//      k elements are not below tau, and only threads whose key, raised to the first index, is not below tau hold one.
+//   2. All threads read these threads' elements again and collect what is not below tau.
 //   3. The k largest of what was collected, by rank.
-// Many equal or unluckily placed elements may overflow the list; then the keys are found one after the other.
+// Many unluckily placed elements may overflow the list; then the keys are found one after the other.
 template <typename T>
 __device__ void top_of_segment(const RowVectors<T>& row, int lo, int hi, int k, float m, int pos, LogprobSmem& sm, key_t* out) {
   constexpr int VE = Vec<T>::VE;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const bool any = lo + tid < hi;
-  const int e0 = row.first(pos);
-  const key_t low = any ? top_key(m, min(e0 + VE, row.V) - 1) : 0;
-  const key_t high = any ? top_key(m, max(e0, 0)) : 0;
-  if (tid == 0) { sm.tau = 0; sm.n_hot = 0; sm.n_cand = 0; }
-  // descending within the warp (bitonic)
-  key_t v = low;
+  const key_t low = any ? top_key(m, min(row.first(pos) + VE, row.V) - 1) : 0;
+  const key_t high = any ? top_key(m, max(row.first(pos), 0)) : 0;
+  key_t tau = 0;
+  const key_t wmin = warp_reduce<false>(any ? low : ~0ull), wmax = warp_reduce<true>(low);
+  if (lane == 0) { sm.low[warp] = wmin; sm.high[warp] = wmax; }
+  if (tid == 0) sm.n_hot = sm.n_cand = 0;
+  if (tid < k) out[tid] = 0;
+  __syncthreads();
+  if (hi - lo >= k && hi - lo >= kLpThreads) {   // every thread has an element; with fewer of them nothing is left out
+    key_t above;
+    tau = sm.low[0];
+    above = sm.high[0];
 #pragma unroll
-  for (int size = 2; size <= 32; size *= 2) {
-#pragma unroll
-    for (int o = size / 2; o > 0; o /= 2) {
-      const key_t other = __shfl_xor_sync(0xffffffffu, v, o);
-      const bool keep_max = ((lane & o) == 0) == ((lane & size) == 0 || size == 32);
-      v = keep_max ? (v > other ? v : other) : (v < other ? v : other);
+    for (int w = 1; w < kWarps; ++w) {
+      tau = min(tau, sm.low[w]);
+      above = max(above, sm.high[w]);
+    }
+    // all threads are at or above tau, k - 1 at the most at or above `above` + 1
+    ++above;
+    while (above - tau > 1) {
+      const key_t mid = tau + (above - tau) / 2;
+      const int n = __syncthreads_count(low >= mid);
+      if (n >= k) tau = mid;
+      else above = mid;
+      if (n >= k && n <= k + k / 2 + 8) break;
     }
   }
-  sm.sorted[tid] = v;
-  __syncthreads();
-  // rank of v among all threads' keys: its place in its own list, and how many of each other list are larger
-  if (v != 0) {
-    int rank = lane;
-    for (int w = 0; w < kWarps; ++w) {
-      if (w == warp) continue;
-      int n = 0;
-#pragma unroll
-      for (int step = 32; step > 0; step /= 2)
-        if (n + step <= 32 && sm.sorted[w * 32 + n + step - 1] > v) n += step;
-      rank += n;
-    }
-    if (rank == k - 1) sm.tau = v;
-  }
-  __syncthreads();
-  const key_t tau = sm.tau;
   if (any && high >= tau) sm.hot[atomicAdd(&sm.n_hot, 1)] = tid;
   __syncthreads();
-  const int n_hot = sm.n_hot;
-  for (int h = warp; h < n_hot; h += kWarps) {
-    for (int j = lo + sm.hot[h] + lane * kLpThreads; j < hi; j += 32 * kLpThreads) {
-      const Vec<T> x = row.load(j);
-      const int first = row.first(j);
+  const int vecs = (hi - lo + kLpThreads - 1) / kLpThreads, total = sm.n_hot * vecs;
+  for (int q = tid; q < total; q += kLpThreads) {
+    const int h = q / vecs;
+    const int j = lo + sm.hot[h] + (q - h * vecs) * kLpThreads;
+    if (j >= hi) continue;
+    float f[VE];
+    row.load(j).floats(f);
+    const int first = row.first(j);
 #pragma unroll
-      for (int i = 0; i < VE / 2; ++i) {
-        float f[2];
-        unpack_f32x2(x.pair(i), f[0], f[1]);
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const int idx = first + 2 * i + e;
-          if ((unsigned)idx < (unsigned)row.V) {
-            const key_t key = top_key(f[e], idx);
-            if (key >= tau) {
-              const int at = atomicAdd(&sm.n_cand, 1);
-              if (at < kCandidates) sm.cand[at] = key;
-            }
-          }
-        }
+    for (int i = 0; i < VE; ++i) {
+      const key_t key = top_key(f[i], first + i);
+      if (key >= tau && (unsigned)(first + i) < (unsigned)row.V) {
+        const int at = atomicAdd(&sm.n_cand, 1);
+        if (at < kCandidates) sm.cand[at] = key;
       }
     }
   }
   __syncthreads();
   const int n = sm.n_cand;
   if (n <= kCandidates) {
-    rank_select(sm.cand, n, k, out);
+    for (int i = tid; i < n; i += kLpThreads) {
+      const key_t mine = sm.cand[i];
+      const int r = count_larger(sm.cand, n, mine);
+      if (r < k) out[r] = mine;
+    }
   } else {
     key_t last = ~0ull;
     for (int r = 0; r < k; ++r) {
       key_t best = 0;
       for (int j = lo + tid; j < hi; j += kLpThreads) {
-        const Vec<T> x = row.load(j);
-        for (int i = 0; i < VE / 2; ++i) {
-          float f[2];
-          unpack_f32x2(x.pair(i), f[0], f[1]);
-          for (int e = 0; e < 2; ++e) {
-            const int idx = row.first(j) + 2 * i + e;
-            const key_t key = (unsigned)idx < (unsigned)row.V ? top_key(f[e], idx) : 0;
-            if (key < last && key > best) best = key;
-          }
+        float f[VE];
+        row.load(j).floats(f);
+#pragma unroll
+        for (int i = 0; i < VE; ++i) {
+          const int idx = row.first(j) + i;
+          const key_t key = (unsigned)idx < (unsigned)row.V ? top_key(f[i], idx) : 0;
+          if (key < last && key > best) best = key;
         }
       }
-      for (int o = 16; o > 0; o >>= 1) { const key_t other = __shfl_xor_sync(0xffffffffu, best, o); if (other > best) best = other; }
-      if (lane == 0) sm.round[warp] = best;
+      best = warp_reduce<true>(best);
+      if (lane == 0) sm.high[warp] = best;
       __syncthreads();
-      for (int w = 0; w < kWarps; ++w) if (sm.round[w] > best) best = sm.round[w];
+      for (int w = 0; w < kWarps; ++w) best = max(best, sm.high[w]);
       if (tid == 0) out[r] = best;
       last = best;
       __syncthreads();
@@ -281,8 +355,8 @@ __device__ __forceinline__ void store_peer_f32(uint32_t addr, float v) {
 
 // One row per cluster; the CTAs of a cluster take consecutive parts of it and send what they found to the first one.
 template <typename T>
-__global__ void __launch_bounds__(kLpThreads, 4) logprobs_kernel(const T* __restrict__ logits, const LogprobParams p) {
-  constexpr int VE = Vec<T>::VE, U = 4;
+__global__ void __launch_bounds__(kLpThreads, 5) logprobs_kernel(const T* __restrict__ logits, const LogprobParams p) {
+  constexpr int VE = Vec<T>::VE;
   __shared__ LogprobSmem sm;
   const int CL = (int)cluster_size(), rank = CL > 1 ? (int)cluster_rank() : 0;
   if (CL > 1) asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory");   // every CTA runs before its memory is written to
@@ -299,60 +373,68 @@ __global__ void __launch_bounds__(kLpThreads, 4) logprobs_kernel(const T* __rest
     if (y >= 0) ly = to_f32(row.x[y]);
   }
 
-  Stats t{-INFINITY, 0.0f, 0.0f};
-  int pos = lo + tid;
   const float c = p.c;
-  const unsigned long long c2 = pack_f32x2(c, c);
-  for (int j0 = lo + tid; j0 < hi; j0 += U * kLpThreads) {
-    Vec<T> v[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int j = j0 + u * kLpThreads;
-      if (j < hi) v[u] = row.load(j);
+  Running run{-INFINITY, 0.0f, {0.0f, 0.0f}, {0.0f, 0.0f}, lo + tid};
+  {
+    int j = lo + tid;
+    const int end = min(hi, (row.a > 0) + row.n_whole);
+    const char* src = reinterpret_cast<const char*>(row.x - row.a);   // vector j starts at src + 32 j
+    Vec<T> v, w;   // one is on its way while the other is summed
+    const bool some = j < hi;
+    if (some) v = row.load(j);
+    if (j + kLpThreads < end) w.load(src + 32ll * (j + kLpThreads));
+    run.M = __fmul_rn(fmaxf(warp_max(some ? v.max_all() : -INFINITY), lowest<T>()), c);
+    if (some) take(run, v, j, c);
+    if (j + 2 * kLpThreads < end) v.load(src + 32ll * (j + 2 * kLpThreads));
+    for (j += kLpThreads; j < end; j += 2 * kLpThreads) {
+      take(run, w, j, c);
+      if (j + 2 * kLpThreads < end) w.load(src + 32ll * (j + 2 * kLpThreads));
+      if (j + kLpThreads >= end) { j += kLpThreads; break; }
+      take(run, v, j + kLpThreads, c);
+      if (j + 3 * kLpThreads < end) v.load(src + 32ll * (j + 3 * kLpThreads));
     }
-    float mx[U], m = t.m;
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      mx[u] = j0 + u * kLpThreads < hi ? v[u].max_all() : -INFINITY;
-      m = max_nan(m, mx[u]);
+    if (j < hi) {   // the row's last vector, hanging over
+      v = row.load(j);
+      take(run, v, j, c);
     }
-    if (m != t.m) {   // (also NaN)
-#pragma unroll
-      for (int u = U - 1; u >= 0; --u)
-        if (mx[u] == m) pos = j0 + u * kLpThreads;
-      move_max(t, m, c);
-    }
-    const unsigned long long neg = pack_f32x2(-m, -m);
-    unsigned long long s2 = pack_f32x2(0.0f, 0.0f), w2 = s2;
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      if (j0 + u * kLpThreads < hi) {
-#pragma unroll
-        for (int i = 0; i < VE / 2; ++i) {
-          float d0, d1;
-          unpack_f32x2(mul_f32x2(add_f32x2(v[u].pair(i), neg), c2), d0, d1);
-          d0 = fmaxf(d0, kFloor);
-          d1 = fmaxf(d1, kFloor);
-          const unsigned long long e = pack_f32x2(ex2(d0), ex2(d1));
-          s2 = add_f32x2(s2, e);
-          w2 = fma_f32x2(e, pack_f32x2(d0, d1), w2);
-        }
-      }
-    }
-    float a, b;
-    unpack_f32x2(s2, a, b);
-    t.s = __fadd_rn(t.s, __fadd_rn(a, b));
-    unpack_f32x2(w2, a, b);
-    t.w = __fadd_rn(t.w, __fadd_rn(a, b));
   }
-
-  const float own_max = t.m;
+  const float own_max = run.m;
+  const int pos = run.pos;
+  Stats t{warp_max(run.m), __fadd_rn(run.s[0], run.s[1]), __fadd_rn(run.w[0], run.w[1])};
+  if (t.m > lowest<T>()) {   // from M to m * c
+    const float d = fmaxf(fmaf(-t.m, c, run.M), kFloor), r = ex2(d), moved = fmaf(t.s, d, t.w);
+    t.s = __fmul_rn(t.s, r);
+    t.w = fabsf(moved) <= 0x1p-22f * fabsf(t.w) ? 0.0f : __fmul_rn(moved, r);   // of equals only rounding would be left
+  } else {
+    t.s = t.w = 0.0f;        // nothing but masked tokens as far as the sums can tell
+  }
   t = warp_stats(t, c);
   if (lane == 0) sm.warp[warp] = t;
+  __syncthreads();
+  {
+    float m = sm.warp[0].m;
+#pragma unroll
+    for (int w = 1; w < kWarps; ++w) m = max_nan(m, sm.warp[w].m);
+    if (fabsf(m) < INFINITY && !sums_hold<T>(m, c)) {   // the same for the whole CTA
+      __syncthreads();
+      t = Stats{m, 0.0f, 0.0f};
+      for (int j = lo + tid; j < hi; j += kLpThreads) {
+        float f[VE];
+        row.load(j).floats(f);
+#pragma unroll
+        for (int i = 0; i < VE; ++i) {
+          const float d = fmaxf(__fmul_rn(__fsub_rn(f[i], m), c), kFloor), e = ex2(d);
+          t.s = __fadd_rn(t.s, e);
+          t.w = fmaf(e, d, t.w);
+        }
+      }
+      t = warp_stats(t, c);
+      if (lane == 0) sm.warp[warp] = t;
+      __syncthreads();
+    }
+  }
   if (p.top_k > 0) {
-    top_of_segment(row, lo, hi, p.top_k, own_max, pos, sm, sm.top + rank * p.top_k);   // begins and ends with a barrier
-  } else {
-    __syncthreads();
+    top_of_segment(row, lo, hi, p.top_k, own_max, pos, sm, sm.top + rank * p.top_k);
   }
   // this CTA's part of the row (every warp works it out; lane w looks at warp w)
   t = lane < kWarps ? sm.warp[lane] : Stats{-INFINITY, 0.0f, 0.0f};
@@ -378,7 +460,11 @@ __global__ void __launch_bounds__(kLpThreads, 4) logprobs_kernel(const T* __rest
     t = lane == 0 ? own : (lane < CL ? sm.part[lane] : Stats{-INFINITY, 0.0f, 0.0f});
     t = warp_stats(t, c);
     if (p.top_k > 0) {
-      rank_select(sm.top, CL * p.top_k, p.top_k, sm.best);
+      for (int i = tid; i < CL * p.top_k; i += kLpThreads) {
+        const key_t k = sm.top[i];
+        const int at = k != 0 ? count_larger(sm.top, CL * p.top_k, k) : kMaxTop;
+        if (at < p.top_k) sm.best[at] = k;
+      }
       __syncthreads();
     }
   }
@@ -387,7 +473,8 @@ __global__ void __launch_bounds__(kLpThreads, 4) logprobs_kernel(const T* __rest
   const float nan = __int_as_float(0x7fffffff);
   const float ls = bad ? nan : (empty ? 0.0f : logf(t.s));
   if (tid == 0) {
-    const float H = bad ? nan : (empty ? 0.0f : __fsub_rn(ls, __fmul_rn(__fdiv_rn(t.w, t.s), 0.693147180559945f)));
+    // (an entropy is not negative; rounding alone could make it so)
+    const float H = bad ? nan : (empty ? 0.0f : fmaxf(__fsub_rn(ls, __fmul_rn(__fdiv_rn(t.w, t.s), 0.693147180559945f)), 0.0f));
     if (bad) flag(p.dev_status, OCS_DEV_NONFINITE);
     if (p.entropy) p.entropy[r] = H;
     if (p.stats)
@@ -417,7 +504,7 @@ template <typename T> __device__ __forceinline__ uint32_t pack_pair(float a, flo
 template <> __device__ __forceinline__ uint32_t pack_pair<__half>(float a, float b) { const __half2 h = __floats2half2_rn(a, b); return *reinterpret_cast<const uint32_t*>(&h); }
 template <> __device__ __forceinline__ uint32_t pack_pair<__nv_bfloat16>(float a, float b) { const __nv_bfloat162 h = __floats2bfloat162_rn(a, b); return *reinterpret_cast<const uint32_t*>(&h); }
 
-constexpr int kGradVecs = 4;   // vectors a thread of the gradient kernel handles
+constexpr int kGradVecs = 2;   // vectors a thread of the gradient kernel handles
 
 // One part of a row per CTA: read, p = 2^((l - m) * c - log2 s), the gradient, write.
 template <typename T>
@@ -446,22 +533,18 @@ __global__ void __launch_bounds__(kLpThreads) logprobs_backward_kernel(const T* 
   const float ls2 = __fmul_rn(st.y, 1.44269504088896f);
   // d = -beta * p * (g + gh * (ln p + H)) = p * (A + B * log2 p)
   const float A = -__fmul_rn(p.beta, fmaf(gh, st.z, g)), B = -__fmul_rn(__fmul_rn(gh, 0.693147180559945f), p.beta);
-  const unsigned long long neg = pack_f32x2(-st.x, -st.x), c2 = pack_f32x2(p.c, p.c), l2 = pack_f32x2(-ls2, -ls2);
-  const unsigned long long A2 = pack_f32x2(A, A), B2 = pack_f32x2(B, B);
-  const bool same = ((reinterpret_cast<uintptr_t>(dst) ^ reinterpret_cast<uintptr_t>(row.x)) & 15) == 0;
+  const bool same = ((reinterpret_cast<uintptr_t>(dst) ^ reinterpret_cast<uintptr_t>(row.x)) & 31) == 0;
 #pragma unroll
   for (int u = 0; u < kGradVecs; ++u) {
     const int j = j0 + u * kLpThreads;
     if (j >= row.count) break;
     const int e0 = row.first(j);
     float d[VE];
+    v[u].floats(d);
 #pragma unroll
-    for (int i = 0; i < VE / 2; ++i) {
-      float q0, q1;
-      unpack_f32x2(fma_f32x2(add_f32x2(v[u].pair(i), neg), c2, l2), q0, q1);
-      q0 = fmaxf(q0, kFloor);
-      q1 = fmaxf(q1, kFloor);
-      unpack_f32x2(mul_f32x2(pack_f32x2(ex2(q0), ex2(q1)), fma_f32x2(B2, pack_f32x2(q0, q1), A2)), d[2 * i], d[2 * i + 1]);
+    for (int i = 0; i < VE; ++i) {
+      const float q = fmaxf(fmaf(__fsub_rn(d[i], st.x), p.c, -ls2), kFloor);   // log2 p; a masked token's p is zero
+      d[i] = __fmul_rn(ex2(q), fmaf(B, q, A));
     }
     if ((unsigned)(y - e0) < (unsigned)VE && y >= 0 && !empty) {   // the given token is in this vector
 #pragma unroll
@@ -469,12 +552,14 @@ __global__ void __launch_bounds__(kLpThreads) logprobs_backward_kernel(const T* 
         if (e0 + e == y) d[e] = fmaf(g, p.beta, d[e]);
     }
     if (same && row.whole(j)) {
-      uint4 o;
-      if constexpr (sizeof(T) == 4)
-        o = make_uint4(__float_as_uint(d[0]), __float_as_uint(d[1]), __float_as_uint(d[2]), __float_as_uint(d[3]));
-      else
-        o = make_uint4(pack_pair<T>(d[0], d[1]), pack_pair<T>(d[2], d[3]), pack_pair<T>(d[4], d[5]), pack_pair<T>(d[6], d[7]));
-      *reinterpret_cast<uint4*>(dst + e0) = o;
+      uint32_t o[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        if constexpr (sizeof(T) == 4) o[i] = __float_as_uint(d[i]);
+        else o[i] = pack_pair<T>(d[2 * i], d[2 * i + 1]);
+      }
+      asm volatile("st.global.v8.b32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};"
+                   ::"r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3]), "r"(o[4]), "r"(o[5]), "r"(o[6]), "r"(o[7]), "l"(dst + e0) : "memory");
     } else {
 #pragma unroll
       for (int e = 0; e < VE; ++e)
@@ -483,10 +568,13 @@ __global__ void __launch_bounds__(kLpThreads) logprobs_backward_kernel(const T* 
   }
 }
 
-// CTAs that share a row: enough of them for every SM to have its four, each with a few vectors for every thread.
+// CTAs that share a row.  A row alone leaves most SMs idle, so few rows are shared, as long as every thread keeps two
+// vectors; but a CTA's fixed cost (about 4 us of start, join and selection, hidden only by other CTAs of its SM) makes
+// many small parts slower than whole rows.  bf16, five alternatives, us with 1 / 2 / 4 / 8 CTAs on a row: 8 rows of
+// 131072: 13.4 / 10.1 / 8.1 / 7.6; 128 rows of 128000: 18.6 / 14.2 / 14.5 / 19.9; 2048 rows of 50257: 50 / 73 / 115 / 196.
 int row_ctas(long long rows, int V, int ve) {
   int cl = 1;
-  while (cl < kMaxCluster && rows * cl < 8ll * kNumSMs && (long long)V > 8ll * cl * kLpThreads * ve) cl *= 2;
+  while (cl < kMaxCluster && rows * cl <= 256 && (long long)V > 2ll * cl * kLpThreads * ve) cl *= 2;
   return cl;
 }
 
