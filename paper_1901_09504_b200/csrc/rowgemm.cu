@@ -36,7 +36,7 @@ struct RowSmem {
   static constexpr int kCtrlBytes = 512;
   static constexpr int kBudget = 227 * 1024 - 1024 - kCtrlBytes - kScaleBytes;
   static constexpr int kStagesFit = (kBudget - kXBytes) / kStageBytes;
-  static constexpr int kStages = kStagesFit < 12 ? kStagesFit : 12;
+  static constexpr int kStages = kStagesFit < 8 ? kStagesFit : 8;
   static constexpr int kDynBytes = 1024 + kStages * kStageBytes + kXBytes + kScaleBytes + kCtrlBytes;
   static constexpr int kAccStride = TN < 32 ? 32 : TN;
   static constexpr uint32_t kTmemCols = 2 * kAccStride;
@@ -64,33 +64,39 @@ template <typename T> struct Pair;
 template <> struct Pair<__half> { static __device__ __forceinline__ uint32_t pack(float a, float b) { __half2 h = __floats2half2_rn(a, b); return *reinterpret_cast<uint32_t*>(&h); } };
 template <> struct Pair<__nv_bfloat16> { static __device__ __forceinline__ uint32_t pack(float a, float b) { __nv_bfloat162 h = __floats2bfloat162_rn(a, b); return *reinterpret_cast<uint32_t*>(&h); } };
 
-// CNT consecutive tokens of channel n: float(acc) * (a_scale * w_scale) + bias, rounded to T and stored.  The lanes of
-// the warp hold consecutive channels.
-template <typename T, int CNT>
-__device__ __forceinline__ void finish(const RowGemm& p, T* __restrict__ Y, const int* acc, const float* sc, int m0, int n,
-                                       float ws, float b, bool pairs) {
-  T* y = Y + (long long)m0 * p.ldy + n;
-  if (sizeof(T) == 2 && pairs) {
-    // neighbouring lanes swap halves, so that a lane stores two channels of one token in 32 bits
-    const int lane = threadIdx.x & 31, odd = lane & 1;
+// One output: float(acc) * (a_scale * w_scale) + bias, each step rounded once.
+__device__ __forceinline__ float one_output(int acc, float as, float ws, float b) {
+  return fmaf(__int2float_rn(acc), __fmul_rn(as, ws), b);
+}
+
+// CNT consecutive tokens of one channel per lane, rounded to T and stored; the lanes of the warp hold consecutive
+// channels.  y: the lane's channel of the first token; left: tokens of the tile that exist, from the first on.
+// WHOLE: all CNT tokens and all 32 channels exist.
+template <bool WHOLE, typename T, int CNT>
+__device__ __forceinline__ void finish(T* y, long long ldy, const int* acc, const float* sc, float ws, float b, int left,
+                                       bool n_ok, bool pairs) {
+  if constexpr (sizeof(T) == 2) {
+    if (pairs) {
+      // neighbouring lanes swap halves, so that a lane stores two channels of one token in 32 bits: the even lane token j,
+      // channels n and n + 1, the odd lane token j + 1, channels n - 1 and n
+      const int odd = threadIdx.x & 1;
+      T* q = y + (odd ? ldy - 1 : 0);
 #pragma unroll
-    for (int j = 0; j < CNT; j += 2) {
-      const float f0 = fmaf(__int2float_rn(acc[j]), __fmul_rn(sc[j], ws), b);
-      const float f1 = fmaf(__int2float_rn(acc[j + 1]), __fmul_rn(sc[j + 1], ws), b);
-      if constexpr (sizeof(T) == 2) {
-        const uint32_t mine = Pair<T>::pack(f0, f1);
+      for (int j = 0; j < CNT; j += 2) {
+        const uint32_t mine = Pair<T>::pack(one_output(acc[j], sc[j], ws, b), one_output(acc[j + 1], sc[j + 1], ws, b));
         const uint32_t other = __shfl_xor_sync(0xffffffffu, mine, 1);
         const uint32_t out = odd ? __byte_perm(other, mine, 0x7632) : __byte_perm(mine, other, 0x5410);
-        // even lane: token j, channels n, n+1; odd lane: token j+1, channels n-1, n
-        if (m0 + j + odd < p.M && n - odd < p.N) *reinterpret_cast<uint32_t*>(y + (long long)(j + odd) * p.ldy - odd) = out;
+        if (WHOLE || (j + odd < left && n_ok)) *reinterpret_cast<uint32_t*>(q) = out;
+        q += 2 * ldy;
       }
+      return;
     }
-  } else if (n < p.N) {
+  }
 #pragma unroll
-    for (int j = 0; j < CNT; ++j) {
-      if (m0 + j < p.M)
-        y[(long long)j * p.ldy] = from_f32<T>(fmaf(__int2float_rn(acc[j]), __fmul_rn(sc[j], ws), b));
-    }
+  for (int j = 0; j < CNT; ++j) {
+    const float f = one_output(acc[j], sc[j], ws, b);
+    if (WHOLE || (j < left && n_ok)) *y = from_f32<T>(f);
+    y += ldy;
   }
 }
 
@@ -227,7 +233,7 @@ row_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant_
     }
   } else {
     // ---------------------------------------------------------------- epilogue
-    constexpr int EC = TN >= 64 ? 32 : 16;              // accumulator columns (tokens) moved at a time
+    constexpr int EC = 16;                              // accumulator columns (tokens) moved at a time
     const int ew = warp - 2, q = warp & 3, part = ew >> 2;   // lanes 32q.. of tensor memory; two warps share a quadrant
     float* sc = scale_buf + ew * L::kWarpTokens;
     const bool pairs = sizeof(T) == 2 && (p.ldy % 2 == 0) && (p.N % 2 == 0) && (reinterpret_cast<uintptr_t>(Y) & 3) == 0;
@@ -273,7 +279,7 @@ row_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant_
             float s4[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) s4[e] = m0 + e < p.M ? __ldcg(p.a_scales + m0 + e) : 0.0f;
-            finish<T, 4>(p, Y, av, s4, m0, n, ws, b, pairs);
+            finish<false, T, 4>(Y + (long long)m0 * p.ldy + n, p.ldy, av, s4, ws, b, p.M - m0, n < p.N, pairs);
           }
         }
         break;   // a K split is used only where every cluster has one tile
@@ -287,21 +293,32 @@ row_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant_
       __syncwarp();
       if (!mbar_wait(accfull_bar(acc), ((uint32_t)j >> 1) & 1u, abort_flag)) break;
       tc_fence_after();
-      for (int c = part * EC, i = 0; c < TN; c += 2 * EC, ++i) {
-        const int m0 = mt * TN + c;
-        if (m0 >= p.M) break;   // warp-uniform
-        uint32_t v[EC];
-        __syncwarp();
-        const uint32_t addr = tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(acc * L::kAccStride + c);
-        if constexpr (EC == 32) tmem_ld32(addr, v);
-        else tmem_ld16(addr, v);
-        float s[EC];
+      // pieces of EC columns; the next one's way out of tensor memory overlaps this one's arithmetic and stores
+      constexpr int kPieces = TN >= 2 * EC ? TN / (2 * EC) : 1;
+      const uint32_t addr = tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(acc * L::kAccStride + part * EC);
+      const bool n_all = (nt * CG + half) * TW + q * 32 + 32 <= p.N;
+      T* y = Y + (long long)(mt * TN + part * EC) * p.ldy + n;
+      int left = p.M - mt * TN - part * EC;   // tokens from this piece's first on
+      uint32_t v[2][EC];
+      if (part * EC < TN && left > 0) {
+        tmem_ld_async<EC>(addr, v[0]);
 #pragma unroll
-        for (int e = 0; e < EC; e += 4) {
-          const float4 f = *reinterpret_cast<const float4*>(sc + i * EC + e);
-          s[e] = f.x; s[e + 1] = f.y; s[e + 2] = f.z; s[e + 3] = f.w;
+        for (int i = 0; i < kPieces; ++i) {
+          if (left <= 0) break;               // the same for the whole warp
+          tmem_wait_ld16(v[i & 1]);
+          if (i + 1 < kPieces && left > 2 * EC) tmem_ld_async<EC>(addr + 2 * EC * (i + 1), v[(i + 1) & 1]);
+          float s[EC];
+#pragma unroll
+          for (int e = 0; e < EC; e += 4) {
+            const float4 f = *reinterpret_cast<const float4*>(sc + i * EC + e);
+            s[e] = f.x; s[e + 1] = f.y; s[e + 2] = f.z; s[e + 3] = f.w;
+          }
+          const int* av = reinterpret_cast<const int*>(v[i & 1]);
+          if (n_all && left >= EC) finish<true, T, EC>(y, p.ldy, av, s, ws, b, left, true, pairs);
+          else finish<false, T, EC>(y, p.ldy, av, s, ws, b, left, n < p.N, pairs);
+          y += 2 * EC * p.ldy;
+          left -= 2 * EC;
         }
-        finish<T, EC>(p, Y, reinterpret_cast<const int*>(v), s, m0, n, ws, b, pairs);
       }
       tc_fence_before();
       __syncwarp();
