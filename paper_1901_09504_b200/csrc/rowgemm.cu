@@ -30,17 +30,21 @@ struct RowSmem {
   static constexpr int kTokens = TN / CG;                       // token rows this CTA stages
   static constexpr int kWBytes = TW * KB, kTBytes = kTokens * KB;
   static constexpr int kStageBytes = kWBytes + kTBytes;
-  static constexpr int kXBytes = TN == 256 ? 0 : TN * TW * 4;   // partial sums of this CTA's share (K split)
+  // partial sums of this CTA's share (K split): a buffer of their own, or the operand ring where it would cost the ring
+  // too many stages
+  static constexpr int kXBytes = TN == 256 ? 0 : TN * TW * 4;
+  static constexpr bool kXInRing = TN == 128;
+  static constexpr int kXExtra = kXInRing ? 0 : kXBytes;
   static constexpr int kWarpTokens = TN < 32 ? 16 : TN / 2;      // columns an epilogue warp finishes
   static constexpr int kScaleBytes = kEpiWarps * kWarpTokens * 4;
   static constexpr int kCtrlBytes = 512;
   static constexpr int kBudget = 227 * 1024 - 1024 - kCtrlBytes - kScaleBytes;
-  static constexpr int kStagesFit = (kBudget - kXBytes) / kStageBytes;
+  static constexpr int kStagesFit = (kBudget - kXExtra) / kStageBytes;
   static constexpr int kStages = kStagesFit < 8 ? kStagesFit : 8;
-  static constexpr int kDynBytes = 1024 + kStages * kStageBytes + kXBytes + kScaleBytes + kCtrlBytes;
+  static constexpr int kDynBytes = 1024 + kStages * kStageBytes + kXExtra + kScaleBytes + kCtrlBytes;
   static constexpr int kAccStride = TN < 32 ? 32 : TN;
   static constexpr uint32_t kTmemCols = 2 * kAccStride;
-  static_assert(kStages >= 3 && kDynBytes <= 227 * 1024 && kTBytes % 1024 == 0, "tile does not fit");
+  static_assert(kStages >= 3 && (!kXInRing || kXBytes <= kStages * kStageBytes) && kDynBytes <= 227 * 1024 && kTBytes % 1024 == 0, "tile does not fit");
 };
 
 __host__ __device__ constexpr uint32_t row_instr_desc(int m, int n, int b_signed) {
@@ -109,17 +113,19 @@ row_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant_
   const uint32_t raw = smem_u32(smem_dyn);
   const uint32_t base = (raw + 1023u) & ~1023u;
   unsigned char* tiles = smem_dyn + (base - raw);
-  unsigned char* xbuf = tiles + L::kStages * L::kStageBytes;
-  float* scale_buf = reinterpret_cast<float*>(xbuf + L::kXBytes);
-  uint64_t* bars = reinterpret_cast<uint64_t*>(xbuf + L::kXBytes + L::kScaleBytes);
+  unsigned char* after = tiles + L::kStages * L::kStageBytes;
+  unsigned char* xbuf = L::kXInRing ? tiles : after;
+  float* scale_buf = reinterpret_cast<float*>(after + L::kXExtra);
+  uint64_t* bars = reinterpret_cast<uint64_t*>(after + L::kXExtra + L::kScaleBytes);
   auto full_bar = [&](int s) { return smem_u32(bars + s); };
   auto empty_bar = [&](int s) { return smem_u32(bars + L::kStages + s); };
   auto accfull_bar = [&](int a) { return smem_u32(bars + 2 * L::kStages + a); };
   auto accempty_bar = [&](int a) { return smem_u32(bars + 2 * L::kStages + 2 + a); };
   const uint32_t xfull_bar = smem_u32(bars + 2 * L::kStages + 4);
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * L::kStages + 5);
+  const uint32_t xready_bar = smem_u32(bars + 2 * L::kStages + 5);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * L::kStages + 6);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
-  static_assert((2 * L::kStages + 5) * 8 + 8 <= L::kCtrlBytes, "control block");
+  static_assert((2 * L::kStages + 6) * 8 + 8 <= L::kCtrlBytes, "control block");
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int CL = CG * p.slices;
@@ -138,6 +144,7 @@ row_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant_
       mbar_init(accempty_bar(a), CG * kEpiWarps);
     }
     mbar_init(xfull_bar, 1);
+    mbar_init(xready_bar, p.slices);
     *abort_flag = 0;
     fence_barrier_init();
     if (L::kXBytes && p.slices > 1) mbar_arrive_expect_tx(xfull_bar, (uint32_t)L::kXBytes);
@@ -252,34 +259,59 @@ row_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant_
         // transaction bytes on the owner's barrier.
         if constexpr (L::kXBytes > 0) {
           const int own = TN / p.slices, groups = own / 4;
+          // the scales of the tokens this CTA finishes, while the main loop runs
+          __syncwarp();
+          for (int i = lane; i < own; i += 32) {
+            const int m = mt * TN + slice * own + i;
+            sc[i] = m < p.M ? __ldcg(p.a_scales + m) : 0.0f;
+          }
+          __syncwarp();
           if (!mbar_wait(accfull_bar(acc), ((uint32_t)j >> 1) & 1u, abort_flag)) break;
           tc_fence_after();
-          for (int c = part * 16; c < TN; c += 32) {
-            uint32_t v[16];
+          if (L::kXInRing) {
+            // this CTA's tensor cores are done with its ring: it may be written to; and so are all the others'
+            if (ew == 0 && lane == 0)
+              for (int o = 0; o < p.slices; ++o) mbar_arrive_peer(peer_addr(xready_bar, (uint32_t)(o * CG + half)));
+            if (!mbar_wait_cluster(xready_bar, 0u, abort_flag)) break;
+          }
+          const uint32_t mine = smem_u32(xbuf) + (uint32_t)(slice * groups * TW + q * 32 + lane) * 16u;
+          const uint32_t addr = tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(acc * L::kAccStride);
+          uint32_t v[2][16];
+          constexpr int kPieces = TN >= 32 ? TN / 32 : 1;
+          if (part * 16 < TN) {
             __syncwarp();
-            tmem_ld16(tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(acc * L::kAccStride + c), v);
+            tmem_ld_async<16>(addr + part * 16, v[0]);
 #pragma unroll
-            for (int e = 0; e < 16; e += 4) {
-              const int owner = (c + e) / own, g = ((c + e) - owner * own) / 4;
-              const uint32_t cell = smem_u32(xbuf) + (uint32_t)((slice * groups + g) * TW + q * 32 + lane) * 16u;
-              const uint32_t peer = (uint32_t)(owner * CG + half);
-              st_async_v4(peer_addr(cell, peer), make_uint4(v[e], v[e + 1], v[e + 2], v[e + 3]), peer_addr(xfull_bar, peer));
+            for (int i = 0; i < kPieces; ++i) {
+              tmem_wait_ld16(v[i & 1]);
+              if (i + 1 < kPieces) tmem_ld_async<16>(addr + part * 16 + 32 * (i + 1), v[(i + 1) & 1]);
+              const uint32_t* w = v[i & 1];
+#pragma unroll
+              for (int e = 0; e < 16; e += 4) {
+                const int col = part * 16 + 32 * i + e;
+                const int owner = col / own, g = (col - owner * own) / 4;
+                const uint32_t peer = (uint32_t)(owner * CG + half);
+                st_async_v4(peer_addr(mine + (uint32_t)g * (TW * 16u), peer), make_uint4(w[e], w[e + 1], w[e + 2], w[e + 3]),
+                            peer_addr(xfull_bar, peer));
+              }
             }
           }
           if (!mbar_wait_cluster(xfull_bar, 0u, abort_flag)) break;
+          const int m_own = mt * TN + slice * own;
+          T* y = Y + (long long)m_own * p.ldy + n;
+          const uint32_t slot = (uint32_t)groups * TW * 16u;   // from one sender's cells to the next one's
           for (int g = part; g < groups; g += 2) {
             const unsigned char* cell = xbuf + (size_t)(g * TW + q * 32 + lane) * 16;
             int4 a = *reinterpret_cast<const int4*>(cell);
+#pragma unroll 4
             for (int sl = 1; sl < p.slices; ++sl) {
-              const int4 v = *reinterpret_cast<const int4*>(cell + (size_t)sl * groups * TW * 16);
-              a.x += v.x; a.y += v.y; a.z += v.z; a.w += v.w;
+              const int4 b4 = *reinterpret_cast<const int4*>(cell + sl * slot);
+              a.x += b4.x; a.y += b4.y; a.z += b4.z; a.w += b4.w;
             }
-            const int m0 = mt * TN + slice * own + g * 4;
             const int av[4] = {a.x, a.y, a.z, a.w};
-            float s4[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) s4[e] = m0 + e < p.M ? __ldcg(p.a_scales + m0 + e) : 0.0f;
-            finish<false, T, 4>(Y + (long long)m0 * p.ldy + n, p.ldy, av, s4, ws, b, p.M - m0, n < p.N, pairs);
+            const float4 s4 = *reinterpret_cast<const float4*>(sc + 4 * g);
+            const float sv[4] = {s4.x, s4.y, s4.z, s4.w};
+            finish<false, T, 4>(y + 4 * g * p.ldy, p.ldy, av, sv, ws, b, p.M - m_own - 4 * g, n < p.N, pairs);
           }
         }
         break;   // a K split is used only where every cluster has one tile
