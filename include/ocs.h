@@ -473,7 +473,7 @@ ocs_status ocs_linear_rows(const void* X, ocs_dtype x_type, int M, int C, int64_
                            int* dev_status, void* stream);
 
 /* ocs_selftest_force_row_plan (for tests): ocs_qlinear_rows / ocs_linear_rows choose how many tokens a tile has (tn in
- * {16, 32, 64, 128, 256}), whether two CTAs share a tensor-core tile (cg in {1, 2}; 2 from 128 tokens on) and how many
+ * {16, 32, 64, 128, 256}), whether two CTAs share a tensor-core tile (cg in {1, 2}; 2 with 256 tokens only) and how many
  * split its contraction (slices in {1, 2, 4, 8}, lowered until it fits the problem).  The outputs must not depend on
  * it.  This process-wide hook fixes the choice for the following calls; tn = 0 returns it to the planner.  Host call. */
 ocs_status ocs_selftest_force_row_plan(int tn, int cg, int slices);
