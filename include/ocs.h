@@ -451,8 +451,8 @@ ocs_status ocs_quantize_rows(const void* X, ocs_dtype x_type, int64_t rows, int 
 /* ocs_qlinear_rows --------------------------------------------------------------------------
  * The integer layer with a scale per token and per output channel:
  *     acc[m][n] = sum_{k < K} A[m][k] * Wc[n][k]                                 (int32, exact)
- *     Y[m][n]   = fmaf((float)acc[m][n], a_scales[m] * w_scales[n], bias[n])     (bias 0 if NULL)
- * rounded once more to y_type.  A codes [M][K] (uint8 when a_signed = 0 else int8), row stride lda bytes;
+ *     Y[m][n]   = fmaf((float)acc[m][n] * a_scales[m], w_scales[n], bias[n])     (bias 0 if NULL)
+ * the conversion, the product and the fused rest rounded once each, and once more to y_type.  A codes [M][K] (uint8 when a_signed = 0 else int8), row stride lda bytes;
  * Wc int8 [N][K], row stride ldw bytes; both 16-byte aligned with strides that are multiples of 16;
  * a_scales fp32 [M], w_scales fp32 [N], bias fp32 [N]; Y [M][N] of y_type, row stride ldy elements.
  * M = 0 is a no-op.  Limits: K * 128 * (a_signed ? 128 : 255) must fit int32, M < 2^30.
@@ -462,11 +462,13 @@ ocs_status ocs_qlinear_rows(const void* A_codes, int a_signed, const float* a_sc
                             void* Y, ocs_dtype y_type, int64_t ldy, int* dev_status, void* stream);
 
 /* ocs_linear_rows ---------------------------------------------------------------------------
- * ocs_quantize_rows on X followed by ocs_qlinear_rows on its codes (K = C + S), in one call: the codes and
- * token scales live in the workspace and the product's launch overlaps the quantization.  Bit-identical to
- * the two calls.  Workspace: ocs_linear_rows_workspace_bytes(M, C, S).  Arguments, limits and device flags
- * of the two calls. */
-size_t ocs_linear_rows_workspace_bytes(int M, int C, int S);
+ * ocs_quantize_rows on X followed by ocs_qlinear_rows on its codes (K = C + S), in one call, bit-identical to
+ * the two.  Few tokens, in rows that are 8-byte aligned, are quantized inside the product's kernel (one launch);
+ * otherwise codes and token scales live in the workspace and the product's launch overlaps the quantization.
+ * Workspace: ocs_linear_rows_workspace_bytes (of the same X: only its alignment counts); 0 means none is
+ * needed and ws may be NULL.  Arguments, limits and device flags of the two calls. */
+size_t ocs_linear_rows_workspace_bytes(const void* X, ocs_dtype x_type, int M, int C, int64_t ldx, int S, int N,
+                                       ocs_dtype y_type);
 ocs_status ocs_linear_rows(const void* X, ocs_dtype x_type, int M, int C, int64_t ldx, int S, const int32_t* idx_map,
                            int bits, int is_signed, const int8_t* W_codes, const float* w_scales, int N, int64_t ldw,
                            const float* bias, void* Y, ocs_dtype y_type, int64_t ldy, void* ws, size_t ws_bytes,

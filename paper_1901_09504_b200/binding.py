@@ -48,7 +48,7 @@ _P, _I, _L, _F = C.c_void_p, C.c_int, C.c_int64, C.c_float
 _ARGTYPES = {
     "ocs_quantize_rows": [_P, _I, _L, _I, _L, _I, _P, _I, _I, _P, _L, _P, _P, _P],
     "ocs_qlinear_rows": [_P, _I, _P, _I, _I, _L, _P, _P, _I, _L, _P, _P, _I, _L, _P, _P],
-    "ocs_linear_rows_workspace_bytes": [_I, _I, _I],
+    "ocs_linear_rows_workspace_bytes": [_P, _I, _I, _I, _L, _I, _I, _I],
     "ocs_linear_rows": [_P, _I, _I, _I, _L, _I, _P, _I, _I, _P, _P, _I, _L, _P, _P, _I, _L, _P, C.c_size_t, _P, _P],
     "ocs_token_logprobs": [_P, _I, _L, _I, _L, _P, _F, _I, _P, _P, _P, _P, _P, _P, _P],
     "ocs_token_logprobs_backward": [_P, _I, _L, _I, _L, _P, _F, _P, _P, _P, _P, _L, _P, _P],
@@ -689,11 +689,14 @@ def ocs_linear_rows(x, W_codes, w_scales, idx_map=None, S: int = 0, bits: int = 
         out = torch.empty((M, N), dtype=x.dtype if out_dtype is None else out_dtype, device=x.device)
     assert out.is_cuda and out.dtype in DTYPES and out.shape == (M, N)
     L = lib()
+    xt, yt = DTYPES[x.dtype], DTYPES[out.dtype]
     if ws is None:
-        ws = torch.empty(L.ocs_linear_rows_workspace_bytes(M, Cn, S), dtype=torch.uint8, device=x.device)
-    st = L.ocs_linear_rows(x.data_ptr(), DTYPES[x.dtype], M, Cn, ldx, S, _addr(idx_map), int(bits), 1 if is_signed else 0,
-                           W_codes.data_ptr(), w_scales.data_ptr(), N, ldw, _addr(bias), out.data_ptr(), DTYPES[out.dtype],
-                           _rows_of(out), ws.data_ptr(), ws.numel(), _addr(dev_status), _raw_stream(x))
+        n_ws = L.ocs_linear_rows_workspace_bytes(x.data_ptr(), xt, M, Cn, ldx, S, N, yt)
+        if n_ws:
+            ws = torch.empty(n_ws, dtype=torch.uint8, device=x.device)
+    st = L.ocs_linear_rows(x.data_ptr(), xt, M, Cn, ldx, S, _addr(idx_map), int(bits), 1 if is_signed else 0,
+                           W_codes.data_ptr(), w_scales.data_ptr(), N, ldw, _addr(bias), out.data_ptr(), yt,
+                           _rows_of(out), _addr(ws), 0 if ws is None else ws.numel(), _addr(dev_status), _raw_stream(x))
     _check(st, "ocs_linear_rows")
     return out
 
@@ -707,15 +710,16 @@ def ocs_selftest_force_row_plan(tn: int = 0, cg: int = 1, slices: int = 1):
 class TokenLogprobs(NamedTuple):
     """What ocs_token_logprobs returns; a part that was not asked for is None."""
     logprob: torch.Tensor | None       # fp32 [rows]: ln p of the given tokens
-    entropy: torch.Tensor              # fp32 [rows]
+    entropy: torch.Tensor | None       # fp32 [rows]
     top_ids: torch.Tensor | None       # int32 [rows, top_k], likeliest first
     top_logprob: torch.Tensor | None   # fp32 [rows, top_k]
-    stats: torch.Tensor                # fp32 [rows, 4], for ocs_token_logprobs_backward
+    stats: torch.Tensor | None         # fp32 [rows, 4], for ocs_token_logprobs_backward
 
 
-def ocs_token_logprobs(logits, targets=None, top_k: int = 0, inv_temperature: float = 1.0, out: TokenLogprobs | None = None,
-                       dev_status=None) -> TokenLogprobs:
-    """logits fp32 / fp16 / bf16 [rows, V], targets int32 [rows] (negative: no given token) -> TokenLogprobs."""
+def ocs_token_logprobs(logits, targets=None, top_k: int = 0, inv_temperature: float = 1.0, want_stats: bool = False,
+                       out: TokenLogprobs | None = None, dev_status=None) -> TokenLogprobs:
+    """logits fp32 / fp16 / bf16 [rows, V], targets int32 [rows] (negative: no given token) -> TokenLogprobs.
+    want_stats: also what the gradient needs.  `out`: tensors to write to; its parts that are None are left out."""
     assert logits.is_cuda and logits.dtype in DTYPES
     ld = _rows_of(logits)
     rows, V = logits.shape
@@ -723,12 +727,12 @@ def ocs_token_logprobs(logits, targets=None, top_k: int = 0, inv_temperature: fl
                                and targets.numel() >= rows)
     k = int(top_k)
     if out is None:
-        dev = logits.device
-        # one allocation for the floats: statistics first (16 bytes a row), then entropy, logprob, alternatives
-        buf = torch.empty(rows * (6 + max(k, 0)), dtype=torch.float32, device=dev)
-        out = TokenLogprobs(buf[5 * rows:6 * rows] if targets is not None else None, buf[4 * rows:5 * rows],
+        dev, f32 = logits.device, torch.float32
+        out = TokenLogprobs(torch.empty(rows, dtype=f32, device=dev) if targets is not None else None,
+                            torch.empty(rows, dtype=f32, device=dev),
                             torch.empty((rows, k), dtype=torch.int32, device=dev) if k > 0 else None,
-                            buf[6 * rows:].view(rows, k) if k > 0 else None, buf[:4 * rows].view(rows, 4))
+                            torch.empty((rows, k), dtype=f32, device=dev) if k > 0 else None,
+                            torch.empty((rows, 4), dtype=f32, device=dev) if want_stats else None)
     else:
         _check_vec(out.logprob, rows), _check_vec(out.entropy, rows), _check_vec(out.top_logprob, rows * k)
         _check_vec(out.stats, 4 * rows)

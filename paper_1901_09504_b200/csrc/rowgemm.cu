@@ -12,6 +12,7 @@ constexpr int KB = 128;        // contraction bytes of a K-block: one 128-byte s
 constexpr int UK = 32;         // contraction indices of one tcgen05.mma.kind::i8
 constexpr int kThreads = 320;  // copy warp, tensor-core warp, 8 epilogue warps
 constexpr int kEpiWarps = 8;
+constexpr int kFusedCodes = 64 * 1024;         // token codes a CTA can hold beside the ring of weights
 
 struct RowGemm {
   int M, N, num_kb, t_signed;
@@ -22,14 +23,22 @@ struct RowGemm {
   const float* bias;
   long long ldy;
   int* dev_status;
+  // tokens that are quantized here (FUSED): unquantized rows and what ocs_quantize_rows takes
+  const void* X;
+  long long ldx;
+  const int32_t* idx_map;
+  int x_type, x_align, C, K;
+  float hi;
 };
 
 // TN tokens, CG CTAs per tensor-core tile
-template <int TN, int CG>
+template <int TN, int CG, bool FUSED>
 struct RowSmem {
   static constexpr int kTokens = TN / CG;                       // token rows this CTA stages
   static constexpr int kWBytes = TW * KB, kTBytes = kTokens * KB;
-  static constexpr int kStageBytes = kWBytes + kTBytes;
+  static constexpr int kStageBytes = FUSED ? kWBytes : kWBytes + kTBytes;
+  // FUSED: the codes of all the K-blocks a CTA takes stay in a region of their own
+  static constexpr int kTokenBytes = FUSED ? kFusedCodes : 0;
   // partial sums of this CTA's share (K split): a buffer of their own, or the operand ring where it would cost the ring
   // too many stages
   static constexpr int kXBytes = TN == 256 ? 0 : TN * TW * 4;
@@ -38,10 +47,11 @@ struct RowSmem {
   static constexpr int kWarpTokens = TN < 32 ? 16 : TN / 2;      // columns an epilogue warp finishes
   static constexpr int kScaleBytes = kEpiWarps * kWarpTokens * 4;
   static constexpr int kCtrlBytes = 512;
-  static constexpr int kBudget = 227 * 1024 - 1024 - kCtrlBytes - kScaleBytes;
+  static constexpr int kRowBytes = FUSED ? TN * 12 : 0;            // a row's maximum, scale and 1 / step
+  static constexpr int kBudget = 227 * 1024 - 1024 - kCtrlBytes - kScaleBytes - kRowBytes - kTokenBytes;
   static constexpr int kStagesFit = (kBudget - kXExtra) / kStageBytes;
   static constexpr int kStages = kStagesFit < 8 ? kStagesFit : 8;
-  static constexpr int kDynBytes = 1024 + kStages * kStageBytes + kXExtra + kScaleBytes + kCtrlBytes;
+  static constexpr int kDynBytes = 1024 + kStages * kStageBytes + kTokenBytes + kXExtra + kScaleBytes + kRowBytes + kCtrlBytes;
   static constexpr int kAccStride = TN < 32 ? 32 : TN;
   static constexpr uint32_t kTmemCols = 2 * kAccStride;
   static_assert(kStages >= 3 && (!kXInRing || kXBytes <= kStages * kStageBytes) && kDynBytes <= 227 * 1024 && kTBytes % 1024 == 0, "tile does not fit");
@@ -68,9 +78,10 @@ template <typename T> struct Pair;
 template <> struct Pair<__half> { static __device__ __forceinline__ uint32_t pack(float a, float b) { __half2 h = __floats2half2_rn(a, b); return *reinterpret_cast<uint32_t*>(&h); } };
 template <> struct Pair<__nv_bfloat16> { static __device__ __forceinline__ uint32_t pack(float a, float b) { __nv_bfloat162 h = __floats2bfloat162_rn(a, b); return *reinterpret_cast<uint32_t*>(&h); } };
 
-// One output: float(acc) * (a_scale * w_scale) + bias, each step rounded once.
+// One output: (float(acc) * a_scale) * w_scale + bias; the conversion, the first product and the fused rest round once each.
+// (The accumulator comes first: the two scales' product alone may leave fp32's normal range for rows of tiny values.)
 __device__ __forceinline__ float one_output(int acc, float as, float ws, float b) {
-  return fmaf(__int2float_rn(acc), __fmul_rn(as, ws), b);
+  return fmaf(__fmul_rn(__int2float_rn(acc), as), ws, b);
 }
 
 // CNT consecutive tokens of one channel per lane, rounded to T and stored; the lanes of the warp hold consecutive
@@ -104,28 +115,146 @@ __device__ __forceinline__ void finish(T* y, long long ldy, const int* acc, cons
   }
 }
 
-template <typename T, int TN, int CG>
+// Four consecutive elements of a row, 8-byte aligned (wide: 16-byte).
+template <typename T>
+struct Four {
+  uint32_t w[sizeof(T)];
+  __device__ __forceinline__ void load(const T* x, bool wide) {
+    if constexpr (sizeof(T) == 2) {
+      const uint2 v = __ldg(reinterpret_cast<const uint2*>(x));
+      w[0] = v.x; w[1] = v.y;
+    } else if (wide) {
+      const uint4 v = __ldg(reinterpret_cast<const uint4*>(x));
+      w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+    } else {
+      const uint2 v = __ldg(reinterpret_cast<const uint2*>(x)), u = __ldg(reinterpret_cast<const uint2*>(x) + 1);
+      w[0] = v.x; w[1] = v.y; w[2] = u.x; w[3] = u.y;
+    }
+  }
+  __device__ __forceinline__ float operator[](int i) const { return to_f32(reinterpret_cast<const T*>(w)[i]); }
+};
+
+// One value's code: ocs_quantize_rows' arithmetic for a row with maximum bits `max_bits`.
+__device__ __forceinline__ int token_code(float x, float inv, uint32_t max_bits, int is_signed) {
+  const float v = __uint_as_float(max_bits) < 0x1p-100f ? __fmul_rn(x, 0x1p64f) : x;
+  return is_signed ? row_code<true>(v, inv) : row_code<false>(v, inv);
+}
+
+// The epilogue warps quantize the token tile that starts at row m0 straight into the operand tiles of K-blocks slice,
+// slice + slices, ...: first the rows' maxima, 512 elements per warp and step, then the codes, one row of a K-block per
+// warp and step.  What does not come in whole fours of channels goes one by one: a row's last C % 4 channels and the
+// duplicated ones (item u: contraction index C4 + u / rows of row u % rows; the first item's value is on its way from the
+// start).  The latency of the loads is what this costs, so the loads of four steps are issued before the first is used.
+template <typename X, int TN>
+__device__ __forceinline__ void quantize_tokens(const RowGemm& p, const X* x0, int m0, int slice, int my_kb, unsigned char* tok,
+                                                uint32_t* max_bits, float* scale, float* inv) {
+  constexpr int B = 4;
+  const int et = threadIdx.x - 64, warp = et >> 5, lane = et & 31;
+  const int rows = min(TN, p.M - m0), C4 = p.C & ~3, n_items = rows * (p.K - C4);
+  const bool wide = p.x_align >= 16;
+  int src = 0;
+  if (et < n_items) {
+    src = C4 + et / rows;
+    if (src >= p.C) src = __ldg(p.idx_map + src);
+  }
+  if (et < TN) max_bits[et] = 0;
+  asm volatile("bar.sync 1, 256;" ::: "memory");
+  const int chunks = (C4 + 511) / 512, units = rows * chunks;
+  for (int u0 = warp; u0 < units; u0 += B * kEpiWarps) {
+    Four<X> f[B][4];
+#pragma unroll
+    for (int b = 0; b < B; ++b) {
+      const int u = min(u0 + b * kEpiWarps, units - 1), r = u / chunks, c = (u - r * chunks) * 512 + lane * 4;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) f[b][j].load(x0 + r * p.ldx + min(c + 128 * j, C4 - 4), wide);   // (twice at the end: harmless)
+    }
+#pragma unroll
+    for (int b = 0; b < B; ++b) {
+      const int u = u0 + b * kEpiWarps;
+      uint32_t m = 0;
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) m = max(m, __float_as_uint(f[b][j][i]) & 0x7fffffffu);
+      m = __reduce_max_sync(0xffffffffu, m);
+      if (lane == 0 && u < units) atomicMax(max_bits + u / chunks, m);
+    }
+  }
+  float value = 0.0f;
+  if (et < n_items) {
+    if ((unsigned)src >= (unsigned)p.C) { flag(p.dev_status, OCS_DEV_BAD_INDEX); src = 0; }
+    value = to_f32(x0[(et % rows) * p.ldx + src]);
+    if (C4 + et / rows < p.C) atomicMax(max_bits + et % rows, __float_as_uint(value) & 0x7fffffffu);   // (all of these are first items)
+  }
+  asm volatile("bar.sync 1, 256;" ::: "memory");
+  if (et < rows) {
+    const float alpha = __uint_as_float(max_bits[et]);
+    scale[et] = __fdiv_rn(alpha, p.hi);
+    inv[et] = row_grid(alpha, p.hi).inv;
+    if (max_bits[et] >= 0x7f800000u) flag(p.dev_status, OCS_DEV_NONFINITE);
+  }
+  asm volatile("bar.sync 1, 256;" ::: "memory");
+  const int steps = C4 > 0 ? my_kb * rows : 0;
+  for (int u0 = warp; u0 < steps; u0 += B * kEpiWarps) {
+    Four<X> f[B];
+#pragma unroll
+    for (int b = 0; b < B; ++b) {
+      const int u = min(u0 + b * kEpiWarps, steps - 1), i = u / rows, r = u - i * rows;
+      f[b].load(x0 + r * p.ldx + min((slice + i * p.slices) * KB + lane * 4, C4 - 4), wide);
+    }
+#pragma unroll
+    for (int b = 0; b < B; ++b) {
+      const int u = u0 + b * kEpiWarps, i = u / rows, r = u - i * rows, k = (slice + i * p.slices) * KB + lane * 4;
+      if (u < steps && k < C4) {   // past the last contraction index the weights' tile is zero
+        int c[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) c[e] = token_code(f[b][e], inv[r], max_bits[r], p.t_signed);
+        *reinterpret_cast<uint32_t*>(tok + (size_t)(i * TN + r) * KB + (((lane >> 2) ^ (r & 7)) << 4) + (lane & 3) * 4) =
+            pack4(c[0], c[1], c[2], c[3]);
+      }
+    }
+  }
+  for (int u = et; u < n_items; u += 256) {
+    const int d = u / rows, r = u - d * rows, k = C4 + d, kb = k / KB;
+    if (kb % p.slices != slice) continue;
+    if (u != et) {
+      src = __ldg(p.idx_map + k);
+      if ((unsigned)src >= (unsigned)p.C) { flag(p.dev_status, OCS_DEV_BAD_INDEX); src = 0; }
+      value = to_f32(x0[r * p.ldx + src]);
+    }
+    const int i = kb / p.slices, in = k % KB;
+    tok[(size_t)(i * TN + r) * KB + (((in >> 4) ^ (r & 7)) << 4) + (in & 15)] =
+        (unsigned char)token_code(value, inv[r], max_bits[r], p.t_signed);
+  }
+  fence_proxy_async_smem();   // the tensor cores read what these threads wrote
+}
+
+template <typename T, int TN, int CG, bool FUSED>
 __global__ void __launch_bounds__(kThreads, 1)
 row_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtensorMap tm_t, const RowGemm p,
                 T* __restrict__ Y) {
-  using L = RowSmem<TN, CG>;
+  using L = RowSmem<TN, CG, FUSED>;
   extern __shared__ unsigned char smem_dyn[];
   const uint32_t raw = smem_u32(smem_dyn);
   const uint32_t base = (raw + 1023u) & ~1023u;
   unsigned char* tiles = smem_dyn + (base - raw);
-  unsigned char* after = tiles + L::kStages * L::kStageBytes;
+  unsigned char* tokens = tiles + L::kStages * L::kStageBytes;
+  unsigned char* after = tokens + L::kTokenBytes;
   unsigned char* xbuf = L::kXInRing ? tiles : after;
   float* scale_buf = reinterpret_cast<float*>(after + L::kXExtra);
-  uint64_t* bars = reinterpret_cast<uint64_t*>(after + L::kXExtra + L::kScaleBytes);
+  uint32_t* row_max = reinterpret_cast<uint32_t*>(after + L::kXExtra + L::kScaleBytes);   // FUSED: [TN] maxima, scales, inv
+  float* row_scale = reinterpret_cast<float*>(row_max + TN);
+  uint64_t* bars = reinterpret_cast<uint64_t*>(after + L::kXExtra + L::kScaleBytes + L::kRowBytes);
   auto full_bar = [&](int s) { return smem_u32(bars + s); };
   auto empty_bar = [&](int s) { return smem_u32(bars + L::kStages + s); };
   auto accfull_bar = [&](int a) { return smem_u32(bars + 2 * L::kStages + a); };
   auto accempty_bar = [&](int a) { return smem_u32(bars + 2 * L::kStages + 2 + a); };
   const uint32_t xfull_bar = smem_u32(bars + 2 * L::kStages + 4);
   const uint32_t xready_bar = smem_u32(bars + 2 * L::kStages + 5);
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * L::kStages + 6);
+  const uint32_t tok_bar = smem_u32(bars + 2 * L::kStages + 6);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * L::kStages + 7);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
-  static_assert((2 * L::kStages + 6) * 8 + 8 <= L::kCtrlBytes, "control block");
+  static_assert((2 * L::kStages + 7) * 8 + 8 <= L::kCtrlBytes, "control block");
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int CL = CG * p.slices;
@@ -134,32 +263,60 @@ row_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant_
   const int cluster = blockIdx.x / CL, n_clusters = gridDim.x / CL;
   const int my_kb = (p.num_kb - slice + p.slices - 1) / p.slices;
 
-  if (threadIdx.x == 0) {
-    for (int s = 0; s < L::kStages; ++s) {
-      mbar_init(full_bar(s), 1);     // the leader's producer announces the bytes of both CTAs
-      mbar_init(empty_bar(s), 1);    // commit of the MMAs that read the stage
+  // Set-up.  Nobody waits for more than it needs: the copy warp asks for the first weights as soon as its own barriers
+  // stand, the tensor-core warp needs these barriers, the epilogue warps the address in tensor memory as well -- after
+  // they have quantized the tokens, where that is theirs to do.  (Named barriers: 2 = set up, 3 = barriers stand.)  A peer
+  // may be written to once all threads of the cluster have arrived; a pair waits for that at once, the others where they
+  // first need it.
+  if (warp == 0) {
+    if (lane == 0) {
+      prefetch_tmap(&tm_w);
+      if (!FUSED) prefetch_tmap(&tm_t);
+      for (int s = 0; s < L::kStages; ++s) {
+        mbar_init(full_bar(s), 1);     // the leader's producer announces the bytes of both CTAs
+        mbar_init(empty_bar(s), 1);    // commit of the MMAs that read the stage
+      }
+      for (int a = 0; a < 2; ++a) {
+        mbar_init(accfull_bar(a), 1);
+        mbar_init(accempty_bar(a), CG * kEpiWarps);
+      }
+      mbar_init(xfull_bar, 1);
+      mbar_init(xready_bar, p.slices);
+      mbar_init(tok_bar, kEpiWarps);
+      *abort_flag = 0;
+      fence_barrier_init();
+      fence_proxy_async_smem();
+      if (L::kXBytes && p.slices > 1) mbar_arrive_expect_tx(xfull_bar, (uint32_t)L::kXBytes);
     }
-    for (int a = 0; a < 2; ++a) {
-      mbar_init(accfull_bar(a), 1);
-      mbar_init(accempty_bar(a), CG * kEpiWarps);
-    }
-    mbar_init(xfull_bar, 1);
-    mbar_init(xready_bar, p.slices);
-    *abort_flag = 0;
-    fence_barrier_init();
-    if (L::kXBytes && p.slices > 1) mbar_arrive_expect_tx(xfull_bar, (uint32_t)L::kXBytes);
-    prefetch_tmap(&tm_w);
-    prefetch_tmap(&tm_t);
-  }
-  if (warp == 1) {
+    __syncwarp();
+    asm volatile("bar.arrive 3, 64;" ::: "memory");
+    asm volatile("bar.arrive 2, 320;" ::: "memory");
+    if (CL > 1) cluster_arrive();
+  } else if (warp == 1) {
     if (CG == 2) tmem_alloc_pair(smem_u32(tmem_slot), L::kTmemCols);
     else tmem_alloc(smem_u32(tmem_slot), L::kTmemCols);
+    tc_fence_before();
+    asm volatile("bar.arrive 2, 320;" ::: "memory");
+    if (CL > 1) cluster_arrive();
+    asm volatile("bar.sync 3, 64;" ::: "memory");
+  } else {
+    if (CL > 1) cluster_arrive();
+    if (FUSED) {
+      // every tile of this CTA has the same tokens; they need nothing of the set-up
+      int mt, nt;
+      tile_of(p, cluster, &mt, &nt);
+      const long long at = (long long)mt * TN * p.ldx;
+      float* inv = row_scale + TN;
+      if (p.x_type == OCS_F32) quantize_tokens<float, TN>(p, static_cast<const float*>(p.X) + at, mt * TN, slice, my_kb, tokens, row_max, row_scale, inv);
+      else if (p.x_type == OCS_F16) quantize_tokens<__half, TN>(p, static_cast<const __half*>(p.X) + at, mt * TN, slice, my_kb, tokens, row_max, row_scale, inv);
+      else quantize_tokens<__nv_bfloat16, TN>(p, static_cast<const __nv_bfloat16*>(p.X) + at, mt * TN, slice, my_kb, tokens, row_max, row_scale, inv);
+      __syncwarp();
+    }
+    asm volatile("bar.sync 2, 320;" ::: "memory");
   }
-  tc_fence_before();
-  __syncthreads();
-  if (CL > 1) cluster_sync_all();   // no peer touches our barriers before they are set up
+  if (CG == 2) cluster_wait();
   tc_fence_after();
-  const uint32_t tmem_base = *tmem_slot;
+  const uint32_t tmem_base = warp == 0 ? 0u : *reinterpret_cast<volatile uint32_t*>(tmem_slot);
 
   if (warp == 0) {
     // ---------------------------------------------------------------- copies
@@ -187,7 +344,7 @@ row_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant_
           load_w(i, slice + i * p.slices);
         }
       }
-      grid_wait_previous();
+      if (!FUSED) grid_wait_previous();
       for (int t = cluster; ok && t < p.total; t += n_clusters) {
         tile_of(p, t, &mt, &nt);
         for (int i = 0; i < my_kb; ++i, ++it) {
@@ -197,7 +354,7 @@ row_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant_
             if (half == 0) mbar_arrive_expect_tx(full_bar(s), CG * L::kStageBytes);
             load_w(s, slice + i * p.slices);
           }
-          load_t(s, slice + i * p.slices);
+          if (!FUSED) load_t(s, slice + i * p.slices);
         }
       }
       // every commit has arrived (also those the other CTA of a pair sends here) before the CTA may leave
@@ -206,6 +363,8 @@ row_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant_
       if (*abort_flag)   // copies that are still in flight land before the CTA's shared memory is released
         for (int i = 0; i < 2000; ++i) __nanosleep(100);
     }
+    __syncwarp();
+    if (CL > 1 && CG == 1) cluster_wait();
   } else if (warp == 1) {
     // ---------------------------------------------------------------- tensor cores
     if (lane == 0 && half == 0) {
@@ -214,6 +373,7 @@ row_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant_
       const uint16_t mask = (uint16_t)(3u << (rank & ~1));
       int it = 0, j = 0;
       bool ok = true;
+      if (FUSED) ok = mbar_wait(tok_bar, 0u, abort_flag);   // the tokens' codes are in place
       for (int t = cluster; ok && t < p.total; t += n_clusters, ++j) {
         const int acc = j & 1;
         if (!mbar_wait_cluster(accempty_bar(acc), (((uint32_t)j >> 1) & 1u) ^ 1u, abort_flag)) break;
@@ -223,7 +383,8 @@ row_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant_
           const int s = it % L::kStages;
           if (!mbar_wait(full_bar(s), (uint32_t)(it / L::kStages) & 1u, abort_flag)) { ok = false; break; }
           tc_fence_after();
-          const uint32_t w = base + s * L::kStageBytes, x = w + L::kWBytes;
+          const uint32_t w = base + s * L::kStageBytes;
+          const uint32_t x = FUSED ? smem_u32(tokens) + (uint32_t)i * L::kTBytes : w + L::kWBytes;
 #pragma unroll
           for (int k = 0; k < KB / UK; ++k) {
             const uint32_t more = (i > 0 || k > 0) ? 1u : 0u;
@@ -238,13 +399,20 @@ row_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant_
         else umma_commit(accfull_bar(acc));
       }
     }
+    __syncwarp();
+    if (CL > 1 && CG == 1) cluster_wait();
   } else {
     // ---------------------------------------------------------------- epilogue
     constexpr int EC = 16;                              // accumulator columns (tokens) moved at a time
     const int ew = warp - 2, q = warp & 3, part = ew >> 2;   // lanes 32q.. of tensor memory; two warps share a quadrant
     float* sc = scale_buf + ew * L::kWarpTokens;
     const bool pairs = sizeof(T) == 2 && (p.ldy % 2 == 0) && (p.N % 2 == 0) && (reinterpret_cast<uintptr_t>(Y) & 3) == 0;
-    grid_wait_previous();
+    if (FUSED) {
+      if (lane == 0) mbar_arrive(tok_bar);   // this warp's codes are in place
+    } else {
+      grid_wait_previous();
+    }
+    if (CL > 1 && CG == 1) cluster_wait();
     int j = 0;
     for (int t = cluster; t < p.total; t += n_clusters, ++j) {
       int mt, nt;
@@ -263,7 +431,7 @@ row_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant_
           __syncwarp();
           for (int i = lane; i < own; i += 32) {
             const int m = mt * TN + slice * own + i;
-            sc[i] = m < p.M ? __ldcg(p.a_scales + m) : 0.0f;
+            sc[i] = m < p.M ? (FUSED ? row_scale[slice * own + i] : __ldcg(p.a_scales + m)) : 0.0f;
           }
           __syncwarp();
           if (!mbar_wait(accfull_bar(acc), ((uint32_t)j >> 1) & 1u, abort_flag)) break;
@@ -319,8 +487,8 @@ row_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant_
       // the token scales of this warp's columns: fetched while the main loop runs
       __syncwarp();
       for (int i = lane; i < L::kWarpTokens; i += 32) {
-        const int m = mt * TN + (i / EC) * 2 * EC + part * EC + i % EC;
-        sc[i] = m < p.M ? __ldcg(p.a_scales + m) : 0.0f;
+        const int col = (i / EC) * 2 * EC + part * EC + i % EC, m = mt * TN + col;
+        sc[i] = m < p.M ? (FUSED ? row_scale[col] : __ldcg(p.a_scales + m)) : 0.0f;
       }
       __syncwarp();
       if (!mbar_wait(accfull_bar(acc), ((uint32_t)j >> 1) & 1u, abort_flag)) break;
@@ -374,6 +542,8 @@ row_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant_
 }
 
 // ------------------------------------------------------------------------------------------------ host
+constexpr long long kFuseBytes = 96 * 1024;   // bytes of unquantized tokens a CTA reads itself
+
 struct RowPlan {
   int tn, cg, slices;
 };
@@ -427,15 +597,15 @@ RowPlan choose_plan(int M, int N, int num_kb, int out_bytes) {
   return best;
 }
 
-template <typename T, int TN, int CG>
+template <typename T, int TN, int CG, bool FUSED = false>
 ocs_status launch_tiles(RowGemm p, int slices, const void* A, long long lda, const int8_t* W, long long ldw, int K, T* Y,
                         bool overlap, cudaStream_t stream) {
-  using L = RowSmem<TN, CG>;
+  using L = RowSmem<TN, CG, FUSED>;
   static std::atomic<unsigned long long> ready{0};   // devices whose copy of the kernel has its attribute set
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess) return OCS_ERR_CUDA;
   if (dev >= 64 || !(ready.load() >> dev & 1)) {
-    if (cudaFuncSetAttribute(row_gemm_kernel<T, TN, CG>, cudaFuncAttributeMaxDynamicSharedMemorySize, L::kDynBytes) != cudaSuccess)
+    if (cudaFuncSetAttribute(row_gemm_kernel<T, TN, CG, FUSED>, cudaFuncAttributeMaxDynamicSharedMemorySize, L::kDynBytes) != cudaSuccess)
       return OCS_ERR_CUDA;
     if (dev < 64) ready.fetch_or(1ull << dev);
   }
@@ -449,7 +619,9 @@ ocs_status launch_tiles(RowGemm p, int slices, const void* A, long long lda, con
   const cuuint64_t wd[2] = {(cuuint64_t)K, (cuuint64_t)p.N}, ws[1] = {(cuuint64_t)ldw};
   const cuuint64_t td[2] = {(cuuint64_t)K, (cuuint64_t)p.M}, ts[1] = {(cuuint64_t)lda};
   const cuuint32_t wb[2] = {KB, TW}, tb[2] = {KB, (cuuint32_t)L::kTokens};
-  if (!encode_u8(&tm_w, W, 2, wd, ws, wb) || !encode_u8(&tm_t, A, 2, td, ts, tb)) return OCS_ERR_CUDA;
+  if (!encode_u8(&tm_w, W, 2, wd, ws, wb)) return OCS_ERR_CUDA;
+  if (FUSED) tm_t = tm_w;   // unused
+  else if (!encode_u8(&tm_t, A, 2, td, ts, tb)) return OCS_ERR_CUDA;
   const int cl = CG * slices;
   const long long slots = cluster_capacity(cl) / cl;
   cudaLaunchConfig_t cfg = {};
@@ -470,9 +642,20 @@ ocs_status launch_tiles(RowGemm p, int slices, const void* A, long long lda, con
     ++n_attr;
   }
   cfg.attrs = attr; cfg.numAttrs = n_attr;
-  LaunchScope scope("row_gemm_kernel", stream);
-  if (cudaLaunchKernelEx(&cfg, row_gemm_kernel<T, TN, CG>, tm_w, tm_t, p, Y) != cudaSuccess) return OCS_ERR_CUDA;
+  LaunchScope scope(FUSED ? "row_gemm_kernel(fused)" : "row_gemm_kernel", stream);
+  if (cudaLaunchKernelEx(&cfg, row_gemm_kernel<T, TN, CG, FUSED>, tm_w, tm_t, p, Y) != cudaSuccess) return OCS_ERR_CUDA;
   return launch_status();
+}
+
+// Whether ocs_linear_rows quantizes inside the product's kernel: every CTA quantizes its token tile itself.  That saves a
+// launch, but each CTA reads the whole rows, so it is for few tokens.
+bool fuse_tokens(const RowPlan& plan, int M, int N, int C, int num_kb, int x_bytes, int x_align) {
+  if (plan.tn > 32 || plan.cg != 1 || x_align < 8) return false;
+  const long long m_tiles = (M + plan.tn - 1) / plan.tn, tiles = m_tiles * ((N + TW - 1) / TW);
+  const int my_kb = (num_kb + plan.slices - 1) / plan.slices;
+  if ((long long)my_kb * plan.tn * KB > kFusedCodes) return false;                                // the codes have to fit
+  if (m_tiles > 1 && tiles > cluster_capacity(plan.slices) / plan.slices) return false;           // one token tile per CTA
+  return (long long)(M < plan.tn ? M : plan.tn) * C * x_bytes <= kFuseBytes;
 }
 
 struct Product {
@@ -484,6 +667,13 @@ struct Product {
   int M, N, K, a_signed;
   long long lda, ldw, ldy;
   int* dev_status;
+  // not quantized yet (A = a_scales = NULL)
+  const void* X;
+  long long ldx;
+  const int32_t* idx_map;
+  ocs_dtype x_type;
+  int x_align, C;
+  float hi;
 };
 
 template <typename T>
@@ -493,6 +683,12 @@ ocs_status launch_product(const Product& g, void* Y_, bool overlap, cudaStream_t
   p.a_scales = g.a_scales; p.w_scales = g.w_scales; p.bias = g.bias; p.ldy = g.ldy; p.dev_status = g.dev_status;
   const RowPlan plan = choose_plan(g.M, g.N, p.num_kb, (int)sizeof(T));
   T* Y = static_cast<T*>(Y_);
+  if (!g.A) {
+    p.X = g.X; p.ldx = g.ldx; p.idx_map = g.idx_map; p.x_type = g.x_type; p.C = g.C; p.K = g.K; p.hi = g.hi;
+    p.x_align = g.x_align;
+    if (plan.tn == 16) return launch_tiles<T, 16, 1, true>(p, plan.slices, nullptr, 16, g.W, g.ldw, g.K, Y, false, stream);
+    return launch_tiles<T, 32, 1, true>(p, plan.slices, nullptr, 16, g.W, g.ldw, g.K, Y, false, stream);
+  }
   switch (plan.tn * 2 + plan.cg - 1) {
     case 32: return launch_tiles<T, 16, 1>(p, plan.slices, g.A, g.lda, g.W, g.ldw, g.K, Y, overlap, stream);
     case 64: return launch_tiles<T, 32, 1>(p, plan.slices, g.A, g.lda, g.W, g.ldw, g.K, Y, overlap, stream);
@@ -540,13 +736,29 @@ extern "C" ocs_status ocs_qlinear_rows(const void* A_codes, int a_signed, const 
   if (!aligned(a_scales, 4)) return OCS_ERR_SHAPE;
   if ((st = check_device()) != OCS_OK) return st;
   Product p{A_codes, a_scales, W_codes, w_scales, bias, M, N, K, a_signed ? 1 : 0,
-            lda, ldw, ldy, dev_status};
+            lda, ldw, ldy, dev_status, nullptr, 0, nullptr, OCS_F32, 0, 0, 0.0f};
   return run_product(p, Y, y_type, false, stream);
 }
 
-extern "C" size_t ocs_linear_rows_workspace_bytes(int M, int C, int S) {
-  if (M <= 0 || C <= 0 || S < 0) return 256;
-  return align_up((size_t)M * align_up((size_t)C + S, 16), 256) + align_up((size_t)M * 4, 256);
+namespace {
+// The plan of an ocs_linear_rows call, and the bytes of codes and scales it keeps in the workspace (0: quantized inside
+// the product's kernel).
+int row_align(const void* X, int M, int64_t ldx, ocs_dtype x_type) {
+  const uintptr_t a = reinterpret_cast<uintptr_t>(X) | (M > 1 ? (uintptr_t)(ldx * elem_bytes(x_type)) : 0);
+  return a % 16 == 0 ? 16 : (a % 8 == 0 ? 8 : 1);
+}
+size_t linear_rows_plan(const void* X, int M, int C, int64_t ldx, int S, int N, ocs_dtype x_type, ocs_dtype y_type) {
+  const int K = C + S, num_kb = (K + KB - 1) / KB;
+  const RowPlan plan = choose_plan(M, N, num_kb, elem_bytes(y_type));
+  if (fuse_tokens(plan, M, N, C, num_kb, elem_bytes(x_type), row_align(X, M, ldx, x_type))) return 0;
+  return align_up((size_t)M * align_up((size_t)K, 16), 256) + align_up((size_t)M * 4, 256);
+}
+}  // namespace
+
+extern "C" size_t ocs_linear_rows_workspace_bytes(const void* X, ocs_dtype x_type, int M, int C, int64_t ldx, int S, int N,
+                                                  ocs_dtype y_type) {
+  if (M <= 0 || C <= 0 || S < 0 || N <= 0 || !valid_dtype(x_type) || !valid_dtype(y_type) || (int64_t)C + S >= (1 << 30)) return 0;
+  return linear_rows_plan(X, M, C, ldx, S, N, x_type, y_type);
 }
 
 extern "C" ocs_status ocs_linear_rows(const void* X, ocs_dtype x_type, int M, int C, int64_t ldx, int S,
@@ -555,21 +767,28 @@ extern "C" ocs_status ocs_linear_rows(const void* X, ocs_dtype x_type, int M, in
                                       ocs_dtype y_type, int64_t ldy, void* ws, size_t ws_bytes, int* dev_status,
                                       void* stream_) {
   cudaStream_t stream = reinterpret_cast<cudaStream_t>(stream_);
-  if (!valid_dtype(x_type) || !valid_dtype(y_type) || S < 0) return OCS_ERR_INVALID_ARG;
+  if (!valid_dtype(x_type) || !valid_dtype(y_type) || S < 0 || bits < 2 || bits > 8) return OCS_ERR_INVALID_ARG;
   if (M < 0 || C <= 0 || N <= 0) return OCS_ERR_SHAPE;
   if (M == 0) return OCS_OK;
+  if (!X || (S > 0 && !idx_map)) return OCS_ERR_INVALID_ARG;
   if ((int64_t)C + S >= (1 << 30)) return OCS_ERR_UNSUPPORTED;
   const int K = C + S;
   const int64_t lda = (int64_t)align_up((size_t)K, 16);
-  if (!ws || !aligned(ws, 256) || ws_bytes < ocs_linear_rows_workspace_bytes(M, C, S)) return OCS_ERR_WORKSPACE;
-  ocs_status st = check_product(is_signed, M, K, lda, ws, W_codes, N, ldw, bias, Y, y_type, ldy, w_scales);
+  const size_t need = linear_rows_plan(X, M, C, ldx, S, N, x_type, y_type);
+  if (need && (!ws || !aligned(ws, 256) || ws_bytes < need)) return OCS_ERR_WORKSPACE;
+  ocs_status st = check_product(is_signed, M, K, lda, nullptr, W_codes, N, ldw, bias, Y, y_type, ldy, w_scales);
   if (st != OCS_OK) return st;
-  int8_t* codes = static_cast<int8_t*>(ws);
-  float* scales = reinterpret_cast<float*>(codes + align_up((size_t)M * lda, 256));
-  st = ocs_quantize_rows(X, x_type, M, C, ldx, S, idx_map, bits, is_signed, codes, lda, scales, dev_status, stream_);
-  if (st != OCS_OK) return st;
-  Product p{codes, scales, W_codes, w_scales, bias, M, N, K, is_signed ? 1 : 0,
-            lda, ldw, ldy, dev_status};
+  if (ldx < C || !aligned(X, elem_bytes(x_type)) || (S > 0 && !aligned(idx_map, 4))) return OCS_ERR_SHAPE;
+  if ((st = check_device()) != OCS_OK) return st;
+  Product p{nullptr, nullptr, W_codes, w_scales, bias, M, N, K, is_signed ? 1 : 0, lda, ldw, ldy, dev_status,
+            X, ldx, idx_map, x_type, row_align(X, M, ldx, x_type), C, (float)(is_signed ? (1 << (bits - 1)) - 1 : (1 << bits) - 1)};
+  if (need) {
+    int8_t* codes = static_cast<int8_t*>(ws);
+    float* scales = reinterpret_cast<float*>(codes + align_up((size_t)M * lda, 256));
+    st = ocs_quantize_rows(X, x_type, M, C, ldx, S, idx_map, bits, is_signed, codes, lda, scales, dev_status, stream_);
+    if (st != OCS_OK) return st;
+    p.A = codes; p.a_scales = scales;
+  }
   return run_product(p, Y, y_type, true, stream);
 }
 

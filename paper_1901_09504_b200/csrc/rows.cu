@@ -33,25 +33,6 @@ union Piece {
   __device__ __forceinline__ Piece() {}
 };
 
-// A grid's constants: codes = rint(x * inv), after a multiplication by 2^64 for rows below 2^-100 (exact; it keeps
-// hi / alpha finite).
-struct RowGrid {
-  float inv, up;
-};
-__device__ __forceinline__ RowGrid row_grid(float alpha, float hi) {
-  RowGrid g;
-  g.up = alpha < 0x1p-100f ? 0x1p64f : 1.0f;
-  g.inv = alpha > 0.0f ? __fdiv_rn(hi, __fmul_rn(alpha, g.up)) : 0.0f;
-  return g;
-}
-// |x| <= alpha, so |x * inv| <= hi * (1 + 2^-23): the rounding itself keeps the upper bound, only the unsigned grid
-// has to clamp (at 0).  The rounding is the magic-number addition of quant_code; the low byte is the code.
-template <bool SIGNED>
-__device__ __forceinline__ int row_code(float x, float inv) {
-  const float t = __fmul_rn(x, inv);
-  return __float_as_int(__fadd_rn(SIGNED ? t : fmaxf(t, 0.0f), 12582912.0f));
-}
-
 template <bool SIGNED, typename T, int VB>
 __device__ __forceinline__ void store_codes(const Piece<T, VB>& p, const RowGrid& g, bool scaled, int8_t* dst, int n, bool vec) {
   constexpr int VE = Piece<T, VB>::VE;

@@ -71,7 +71,7 @@ def _close(got, want, tol, what):
 def check(logits, targets, k, beta, status=0):
     T, V = logits.shape
     st = ocs.new_status()
-    r = ocs.ocs_token_logprobs(logits, targets, top_k=k, inv_temperature=beta, dev_status=st)
+    r = ocs.ocs_token_logprobs(logits, targets, top_k=k, inv_temperature=beta, want_stats=True, dev_status=st)
     assert ocs.ocs_poll_status(st) == status
     ref = _ref(logits, beta, targets, k)
     ts = _tol_sum(ref, V)
@@ -111,7 +111,7 @@ def test_parts_are_optional():
     y = torch.arange(6, dtype=torch.int32, device="cuda")
     full = ocs.ocs_token_logprobs(x, y, top_k=4)
     none = ocs.ocs_token_logprobs(x)
-    assert none.logprob is None and none.top_ids is None and torch.equal(none.entropy, full.entropy)
+    assert none.logprob is None and none.top_ids is None and none.stats is None and torch.equal(none.entropy, full.entropy)
     only = ocs.TokenLogprobs(None, None, torch.empty((6, 4), dtype=torch.int32, device="cuda"), None, None)
     ocs.ocs_token_logprobs(x, None, top_k=4, out=only)
     assert torch.equal(only.top_ids, full.top_ids)
@@ -236,7 +236,7 @@ def test_gradient_against_differences():
     x[2, 5:9] = -float("inf")
     y = torch.tensor([3, 0, 36, -1], dtype=torch.int32, device="cuda")
     g, gh = torch.randn(T, generator=_gen(8), device="cuda"), torch.randn(T, generator=_gen(9), device="cuda")
-    r = ocs.ocs_token_logprobs(x, y, inv_temperature=beta)
+    r = ocs.ocs_token_logprobs(x, y, inv_temperature=beta, want_stats=True)
     d = ocs.ocs_token_logprobs_backward(x, y, r.stats, g, gh, inv_temperature=beta).double()
 
     def value(z):
@@ -254,7 +254,7 @@ def test_gradient_against_differences():
 def test_missing_gradients_count_as_zero():
     x = _logits(5, 3, 700, "f32")
     y = torch.tensor([1, 2, 3], dtype=torch.int32, device="cuda")
-    r = ocs.ocs_token_logprobs(x, y)
+    r = ocs.ocs_token_logprobs(x, y, want_stats=True)
     g, z = torch.randn(3, device="cuda"), torch.zeros(3, device="cuda")
     assert torch.equal(ocs.ocs_token_logprobs_backward(x, y, r.stats, g), ocs.ocs_token_logprobs_backward(x, y, r.stats, g, z))
     assert torch.equal(ocs.ocs_token_logprobs_backward(x, None, r.stats, None, g), ocs.ocs_token_logprobs_backward(x, y, r.stats, z, g))
@@ -294,7 +294,7 @@ def test_results_do_not_depend_on_the_rows_beside():
 def test_refusals_of_the_binding():
     x = torch.zeros((4, 32), device="cuda")
     y = torch.zeros(4, dtype=torch.int32, device="cuda")
-    r = ocs.ocs_token_logprobs(x, y)
+    r = ocs.ocs_token_logprobs(x, y, want_stats=True)
     for bad in (lambda: ocs.ocs_token_logprobs(x.double(), y), lambda: ocs.ocs_token_logprobs(x, y.long()),
                 lambda: ocs.ocs_token_logprobs(x, y[:3]), lambda: ocs.ocs_token_logprobs(x.t(), y),
                 lambda: ocs.ocs_token_logprobs(x[0], y), lambda: ocs.ocs_token_logprobs(x[:1].expand(4, 32), y),

@@ -197,9 +197,15 @@ def test_qlinear_rows_extreme_codes():
     (1, 4096, 0, 512, "bf16", "bf16", True), (1, 100, 3, 7, "f16", "f32", False), (20, 650, 13, 2600, "f32", "f32", True),
     (48, 5000, 100, 700, "bf16", "f16", True), (130, 650, 13, 33278, "f32", "f32", True), (333, 1000, 20, 1000, "f16", "bf16", False),
     (2047, 512, 10, 600, "bf16", "bf16", True), (8, 25088, 251, 128, "f32", "f32", False),
+    # few tokens: quantized inside the product's kernel, by every row alignment, with K splits and many channel tiles
+    (1, 1, 0, 1, "f32", "f32", True), (1, 1, 1, 5, "bf16", "f32", True), (3, 127, 2, 300, "bf16", "bf16", False),
+    (5, 1000, 24, 40000, "f16", "f16", True), (16, 1024, 0, 4096, "f32", "bf16", True), (17, 640, 13, 3000, "f32", "f32", False),
+    (20, 650, 0, 33278, "f32", "f32", True), (31, 96, 32, 64, "bf16", "f32", True), (32, 520, 5, 2000, "bf16", "bf16", True),
+    (1, 16384, 300, 256, "f16", "f32", True), (2, 8192, 0, 8192, "bf16", "bf16", True), (40, 300, 3, 900, "f32", "f32", True),
 ])
-def test_linear_rows_is_its_two_halves(M, C, S, N, x, y, signed):
-    X = _x(M, M, C, x, ld=C + 1)
+@pytest.mark.parametrize("pad", [0, 1, 8])
+def test_linear_rows_is_its_two_halves(M, C, S, N, x, y, signed, pad):
+    X = _x(M, M, C, x, ld=(C + pad) if pad < 8 else ocs.round_up(C, 8) + 8)
     idx, W = _idx(M, C, S), _codes(N, N, C + S, True)
     w_s = torch.rand(N, generator=_gen(2), device="cuda") * 0.001
     bias = torch.randn(N, generator=_gen(3), device="cuda")
@@ -216,11 +222,12 @@ def test_linear_rows_is_its_two_halves(M, C, S, N, x, y, signed):
     check_product(codes[:, :C + S], a_s, W, w_s, bias, Y)
 
 
-def test_linear_rows_back_to_back_and_in_a_graph():
+@pytest.mark.parametrize("M", [24, 300])
+def test_linear_rows_back_to_back_and_in_a_graph(M):
     """Calls that follow one another reuse the same workspace, outputs and input buffers; then the same under graph replay."""
-    M, C, N = 24, 1024, 1152
+    C, N = 1024, 1152
     W, w_s = _codes(5, N, C, True), torch.rand(N, generator=_gen(2), device="cuda") * 0.001
-    ws = torch.empty(ocs.lib().ocs_linear_rows_workspace_bytes(M, C, 0), dtype=torch.uint8, device="cuda")
+    ws = torch.empty(max(256, ocs.lib().ocs_linear_rows_workspace_bytes(0, 2, M, C, C, 0, N, 0)), dtype=torch.uint8, device="cuda")
     xs = [_x(s, M, C, "bf16") for s in range(8)]
     refs = [ocs.ocs_linear_rows(x, W, w_s, out_dtype=torch.float32) for x in xs]
     torch.cuda.synchronize()
@@ -240,6 +247,33 @@ def test_linear_rows_back_to_back_and_in_a_graph():
         graph.replay()
         assert torch.equal(out, refs[i])
     del graph
+
+
+def test_linear_rows_zero_tiny_and_bad_rows():
+    """Rows of zeros, rows below 2^-100, a row that is not finite and indices out of range, in both forms of the call."""
+    for M in (12, 600):
+        x = _x(9, M, 256, "f32").contiguous()
+        x[1] = 0
+        x[2] *= 1e-35
+        x[3] = 0
+        x[3, 255] = 1e-45
+        idx = _idx(0, 256, 2)
+        W, w_s = _codes(3, 130, 258, True), torch.rand(130, generator=_gen(2), device="cuda")
+        st = ocs.new_status()
+        Y = ocs.ocs_linear_rows(x, W, w_s, idx_map=idx, S=2, dev_status=st)
+        q, sc = ref_rows(x, idx, 8, True)
+        assert ocs.ocs_poll_status(st) == 0
+        check_product(torch.from_numpy(q).cuda(), torch.from_numpy(sc).cuda(), W, w_s, None, Y)
+        assert (Y[1] == 0).all()
+        x[5, 77] = float("nan")
+        Y2 = ocs.ocs_linear_rows(x, W, w_s, idx_map=idx, S=2, dev_status=st)
+        assert ocs.ocs_poll_status(st) == ocs.DEV_NONFINITE
+        keep = torch.arange(M, device="cuda") != 5
+        assert torch.equal(Y2[keep], Y[keep])
+        idx[257] = 256
+        st = ocs.new_status()
+        ocs.ocs_linear_rows(x[:5], W, w_s, idx_map=idx, S=2, dev_status=st)
+        assert ocs.ocs_poll_status(st) == ocs.DEV_BAD_INDEX
 
 
 def test_rows_beyond_32_bit_offsets():
@@ -282,7 +316,8 @@ def test_refusals_of_the_binding():
         ocs.ocs_qlinear_rows(W[:, :24].contiguous(), s, W, s)      # rows of 24 bytes
     assert e.value.status == 2
     with pytest.raises(ocs.OcsError) as e:
-        ocs.ocs_linear_rows(x, W, s, ws=torch.empty(256, dtype=torch.uint8, device="cuda")[:128])
+        big = torch.zeros((5000, 32), dtype=torch.int8, device="cuda")
+        ocs.ocs_linear_rows(torch.zeros((900, 32), device="cuda"), big, torch.ones(5000, device="cuda"), ws=torch.empty(256, dtype=torch.uint8, device="cuda")[:128])
     assert e.value.status == 3
     empty = ocs.ocs_linear_rows(x[:0], W, s)
     assert empty.shape == (0, 8) and ocs.ocs_quantize_rows(x[:0])[0].shape == (0, 32)

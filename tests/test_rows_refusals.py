@@ -44,7 +44,8 @@ def backward(x=P, type=0, rows=4, V=100, ld=100, targets=P, beta=1.0, stats=P, g
     (qlinear, dict(Y=P + 2), SHAPE), (qlinear, dict(bias=P + 1), SHAPE),
     (qlinear, dict(K=140000, lda=140000, ldw=140000), UNSUPPORTED),
     (qlinear, dict(K=66000, lda=66000, ldw=66000, signed=0), UNSUPPORTED), (qlinear, dict(M=1 << 30), UNSUPPORTED),
-    (linear, dict(ws=None), WORKSPACE), (linear, dict(ws_bytes=100), WORKSPACE), (linear, dict(ws=P + 16), WORKSPACE),
+    (linear, dict(M=900, N=5000, ldy=5000, ws=None), WORKSPACE), (linear, dict(M=900, N=5000, ldy=5000, ws_bytes=100), WORKSPACE),
+    (linear, dict(M=900, N=5000, ldy=5000, ws=P + 16), WORKSPACE),
     (linear, dict(x_type=7), INVALID), (linear, dict(bits=0), INVALID), (linear, dict(S=1, ldw=48), INVALID),
     (linear, dict(X=None), INVALID), (linear, dict(ldx=8), SHAPE), (linear, dict(S=8, idx=P), SHAPE), (linear, dict(M=-2), SHAPE),
     (logprobs, dict(type=3), INVALID), (logprobs, dict(beta=0.0), INVALID), (logprobs, dict(beta=-1.0), INVALID),
@@ -70,8 +71,10 @@ def test_calls_without_rows_are_no_ops():
 
 
 def test_workspace_query():
-    L = ocs.lib()
-    assert L.ocs_linear_rows_workspace_bytes(0, 10, 0) == 256
-    assert L.ocs_linear_rows_workspace_bytes(5, 650, 13) >= 5 * 672 + 20
-    # 32-bit products would wrap here
-    assert L.ocs_linear_rows_workspace_bytes(1 << 20, 25088, 251) > (1 << 20) * 25088
+    def q(M, C, S, N, x_type=0, y_type=0, X=P, ldx=None):
+        return ocs.lib().ocs_linear_rows_workspace_bytes(X, x_type, M, C, ldx or C, S, N, y_type)
+    assert q(0, 10, 0, 10) == 0 and q(5, 10, 0, 10, x_type=7) == 0
+    assert q(5, 650, 13, 2600) == 0                               # few tokens: quantized inside the product
+    assert q(5, 650, 13, 2600, ldx=651) >= 5 * 672 + 20           # ... unless their rows start at any four bytes
+    assert q(900, 650, 13, 2600) >= 900 * 672 + 900 * 4
+    assert q(1 << 20, 25088, 251, 4096) > (1 << 20) * 25088       # 32-bit products would wrap here
