@@ -607,13 +607,12 @@ def _rows_of(t):
     """Row stride of a 2-D tensor whose rows are contiguous and do not overlap.  A single row has no stride of its own:
     it counts as padded to 16 elements, which no call reads or writes."""
     assert t.dim() == 2
-    rows, cols = t.shape
+    (rows, cols), (ld, one) = t.shape, t.stride()
+    assert one == 1 or cols <= 1
     if rows == 1:
-        assert cols <= 1 or t.stride(1) == 1
         return (cols + 15) & ~15
-    ld = t.stride(0)
-    assert (cols <= 1 or t.stride(1) == 1) and (ld >= cols or rows == 0)
-    return max(ld, cols)
+    assert ld >= cols or rows == 0
+    return ld if ld > cols else cols
 
 
 def _check_idx(idx_map, Cn: int, S: int):
@@ -641,12 +640,14 @@ def ocs_quantize_rows(x, bits: int = 8, is_signed: bool = True, idx_map=None, S:
         codes, scales = out
         assert codes.is_cuda and codes.element_size() == 1 and codes.shape[0] == rows and codes.shape[1] >= Cn + S
         _check_vec(scales, rows)
+        ld_codes = _rows_of(codes)
     else:
-        codes = torch.empty((rows, round_up(Cn + S, 16) if ld_codes is None else ld_codes),
-                            dtype=torch.int8 if is_signed else torch.uint8, device=x.device)
+        if ld_codes is None:
+            ld_codes = (Cn + S + 15) & ~15
+        codes = torch.empty((rows, ld_codes), dtype=torch.int8 if is_signed else torch.uint8, device=x.device)
         scales = torch.empty(rows, dtype=torch.float32, device=x.device)
     st = lib().ocs_quantize_rows(x.data_ptr(), DTYPES[x.dtype], rows, Cn, ldx, S, _addr(idx_map), int(bits),
-                                 1 if is_signed else 0, codes.data_ptr(), _rows_of(codes), scales.data_ptr(),
+                                 1 if is_signed else 0, codes.data_ptr(), ld_codes, scales.data_ptr(),
                                  _addr(dev_status), _raw_stream(x))
     _check(st, "ocs_quantize_rows")
     return codes, scales
@@ -665,11 +666,14 @@ def ocs_qlinear_rows(A_codes, a_scales, W_codes, w_scales, K: int | None = None,
     assert a_scales is not None and w_scales is not None
     _check_vec(a_scales, M), _check_vec(w_scales, N), _check_vec(bias, N)
     if out is None:
-        out = torch.empty((M, N), dtype=out_dtype, device=A_codes.device)
-    assert out.is_cuda and out.dtype in DTYPES and out.shape == (M, N)
+        out, ldy = torch.empty((M, N), dtype=out_dtype, device=A_codes.device), N
+    else:
+        assert out.is_cuda and out.shape == (M, N)
+        ldy = _rows_of(out)
+    assert out.dtype in DTYPES
     st = lib().ocs_qlinear_rows(A_codes.data_ptr(), 1 if A_codes.dtype == torch.int8 else 0, a_scales.data_ptr(), M, K, lda,
                                 W_codes.data_ptr(), w_scales.data_ptr(), N, ldw, _addr(bias), out.data_ptr(),
-                                DTYPES[out.dtype], _rows_of(out), _addr(dev_status), _raw_stream(A_codes))
+                                DTYPES[out.dtype], ldy, _addr(dev_status), _raw_stream(A_codes))
     _check(st, "ocs_qlinear_rows")
     return out
 
@@ -686,8 +690,12 @@ def ocs_linear_rows(x, W_codes, w_scales, idx_map=None, S: int = 0, bits: int = 
     assert W_codes.shape[1] >= Cn + S and w_scales is not None
     _check_vec(w_scales, N), _check_vec(bias, N)
     if out is None:
-        out = torch.empty((M, N), dtype=x.dtype if out_dtype is None else out_dtype, device=x.device)
-    assert out.is_cuda and out.dtype in DTYPES and out.shape == (M, N)
+        out = x.new_empty((M, N)) if out_dtype is None else torch.empty((M, N), dtype=out_dtype, device=x.device)
+        ldy = N
+    else:
+        assert out.is_cuda and out.shape == (M, N)
+        ldy = _rows_of(out)
+    assert out.dtype in DTYPES
     L = lib()
     xt, yt = DTYPES[x.dtype], DTYPES[out.dtype]
     if ws is None:
@@ -696,7 +704,7 @@ def ocs_linear_rows(x, W_codes, w_scales, idx_map=None, S: int = 0, bits: int = 
             ws = torch.empty(n_ws, dtype=torch.uint8, device=x.device)
     st = L.ocs_linear_rows(x.data_ptr(), xt, M, Cn, ldx, S, _addr(idx_map), int(bits), 1 if is_signed else 0,
                            W_codes.data_ptr(), w_scales.data_ptr(), N, ldw, _addr(bias), out.data_ptr(), yt,
-                           _rows_of(out), _addr(ws), 0 if ws is None else ws.numel(), _addr(dev_status), _raw_stream(x))
+                           ldy, _addr(ws), 0 if ws is None else ws.numel(), _addr(dev_status), _raw_stream(x))
     _check(st, "ocs_linear_rows")
     return out
 
@@ -757,10 +765,12 @@ def ocs_token_logprobs_backward(logits, targets, stats, g_logprob=None, g_entrop
     assert stats is not None
     _check_vec(stats, 4 * rows), _check_vec(g_logprob, rows), _check_vec(g_entropy, rows)
     if out is None:
-        out = torch.empty((rows, V), dtype=logits.dtype, device=logits.device)
-    assert out.is_cuda and out.dtype == logits.dtype and out.shape == (rows, V)
+        out, ld_d = logits.new_empty((rows, V)), V
+    else:
+        assert out.is_cuda and out.dtype == logits.dtype and out.shape == (rows, V)
+        ld_d = _rows_of(out)
     st = lib().ocs_token_logprobs_backward(logits.data_ptr(), DTYPES[logits.dtype], rows, V, ld, _addr(targets),
                                            inv_temperature, stats.data_ptr(), _addr(g_logprob), _addr(g_entropy),
-                                           out.data_ptr(), _rows_of(out), _addr(dev_status), _raw_stream(logits))
+                                           out.data_ptr(), ld_d, _addr(dev_status), _raw_stream(logits))
     _check(st, "ocs_token_logprobs_backward")
     return out

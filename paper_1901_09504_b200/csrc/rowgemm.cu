@@ -144,47 +144,56 @@ __device__ __forceinline__ int token_code(float x, float inv, uint32_t max_bits,
 // slice + slices, ...: first the rows' maxima, 512 elements per warp and step, then the codes, one row of a K-block per
 // warp and step.  What does not come in whole fours of channels goes one by one: a row's last C % 4 channels and the
 // duplicated ones (item u: contraction index C4 + u / rows of row u % rows; the first item's value is on its way from the
-// start).  The latency of the loads is what this costs, so the loads of four steps are issued before the first is used.
+// start).  The latency of the loads is what this costs, so those of several steps are issued before the first is used.
 template <typename X, int TN>
 __device__ __forceinline__ void quantize_tokens(const RowGemm& p, const X* x0, int m0, int slice, int my_kb, unsigned char* tok,
                                                 uint32_t* max_bits, float* scale, float* inv) {
-  constexpr int B = 4;
+  constexpr int B = 4, D = 4;   // steps whose loads are under way together
   const int et = threadIdx.x - 64, warp = et >> 5, lane = et & 31;
   const int rows = min(TN, p.M - m0), C4 = p.C & ~3, n_items = rows * (p.K - C4);
   const bool wide = p.x_align >= 16;
-  int src = 0;
+  // where the code of item (contraction index k, row r) goes; -1: not in this CTA's share
+  auto place = [&](int k, int r) {
+    const int kb = k / KB, i = kb / p.slices, in = k % KB;
+    return kb - i * p.slices == slice ? (i * TN + r) * KB + (((in >> 4) ^ (r & 7)) << 4) + (in & 15) : -1;
+  };
+  int src = 0, at = -1, item_row = 0, item_k = 0;
   if (et < n_items) {
-    src = C4 + et / rows;
+    item_k = et / rows;
+    item_row = et - item_k * rows;
+    src = item_k += C4;
     if (src >= p.C) src = __ldg(p.idx_map + src);
+    at = place(item_k, item_row);
   }
   if (et < TN) max_bits[et] = 0;
   asm volatile("bar.sync 1, 256;" ::: "memory");
   const int chunks = (C4 + 511) / 512, units = rows * chunks;
   for (int u0 = warp; u0 < units; u0 += B * kEpiWarps) {
     Four<X> f[B][4];
+    int rr[B];
 #pragma unroll
     for (int b = 0; b < B; ++b) {
       const int u = min(u0 + b * kEpiWarps, units - 1), r = u / chunks, c = (u - r * chunks) * 512 + lane * 4;
+      rr[b] = r;
 #pragma unroll
       for (int j = 0; j < 4; ++j) f[b][j].load(x0 + r * p.ldx + min(c + 128 * j, C4 - 4), wide);   // (twice at the end: harmless)
     }
 #pragma unroll
     for (int b = 0; b < B; ++b) {
-      const int u = u0 + b * kEpiWarps;
       uint32_t m = 0;
 #pragma unroll
       for (int j = 0; j < 4; ++j)
 #pragma unroll
         for (int i = 0; i < 4; ++i) m = max(m, __float_as_uint(f[b][j][i]) & 0x7fffffffu);
       m = __reduce_max_sync(0xffffffffu, m);
-      if (lane == 0 && u < units) atomicMax(max_bits + u / chunks, m);
+      if (lane == 0) atomicMax(max_bits + rr[b], m);
     }
   }
   float value = 0.0f;
   if (et < n_items) {
     if ((unsigned)src >= (unsigned)p.C) { flag(p.dev_status, OCS_DEV_BAD_INDEX); src = 0; }
-    value = to_f32(x0[(et % rows) * p.ldx + src]);
-    if (C4 + et / rows < p.C) atomicMax(max_bits + et % rows, __float_as_uint(value) & 0x7fffffffu);   // (all of these are first items)
+    value = to_f32(x0[item_row * p.ldx + src]);
+    if (item_k < p.C) atomicMax(max_bits + item_row, __float_as_uint(value) & 0x7fffffffu);   // (all of these are first items)
   }
   asm volatile("bar.sync 1, 256;" ::: "memory");
   if (et < rows) {
@@ -194,37 +203,33 @@ __device__ __forceinline__ void quantize_tokens(const RowGemm& p, const X* x0, i
     if (max_bits[et] >= 0x7f800000u) flag(p.dev_status, OCS_DEV_NONFINITE);
   }
   asm volatile("bar.sync 1, 256;" ::: "memory");
+  if (at >= 0) tok[at] = (unsigned char)token_code(value, inv[item_row], max_bits[item_row], p.t_signed);
   const int steps = C4 > 0 ? my_kb * rows : 0;
-  for (int u0 = warp; u0 < steps; u0 += B * kEpiWarps) {
-    Four<X> f[B];
+  for (int u0 = warp; u0 < steps; u0 += D * kEpiWarps) {
+    Four<X> f[D];
+    int rr[D], to[D];
 #pragma unroll
-    for (int b = 0; b < B; ++b) {
-      const int u = min(u0 + b * kEpiWarps, steps - 1), i = u / rows, r = u - i * rows;
-      f[b].load(x0 + r * p.ldx + min((slice + i * p.slices) * KB + lane * 4, C4 - 4), wide);
+    for (int b = 0; b < D; ++b) {
+      const int u = u0 + b * kEpiWarps, i = u / rows, r = u - i * rows, k = (slice + i * p.slices) * KB + lane * 4;
+      rr[b] = u < steps ? r : 0;
+      // past the last contraction index the weights' tile is zero
+      to[b] = u < steps && k < C4 ? (i * TN + r) * KB + (((lane >> 2) ^ (r & 7)) << 4) + (lane & 3) * 4 : -1;
+      f[b].load(x0 + rr[b] * p.ldx + (to[b] >= 0 ? k : 0), wide);
     }
 #pragma unroll
-    for (int b = 0; b < B; ++b) {
-      const int u = u0 + b * kEpiWarps, i = u / rows, r = u - i * rows, k = (slice + i * p.slices) * KB + lane * 4;
-      if (u < steps && k < C4) {   // past the last contraction index the weights' tile is zero
-        int c[4];
+    for (int b = 0; b < D; ++b) {
+      int c[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) c[e] = token_code(f[b][e], inv[r], max_bits[r], p.t_signed);
-        *reinterpret_cast<uint32_t*>(tok + (size_t)(i * TN + r) * KB + (((lane >> 2) ^ (r & 7)) << 4) + (lane & 3) * 4) =
-            pack4(c[0], c[1], c[2], c[3]);
-      }
+      for (int e = 0; e < 4; ++e) c[e] = token_code(f[b][e], inv[rr[b]], max_bits[rr[b]], p.t_signed);
+      if (to[b] >= 0) *reinterpret_cast<uint32_t*>(tok + to[b]) = pack4(c[0], c[1], c[2], c[3]);
     }
   }
-  for (int u = et; u < n_items; u += 256) {
-    const int d = u / rows, r = u - d * rows, k = C4 + d, kb = k / KB;
-    if (kb % p.slices != slice) continue;
-    if (u != et) {
-      src = __ldg(p.idx_map + k);
-      if ((unsigned)src >= (unsigned)p.C) { flag(p.dev_status, OCS_DEV_BAD_INDEX); src = 0; }
-      value = to_f32(x0[r * p.ldx + src]);
-    }
-    const int i = kb / p.slices, in = k % KB;
-    tok[(size_t)(i * TN + r) * KB + (((in >> 4) ^ (r & 7)) << 4) + (in & 15)] =
-        (unsigned char)token_code(value, inv[r], max_bits[r], p.t_signed);
+  for (int u = et + 256; u < n_items; u += 256) {
+    const int d = u / rows, r = u - d * rows, to = place(C4 + d, r);
+    if (to < 0) continue;
+    src = __ldg(p.idx_map + C4 + d);
+    if ((unsigned)src >= (unsigned)p.C) { flag(p.dev_status, OCS_DEV_BAD_INDEX); src = 0; }
+    tok[to] = (unsigned char)token_code(to_f32(x0[r * p.ldx + src]), inv[r], max_bits[r], p.t_signed);
   }
   fence_proxy_async_smem();   // the tensor cores read what these threads wrote
 }
@@ -251,10 +256,9 @@ row_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant_
   auto accempty_bar = [&](int a) { return smem_u32(bars + 2 * L::kStages + 2 + a); };
   const uint32_t xfull_bar = smem_u32(bars + 2 * L::kStages + 4);
   const uint32_t xready_bar = smem_u32(bars + 2 * L::kStages + 5);
-  const uint32_t tok_bar = smem_u32(bars + 2 * L::kStages + 6);
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * L::kStages + 7);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * L::kStages + 6);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
-  static_assert((2 * L::kStages + 7) * 8 + 8 <= L::kCtrlBytes, "control block");
+  static_assert((2 * L::kStages + 6) * 8 + 8 <= L::kCtrlBytes, "control block");
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int CL = CG * p.slices;
@@ -265,7 +269,7 @@ row_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant_
 
   // Set-up.  Nobody waits for more than it needs: the copy warp asks for the first weights as soon as its own barriers
   // stand, the tensor-core warp needs these barriers, the epilogue warps the address in tensor memory as well -- after
-  // they have quantized the tokens, where that is theirs to do.  (Named barriers: 2 = set up, 3 = barriers stand.)  A peer
+  // they have quantized the tokens, where that is theirs to do.  (Named barriers: 2 = set up, 3 = barriers stand, 4 = tokens in place.)  A peer
   // may be written to once all threads of the cluster have arrived; a pair waits for that at once, the others where they
   // first need it.
   if (warp == 0) {
@@ -282,7 +286,6 @@ row_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant_
       }
       mbar_init(xfull_bar, 1);
       mbar_init(xready_bar, p.slices);
-      mbar_init(tok_bar, kEpiWarps);
       *abort_flag = 0;
       fence_barrier_init();
       fence_proxy_async_smem();
@@ -310,7 +313,7 @@ row_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant_
       if (p.x_type == OCS_F32) quantize_tokens<float, TN>(p, static_cast<const float*>(p.X) + at, mt * TN, slice, my_kb, tokens, row_max, row_scale, inv);
       else if (p.x_type == OCS_F16) quantize_tokens<__half, TN>(p, static_cast<const __half*>(p.X) + at, mt * TN, slice, my_kb, tokens, row_max, row_scale, inv);
       else quantize_tokens<__nv_bfloat16, TN>(p, static_cast<const __nv_bfloat16*>(p.X) + at, mt * TN, slice, my_kb, tokens, row_max, row_scale, inv);
-      __syncwarp();
+      asm volatile("bar.arrive 4, 288;" ::: "memory");   // this warp's codes are in place
     }
     asm volatile("bar.sync 2, 320;" ::: "memory");
   }
@@ -367,13 +370,13 @@ row_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant_
     if (CL > 1 && CG == 1) cluster_wait();
   } else if (warp == 1) {
     // ---------------------------------------------------------------- tensor cores
+    if (FUSED) asm volatile("bar.sync 4, 288;" ::: "memory");   // the tokens' codes are in place
     if (lane == 0 && half == 0) {
       constexpr uint32_t kDescM = TW * CG;
       const uint32_t idesc = row_instr_desc(kDescM, TN, p.t_signed);
       const uint16_t mask = (uint16_t)(3u << (rank & ~1));
       int it = 0, j = 0;
       bool ok = true;
-      if (FUSED) ok = mbar_wait(tok_bar, 0u, abort_flag);   // the tokens' codes are in place
       for (int t = cluster; ok && t < p.total; t += n_clusters, ++j) {
         const int acc = j & 1;
         if (!mbar_wait_cluster(accempty_bar(acc), (((uint32_t)j >> 1) & 1u) ^ 1u, abort_flag)) break;
@@ -407,11 +410,7 @@ row_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant_
     const int ew = warp - 2, q = warp & 3, part = ew >> 2;   // lanes 32q.. of tensor memory; two warps share a quadrant
     float* sc = scale_buf + ew * L::kWarpTokens;
     const bool pairs = sizeof(T) == 2 && (p.ldy % 2 == 0) && (p.N % 2 == 0) && (reinterpret_cast<uintptr_t>(Y) & 3) == 0;
-    if (FUSED) {
-      if (lane == 0) mbar_arrive(tok_bar);   // this warp's codes are in place
-    } else {
-      grid_wait_previous();
-    }
+    if (!FUSED) grid_wait_previous();
     if (CL > 1 && CG == 1) cluster_wait();
     int j = 0;
     for (int t = cluster; t < p.total; t += n_clusters, ++j) {
@@ -542,7 +541,11 @@ row_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant_
 }
 
 // ------------------------------------------------------------------------------------------------ host
-constexpr long long kFuseBytes = 96 * 1024;   // bytes of unquantized tokens a CTA reads itself
+// Bytes of unquantized tokens that a CTA may read itself.  Against two launches (a graph's time per call / an eager call's
+// host time): (M, C, N) = (1, 8192, 8192), 16 KB: 16.9 / 13.8 us against 17.5 / 19.0; (16, 1024, 4096), 32 KB: 6.8 / 14.5
+// against 6.4 / 19.5; (20, 650, 2600) in fp32, 42 KB: 7.9 / 14.8 against 6.0 / 19.6; but (4, 8192, 8192), 64 KB: 20.2
+// against 17.4 on the device.
+constexpr long long kFuseBytes = 48 * 1024;
 
 struct RowPlan {
   int tn, cg, slices;
