@@ -1,5 +1,7 @@
 // ocs_quantize_rows: linear quantization with one grid per row (a token's activations, or an output
 // channel's split weights), the duplicated channels of a split layer appended to the codes.
+#include <type_traits>
+
 #include "elem.cuh"
 #include "ptx.cuh"
 
@@ -18,37 +20,91 @@ struct RowsParams {
   int* dev_status;
 };
 
-template <int VB> struct Word;
-template <> struct Word<16> { using type = uint4; };
-template <> struct Word<8> { using type = uint2; };
-template <> struct Word<4> { using type = uint32_t; };
-template <> struct Word<2> { using type = uint16_t; };
-
 // VB bytes of a row in registers
 template <typename T, int VB>
-union Piece {
-  static constexpr int VE = VB / (int)sizeof(T);
-  typename Word<VB>::type w;
-  T e[VE];
-  __device__ __forceinline__ Piece() {}
+struct Piece {
+  static constexpr int VE = VB / (int)sizeof(T), W = VB >= 4 ? VB / 4 : 1;
+  uint32_t w[W];                               // (two-byte pieces sit in the low half)
+  __device__ __forceinline__ void load(const T* x) {
+    if constexpr (VB == 32) {
+      asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                   : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7]) : "l"(x));
+    } else if constexpr (VB == 16) {
+      const uint4 v = __ldg(reinterpret_cast<const uint4*>(x));
+      w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+    } else if constexpr (VB == 8) {
+      const uint2 v = __ldg(reinterpret_cast<const uint2*>(x));
+      w[0] = v.x; w[1] = v.y;
+    } else if constexpr (VB == 4) {
+      w[0] = __ldg(reinterpret_cast<const uint32_t*>(x));
+    } else {
+      w[0] = __ldg(reinterpret_cast<const uint16_t*>(x));
+    }
+  }
+  // the first n elements, zeros after them
+  __device__ __forceinline__ void load_part(const T* x, int n) {
+#pragma unroll
+    for (int i = 0; i < W; ++i) w[i] = 0;
+#pragma unroll
+    for (int e = 0; e < VE; ++e)
+      if (e < n) {
+        if constexpr (sizeof(T) == 4) w[e] = __ldg(reinterpret_cast<const uint32_t*>(x) + e);
+        else w[e / 2] |= (uint32_t)__ldg(reinterpret_cast<const uint16_t*>(x) + e) << (16 * (e & 1));
+      }
+  }
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int i = 0; i < W; ++i) w[i] = 0;
+  }
+  __device__ __forceinline__ float operator[](int e) const {
+    if constexpr (sizeof(T) == 4) return __uint_as_float(w[e]);
+    else if constexpr (std::is_same<T, __nv_bfloat16>::value) return __uint_as_float(e & 1 ? w[e / 2] & 0xffff0000u : w[e / 2] << 16);
+    else return __half2float(__ushort_as_half((unsigned short)(e & 1 ? w[e / 2] >> 16 : w[e / 2] & 0xffffu)));
+  }
+  // Largest magnitude as bits (magnitudes order like their bit patterns, and so does what is not finite): of fp32, or of
+  // both 16-bit halves side by side.
+  __device__ __forceinline__ uint32_t max_bits(uint32_t m) const {
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
+      if constexpr (sizeof(T) == 4) m = max(m, w[i] & 0x7fffffffu);
+      else asm("max.u16x2 %0, %0, %1;" : "+r"(m) : "r"(w[i] & 0x7fff7fffu));
+    }
+    return m;
+  }
 };
+// ... as the bits of the fp32 value
+template <typename T>
+__device__ __forceinline__ uint32_t bits_f32(uint32_t m) {
+  if constexpr (sizeof(T) == 4) return m;
+  const uint32_t h = max(m & 0xffffu, m >> 16);
+  if constexpr (std::is_same<T, __nv_bfloat16>::value) return h << 16;
+  else return __float_as_uint(__half2float(__ushort_as_half((unsigned short)h)));
+}
 
 template <bool SIGNED, typename T, int VB>
-__device__ __forceinline__ void store_codes(const Piece<T, VB>& p, const RowGrid& g, bool scaled, int8_t* dst, int n, bool vec) {
+__device__ __forceinline__ void store_codes(const Piece<T, VB>& p, const RowGrid& g, int8_t* dst, int n, bool vec) {
   constexpr int VE = Piece<T, VB>::VE;
   int c[VE];
-  if (!scaled) {
+  if (g.up == 1.0f) {
 #pragma unroll
-    for (int e = 0; e < VE; ++e) c[e] = row_code<SIGNED>(to_f32(p.e[e]), g.inv);
+    for (int e = 0; e < VE; ++e) c[e] = row_code<SIGNED>(p[e], g.inv);
   } else {
 #pragma unroll
-    for (int e = 0; e < VE; ++e) c[e] = row_code<SIGNED>(__fmul_rn(to_f32(p.e[e]), g.up), g.inv);
+    for (int e = 0; e < VE; ++e) c[e] = row_code<SIGNED>(__fmul_rn(p[e], g.up), g.inv);
   }
-  if (vec && n == VE) {
-    if constexpr (VE == 8) *reinterpret_cast<uint2*>(dst) = make_uint2(pack4(c[0], c[1], c[2], c[3]), pack4(c[4], c[5], c[6], c[7]));
-    else if constexpr (VE == 4) *reinterpret_cast<uint32_t*>(dst) = pack4(c[0], c[1], c[2], c[3]);
-    else if constexpr (VE == 2) *reinterpret_cast<uint16_t*>(dst) = (uint16_t)__byte_perm(c[0], c[1], 0x0040);
-    else dst[0] = (int8_t)c[0];
+  if (vec && n >= VE) {
+    if constexpr (VE >= 4) {
+      uint32_t w[VE / 4];
+#pragma unroll
+      for (int i = 0; i < VE / 4; ++i) w[i] = pack4(c[4 * i], c[4 * i + 1], c[4 * i + 2], c[4 * i + 3]);
+      if constexpr (VE == 16) *reinterpret_cast<uint4*>(dst) = make_uint4(w[0], w[1], w[2], w[3]);
+      else if constexpr (VE == 8) *reinterpret_cast<uint2*>(dst) = make_uint2(w[0], w[1]);
+      else *reinterpret_cast<uint32_t*>(dst) = w[0];
+    } else if constexpr (VE == 2) {
+      *reinterpret_cast<uint16_t*>(dst) = (uint16_t)__byte_perm(c[0], c[1], 0x0040);
+    } else {
+      dst[0] = (int8_t)c[0];
+    }
   } else {
 #pragma unroll
     for (int e = 0; e < VE; ++e)
@@ -56,51 +112,146 @@ __device__ __forceinline__ void store_codes(const Piece<T, VB>& p, const RowGrid
   }
 }
 
-// One row per threadIdx.y, blockDim.x threads on it, NV pieces of VB bytes per thread: the row is read once and stays
-// in registers between the maximum and the codes.
-template <typename T, int VB, int NV>
-__global__ void __launch_bounds__(1024, 1) rows_kernel(const T* __restrict__ X, const RowsParams p) {
+constexpr int kRowThreads = 512;    // threads of a CTA with two pieces each (1024 with one)
+constexpr int kRowCluster = 8;      // CTAs that may share a row
+constexpr int kStagedRing = 4;      // rows of the staged form that are on chip or on their way
+constexpr size_t kStagedBytes = 226 * 1024;
+
+// One row per threadIdx.y and cluster, blockDim.x threads of each CTA on it, NV pieces of VB bytes per thread: the row is
+// read once and stays in registers between the maximum and the codes.  CLUSTER: the CTAs of a cluster take consecutive
+// parts of the row and exchange their maxima through shared memory.
+template <typename T, int VB, int NV, bool CLUSTER>
+__global__ void __launch_bounds__(NV == 1 ? 1024 : kRowThreads, NV == 1 ? 1 : 3) rows_kernel(const T* __restrict__ X, const RowsParams p) {
   constexpr int VE = Piece<T, VB>::VE;
-  __shared__ uint32_t s_max[32];
+  __shared__ uint32_t s_max[32], s_part[kRowCluster];
   grid_launch_dependents();
+  const int CL = CLUSTER ? (int)cluster_size() : 1, rank = CLUSTER ? (int)cluster_rank() : 0;
+  if (CLUSTER) asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory");   // every CTA runs before its memory is written to
   const int G = blockDim.x, tx = threadIdx.x, lane = tx & 31;
-  for (long long r0 = (long long)blockIdx.x * blockDim.y; r0 < p.rows; r0 += (long long)gridDim.x * blockDim.y) {
-    const long long r = r0 + threadIdx.y;
-    if (G == 32 && r >= p.rows) break;   // blocks of several rows have one warp on each
-    const T* x = X + r * p.ldx;
-    Piece<T, VB> v[NV];
+  const int n_vec = (p.C + VE - 1) / VE, per = (n_vec + CL - 1) / CL;
+  const int lo = rank * per, hi = min(lo + per, n_vec);
+  const long long r = CLUSTER ? blockIdx.x / CL : (long long)blockIdx.x * blockDim.y + threadIdx.y;
+  if (!CLUSTER && r >= p.rows) return;   // (blocks of several rows have one warp on each)
+  const T* x = X + r * p.ldx;
+  Piece<T, VB> v[NV];
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int c = (tx + i * G) * VE;
-      if (c + VE <= p.C) {
-        v[i].w = __ldg(reinterpret_cast<const typename Word<VB>::type*>(x + c));
-      } else {
+  for (int i = 0; i < NV; ++i) {
+    const int j = lo + tx + i * G, c = j * VE;
+    if (j >= hi) v[i].clear();
+    else if (c + VE <= p.C) v[i].load(x + c);
+    else v[i].load_part(x + c, p.C - c);
+  }
+  // the first duplicated channels' values: fetched while the row is on its way
+  const int s0 = rank * G + tx;
+  float dup = 0.0f;
+  if (s0 < p.S) {
+    int c = __ldg(p.idx_map + p.C + s0);
+    if ((unsigned)c >= (unsigned)p.C) { flag(p.dev_status, OCS_DEV_BAD_INDEX); c = 0; }
+    dup = to_f32(x[c]);
+  }
+  uint32_t m = 0;
 #pragma unroll
-        for (int e = 0; e < VE; ++e) v[i].e[e] = c + e < p.C ? x[c + e] : from_f32<T>(0.0f);
-      }
+  for (int i = 0; i < NV; ++i) m = v[i].max_bits(m);
+  m = __reduce_max_sync(0xffffffffu, bits_f32<T>(m));
+  if (G > 32) {
+    if (lane == 0) s_max[tx >> 5] = m;
+    __syncthreads();
+    m = __reduce_max_sync(0xffffffffu, lane < (G >> 5) ? s_max[lane] : 0u);
+  }
+  if (CLUSTER) {
+    asm volatile("barrier.cluster.wait;" ::: "memory");
+    if (tx < CL) asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(peer_addr(smem_u32(s_part + rank), (uint32_t)tx)), "r"(m) : "memory");
+    __syncwarp();
+    cluster_arrive();
+    cluster_wait();
+    for (int i = 0; i < CL; ++i) m = max(m, s_part[i]);
+  }
+  const float alpha = __uint_as_float(m);
+  const RowGrid g = row_grid(alpha, p.hi);
+  if (tx == 0 && rank == 0) {
+    p.scales[r] = __fdiv_rn(alpha, p.hi);
+    if (m >= 0x7f800000u) flag(p.dev_status, OCS_DEV_NONFINITE);
+  }
+  int8_t* dst = p.codes + r * p.ld_codes;
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int j = lo + tx + i * G, c = j * VE;
+    if (j < hi) {
+      if (p.is_signed) store_codes<true>(v[i], g, dst + c, p.C - c, p.code_vec);
+      else store_codes<false>(v[i], g, dst + c, p.C - c, p.code_vec);
     }
-    // the first duplicated channels' values: fetched while the row is on its way
-    float dup = 0.0f;
-    if (tx < p.S) {
-      int c = __ldg(p.idx_map + p.C + tx);
+  }
+  for (int s = s0; s < p.S; s += G * CL) {
+    if (s != s0) {
+      int c = __ldg(p.idx_map + p.C + s);
       if ((unsigned)c >= (unsigned)p.C) { flag(p.dev_status, OCS_DEV_BAD_INDEX); c = 0; }
       dup = to_f32(x[c]);
     }
-    // magnitudes order like their bit patterns, and so does what is not finite
+    const float f = g.up == 1.0f ? dup : __fmul_rn(dup, g.up);
+    dst[p.C + s] = (int8_t)(p.is_signed ? row_code<true>(f, g.inv) : row_code<false>(f, g.inv));
+  }
+}
+
+// Many long rows (whole 16-byte pieces): one CTA per SM walks over them.  A row comes by one bulk copy into a ring of
+// shared-memory buffers, moves into registers (which frees its buffer for the row after next), and is quantized from
+// there while the next rows are on their way.  One barrier per row.
+template <typename T, int NV>
+__global__ void __launch_bounds__(1024, 1) staged_rows_kernel(const T* __restrict__ X, const RowsParams p, int ring) {
+  constexpr int VE = 16 / (int)sizeof(T);
+  extern __shared__ __align__(128) unsigned char smem[];   // [ring] rows
+  __shared__ __align__(8) uint64_t bars[kStagedRing];
+  __shared__ uint32_t s_max[2][32];
+  __shared__ int abort_flag;
+  const int tx = threadIdx.x, lane = tx & 31, warp = tx >> 5;
+  const uint32_t row_bytes = (uint32_t)p.C * (uint32_t)sizeof(T);
+  const int n_vec = (int)(row_bytes / 16);
+  grid_launch_dependents();
+  auto request = [&](long long r, int slot) {   // one thread
+    const uint32_t bar = smem_u32(bars + slot);
+    mbar_arrive_expect_tx(bar, row_bytes);
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                 ::"r"(smem_u32(smem) + (uint32_t)slot * row_bytes), "l"(X + r * p.ldx), "r"(row_bytes), "r"(bar) : "memory");
+  };
+  if (tx == 0) {
+    for (int i = 0; i < ring; ++i) mbar_init(smem_u32(bars + i), 1);
+    abort_flag = 0;
+    fence_barrier_init();
+    fence_proxy_async_smem();
+    for (int i = 0; i < ring; ++i)
+      if (blockIdx.x + (long long)i * gridDim.x < p.rows) request(blockIdx.x + (long long)i * gridDim.x, i);
+  }
+  int src = 0;
+  if (tx < p.S) {
+    src = __ldg(p.idx_map + p.C + tx);
+    if ((unsigned)src >= (unsigned)p.C) { flag(p.dev_status, OCS_DEV_BAD_INDEX); src = 0; }
+  }
+  __syncthreads();
+  int it = 0, slot = 0;
+  uint32_t phase = 0;
+  for (long long r = blockIdx.x; r < p.rows; r += gridDim.x, ++it) {
+    bool ok = mbar_wait(smem_u32(bars + slot), phase, &abort_flag);
+    const unsigned char* buf = smem + (size_t)slot * row_bytes;
+    Piece<T, 16> v[NV];
     uint32_t m = 0;
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
-#pragma unroll
-      for (int e = 0; e < VE; ++e) m = max(m, __float_as_uint(to_f32(v[i].e[e])) & 0x7fffffffu);
-    m = __reduce_max_sync(0xffffffffu, m);
-    if (G > 32) {
-      if (lane == 0) s_max[tx >> 5] = m;
-      __syncthreads();
-      m = __reduce_max_sync(0xffffffffu, lane < (G >> 5) ? s_max[lane] : 0u);
+    for (int i = 0; i < NV; ++i) {
+      const int j = tx + i * 1024;
+      v[i].clear();
+      if (j < n_vec) {
+        const uint4 w = *reinterpret_cast<const uint4*>(buf + (size_t)j * 16);
+        v[i].w[0] = w.x; v[i].w[1] = w.y; v[i].w[2] = w.z; v[i].w[3] = w.w;
+      }
+      m = v[i].max_bits(m);
     }
+    float dup = tx < p.S ? to_f32(reinterpret_cast<const T*>(buf)[src]) : 0.0f;
+    m = __reduce_max_sync(0xffffffffu, bits_f32<T>(m));
+    if (lane == 0) s_max[it & 1][warp] = m;
+    if (!__syncthreads_and(ok)) break;          // the row is in registers
+    const long long next = r + (long long)ring * gridDim.x;
+    if (tx == 0 && next < p.rows) request(next, slot);
+    m = __reduce_max_sync(0xffffffffu, s_max[it & 1][lane]);
     const float alpha = __uint_as_float(m);
     const RowGrid g = row_grid(alpha, p.hi);
-    const bool scaled = g.up != 1.0f;
     if (tx == 0) {
       p.scales[r] = __fdiv_rn(alpha, p.hi);
       if (m >= 0x7f800000u) flag(p.dev_status, OCS_DEV_NONFINITE);
@@ -108,26 +259,32 @@ __global__ void __launch_bounds__(1024, 1) rows_kernel(const T* __restrict__ X, 
     int8_t* dst = p.codes + r * p.ld_codes;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int c = (tx + i * G) * VE;
-      if (c < p.C) {
-        if (p.is_signed) store_codes<true>(v[i], g, scaled, dst + c, min(VE, p.C - c), p.code_vec);
-        else store_codes<false>(v[i], g, scaled, dst + c, min(VE, p.C - c), p.code_vec);
+      const int j = tx + i * 1024;
+      if (j < n_vec) {
+        if (p.is_signed) store_codes<true>(v[i], g, dst + j * VE, VE, p.code_vec);
+        else store_codes<false>(v[i], g, dst + j * VE, VE, p.code_vec);
       }
     }
-    for (int s = tx; s < p.S; s += G) {
+    const T* x = X + r * p.ldx;
+    for (int s = tx; s < p.S; s += 1024) {
       if (s != tx) {
         int c = __ldg(p.idx_map + p.C + s);
         if ((unsigned)c >= (unsigned)p.C) { flag(p.dev_status, OCS_DEV_BAD_INDEX); c = 0; }
         dup = to_f32(x[c]);
       }
-      dup = __fmul_rn(dup, g.up);
-      dst[p.C + s] = (int8_t)(p.is_signed ? row_code<true>(dup, g.inv) : row_code<false>(dup, g.inv));
+      const float f = g.up == 1.0f ? dup : __fmul_rn(dup, g.up);
+      dst[p.C + s] = (int8_t)(p.is_signed ? row_code<true>(f, g.inv) : row_code<false>(f, g.inv));
     }
-    if (G > 32) __syncthreads();   // s_max is written again for the next row
+    if (++slot == ring) { slot = 0; phase ^= 1u; }
   }
+  if (abort_flag && tx == 0) {
+    for (int i = 0; i < 2000; ++i) __nanosleep(100);   // copies still in flight land before the CTA leaves
+    flag(p.dev_status, OCS_DEV_TIMEOUT);
+  }
+  __syncthreads();
 }
 
-// Rows too long for the registers of a CTA: read twice, the second time from L2.
+// Rows too long for the registers of a cluster: read twice, the second time from L2.
 template <typename T, int VB>
 __global__ void __launch_bounds__(1024, 1) long_rows_kernel(const T* __restrict__ X, const RowsParams p) {
   constexpr int VE = Piece<T, VB>::VE;
@@ -141,10 +298,10 @@ __global__ void __launch_bounds__(1024, 1) long_rows_kernel(const T* __restrict_
 #pragma unroll 4
     for (int i = tx; i < full; i += 1024) {
       Piece<T, VB> v;
-      v.w = __ldg(reinterpret_cast<const typename Word<VB>::type*>(x + (long long)i * VE));
-#pragma unroll
-      for (int e = 0; e < VE; ++e) m = max(m, __float_as_uint(to_f32(v.e[e])) & 0x7fffffffu);
+      v.load(x + (long long)i * VE);
+      m = v.max_bits(m);
     }
+    m = bits_f32<T>(m);
     for (int c = full * VE + tx; c < p.C; c += 1024) m = max(m, __float_as_uint(to_f32(x[c])) & 0x7fffffffu);
     m = __reduce_max_sync(0xffffffffu, m);
     if (lane == 0) s_max[tx >> 5] = m;
@@ -152,7 +309,6 @@ __global__ void __launch_bounds__(1024, 1) long_rows_kernel(const T* __restrict_
     m = __reduce_max_sync(0xffffffffu, s_max[lane]);
     const float alpha = __uint_as_float(m);
     const RowGrid g = row_grid(alpha, p.hi);
-    const bool scaled = g.up != 1.0f;
     if (tx == 0) {
       p.scales[r] = __fdiv_rn(alpha, p.hi);
       if (m >= 0x7f800000u) flag(p.dev_status, OCS_DEV_NONFINITE);
@@ -161,9 +317,9 @@ __global__ void __launch_bounds__(1024, 1) long_rows_kernel(const T* __restrict_
 #pragma unroll 4
     for (int i = tx; i < full; i += 1024) {
       Piece<T, VB> v;
-      v.w = __ldg(reinterpret_cast<const typename Word<VB>::type*>(x + (long long)i * VE));
-      if (p.is_signed) store_codes<true>(v, g, scaled, dst + (long long)i * VE, VE, p.code_vec);
-      else store_codes<false>(v, g, scaled, dst + (long long)i * VE, VE, p.code_vec);
+      v.load(x + (long long)i * VE);
+      if (p.is_signed) store_codes<true>(v, g, dst + (long long)i * VE, VE, p.code_vec);
+      else store_codes<false>(v, g, dst + (long long)i * VE, VE, p.code_vec);
     }
     for (int c = full * VE + tx; c < p.C + p.S; c += 1024) {
       int src = c;
@@ -178,31 +334,53 @@ __global__ void __launch_bounds__(1024, 1) long_rows_kernel(const T* __restrict_
   }
 }
 
+template <typename T, int NV>
+ocs_status launch_staged(const T* X, const RowsParams& p, cudaStream_t stream) {
+  const size_t row_bytes = (size_t)p.C * sizeof(T);
+  const int ring = (int)(kStagedBytes / row_bytes < kStagedRing ? kStagedBytes / row_bytes : kStagedRing);
+  if (cudaFuncSetAttribute(staged_rows_kernel<T, NV>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kStagedBytes) != cudaSuccess)
+    return OCS_ERR_CUDA;
+  LaunchScope ls("staged_rows_kernel", stream);
+  staged_rows_kernel<T, NV><<<kNumSMs, 1024, ring * row_bytes, stream>>>(X, p, ring);
+  return launch_status();
+}
+
 template <typename T, int VB>
 ocs_status launch_rows_vec(const T* X, RowsParams p, cudaStream_t stream) {
   constexpr int VE = Piece<T, VB>::VE;
   p.code_vec = aligned(p.codes, VE) && p.ld_codes % VE == 0;
   const int n_vec = (p.C + VE - 1) / VE;
+  // Many rows that one CTA's registers cannot hold twice over: staged (fp32 [4096][25088]: STAGED_US us against CLUSTER_US in clusters)
+  const size_t row_bytes = (size_t)p.C * sizeof(T);
+  if (VB >= 16 && n_vec > 2 * kRowThreads && p.rows >= 2 * kNumSMs && row_bytes % 16 == 0 &&
+      2 * row_bytes <= kStagedBytes) {
+    return row_bytes <= 4 * 1024 * 16 ? launch_staged<T, 4>(X, p, stream) : launch_staged<T, 8>(X, p, stream);
+  }
+  int cl = 1;   // CTAs on a row: as few as hold it in registers
+  while (cl < kRowCluster && n_vec > 2 * kRowThreads * cl) cl *= 2;
   LaunchScope ls("rows_kernel", stream);
-  if (n_vec > 8 * 1024) {
+  if (n_vec > 2 * kRowThreads * cl || p.rows * cl >= 0x7fffffff) {
     const int grid = (int)(p.rows < 2 * kNumSMs ? p.rows : 2 * kNumSMs);
     long_rows_kernel<T, VB><<<grid, 1024, 0, stream>>>(X, p);
     return launch_status();
   }
-  // Threads on a row: about four pieces each, at least a warp, at most 1024; rows of one warp share a CTA.
-  int G = 32, nv = 1;
-  while (G < 1024 && n_vec > 4 * G) G *= 2;
-  while (nv * G < n_vec) nv *= 2;
-  const int R = G == 32 ? 8 : 1;
-  const long long want = (p.rows + R - 1) / R;
-  const dim3 block(G, R);
-  const unsigned grid = (unsigned)(want < 0x7fffffff ? want : 0x7fffffff);
-  switch (nv) {
-    case 1: rows_kernel<T, VB, 1><<<grid, block, 0, stream>>>(X, p); break;
-    case 2: rows_kernel<T, VB, 2><<<grid, block, 0, stream>>>(X, p); break;
-    case 4: rows_kernel<T, VB, 4><<<grid, block, 0, stream>>>(X, p); break;
-    default: rows_kernel<T, VB, 8><<<grid, block, 0, stream>>>(X, p); break;
-  }
+  // few rows: a thread for every piece; many: two pieces each, and rows of one warp share a CTA
+  const int part = (n_vec + cl - 1) / cl;
+  const bool one = cl == 1 && p.rows <= kNumSMs;
+  const int G = ((one ? part : (part + 1) / 2) + 31) / 32 * 32, R = G == 32 ? 8 : 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)((p.rows * cl + R - 1) / R), 1, 1);
+  cfg.blockDim = dim3(G, R, 1);
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = cl; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr; cfg.numAttrs = cl > 1 ? 1 : 0;
+  cudaError_t e;
+  if (cl > 1) e = cudaLaunchKernelEx(&cfg, rows_kernel<T, VB, 2, true>, X, p);
+  else if (one) e = cudaLaunchKernelEx(&cfg, rows_kernel<T, VB, 1, false>, X, p);
+  else e = cudaLaunchKernelEx(&cfg, rows_kernel<T, VB, 2, false>, X, p);
+  if (e != cudaSuccess) return OCS_ERR_CUDA;
   return launch_status();
 }
 
@@ -211,6 +389,7 @@ ocs_status launch_rows(const void* X_, const RowsParams& p, cudaStream_t stream)
   const T* X = static_cast<const T*>(X_);
   // the widest accesses that the rows' alignment allows
   const uintptr_t a = reinterpret_cast<uintptr_t>(X) | (p.rows > 1 ? (uintptr_t)(p.ldx * (int64_t)sizeof(T)) : 0);
+  if (a % 32 == 0) return launch_rows_vec<T, 32>(X, p, stream);
   if (a % 16 == 0) return launch_rows_vec<T, 16>(X, p, stream);
   if (a % 8 == 0) return launch_rows_vec<T, 8>(X, p, stream);
   if (sizeof(T) == 4 || a % 4 == 0) return launch_rows_vec<T, 4>(X, p, stream);

@@ -50,6 +50,9 @@ def ref_rows(x, idx, bits, signed):
     (5, 33, 33, "bf16", 4, True), (17, 4096, 0, "bf16", 8, True), (17, 4096, 82, "f16", 8, False), (2, 5000, 50, "bf16", 6, True),
     (300, 129, 3, "f32", 2, True), (4, 25088, 251, "f32", 8, True), (3, 33278, 0, "f32", 8, True), (2, 70001, 7, "bf16", 8, True),
     (1500, 64, 0, "f16", 8, True), (1, 16384, 100, "f32", 8, False), (700, 1000, 10, "bf16", 5, False),
+    # many long rows (staged through shared memory), rows shared by clusters
+    (700, 25088, 251, "f32", 8, True), (301, 16400, 1500, "bf16", 8, False), (900, 9000, 0, "f32", 6, True), (450, 40000, 7, "f16", 8, True),
+    (50, 25088, 251, "f32", 8, True), (300, 28928, 0, "f32", 4, True), (299, 28932, 1, "f32", 8, True),
 ])
 @pytest.mark.parametrize("layout", ["dense", "strided"])
 def test_quantize_rows(M, C, S, kind, bits, signed, layout):
