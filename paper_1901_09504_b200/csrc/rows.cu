@@ -192,11 +192,11 @@ __global__ void __launch_bounds__(NV == 1 ? 1024 : kRowThreads, NV == 1 ? 1 : 3)
   }
 }
 
-// Many long rows (whole 16-byte pieces): one CTA per SM walks over them.  A row comes by one bulk copy into a ring of
+// Many long rows (whole 16-byte pieces): one CTA per SM, or two with half the threads, walk over them.  A row comes by one bulk copy into a ring of
 // shared-memory buffers, moves into registers (which frees its buffer for the row after next), and is quantized from
 // there while the next rows are on their way.  One barrier per row.
-template <typename T, int NV>
-__global__ void __launch_bounds__(1024, 1) staged_rows_kernel(const T* __restrict__ X, const RowsParams p, int ring) {
+template <typename T, int NV, int THREADS>
+__global__ void __launch_bounds__(THREADS, 1024 / THREADS) staged_rows_kernel(const T* __restrict__ X, const RowsParams p, int ring) {
   constexpr int VE = 16 / (int)sizeof(T);
   extern __shared__ __align__(128) unsigned char smem[];   // [ring] rows
   __shared__ __align__(8) uint64_t bars[kStagedRing];
@@ -235,7 +235,7 @@ __global__ void __launch_bounds__(1024, 1) staged_rows_kernel(const T* __restric
     uint32_t m = 0;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int j = tx + i * 1024;
+      const int j = tx + i * THREADS;
       v[i].clear();
       if (j < n_vec) {
         const uint4 w = *reinterpret_cast<const uint4*>(buf + (size_t)j * 16);
@@ -249,7 +249,7 @@ __global__ void __launch_bounds__(1024, 1) staged_rows_kernel(const T* __restric
     if (!__syncthreads_and(ok)) break;          // the row is in registers
     const long long next = r + (long long)ring * gridDim.x;
     if (tx == 0 && next < p.rows) request(next, slot);
-    m = __reduce_max_sync(0xffffffffu, s_max[it & 1][lane]);
+    m = __reduce_max_sync(0xffffffffu, lane < THREADS / 32 ? s_max[it & 1][lane] : 0u);
     const float alpha = __uint_as_float(m);
     const RowGrid g = row_grid(alpha, p.hi);
     if (tx == 0) {
@@ -259,14 +259,14 @@ __global__ void __launch_bounds__(1024, 1) staged_rows_kernel(const T* __restric
     int8_t* dst = p.codes + r * p.ld_codes;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int j = tx + i * 1024;
+      const int j = tx + i * THREADS;
       if (j < n_vec) {
         if (p.is_signed) store_codes<true>(v[i], g, dst + j * VE, VE, p.code_vec);
         else store_codes<false>(v[i], g, dst + j * VE, VE, p.code_vec);
       }
     }
     const T* x = X + r * p.ldx;
-    for (int s = tx; s < p.S; s += 1024) {
+    for (int s = tx; s < p.S; s += THREADS) {
       if (s != tx) {
         int c = __ldg(p.idx_map + p.C + s);
         if ((unsigned)c >= (unsigned)p.C) { flag(p.dev_status, OCS_DEV_BAD_INDEX); c = 0; }
@@ -334,14 +334,14 @@ __global__ void __launch_bounds__(1024, 1) long_rows_kernel(const T* __restrict_
   }
 }
 
-template <typename T, int NV>
+template <typename T, int NV, int THREADS>
 ocs_status launch_staged(const T* X, const RowsParams& p, cudaStream_t stream) {
-  const size_t row_bytes = (size_t)p.C * sizeof(T);
-  const int ring = (int)(kStagedBytes / row_bytes < kStagedRing ? kStagedBytes / row_bytes : kStagedRing);
-  if (cudaFuncSetAttribute(staged_rows_kernel<T, NV>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kStagedBytes) != cudaSuccess)
+  const size_t row_bytes = (size_t)p.C * sizeof(T), budget = kStagedBytes * THREADS / 1024;
+  const int ring = (int)(budget / row_bytes < kStagedRing ? budget / row_bytes : kStagedRing);
+  if (cudaFuncSetAttribute(staged_rows_kernel<T, NV, THREADS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)budget) != cudaSuccess)
     return OCS_ERR_CUDA;
   LaunchScope ls("staged_rows_kernel", stream);
-  staged_rows_kernel<T, NV><<<kNumSMs, 1024, ring * row_bytes, stream>>>(X, p, ring);
+  staged_rows_kernel<T, NV, THREADS><<<kNumSMs * 1024 / THREADS, THREADS, ring * row_bytes, stream>>>(X, p, ring);
   return launch_status();
 }
 
@@ -350,11 +350,15 @@ ocs_status launch_rows_vec(const T* X, RowsParams p, cudaStream_t stream) {
   constexpr int VE = Piece<T, VB>::VE;
   p.code_vec = aligned(p.codes, VE) && p.ld_codes % VE == 0;
   const int n_vec = (p.C + VE - 1) / VE;
-  // Many rows that one CTA's registers cannot hold twice over: staged (fp32 [4096][25088]: STAGED_US us against CLUSTER_US in clusters)
+  // Many rows that are too long for one CTA's registers are staged: two CTAs of 512 threads per SM (whose rows overlap) as
+  // long as their registers hold a row, else one of 1024.  Against the same rows in clusters, us: fp32 [4096][25088] 78.5
+  // / 124.5; fp32 [4096][10000] 37.4 / 49.8 (47.3 with one CTA per SM); bf16 [2000][33280] 35.8 / 51.3; at 300 rows they
+  // are even (13.1 / 12.3), and rows that fit one CTA's registers are as fast unstaged (bf16 [8192][8192] 31.7, staged 40).
   const size_t row_bytes = (size_t)p.C * sizeof(T);
-  if (VB >= 16 && n_vec > 2 * kRowThreads && p.rows >= 2 * kNumSMs && row_bytes % 16 == 0 &&
-      2 * row_bytes <= kStagedBytes) {
-    return row_bytes <= 4 * 1024 * 16 ? launch_staged<T, 4>(X, p, stream) : launch_staged<T, 8>(X, p, stream);
+  if (VB >= 16 && n_vec > 2 * kRowThreads && p.rows >= 2 * kNumSMs && row_bytes % 16 == 0 && 2 * row_bytes <= kStagedBytes) {
+    if (row_bytes <= 6 * 512 * 16) return launch_staged<T, 6, 512>(X, p, stream);
+    if (row_bytes <= 10 * 512 * 16) return launch_staged<T, 10, 512>(X, p, stream);
+    return launch_staged<T, 8, 1024>(X, p, stream);
   }
   int cl = 1;   // CTAs on a row: as few as hold it in registers
   while (cl < kRowCluster && n_vec > 2 * kRowThreads * cl) cl *= 2;

@@ -94,6 +94,40 @@ def linear_forward(L: QLayer, x, a_signed: bool, a_bits: int = 8, dev_status=Non
                          A_codes_T=codes_T)
 
 
+# ------------------------------------------------------------- linear layers with token and channel scales
+@dataclass
+class RowLayer:
+    """A split linear layer quantized with one scale per output channel; its activations get one per row (token)."""
+    codes: torch.Tensor        # int8 [O, ld >= C + S]
+    w_scales: torch.Tensor     # fp32 [O]
+    idx_map: torch.Tensor      # int32 [C + S]
+    bias: torch.Tensor | None  # fp32 [O]
+    C: int
+    O: int
+    S: int
+
+
+def prepare_row_layer(W, bias, ratio: float, bits: int, qa_bits: int = 0, dev_status=None) -> RowLayer:
+    """W fp32 [O, C] on the device -> RowLayer (ocs_split, then ocs_quantize_rows: every output channel its own grid)."""
+    O, Cn = W.shape
+    S = B.ocs_num_splits(Cn, ratio)
+    W_out, idx_map, _, _ = B.ocs_split(W.contiguous(), S, qa_bits=qa_bits, dev_status=dev_status, want_order=False)
+    codes, w_scales = B.ocs_quantize_rows(W_out[:, :Cn + S], bits, True, dev_status=dev_status)
+    return RowLayer(codes, w_scales, idx_map, bias, Cn, O, S)
+
+
+def row_linear_forward(L: RowLayer, x, a_signed: bool = True, a_bits: int = 8, out_dtype=None, dev_status=None):
+    """x fp32 / fp16 / bf16 [M, C] -> [M, O] of x's type or out_dtype (ocs_linear_rows: every row of x its own grid)."""
+    return B.ocs_linear_rows(x, L.codes, L.w_scales, idx_map=L.idx_map, S=L.S, bits=a_bits, is_signed=a_signed, bias=L.bias,
+                             out_dtype=out_dtype, dev_status=dev_status)
+
+
+def _any_linear_forward(L, x, a_signed: bool, a_bits: int, dev_status):
+    if isinstance(L, RowLayer):
+        return row_linear_forward(L, x, a_signed, a_bits, dev_status=dev_status)
+    return linear_forward(L, x, a_signed, a_bits, dev_status)
+
+
 # ------------------------------------------------------------------------------------------ ResNet-50
 def batchable(W) -> bool:
     """True when ocs_split_quantize_batch can take this layer (the fused path's staging limits)."""
@@ -213,10 +247,17 @@ def _side_stream(device, which: int = 0):
     return _SIDE_STREAMS[key]
 
 
-def prepare_lstm(cfg, device, dev_status=None, fold: bool = False):
-    """cfg from ocs_inputs.configs.config5 -> dict of QLayers and the embedding table."""
+def prepare_lstm(cfg, device, dev_status=None, fold: bool = False, row_scales: bool = False):
+    """cfg from ocs_inputs.configs.config5 -> dict of QLayers and the embedding table.  row_scales: RowLayers instead
+    (a scale per output channel and per token; no clip search)."""
     p = cfg["params"]
     mode = B.CLIP_MSE if cfg["clip"] == "mse" else B.CLIP_NONE
+    if row_scales:
+        assert mode == B.CLIP_NONE and not fold
+        names = [(f"{nm}{l}", f"{bn}{l}") for l in range(2) for nm, bn in (("W_ih", "b_ih"), ("W_hh", "b_hh"))] + [("W_dec", "b_dec")]
+        out = {nm: prepare_row_layer(torch.from_numpy(p[nm]).to(device), torch.from_numpy(p[bn]).to(device), cfg["ratio"],
+                                     cfg["w_bits"], dev_status=dev_status) for nm, bn in names}
+        return {"emb": torch.from_numpy(p["emb"]).to(device), **out}
     out = {"emb": torch.from_numpy(p["emb"]).to(device)}
     for layer in range(2):
         for nm, bn in (("W_ih", "b_ih"), ("W_hh", "b_hh")):
@@ -228,10 +269,9 @@ def prepare_lstm(cfg, device, dev_status=None, fold: bool = False):
     return out
 
 
-def lstm_forward(cfg, layers, tokens, a_bits: int = 8, keep: bool = False, dev_status=None, before_decoder=None):
-    """tokens int32 [seq, batch] on the device -> logits fp32 [seq * batch, vocab] (h0 = c0 = 0).
-    before_decoder: called right before the decoder layer (a caller that prepares the decoder's weights on
-    another stream while the time steps run makes its stream wait there)."""
+def lstm_hidden(cfg, layers, tokens, a_bits: int = 8, dev_status=None):
+    """tokens int32 [seq, batch] on the device -> the upper layer's states fp32 [seq, batch, hidden], the embeddings and
+    both cells' last states (h0 = c0 = 0)."""
     seq, batch = tokens.shape
     hidden = cfg["hidden"]
     dev = tokens.device
@@ -265,9 +305,9 @@ def lstm_forward(cfg, layers, tokens, a_bits: int = 8, keep: bool = False, dev_s
                 ev_in[l].record(lay[l])              # h_prev is complete on this layer's stream
                 with torch.cuda.stream(helper[l]):
                     helper[l].wait_event(ev_in[l])
-                    g_hh = linear_forward(layers[f"W_hh{l}"], h_prev, True, a_bits, dev_status)
+                    g_hh = _any_linear_forward(layers[f"W_hh{l}"], h_prev, True, a_bits, dev_status)
                     ev_hh[l].record(helper[l])
-                g_ih = linear_forward(layers[f"W_ih{l}"], x, True, a_bits, dev_status)
+                g_ih = _any_linear_forward(layers[f"W_ih{l}"], x, True, a_bits, dev_status)
                 lay[l].wait_event(ev_hh[l])
                 B.ocs_lstm_cell(g_ih, g_hh, c[l], hs[l][t])
                 if l == 0:
@@ -275,10 +315,28 @@ def lstm_forward(cfg, layers, tokens, a_bits: int = 8, keep: bool = False, dev_s
     ev_end = torch.cuda.Event()
     ev_end.record(lay[1])
     main.wait_event(ev_end)
+    return tops, emb, c
+
+
+def lstm_forward(cfg, layers, tokens, a_bits: int = 8, keep: bool = False, dev_status=None, before_decoder=None):
+    """tokens int32 [seq, batch] on the device -> logits fp32 [seq * batch, vocab] (h0 = c0 = 0).
+    before_decoder: called right before the decoder layer (a caller that prepares the decoder's weights on
+    another stream while the time steps run makes its stream wait there)."""
+    tops, emb, c = lstm_hidden(cfg, layers, tokens, a_bits, dev_status)
     if before_decoder is not None:
         before_decoder()
-    logits = linear_forward(layers["W_dec"], tops.view(seq * batch, hidden), True, a_bits, dev_status)
+    logits = _any_linear_forward(layers["W_dec"], tops.view(-1, cfg["hidden"]), True, a_bits, dev_status)
     return (logits, dict(emb=emb, tops=tops, c=c)) if keep else logits
+
+
+def lstm_score(cfg, layers, tokens, targets, a_bits: int = 8, top_k: int = 0, inv_temperature: float = 1.0,
+               want_stats: bool = False, dev_status=None) -> B.TokenLogprobs:
+    """What the language model says of given tokens: tokens int32 [seq, batch] and the tokens to score after each of them,
+    targets int32 [seq, batch] (negative: none) -> TokenLogprobs over the seq * batch positions (ocs_token_logprobs on
+    the decoder's logits).  The model's perplexity (Section 6) is exp(-mean of logprob)."""
+    logits = lstm_forward(cfg, layers, tokens, a_bits, dev_status=dev_status)
+    return B.ocs_token_logprobs(logits, targets.reshape(-1), top_k=top_k, inv_temperature=inv_temperature,
+                                want_stats=want_stats, dev_status=dev_status)
 
 
 # ------------------------------------------------------------------------------ activation OCS
