@@ -375,27 +375,34 @@ row_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant_
       constexpr uint32_t kDescM = TW * CG;
       const uint32_t idesc = row_instr_desc(kDescM, TN, p.t_signed);
       const uint16_t mask = (uint16_t)(3u << (rank & ~1));
-      int it = 0, j = 0;
+      // This thread's instructions between two K-blocks are what bounds the narrow forms, so the loop carries a stage's
+      // addresses along instead of working them out.
+      const uint64_t w_desc0 = smem_desc_sw128(base), t_desc0 = smem_desc_sw128(FUSED ? smem_u32(tokens) : base + L::kWBytes);
+      int j = 0, s = 0;
+      uint32_t phase = 0;
       bool ok = true;
       for (int t = cluster; ok && t < p.total; t += n_clusters, ++j) {
         const int acc = j & 1;
         if (!mbar_wait_cluster(accempty_bar(acc), (((uint32_t)j >> 1) & 1u) ^ 1u, abort_flag)) break;
         tc_fence_after();
         const uint32_t d = tmem_base + (uint32_t)(acc * L::kAccStride);
-        for (int i = 0; i < my_kb; ++i, ++it) {
-          const int s = it % L::kStages;
-          if (!mbar_wait(full_bar(s), (uint32_t)(it / L::kStages) & 1u, abort_flag)) { ok = false; break; }
+        uint32_t more = 0;
+        uint64_t t_desc = t_desc0;   // FUSED: one token tile after the other
+        for (int i = 0; i < my_kb; ++i) {
+          if (!mbar_wait(full_bar(s), phase, abort_flag)) { ok = false; break; }
           tc_fence_after();
-          const uint32_t w = base + s * L::kStageBytes;
-          const uint32_t x = FUSED ? smem_u32(tokens) + (uint32_t)i * L::kTBytes : w + L::kWBytes;
+          const uint64_t w_desc = w_desc0 + (uint32_t)(s * (L::kStageBytes >> 4));
+          if (!FUSED) t_desc = t_desc0 + (uint32_t)(s * (L::kStageBytes >> 4));
 #pragma unroll
-          for (int k = 0; k < KB / UK; ++k) {
-            const uint32_t more = (i > 0 || k > 0) ? 1u : 0u;
-            if (CG == 2) umma_i8_pair(d, smem_desc_sw128(w + k * UK), smem_desc_sw128(x + k * UK), idesc, more);
-            else umma_i8(d, smem_desc_sw128(w + k * UK), smem_desc_sw128(x + k * UK), idesc, more);
+          for (int k = 0; k < KB / UK; ++k) {   // 32 bytes on, 2 in the descriptors' units of 16
+            if (CG == 2) umma_i8_pair(d, w_desc + 2 * k, t_desc + 2 * k, idesc, k == 0 ? more : 1u);
+            else umma_i8(d, w_desc + 2 * k, t_desc + 2 * k, idesc, k == 0 ? more : 1u);
           }
+          more = 1;
+          if (FUSED) t_desc += L::kTBytes >> 4;
           if (CG == 2) umma_commit_pair(empty_bar(s), mask);
           else umma_commit(empty_bar(s));
+          if (++s == L::kStages) { s = 0; phase ^= 1; }
         }
         if (!ok) break;
         if (CG == 2) umma_commit_pair(accfull_bar(acc), mask);
