@@ -7,6 +7,12 @@
 namespace ocs {
 namespace {
 
+// K-blocks of one ring stage.  A stage costs the tensor-core thread about 0.2 us of waiting, issuing and committing
+// whatever it holds, which bounds the narrow forms: with two K-blocks a stage the 64-token form takes 89 instead of 110 us
+// at (M, K, N) = (1024, 8192, 8192), the 16-token form 46.0 instead of 48.0 at (1, 16384, 16384); the wide forms are even
+// (128 tokens) or slower (256: 344 instead of 331 at 8192 cubed) with half as many stages.
+__host__ __device__ constexpr int stage_blocks(int tn) { return tn <= 64 ? 2 : 1; }
+
 constexpr int TW = 128;        // channels (weight rows) of one CTA's tile: the lanes of tensor memory
 constexpr int KB = 128;        // contraction bytes of a K-block: one 128-byte swizzle span
 constexpr int UK = 32;         // contraction indices of one tcgen05.mma.kind::i8
@@ -15,7 +21,7 @@ constexpr int kEpiWarps = 8;
 constexpr int kFusedCodes = 64 * 1024;         // token codes a CTA can hold beside the ring of weights
 
 struct RowGemm {
-  int M, N, num_kb, t_signed;
+  int M, N, num_kb, t_signed;     // num_kb: stages' worth of contraction (K-blocks, or pairs of them)
   int n_tiles, m_tiles, total;   // channel tiles (TW * CG), token tiles (TN)
   int slices;                    // CTAs (pairs) that share a tile and split its K-blocks
   const float* a_scales;
@@ -36,7 +42,8 @@ template <int TN, int CG, bool FUSED>
 struct RowSmem {
   static constexpr int kTokens = TN / CG;                       // token rows this CTA stages
   static constexpr int kWBytes = TW * KB, kTBytes = kTokens * KB;
-  static constexpr int kStageBytes = FUSED ? kWBytes : kWBytes + kTBytes;
+  static constexpr int kSub = stage_blocks(TN);
+  static constexpr int kStageBytes = kSub * (FUSED ? kWBytes : kWBytes + kTBytes);
   // FUSED: the codes of all the K-blocks a CTA takes stay in a region of their own
   static constexpr int kTokenBytes = FUSED ? kFusedCodes : 0;
   // partial sums of this CTA's share (K split): a buffer of their own, or the operand ring where it would cost the ring
@@ -140,7 +147,7 @@ __device__ __forceinline__ int token_code(float x, float inv, uint32_t max_bits,
   return is_signed ? row_code<true>(v, inv) : row_code<false>(v, inv);
 }
 
-// The epilogue warps quantize the token tile that starts at row m0 straight into the operand tiles of K-blocks slice,
+// The epilogue warps quantize the token tile that starts at row m0 straight into the operand tiles of stages slice,
 // slice + slices, ...: first the rows' maxima, 512 elements per warp and step, then the codes, one row of a K-block per
 // warp and step.  What does not come in whole fours of channels goes one by one: a row's last C % 4 channels and the
 // duplicated ones (item u: contraction index C4 + u / rows of row u % rows; the first item's value is on its way from the
@@ -154,8 +161,9 @@ __device__ __forceinline__ void quantize_tokens(const RowGemm& p, const X* x0, i
   const bool wide = p.x_align >= 16;
   // where the code of item (contraction index k, row r) goes; -1: not in this CTA's share
   auto place = [&](int k, int r) {
-    const int kb = k / KB, i = kb / p.slices, in = k % KB;
-    return kb - i * p.slices == slice ? (i * TN + r) * KB + (((in >> 4) ^ (r & 7)) << 4) + (in & 15) : -1;
+    constexpr int kSub = stage_blocks(TN);
+    const int st = k / (kSub * KB), i = st / p.slices, in = k % KB;
+    return st - i * p.slices == slice ? ((i * kSub + k / KB % kSub) * TN + r) * KB + (((in >> 4) ^ (r & 7)) << 4) + (in & 15) : -1;
   };
   int src = 0, at = -1, item_row = 0, item_k = 0;
   if (et < n_items) {
@@ -204,13 +212,14 @@ __device__ __forceinline__ void quantize_tokens(const RowGemm& p, const X* x0, i
   }
   asm volatile("bar.sync 1, 256;" ::: "memory");
   if (at >= 0) tok[at] = (unsigned char)token_code(value, inv[item_row], max_bits[item_row], p.t_signed);
-  const int steps = C4 > 0 ? my_kb * rows : 0;
+  constexpr int kSub = stage_blocks(TN);
+  const int steps = C4 > 0 ? my_kb * kSub * rows : 0;
   for (int u0 = warp; u0 < steps; u0 += D * kEpiWarps) {
     Four<X> f[D];
     int rr[D], to[D];
 #pragma unroll
     for (int b = 0; b < D; ++b) {
-      const int u = u0 + b * kEpiWarps, i = u / rows, r = u - i * rows, k = (slice + i * p.slices) * KB + lane * 4;
+      const int u = u0 + b * kEpiWarps, i = u / rows, r = u - i * rows, k = ((slice + i / kSub * p.slices) * kSub + i % kSub) * KB + lane * 4;
       rr[b] = u < steps ? r : 0;
       // past the last contraction index the weights' tile is zero
       to[b] = u < steps && k < C4 ? (i * TN + r) * KB + (((lane >> 2) ^ (r & 7)) << 4) + (lane & 3) * 4 : -1;
@@ -331,13 +340,22 @@ row_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant_
       int ahead = 0;
       int mt, nt;
       auto load_w = [&](int s, int kb) {
-        if (CG == 2) tma_load_2d_pair(base + s * L::kStageBytes, &tm_w, peer_addr(full_bar(s), lead), kb * KB, (nt * CG + half) * TW);
-        else tma_load_2d(base + s * L::kStageBytes, &tm_w, full_bar(s), kb * KB, nt * TW);
+#pragma unroll
+        for (int u = 0; u < L::kSub; ++u) {
+          const uint32_t dst = base + s * L::kStageBytes + u * L::kWBytes;
+          const int x = (kb * L::kSub + u) * KB;
+          if (CG == 2) tma_load_2d_pair(dst, &tm_w, peer_addr(full_bar(s), lead), x, (nt * CG + half) * TW);
+          else tma_load_2d(dst, &tm_w, full_bar(s), x, nt * TW);
+        }
       };
       auto load_t = [&](int s, int kb) {
-        const uint32_t dst = base + s * L::kStageBytes + L::kWBytes;
-        if (CG == 2) tma_load_2d_pair(dst, &tm_t, peer_addr(full_bar(s), lead), kb * KB, mt * TN + half * L::kTokens);
-        else tma_load_2d(dst, &tm_t, full_bar(s), kb * KB, mt * TN);
+#pragma unroll
+        for (int u = 0; u < L::kSub; ++u) {
+          const uint32_t dst = base + s * L::kStageBytes + L::kSub * L::kWBytes + u * L::kTBytes;
+          const int x = (kb * L::kSub + u) * KB;
+          if (CG == 2) tma_load_2d_pair(dst, &tm_t, peer_addr(full_bar(s), lead), x, mt * TN + half * L::kTokens);
+          else tma_load_2d(dst, &tm_t, full_bar(s), x, mt * TN);
+        }
       };
       if (cluster < p.total) {
         tile_of(p, cluster, &mt, &nt);
@@ -377,7 +395,7 @@ row_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant_
       const uint16_t mask = (uint16_t)(3u << (rank & ~1));
       // This thread's instructions between two K-blocks are what bounds the narrow forms, so the loop carries a stage's
       // addresses along instead of working them out.
-      const uint64_t w_desc0 = smem_desc_sw128(base), t_desc0 = smem_desc_sw128(FUSED ? smem_u32(tokens) : base + L::kWBytes);
+      const uint64_t w_desc0 = smem_desc_sw128(base), t_desc0 = smem_desc_sw128(FUSED ? smem_u32(tokens) : base + L::kSub * L::kWBytes);
       int j = 0, s = 0;
       uint32_t phase = 0;
       bool ok = true;
@@ -394,12 +412,14 @@ row_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant_
           const uint64_t w_desc = w_desc0 + (uint32_t)(s * (L::kStageBytes >> 4));
           if (!FUSED) t_desc = t_desc0 + (uint32_t)(s * (L::kStageBytes >> 4));
 #pragma unroll
-          for (int k = 0; k < KB / UK; ++k) {   // 32 bytes on, 2 in the descriptors' units of 16
-            if (CG == 2) umma_i8_pair(d, w_desc + 2 * k, t_desc + 2 * k, idesc, k == 0 ? more : 1u);
-            else umma_i8(d, w_desc + 2 * k, t_desc + 2 * k, idesc, k == 0 ? more : 1u);
+          for (int k = 0; k < L::kSub * KB / UK; ++k) {   // 32 bytes on, 2 in the descriptors' units of 16
+            const int u = k / (KB / UK), in = k % (KB / UK);
+            const uint64_t w = w_desc + u * (L::kWBytes >> 4) + 2 * in, x = t_desc + u * (L::kTBytes >> 4) + 2 * in;
+            if (CG == 2) umma_i8_pair(d, w, x, idesc, k == 0 ? more : 1u);
+            else umma_i8(d, w, x, idesc, k == 0 ? more : 1u);
           }
           more = 1;
-          if (FUSED) t_desc += L::kTBytes >> 4;
+          if (FUSED) t_desc += L::kSub * (L::kTBytes >> 4);
           if (CG == 2) umma_commit_pair(empty_bar(s), mask);
           else umma_commit(empty_bar(s));
           if (++s == L::kStages) { s = 0; phase ^= 1; }
@@ -564,43 +584,46 @@ std::atomic<int> g_force_tn{0}, g_force_cg{0}, g_force_slices{0};
 // CTAs resident at once, one per SM, for cluster sizes 1, 2, 4, 8 (a cluster lies inside one GPC)
 int cluster_capacity(int cl) { return cl <= 2 ? 148 : (cl == 4 ? 132 : 120); }
 
-bool split_fits(int tn, int cg, int slices, long long tiles, int num_kb) {
+int stages_of(int tn, int num_kb) { return (num_kb + stage_blocks(tn) - 1) / stage_blocks(tn); }
+
+bool split_fits(int tn, int cg, int slices, long long tiles, int stages) {
   if (slices == 1) return true;
-  return cg == 1 && tn < 256 && tn / slices >= 4 && slices <= num_kb && tiles * slices <= cluster_capacity(slices);
+  return cg == 1 && tn < 256 && tn / slices >= 4 && slices <= stages && tiles * slices <= cluster_capacity(slices);
 }
 
-// The plan by a time model in microseconds, fitted to 1200 measurements (M 1..4096, K 300..25339, N 1024..33278, fp32
-// and 16-bit outputs, every plan that fits): root mean square error 7 %; the plan it picks is 0.3 % slower than the best
-// measured one on average, 7 % at worst.  A tile costs its K-blocks, 0.25 us each in the narrow forms (bound by how fast
-// one SM takes operands in), and its epilogue, which adds to them instead of hiding behind them: the stores and the next
-// tile's operand requests share the SM's way out.  A K split adds the exchange.  Nothing is faster than the operands'
-// and outputs' bytes at 4.3 TB/s, and 3.85 us pass before the first and after the last tile.
+// The plan by a time model in microseconds, fitted to 806 measurements (M 1..4096, K 300..25339, N 1024..33278, fp32 and
+// 16-bit outputs, every plan that fits): root mean square error 5.5 %; the plan it picks is 0.4 % slower than the best
+// measured one on average, 10 % at worst.  A tile costs its K-blocks and its epilogue, which adds to them instead of hiding
+// behind them (the stores and the next tile's operand requests share the SM's way out), and 0.29 us; a K split adds the
+// exchange; the bytes take their time at 6.2 TB/s; of the two the longer one counts most (root of the sum of squares); and
+// 3.9 us pass before the first and after the last tile.
 RowPlan choose_plan(int M, int N, int num_kb, int out_bytes) {
   struct Form { int tn, cg; double block_us, epilogue_us; };
-  static const Form forms[6] = {{16, 1, 0.25, 0.0},  {32, 1, 0.25, 0.03},  {64, 1, 0.25, 0.2},
-                                {128, 1, 0.25, 0.96}, {256, 1, 0.34, 2.27}, {256, 2, 0.28, 3.16}};
+  static const Form forms[6] = {{16, 1, 0.18, 0.0},  {32, 1, 0.18, 0.01},  {64, 1, 0.18, 0.27},
+                                {128, 1, 0.23, 0.91}, {256, 1, 0.33, 2.17}, {256, 2, 0.27, 3.02}};
   auto tiles_of = [&](int tn, int cg) {
     return (long long)((M + (long long)tn - 1) / tn) * ((N + (long long)TW * cg - 1) / (TW * cg));
   };
   const int ft = g_force_tn.load(), fc = g_force_cg.load(), fs = g_force_slices.load();
   if (ft) {
     RowPlan r{ft, fc, fs};
-    while (r.slices > 1 && !split_fits(r.tn, r.cg, r.slices, tiles_of(r.tn, r.cg), num_kb)) r.slices /= 2;
+    while (r.slices > 1 && !split_fits(r.tn, r.cg, r.slices, tiles_of(r.tn, r.cg), stages_of(r.tn, num_kb))) r.slices /= 2;
     return r;
   }
   const double K = (double)num_kb * KB;
-  const double bytes_us = ((double)N * K + (double)M * K + (double)M * N * out_bytes) / 4.3e6;
+  const double bytes_us = ((double)N * K + (double)M * K + (double)M * N * out_bytes) / 6.22e6;
   RowPlan best{16, 1, 1};
-  double best_us = 1e300;
+  double best_us = 1e300;   // squared
   for (const Form& f : forms) {
     const long long tiles = tiles_of(f.tn, f.cg);
     for (int s = 1; s <= 8; s *= 2) {
-      if (!split_fits(f.tn, f.cg, s, tiles, num_kb)) continue;
+      if (!split_fits(f.tn, f.cg, s, tiles, stages_of(f.tn, num_kb))) continue;
       const long long slots = cluster_capacity(f.cg * s) / (f.cg * s);
       const double waves = (double)((tiles + slots - 1) / slots);
-      double us = waves * (((num_kb + s - 1) / s) * f.block_us + f.epilogue_us * (out_bytes == 4 ? 1.5 : 1.0) + 0.27);
-      if (s > 1) us += 0.16 + 3.62 * f.tn / 128.0;
-      if (bytes_us > us) us = bytes_us + 1e-3 * us;   // equally bound by bytes: the one with less other work
+      const int blocks = (stages_of(f.tn, num_kb) + s - 1) / s * stage_blocks(f.tn);
+      double us = waves * (blocks * f.block_us + f.epilogue_us * (out_bytes == 4 ? 1.2 : 1.0) + 0.29);
+      if (s > 1) us += 3.85 * f.tn / 128.0;
+      us = us * us + bytes_us * bytes_us;   // (its root, plus a constant)
       if (us < best_us) { best_us = us; best = RowPlan{f.tn, f.cg, s}; }
     }
   }
@@ -662,7 +685,7 @@ ocs_status launch_tiles(RowGemm p, int slices, const void* A, long long lda, con
 bool fuse_tokens(const RowPlan& plan, int M, int N, int C, int num_kb, int x_bytes, int x_align) {
   if (plan.tn > 32 || plan.cg != 1 || x_align < 8) return false;
   const long long m_tiles = (M + plan.tn - 1) / plan.tn, tiles = m_tiles * ((N + TW - 1) / TW);
-  const int my_kb = (num_kb + plan.slices - 1) / plan.slices;
+  const int my_kb = (stages_of(plan.tn, num_kb) + plan.slices - 1) / plan.slices * stage_blocks(plan.tn);
   if ((long long)my_kb * plan.tn * KB > kFusedCodes) return false;                                // the codes have to fit
   if (m_tiles > 1 && tiles > cluster_capacity(plan.slices) / plan.slices) return false;           // one token tile per CTA
   return (long long)(M < plan.tn ? M : plan.tn) * C * x_bytes <= kFuseBytes;
@@ -689,9 +712,11 @@ struct Product {
 template <typename T>
 ocs_status launch_product(const Product& g, void* Y_, bool overlap, cudaStream_t stream) {
   RowGemm p{};
-  p.M = g.M; p.N = g.N; p.num_kb = (g.K + KB - 1) / KB; p.t_signed = g.a_signed;
+  p.M = g.M; p.N = g.N; p.t_signed = g.a_signed;
   p.a_scales = g.a_scales; p.w_scales = g.w_scales; p.bias = g.bias; p.ldy = g.ldy; p.dev_status = g.dev_status;
-  const RowPlan plan = choose_plan(g.M, g.N, p.num_kb, (int)sizeof(T));
+  const int num_kb = (g.K + KB - 1) / KB;
+  const RowPlan plan = choose_plan(g.M, g.N, num_kb, (int)sizeof(T));
+  p.num_kb = stages_of(plan.tn, num_kb);
   T* Y = static_cast<T*>(Y_);
   if (!g.A) {
     p.X = g.X; p.ldx = g.ldx; p.idx_map = g.idx_map; p.x_type = g.x_type; p.C = g.C; p.K = g.K; p.hi = g.hi;
