@@ -9,6 +9,7 @@ constexpr int kMaxTop = 64;
 constexpr int kLpThreads = 256;
 constexpr int kWarps = kLpThreads / 32;
 constexpr int kMaxCluster = 8;        // CTAs that may share a row
+static_assert(kWarps == 8 && kMaxCluster == 8, "join_eight");
 constexpr int kCandidates = 2048;     // elements that can still be among the largest
 constexpr float kFloor = -200.0f;     // 2^-200 is zero in fp32: exponents are clamped here, so that a masked token (d = -infinity)
                                       // contributes 0 to the sums and not 0 * infinity
@@ -159,15 +160,24 @@ template <typename T>
 __device__ __forceinline__ bool sums_hold(float m, float c) {
   return fabsf(m) < 0x1p90f && c < 0x1p20f && __fmul_rn(__fsub_rn(lowest<T>(), m), c) <= -160.0f;
 }
-__device__ __forceinline__ Stats warp_stats(Stats t, float c) {
-  float m = t.m;
-  for (int o = 16; o > 0; o >>= 1) m = max_nan(m, __shfl_xor_sync(0xffffffffu, m, o));
-  move_max(t, m, c);
+__device__ __forceinline__ float warp_max(float m) {   // NaN if any lane's is
+  float r;
+  asm("redux.sync.max.NaN.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(m));
+  return r;
+}
+// Sums over groups of LANES lanes, whose statistics are relative to one maximum.
+template <int LANES>
+__device__ __forceinline__ void add_lanes(Stats& t) {
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
+  for (int o = LANES / 2; o > 0; o >>= 1) {
     t.s = __fadd_rn(t.s, __shfl_xor_sync(0xffffffffu, t.s, o));
     t.w = __fadd_rn(t.w, __shfl_xor_sync(0xffffffffu, t.w, o));
   }
+}
+// The eight parts that lanes 0..7 hold (and lanes 8..15, ... again) as one, in every lane.
+__device__ __forceinline__ Stats join_eight(Stats t, float c) {
+  move_max(t, warp_max(t.m), c);
+  add_lanes<8>(t);
   return t;
 }
 
@@ -204,10 +214,6 @@ __device__ __forceinline__ void take(Running& t, const Vec<T>& v, int j, float c
     t.w[i & 1] = fmaf(e, d, t.w[i & 1]);
   }
 }
-__device__ __forceinline__ float warp_max(float m) {   // NaN if any lane's is
-  for (int o = 16; o > 0; o >>= 1) m = max_nan(m, __shfl_xor_sync(0xffffffffu, m, o));
-  return m;
-}
 
 struct LogprobParams {
   long long rows, ld;
@@ -225,7 +231,8 @@ struct LogprobSmem {
   __align__(16) key_t cand[kCandidates];
   __align__(16) key_t top[kMaxCluster * kMaxTop];      // each CTA's largest, descending
   key_t best[kMaxTop];                                 // the row's
-  key_t low[kWarps], high[kWarps];
+  uint32_t low[kWarps];                                // the smallest of a warp's threads' largest elements, as ord_encode
+  key_t next[kWarps];
   int hot[kLpThreads];
   int n_hot, n_cand;
 };
@@ -243,18 +250,18 @@ __device__ __forceinline__ int count_larger(const key_t* list, int n, key_t v) {
   return r;
 }
 
-template <bool MAX>
-__device__ __forceinline__ key_t warp_reduce(key_t v) {
+__device__ __forceinline__ key_t warp_max_key(key_t v) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) {
     const key_t other = __shfl_xor_sync(0xffffffffu, v, o);
-    v = (other > v) == MAX ? other : v;
+    v = other > v ? other : v;
   }
   return v;
 }
 
 // The k largest elements of vectors [lo, hi) of the row, descending, as keys in out (zeros where there are fewer), given
-// every thread's largest element (its value, and the vector that holds it first).
+// every thread's largest element (its value m, and the vector that holds it first), the segment's, and in sm every warp's
+// smallest m, a count of zero and zeros in out.
 //   1. tau: a key that at least k of the threads' largest elements are not below, and not many more than k, by bisection
 //      (each step counts with one barrier).  The threads' keys are lowered to the last index of their vector, so at least
 //      k elements are not below tau, and only threads whose key, raised to the first index, is not below tau hold one.
@@ -262,29 +269,20 @@ __device__ __forceinline__ key_t warp_reduce(key_t v) {
 //   3. The k largest of what was collected, by rank.
 // Many unluckily placed elements may overflow the list; then the keys are found one after the other.
 template <typename T>
-__device__ void top_of_segment(const RowVectors<T>& row, int lo, int hi, int k, float m, int pos, LogprobSmem& sm, key_t* out) {
+__device__ void top_of_segment(const RowVectors<T>& row, int lo, int hi, int k, float m, int pos, float largest, LogprobSmem& sm,
+                               key_t* out) {
   constexpr int VE = Vec<T>::VE;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const bool any = lo + tid < hi;
-  const key_t low = any ? top_key(m, min(row.first(pos) + VE, row.V) - 1) : 0;
-  const key_t high = any ? top_key(m, max(row.first(pos), 0)) : 0;
   key_t tau = 0;
-  const key_t wmin = warp_reduce<false>(any ? low : ~0ull), wmax = warp_reduce<true>(low);
-  if (lane == 0) { sm.low[warp] = wmin; sm.high[warp] = wmax; }
-  if (tid == 0) sm.n_hot = sm.n_cand = 0;
-  if (tid < k) out[tid] = 0;
-  __syncthreads();
   if (hi - lo >= k && hi - lo >= kLpThreads) {   // every thread has an element; with fewer of them nothing is left out
-    key_t above;
-    tau = sm.low[0];
-    above = sm.high[0];
+    const key_t low = top_key(m, min(row.first(pos) + VE, row.V) - 1);
+    uint32_t least = sm.low[0];
 #pragma unroll
-    for (int w = 1; w < kWarps; ++w) {
-      tau = min(tau, sm.low[w]);
-      above = max(above, sm.high[w]);
-    }
-    // all threads are at or above tau, k - 1 at the most at or above `above` + 1
-    ++above;
+    for (int w = 1; w < kWarps; ++w) least = min(least, sm.low[w]);
+    // all threads are at or above tau, k - 1 at the most at or above `above`
+    tau = (key_t)least << 32;
+    key_t above = (key_t)ord_encode(largest + 0.0f) << 32 | 0xffffffffu;
     while (above - tau > 1) {
       const key_t mid = tau + (above - tau) / 2;
       const int n = __syncthreads_count(low >= mid);
@@ -293,15 +291,17 @@ __device__ void top_of_segment(const RowVectors<T>& row, int lo, int hi, int k, 
       if (n >= k && n <= k + k / 2 + 8) break;
     }
   }
-  if (any && high >= tau) sm.hot[atomicAdd(&sm.n_hot, 1)] = tid;
+  if (any && top_key(m, max(row.first(pos), 0)) >= tau) sm.hot[atomicAdd(&sm.n_hot, 1)] = tid;
   __syncthreads();
   const int vecs = (hi - lo + kLpThreads - 1) / kLpThreads, total = sm.n_hot * vecs;
   for (int q = tid; q < total; q += kLpThreads) {
     const int h = q / vecs;
     const int j = lo + sm.hot[h] + (q - h * vecs) * kLpThreads;
     if (j >= hi) continue;
+    const Vec<T> v = row.load(j);
+    if (ord_encode(v.max_all() + 0.0f) < (uint32_t)(tau >> 32)) continue;
     float f[VE];
-    row.load(j).floats(f);
+    v.floats(f);
     const int first = row.first(j);
 #pragma unroll
     for (int i = 0; i < VE; ++i) {
@@ -334,10 +334,10 @@ __device__ void top_of_segment(const RowVectors<T>& row, int lo, int hi, int k, 
           if (key < last && key > best) best = key;
         }
       }
-      best = warp_reduce<true>(best);
-      if (lane == 0) sm.high[warp] = best;
+      best = warp_max_key(best);
+      if (lane == 0) sm.next[warp] = best;
       __syncthreads();
-      for (int w = 0; w < kWarps; ++w) best = max(best, sm.high[w]);
+      for (int w = 0; w < kWarps; ++w) best = max(best, sm.next[w]);
       if (tid == 0) out[r] = best;
       last = best;
       __syncthreads();
@@ -398,8 +398,6 @@ __global__ void __launch_bounds__(kLpThreads, 5) logprobs_kernel(const T* __rest
       take(run, v, j, c);
     }
   }
-  const float own_max = run.m;
-  const int pos = run.pos;
   Stats t{warp_max(run.m), __fadd_rn(run.s[0], run.s[1]), __fadd_rn(run.w[0], run.w[1])};
   if (t.m > lowest<T>()) {   // from M to m * c
     const float d = fmaxf(fmaf(-t.m, c, run.M), kFloor), r = ex2(d), moved = fmaf(t.s, d, t.w);
@@ -408,37 +406,38 @@ __global__ void __launch_bounds__(kLpThreads, 5) logprobs_kernel(const T* __rest
   } else {
     t.s = t.w = 0.0f;        // nothing but masked tokens as far as the sums can tell
   }
-  t = warp_stats(t, c);
+  add_lanes<32>(t);
+  key_t* top = sm.top + rank * p.top_k;
+  if (p.top_k > 0) {         // what top_of_segment() expects
+    const uint32_t least = __reduce_min_sync(0xffffffffu, ord_encode(run.m + 0.0f));
+    if (lane == 0) sm.low[warp] = least;
+    if (tid < p.top_k) top[tid] = 0;
+    if (tid == 0) sm.n_hot = sm.n_cand = 0;
+  }
   if (lane == 0) sm.warp[warp] = t;
   __syncthreads();
-  {
-    float m = sm.warp[0].m;
+  float largest = sm.warp[0].m;
 #pragma unroll
-    for (int w = 1; w < kWarps; ++w) m = max_nan(m, sm.warp[w].m);
-    if (fabsf(m) < INFINITY && !sums_hold<T>(m, c)) {   // the same for the whole CTA
-      __syncthreads();
-      t = Stats{m, 0.0f, 0.0f};
-      for (int j = lo + tid; j < hi; j += kLpThreads) {
-        float f[VE];
-        row.load(j).floats(f);
+  for (int w = 1; w < kWarps; ++w) largest = max_nan(largest, sm.warp[w].m);
+  if (fabsf(largest) < INFINITY && !sums_hold<T>(largest, c)) {   // the same for the whole CTA
+    __syncthreads();
+    t = Stats{largest, 0.0f, 0.0f};
+    for (int j = lo + tid; j < hi; j += kLpThreads) {
+      float f[VE];
+      row.load(j).floats(f);
 #pragma unroll
-        for (int i = 0; i < VE; ++i) {
-          const float d = fmaxf(__fmul_rn(__fsub_rn(f[i], m), c), kFloor), e = ex2(d);
-          t.s = __fadd_rn(t.s, e);
-          t.w = fmaf(e, d, t.w);
-        }
+      for (int i = 0; i < VE; ++i) {
+        const float d = fmaxf(__fmul_rn(__fsub_rn(f[i], largest), c), kFloor), e = ex2(d);
+        t.s = __fadd_rn(t.s, e);
+        t.w = fmaf(e, d, t.w);
       }
-      t = warp_stats(t, c);
-      if (lane == 0) sm.warp[warp] = t;
-      __syncthreads();
     }
+    add_lanes<32>(t);
+    if (lane == 0) sm.warp[warp] = t;
+    __syncthreads();
   }
-  if (p.top_k > 0) {
-    top_of_segment(row, lo, hi, p.top_k, own_max, pos, sm, sm.top + rank * p.top_k);
-  }
-  // this CTA's part of the row (every warp works it out; lane w looks at warp w)
-  t = lane < kWarps ? sm.warp[lane] : Stats{-INFINITY, 0.0f, 0.0f};
-  t = warp_stats(t, c);
+  if (p.top_k > 0) top_of_segment(row, lo, hi, p.top_k, run.m, run.pos, largest, sm, top);
+  t = join_eight(sm.warp[lane & 7], c);   // this CTA's part of the row, in every thread
   if (CL > 1) {
     asm volatile("barrier.cluster.wait;" ::: "memory");
     if (rank != 0) {
@@ -457,8 +456,9 @@ __global__ void __launch_bounds__(kLpThreads, 5) logprobs_kernel(const T* __rest
     asm volatile("barrier.cluster.arrive.release;" ::: "memory");
     asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
     const Stats own = t;
-    t = lane == 0 ? own : (lane < CL ? sm.part[lane] : Stats{-INFINITY, 0.0f, 0.0f});
-    t = warp_stats(t, c);
+    const int part = lane & 7;
+    t = part == 0 ? own : (part < CL ? sm.part[part] : Stats{-INFINITY, 0.0f, 0.0f});
+    t = join_eight(t, c);
     if (p.top_k > 0) {
       for (int i = tid; i < CL * p.top_k; i += kLpThreads) {
         const key_t k = sm.top[i];
