@@ -275,12 +275,12 @@ __device__ void top_of_segment(const RowVectors<T>& row, int lo, int hi, int k, 
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const bool any = lo + tid < hi;
   key_t tau = 0;
-  if (hi - lo >= k && hi - lo >= kLpThreads) {   // every thread has an element; with fewer of them nothing is left out
-    const key_t low = top_key(m, min(row.first(pos) + VE, row.V) - 1);
+  if (hi - lo >= k) {   // k threads have an element; with fewer of them nothing is left out
+    const key_t low = any ? top_key(m, min(row.first(pos) + VE, row.V) - 1) : 0;
     uint32_t least = sm.low[0];
 #pragma unroll
     for (int w = 1; w < kWarps; ++w) least = min(least, sm.low[w]);
-    // all threads are at or above tau, k - 1 at the most at or above `above`
+    // all threads that have one are at or above tau, k - 1 at the most at or above `above`
     tau = (key_t)least << 32;
     key_t above = (key_t)ord_encode(largest + 0.0f) << 32 | 0xffffffffu;
     while (above - tau > 1) {
@@ -409,7 +409,7 @@ __global__ void __launch_bounds__(kLpThreads, 5) logprobs_kernel(const T* __rest
   add_lanes<32>(t);
   key_t* top = sm.top + rank * p.top_k;
   if (p.top_k > 0) {         // what top_of_segment() expects
-    const uint32_t least = __reduce_min_sync(0xffffffffu, ord_encode(run.m + 0.0f));
+    const uint32_t least = __reduce_min_sync(0xffffffffu, lo + tid < hi ? ord_encode(run.m + 0.0f) : 0xffffffffu);
     if (lane == 0) sm.low[warp] = least;
     if (tid < p.top_k) top[tid] = 0;
     if (tid == 0) sm.n_hot = sm.n_cand = 0;
@@ -569,12 +569,16 @@ __global__ void __launch_bounds__(kLpThreads) logprobs_backward_kernel(const T* 
 }
 
 // CTAs that share a row.  A row alone leaves most SMs idle, so few rows are shared, as long as every thread keeps two
-// vectors; but a CTA's fixed cost (about 4 us of start, join and selection, hidden only by other CTAs of its SM) makes
-// many small parts slower than whole rows.  bf16, five alternatives, us with 1 / 2 / 4 / 8 CTAs on a row: 8 rows of
-// 131072: 13.4 / 10.1 / 8.1 / 7.6; 128 rows of 128000: 18.6 / 14.2 / 14.5 / 19.9; 2048 rows of 50257: 50 / 73 / 115 / 196.
+// vectors; but a CTA's fixed cost (about 3 us of start, join and selection, hidden only by other CTAs of its SM) grows with
+// their number: the more CTAs a row gets, the fewer there may be in all, and never more than the 740 that are resident at
+// once.  Five alternatives, us with 1 / 2 / 4 / 8 CTAs on a row, 16-bit logits unless noted: 1 row of 33278 fp32: 7.8 / 7.0 /
+// 6.4 / 6.0; 8 of 131072: 13.2 / 9.5 / 7.7 / 7.1; 64 of 131072: 13.4 / 9.8 / 9.0 / 10.3; 128 of 128000: 18.6 / 13.7 / 13.5 /
+// 18.2; 370 of 128000: 26.0 / 23.7 / 33 / 44; 450 of 128000: 31.7 / 34.6 / 37 / 51; 2048 of 50257: 47.6 / 67 / 104 / 176.
 int row_ctas(long long rows, int V, int ve) {
   int cl = 1;
-  while (cl < kMaxCluster && rows * cl <= 256 && (long long)V > 2ll * cl * kLpThreads * ve) cl *= 2;
+  while (cl < kMaxCluster && rows * 2 * cl <= 5 * kNumSMs && rows * 4 * cl * cl <= 2048 &&
+         (long long)V > 2ll * cl * kLpThreads * ve)
+    cl *= 2;
   return cl;
 }
 
