@@ -443,7 +443,7 @@ typedef enum {
  * pattern when is_signed = 0) [rows][C+S], row stride ld_codes >= C+S bytes, bytes beyond C+S untouched;
  * scales fp32 [rows]; idx_map int32 [C+S] as ocs_split writes it (NULL when S = 0).  bits in [2,8].
  * rows = 0 is a no-op.  Limits: C + S < 2^30.  Device flags: NONFINITE (that row's outputs are
- * unspecified), BAD_INDEX. */
+ * unspecified), BAD_INDEX, TIMEOUT. */
 ocs_status ocs_quantize_rows(const void* X, ocs_dtype x_type, int64_t rows, int C, int64_t ldx, int S,
                              const int32_t* idx_map, int bits, int is_signed, int8_t* codes, int64_t ld_codes,
                              float* scales, int* dev_status, void* stream);
@@ -452,9 +452,10 @@ ocs_status ocs_quantize_rows(const void* X, ocs_dtype x_type, int64_t rows, int 
  * The integer layer with a scale per token and per output channel:
  *     acc[m][n] = sum_{k < K} A[m][k] * Wc[n][k]                                 (int32, exact)
  *     Y[m][n]   = fmaf((float)acc[m][n] * a_scales[m], w_scales[n], bias[n])     (bias 0 if NULL)
- * the conversion, the product and the fused rest rounded once each, and once more to y_type.  A codes [M][K] (uint8 when a_signed = 0 else int8), row stride lda bytes;
- * Wc int8 [N][K], row stride ldw bytes; both 16-byte aligned with strides that are multiples of 16;
- * a_scales fp32 [M], w_scales fp32 [N], bias fp32 [N]; Y [M][N] of y_type, row stride ldy elements.
+ * the conversion, the product and the fused rest rounded once each, and once more to y_type.
+ * A codes [M][K] (uint8 when a_signed = 0 else int8), row stride lda bytes; Wc int8 [N][K], row stride ldw
+ * bytes; both 16-byte aligned with strides that are multiples of 16; a_scales fp32 [M], w_scales fp32 [N],
+ * bias fp32 [N]; Y [M][N] of y_type, row stride ldy elements.
  * M = 0 is a no-op.  Limits: K * 128 * (a_signed ? 128 : 255) must fit int32, M < 2^30.
  * Device flag: TIMEOUT. */
 ocs_status ocs_qlinear_rows(const void* A_codes, int a_signed, const float* a_scales, int M, int K, int64_t lda,
@@ -493,7 +494,8 @@ ocs_status ocs_selftest_force_row_plan(int tn, int cg, int slices);
  * exp(z - max z), entropy, ln of the sum of exp(z).
  * A logit of -infinity is a masked token: p = 0, no part in the entropy.  A row with nothing but
  * -infinity has logprob and top_logprob -infinity, entropy 0.  A row with NaN or +infinity sets NONFINITE;
- * its floats are NaN and its top_ids -1.  A target >= V sets BAD_INDEX and counts as none.
+ * its floats are NaN and its top_ids -1.  A target >= V sets BAD_INDEX (where logprob is wanted) and
+ * counts as none.
  * Sums and statistics are fp32.  rows = 0 is a no-op.  inv_temperature > 0 and finite. */
 ocs_status ocs_token_logprobs(const void* logits, ocs_dtype type, int64_t rows, int V, int64_t ld,
                               const int32_t* targets, float inv_temperature, int top_k, float* logprob, float* entropy,

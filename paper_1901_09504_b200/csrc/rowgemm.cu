@@ -1,4 +1,26 @@
-// ocs_qlinear_rows / ocs_linear_rows: the int8 layer with a scale per token and per output channel.
+// ocs_qlinear_rows / ocs_linear_rows: the int8 layer with a scale per token and per output channel,
+//     Y[m][n] = (float(sum_k A[m][k] * W[n][k]) * a[m]) * w[n] + bias[n].
+// The contraction is exact in int32 whatever its order, so tiles and splits are free; only the epilogue rounds.
+//
+// Layout: the weights are the rows of the tensor-core tile (128 channels = the lanes of tensor memory) and the tokens its
+// columns.  The instruction's row count is fixed and its column count is free in steps of 16, and a layer always has many
+// channels but often few tokens: one decoded token costs a 16-column tile, not 128 rows of padding.  An epilogue lane then
+// holds one channel of many tokens, so w[n] and bias[n] are registers and a[m] a broadcast from shared memory.
+// Forms: 16, 32, 64, 128 or 256 tokens per CTA, or 256 by a pair of CTAs (256 channels, each CTA stages half the tokens);
+// 128-byte swizzled K-blocks come by TMA into a ring that a copy warp keeps full, one thread issues the MMAs, eight warps
+// empty one of two accumulators while the other fills.  Few tiles: 2, 4 or 8 CTAs of a cluster split the contraction, send
+// each other their partial sums as 16-byte cells through distributed shared memory, and finish a share of the tokens each.
+//
+// What bounds it (device times; HBM 6.54 TB/s and 3.0 int8 POPS measured on the same card; the floor is the larger of bytes
+// and operations at these rates):
+// M x K x N
+//   8192 x 8192 x 8192, bf16 out   331 us, 3.3 POPS: the tensor pipe (93 % busy at 4096 x 8192 x 8192)
+//   2047 x 4178 x 4096, bf16 out   28.7 us (floor 23.4): the tensor pipe, in two waves of which the second is not full
+//   128 x 25339 x 4096, fp32 out   27.5 us (floor 16.7): HBM latency of 128 CTAs' rings, the exchange and the epilogue
+//   700 x 663 x 33278, fp32 out    36.3 us (floor 17.7): 225 MB of operand tiles from L2 and the stores of the output (93 MB)
+//                                  share the SMs' way to L2; 23.3 us without the stores
+//   1 x 8192 x 8192, quantized here, bf16   16.3 us (floor 10.3): HBM, and 6 us of start, quantization, exchange and end
+//   1 x 16384 x 16384, likewise    46 us: HBM at 5.8 TB/s
 #include <atomic>
 
 #include "elem.cuh"
@@ -278,9 +300,9 @@ row_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant_
 
   // Set-up.  Nobody waits for more than it needs: the copy warp asks for the first weights as soon as its own barriers
   // stand, the tensor-core warp needs these barriers, the epilogue warps the address in tensor memory as well -- after
-  // they have quantized the tokens, where that is theirs to do.  (Named barriers: 2 = set up, 3 = barriers stand, 4 = tokens in place.)  A peer
-  // may be written to once all threads of the cluster have arrived; a pair waits for that at once, the others where they
-  // first need it.
+  // they have quantized the tokens, where that is theirs to do.  (Named barriers: 2 = set up, 3 = barriers stand, 4 =
+  // tokens in place.)  A peer may be written to once all threads of the cluster have arrived; a pair waits for that at
+  // once, the others where they first need it.
   if (warp == 0) {
     if (lane == 0) {
       prefetch_tmap(&tm_w);
@@ -465,7 +487,7 @@ row_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant_
           if (L::kXInRing) {
             // this CTA's tensor cores are done with its ring: it may be written to; and so are all the others'
             if (ew == 0 && lane == 0)
-              for (int o = 0; o < p.slices; ++o) mbar_arrive_peer(peer_addr(xready_bar, (uint32_t)(o * CG + half)));
+              for (int o = 0; o < p.slices; ++o) mbar_arrive_peer(peer_addr(xready_bar, (uint32_t)o));
             if (!mbar_wait_cluster(xready_bar, 0u, abort_flag)) break;
           }
           const uint32_t mine = smem_u32(xbuf) + (uint32_t)(slice * groups * TW + q * 32 + lane) * 16u;
@@ -484,7 +506,7 @@ row_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant_
               for (int e = 0; e < 16; e += 4) {
                 const int col = part * 16 + 32 * i + e;
                 const int owner = col / own, g = (col - owner * own) / 4;
-                const uint32_t peer = (uint32_t)(owner * CG + half);
+                const uint32_t peer = (uint32_t)owner;
                 st_async_v4(peer_addr(mine + (uint32_t)g * (TW * 16u), peer), make_uint4(w[e], w[e + 1], w[e + 2], w[e + 3]),
                             peer_addr(xfull_bar, peer));
               }
@@ -568,10 +590,10 @@ row_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant_
 }
 
 // ------------------------------------------------------------------------------------------------ host
-// Bytes of unquantized tokens that a CTA may read itself.  Against two launches (a graph's time per call / an eager call's
-// host time): (M, C, N) = (1, 8192, 8192), 16 KB: 16.9 / 13.8 us against 17.5 / 19.0; (16, 1024, 4096), 32 KB: 6.8 / 14.5
-// against 6.4 / 19.5; (20, 650, 2600) in fp32, 42 KB: 7.9 / 14.8 against 6.0 / 19.6; but (4, 8192, 8192), 64 KB: 20.2
-// against 17.4 on the device.
+// Bytes of unquantized tokens that a CTA may read itself.  Against two launches, us of a graph's time per call / of an eager
+// call's host time: (M, C, N) = (1, 4096, 4096), 8 KB: 8.7 / 15.5 against 8.9 / 22.1; (1, 8192, 8192), 16 KB: 17.1 / 12.1
+// against 17.4 / 16.1; (16, 1024, 4096), 32 KB: 6.7 / 15.4 against 6.1 / 22.5; (20, 650, 2600) in fp32, 50 KB: 8.2 / 15.7
+// against 5.8 / 22.9; but (4, 8192, 8192), 64 KB: 20.6 against 17.5 on the device, more than the launch costs the host.
 constexpr long long kFuseBytes = 48 * 1024;
 
 struct RowPlan {

@@ -1,5 +1,8 @@
 // ocs_quantize_rows: linear quantization with one grid per row (a token's activations, or an output
 // channel's split weights), the duplicated channels of a split layer appended to the codes.
+//     alpha = max |x|,  scale = alpha / L,  code = rint(x * (L / alpha))
+// The codes need the whole row's maximum first.  HBM bounds it as long as a row is read once, so the row waits on chip for its
+// maximum: in one CTA's registers, in a cluster's, or (many long rows) in shared memory.
 #include <type_traits>
 
 #include "elem.cuh"
@@ -119,7 +122,9 @@ constexpr size_t kStagedBytes = 226 * 1024;
 
 // One row per threadIdx.y and cluster, blockDim.x threads of each CTA on it, NV pieces of VB bytes per thread: the row is
 // read once and stays in registers between the maximum and the codes.  CLUSTER: the CTAs of a cluster take consecutive
-// parts of the row and exchange their maxima through shared memory.
+// parts of the row and exchange their maxima through shared memory.  Three CTAs of 512 threads fit an SM, so that one
+// row's loads cover another's maximum and stores: 8192 x 8192 bf16 (201 MB) takes 31.6 us, 6.4 TB/s.  With pieces of 16
+// instead of 32 bytes and maxima of single elements instead of packed pairs it took 62 us: instructions bounded it.
 template <typename T, int VB, int NV, bool CLUSTER>
 __global__ void __launch_bounds__(NV == 1 ? 1024 : kRowThreads, NV == 1 ? 1 : 3) rows_kernel(const T* __restrict__ X, const RowsParams p) {
   constexpr int VE = Piece<T, VB>::VE;
@@ -192,9 +197,11 @@ __global__ void __launch_bounds__(NV == 1 ? 1024 : kRowThreads, NV == 1 ? 1 : 3)
   }
 }
 
-// Many long rows (whole 16-byte pieces): one CTA per SM, or two with half the threads, walk over them.  A row comes by one bulk copy into a ring of
-// shared-memory buffers, moves into registers (which frees its buffer for the row after next), and is quantized from
-// there while the next rows are on their way.  One barrier per row.
+// Many long rows (whole 16-byte pieces): one CTA per SM, or two with half the threads, walk over them.  A row comes by
+// one bulk copy into a ring of shared-memory buffers, moves into registers (which frees its buffer for the row after
+// next), and is quantized from there while the next rows are on their way.  One barrier per row.  4096 x 25088 fp32 (514
+// MB): 78.1 us, 6.6 TB/s, the measured copy rate; in clusters of four CTAs 124 us, since a cluster's three meetings per
+// row leave its SMs without loads.
 template <typename T, int NV, int THREADS>
 __global__ void __launch_bounds__(THREADS, 1024 / THREADS) staged_rows_kernel(const T* __restrict__ X, const RowsParams p, int ring) {
   constexpr int VE = 16 / (int)sizeof(T);
