@@ -735,12 +735,11 @@ def ocs_token_logprobs(logits, targets=None, top_k: int = 0, inv_temperature: fl
                                and targets.numel() >= rows)
     k = int(top_k)
     if out is None:
-        dev, f32 = logits.device, torch.float32
-        out = TokenLogprobs(torch.empty(rows, dtype=f32, device=dev) if targets is not None else None,
-                            torch.empty(rows, dtype=f32, device=dev),
-                            torch.empty((rows, k), dtype=torch.int32, device=dev) if k > 0 else None,
-                            torch.empty((rows, k), dtype=f32, device=dev) if k > 0 else None,
-                            torch.empty((rows, 4), dtype=f32, device=dev) if want_stats else None)
+        entropy = torch.empty(rows, dtype=torch.float32, device=logits.device)   # (new_empty takes its type at less cost)
+        out = TokenLogprobs(entropy.new_empty(rows) if targets is not None else None, entropy,
+                            torch.empty((rows, k), dtype=torch.int32, device=logits.device) if k > 0 else None,
+                            entropy.new_empty((rows, k)) if k > 0 else None,
+                            entropy.new_empty((rows, 4)) if want_stats else None)
     else:
         _check_vec(out.logprob, rows), _check_vec(out.entropy, rows), _check_vec(out.top_logprob, rows * k)
         _check_vec(out.stats, 4 * rows)
