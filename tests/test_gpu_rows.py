@@ -77,6 +77,28 @@ def test_quantize_rows(M, C, S, kind, bits, signed, layout):
         assert np.abs(host(codes)[:, :C + S] - real * hi).max() <= 0.5 + 3 * hi * 2.0 ** -24
 
 
+@pytest.mark.parametrize("M,C,S", [(1, 1, 1), (9, 3, 2), (40, 31, 0), (200, 17, 5), (300, 513, 9), (160, 7279, 145), (20, 25001, 3),
+                                   (310, 16389, 2), (3, 70003, 11), (2, 140009, 5)])
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("first", [0, 1, 6, 15])
+@pytest.mark.parametrize("even", [True, False])
+def test_quantize_rows_from_any_offset_to_any_offset(M, C, S, kind, first, even):
+    """Rows that start anywhere relative to a 32-byte boundary, all of them alike (even) or each elsewhere, and codes that
+    start at any byte; lengths of one piece up to more than a cluster's registers hold."""
+    x = _x(M + C, M, C, kind, ld=-(-C // 32) * 32 if even else C + 1 + C % 2, offset=first)
+    idx = _idx(C, C, S)
+    ld = C + S + first % 4
+    buf = torch.full((M * ld + first + 8,), 77, dtype=torch.int8, device="cuda")
+    codes = buf[first:first + M * ld].view(M, ld)
+    st = ocs.new_status()
+    _, scales = ocs.ocs_quantize_rows(x, 8, True, idx_map=idx, S=S, out=(codes, torch.empty(M, device="cuda")), dev_status=st)
+    q, sc = ref_rows(x, idx, 8, True)
+    assert ocs.ocs_poll_status(st) == 0
+    np.testing.assert_array_equal(host(scales), sc)
+    np.testing.assert_array_equal(host(codes)[:, :C + S], q)
+    assert (host(codes)[:, C + S:] == 77).all() and (host(buf)[:first] == 77).all() and (host(buf)[first + M * ld:] == 77).all()
+
+
 def test_quantize_rows_zero_tiny_and_huge_rows():
     x = torch.zeros((6, 300), device="cuda")
     x[1, 5] = 1e-45                                       # the smallest subnormal
