@@ -10,11 +10,8 @@ namespace ocs {
 namespace {
 
 constexpr int kMaxTop = 64;
-constexpr int kLpThreads = 256;
-constexpr int kWarps = kLpThreads / 32;
+constexpr int kLpThreads = 256;       // threads of a CTA; the forward kernel also has forms with fewer (NT)
 constexpr int kMaxCluster = 8;        // CTAs that may share a row
-static_assert(kWarps == 8 && kMaxCluster == 8, "join_eight");
-constexpr int kCandidates = 2048;     // elements that can still be among the largest
 constexpr float kFloor = -200.0f;     // 2^-200 is zero in fp32: exponents are clamped here, so that a masked token (d = -inf)
                                       // contributes 0 to the sums and not 0 * infinity
 
@@ -229,15 +226,22 @@ struct LogprobParams {
   int* dev_status;
 };
 
+// NT threads; only CTAs of kLpThreads share rows
+template <int NT>
 struct LogprobSmem {
-  Stats warp[kWarps];
+  static constexpr int kWarps = NT / 32;
+  static constexpr int kCandidates = 8 * NT;   // elements that can still be among the largest
+  static_assert(kCandidates >= 16 * (kMaxTop - 1), "fewer vectors than alternatives are collected whole");
+  static constexpr int kLists = NT == kLpThreads ? kMaxCluster : 1;
+  static_assert(kWarps <= 8 && kMaxCluster == 8, "join_eight");
+  Stats warp[8];
   Stats part[kMaxCluster];                             // of the CTAs that share the row
   __align__(16) key_t cand[kCandidates];
-  __align__(16) key_t top[kMaxCluster * kMaxTop];      // each CTA's largest, descending
+  __align__(16) key_t top[kLists * kMaxTop];           // each CTA's largest, descending
   key_t best[kMaxTop];                                 // the row's
   uint32_t low[kWarps];                                // the smallest of a warp's threads' largest elements, as ord_encode
   key_t next[kWarps];
-  int hot[kLpThreads];
+  int hot[NT];
   int n_hot, n_cand;
 };
 
@@ -272,10 +276,10 @@ __device__ __forceinline__ key_t warp_max_key(key_t v) {
 //   2. All threads read these threads' elements again and collect what is not below tau.
 //   3. The k largest of what was collected, by rank.
 // Many unluckily placed elements may overflow the list; then the keys are found one after the other.
-template <typename T>
-__device__ void top_of_segment(const RowVectors<T>& row, int lo, int hi, int k, float m, int pos, float largest, LogprobSmem& sm,
-                               key_t* out) {
-  constexpr int VE = Vec<T>::VE;
+template <int NT, typename T>
+__device__ void top_of_segment(const RowVectors<T>& row, int lo, int hi, int k, float m, int pos, float largest,
+                               LogprobSmem<NT>& sm, key_t* out) {
+  constexpr int VE = Vec<T>::VE, kWarps = LogprobSmem<NT>::kWarps, kCandidates = LogprobSmem<NT>::kCandidates;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const bool any = lo + tid < hi;
   key_t tau = 0;
@@ -297,10 +301,10 @@ __device__ void top_of_segment(const RowVectors<T>& row, int lo, int hi, int k, 
   }
   if (any && top_key(m, max(row.first(pos), 0)) >= tau) sm.hot[atomicAdd(&sm.n_hot, 1)] = tid;
   __syncthreads();
-  const int vecs = (hi - lo + kLpThreads - 1) / kLpThreads, total = sm.n_hot * vecs;
-  for (int q = tid; q < total; q += kLpThreads) {
+  const int vecs = (hi - lo + NT - 1) / NT, total = sm.n_hot * vecs;
+  for (int q = tid; q < total; q += NT) {
     const int h = q / vecs;
-    const int j = lo + sm.hot[h] + (q - h * vecs) * kLpThreads;
+    const int j = lo + sm.hot[h] + (q - h * vecs) * NT;
     if (j >= hi) continue;
     const Vec<T> v = row.load(j);
     if (ord_encode(v.max_all() + 0.0f) < (uint32_t)(tau >> 32)) continue;
@@ -319,7 +323,7 @@ __device__ void top_of_segment(const RowVectors<T>& row, int lo, int hi, int k, 
   __syncthreads();
   const int n = sm.n_cand;
   if (n <= kCandidates) {
-    for (int i = tid; i < n; i += kLpThreads) {
+    for (int i = tid; i < n; i += NT) {
       const key_t mine = sm.cand[i];
       const int r = count_larger(sm.cand, n, mine);
       if (r < k) out[r] = mine;
@@ -328,7 +332,7 @@ __device__ void top_of_segment(const RowVectors<T>& row, int lo, int hi, int k, 
     key_t last = ~0ull;
     for (int r = 0; r < k; ++r) {
       key_t best = 0;
-      for (int j = lo + tid; j < hi; j += kLpThreads) {
+      for (int j = lo + tid; j < hi; j += NT) {
         float f[VE];
         row.load(j).floats(f);
 #pragma unroll
@@ -365,11 +369,11 @@ __device__ __forceinline__ void store_peer_f32(uint32_t addr, float v) {
 // exponential (2048 x 50257 bf16, 206 MB: 39.3 us, 5.2 TB/s).  Five alternatives add about 3 us per wave of CTAs: 47.5 us
 // there; 20.5 instead of 17.4 us for 700 rows of 33278 fp32 logits (93 MB), which are one wave.  Few rows are latency:
 // 8 x 131072 bf16 takes 4.2 us, 8.4 with twenty alternatives.
-template <typename T>
-__global__ void __launch_bounds__(kLpThreads, 5) logprobs_kernel(const T* __restrict__ logits, const LogprobParams p) {
-  constexpr int VE = Vec<T>::VE;
-  __shared__ LogprobSmem sm;
-  const int CL = (int)cluster_size(), rank = CL > 1 ? (int)cluster_rank() : 0;
+template <typename T, int NT>
+__global__ void __launch_bounds__(NT, 5 * 256 / NT) logprobs_kernel(const T* __restrict__ logits, const LogprobParams p) {
+  constexpr int VE = Vec<T>::VE, kWarps = NT / 32;
+  __shared__ LogprobSmem<NT> sm;
+  const int CL = NT == kLpThreads ? (int)cluster_size() : 1, rank = CL > 1 ? (int)cluster_rank() : 0;
   if (CL > 1) asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory");   // every CTA runs before its memory is written to
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const long long r = blockIdx.x / CL;
@@ -393,16 +397,16 @@ __global__ void __launch_bounds__(kLpThreads, 5) logprobs_kernel(const T* __rest
     Vec<T> v, w;   // one is on its way while the other is summed
     const bool some = j < hi;
     if (some) v = row.load(j);
-    if (j + kLpThreads < end) w.load(src + 32ll * (j + kLpThreads));
+    if (j + NT < end) w.load(src + 32ll * (j + NT));
     run.M = __fmul_rn(fmaxf(warp_max(some ? v.max_all() : -INFINITY), lowest<T>()), c);
     if (some) take(run, v, j, c);
-    if (j + 2 * kLpThreads < end) v.load(src + 32ll * (j + 2 * kLpThreads));
-    for (j += kLpThreads; j < end; j += 2 * kLpThreads) {
+    if (j + 2 * NT < end) v.load(src + 32ll * (j + 2 * NT));
+    for (j += NT; j < end; j += 2 * NT) {
       take(run, w, j, c);
-      if (j + 2 * kLpThreads < end) w.load(src + 32ll * (j + 2 * kLpThreads));
-      if (j + kLpThreads >= end) { j += kLpThreads; break; }
-      take(run, v, j + kLpThreads, c);
-      if (j + 3 * kLpThreads < end) v.load(src + 32ll * (j + 3 * kLpThreads));
+      if (j + 2 * NT < end) w.load(src + 32ll * (j + 2 * NT));
+      if (j + NT >= end) { j += NT; break; }
+      take(run, v, j + NT, c);
+      if (j + 3 * NT < end) v.load(src + 32ll * (j + 3 * NT));
     }
     if (j < hi) {   // the row's last vector, hanging over
       v = row.load(j);
@@ -426,6 +430,7 @@ __global__ void __launch_bounds__(kLpThreads, 5) logprobs_kernel(const T* __rest
     if (tid == 0) sm.n_hot = sm.n_cand = 0;
   }
   if (lane == 0) sm.warp[warp] = t;
+  if (kWarps < 8 && tid >= kWarps && tid < 8) sm.warp[tid] = Stats{-INFINITY, 0.0f, 0.0f};
   __syncthreads();
   float largest = sm.warp[0].m;
 #pragma unroll
@@ -433,7 +438,7 @@ __global__ void __launch_bounds__(kLpThreads, 5) logprobs_kernel(const T* __rest
   if (fabsf(largest) < INFINITY && !sums_hold<T>(largest, c)) {   // the same for the whole CTA
     __syncthreads();
     t = Stats{largest, 0.0f, 0.0f};
-    for (int j = lo + tid; j < hi; j += kLpThreads) {
+    for (int j = lo + tid; j < hi; j += NT) {
       float f[VE];
       row.load(j).floats(f);
 #pragma unroll
@@ -458,7 +463,7 @@ __global__ void __launch_bounds__(kLpThreads, 5) logprobs_kernel(const T* __rest
         store_peer_f32(dst + 4, t.s);
         store_peer_f32(dst + 8, t.w);
       }
-      for (int i = tid; i < p.top_k; i += kLpThreads)
+      for (int i = tid; i < p.top_k; i += NT)
         store_peer_u64(peer_addr(smem_u32(&sm.top[rank * p.top_k + i]), 0), sm.top[rank * p.top_k + i]);
       __syncwarp();
       asm volatile("barrier.cluster.arrive.release;" ::: "memory");
@@ -471,7 +476,7 @@ __global__ void __launch_bounds__(kLpThreads, 5) logprobs_kernel(const T* __rest
     t = part == 0 ? own : (part < CL ? sm.part[part] : Stats{-INFINITY, 0.0f, 0.0f});
     t = join_eight(t, c);
     if (p.top_k > 0) {
-      for (int i = tid; i < CL * p.top_k; i += kLpThreads) {
+      for (int i = tid; i < CL * p.top_k; i += NT) {
         const key_t k = sm.top[i];
         const int at = k != 0 ? count_larger(sm.top, CL * p.top_k, k) : kMaxTop;
         if (at < p.top_k) sm.best[at] = k;
@@ -493,7 +498,7 @@ __global__ void __launch_bounds__(kLpThreads, 5) logprobs_kernel(const T* __rest
     if (p.logprob)
       p.logprob[r] = bad ? nan : (y < 0 ? 0.0f : (empty ? -INFINITY : __fsub_rn(__fmul_rn(__fsub_rn(ly, t.m), p.beta), ls)));
   }
-  for (int i = tid; i < p.top_k; i += kLpThreads) {
+  for (int i = tid; i < p.top_k; i += NT) {
     const key_t k = best[i];
     if (p.top_ids) p.top_ids[r * p.top_k + i] = bad ? -1 : key_index(k);
     if (p.top_logprob)
@@ -596,23 +601,35 @@ int row_ctas(long long rows, int V, int ve) {
   return cl;
 }
 
+// Threads of a CTA that has a row to itself.  With 128 of them ten rows are under way on an SM instead of five, which hides
+// twice as much of the fixed cost; but the alternatives' threads have twice as many vectors each, which are read again, and
+// where all rows are resident at once anyway (740 CTAs of 256) a long row takes its threads' time.  us with 128 / 256 threads
+// (64 threads were ahead only below 2000 logits): five alternatives, bf16 4096 x 1116: 17.5 / 32.4, 4096 x 8200: 28.4 / 43.0,
+// 1000 x 50257: 27.9 / 29.4, fp32 450 x 8200: 7.2 / 7.9, but 450 x 16228: 9.9 / 9.5 and 450 x 33278: 20.3 / 16.2; twenty
+// alternatives: bf16 2500 x 16228: 32.5 / 35.9, 2500 x 33278: 53.3 / 52.0, fp32 2500 x 33278: 83 / 74 (none: 54.3 / 57.1).
+int row_threads(long long rows, int V, int ve, int top_k) {
+  const long long vecs = V / (128 * ve);   // a thread's, of 128
+  return top_k * vecs <= 320 && (rows > 5 * kNumSMs || vecs <= 8) ? 128 : kLpThreads;
+}
+
 template <typename T>
 ocs_status launch_logprobs(const void* logits_, LogprobParams p, cudaStream_t stream) {
   const T* logits = static_cast<const T*>(logits_);
-  const int cl = row_ctas(p.rows, p.V, Vec<T>::VE);
+  const int cl = row_ctas(p.rows, p.V, Vec<T>::VE), nt = cl > 1 ? kLpThreads : row_threads(p.rows, p.V, Vec<T>::VE, p.top_k);
   const long long rows = p.rows, step = 1ll << 27;   // rows of one launch (the grid's limit)
   for (long long r0 = 0; r0 < rows; r0 += step) {
     const long long n = rows - r0 < step ? rows - r0 : step;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(n * cl), 1, 1);
-    cfg.blockDim = dim3(kLpThreads, 1, 1);
+    cfg.blockDim = dim3(nt, 1, 1);
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = cl; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr; cfg.numAttrs = cl > 1 ? 1 : 0;
     LaunchScope ls("logprobs_kernel", stream);
-    if (cudaLaunchKernelEx(&cfg, logprobs_kernel<T>, logits + r0 * p.ld, p) != cudaSuccess) return OCS_ERR_CUDA;
+    const auto kernel = nt == 128 ? logprobs_kernel<T, 128> : logprobs_kernel<T, kLpThreads>;
+    if (cudaLaunchKernelEx(&cfg, kernel, logits + r0 * p.ld, p) != cudaSuccess) return OCS_ERR_CUDA;
     if (p.targets) p.targets += n;
     if (p.logprob) p.logprob += n;
     if (p.entropy) p.entropy += n;

@@ -106,6 +106,23 @@ def test_logprobs(T, V, kind, k, beta, layout):
     check(x, y, k, beta)
 
 
+@pytest.mark.parametrize("T,V,kind,k,beta", [
+    (800, 9001, "bf16", 20, 1.0), (760, 20011, "f32", 5, 0.8), (745, 16384, "f16", 64, 1.0), (741, 33278, "bf16", 9, 1.25),
+    (400, 8191, "f32", 39, 1.0), (372, 16300, "f16", 1, 1.0),
+])
+@pytest.mark.parametrize("masked", [False, True])
+def test_logprobs_many_rows(T, V, kind, k, beta, masked):
+    """More rows than are resident at once and somewhat fewer, where a CTA has a row to itself."""
+    x = _logits(T + V, T, V, kind, ld=V + 1, offset=1)
+    if masked:
+        x[:, 1::3] = float("-inf")
+        x[5] = float("-inf")
+        x[6, :V - 2] = float("-inf")
+    y = torch.randint(0, V, (T,), generator=_gen(7), device="cuda", dtype=torch.int32)
+    y[::11] = -1
+    check(x, y, k, beta)
+
+
 def test_parts_are_optional():
     x = _logits(1, 6, 999, "f32")
     y = torch.arange(6, dtype=torch.int32, device="cuda")
