@@ -362,8 +362,8 @@ __device__ __forceinline__ void store_peer_f32(uint32_t addr, float v) {
 }
 
 // One row per cluster; the CTAs of a cluster take consecutive parts of it and send what they found to the first one.
-// A thread strides over its CTA's part in vectors of 32 bytes, one of them on its way while another is summed; five CTAs per
-// SM (48 registers).  Deeper prefetch with fewer CTAs is slower (three and four vectors, four CTAs: 52 us at 2048 rows of
+// A thread strides over its CTA's part in vectors of 32 bytes, one of them on its way while another is summed; five CTAs of
+// 256 threads per SM, or ten of 128 (48 registers).  Deeper prefetch with fewer CTAs is slower (three and four vectors, four CTAs: 52 us at 2048 rows of
 // 50257 bf16 logits; one vector, six CTAs: 53; this form 50 at the time).  What bounds it: fp32 rows the loads (2048 x 50257:
 // 65 us for 412 MB, 6.3 TB/s, without alternatives); 16-bit rows the instructions, six per element and one of them an
 // exponential (2048 x 50257 bf16, 206 MB: 39.3 us, 5.2 TB/s).  Five alternatives add about 3 us per wave of CTAs: 47.5 us
@@ -605,11 +605,12 @@ int row_ctas(long long rows, int V, int ve) {
 // twice as much of the fixed cost; but the alternatives' threads have twice as many vectors each, which are read again, and
 // where all rows are resident at once anyway (740 CTAs of 256) a long row takes its threads' time.  us with 128 / 256 threads
 // (64 threads were ahead only below 2000 logits): five alternatives, bf16 4096 x 1116: 17.5 / 32.4, 4096 x 8200: 28.4 / 43.0,
-// 1000 x 50257: 27.9 / 29.4, fp32 450 x 8200: 7.2 / 7.9, but 450 x 16228: 9.9 / 9.5 and 450 x 33278: 20.3 / 16.2; twenty
-// alternatives: bf16 2500 x 16228: 32.5 / 35.9, 2500 x 33278: 53.3 / 52.0, fp32 2500 x 33278: 83 / 74 (none: 54.3 / 57.1).
+// 2500 x 33278: 42.4 / 46.5, 2048 x 50257: 51.4 / 47.5, fp32 2500 x 33278: 65.5 / 66.7, 2048 x 50257: 83.1 / 76.4, 450 x 8200:
+// 7.2 / 7.9, but 450 x 16228: 9.9 / 9.5 and 450 x 33278: 20.3 / 16.2; twenty alternatives: bf16 2500 x 16228: 32.5 / 35.9,
+// 2500 x 33278: 53.3 / 52.0, fp32 2500 x 33278: 83 / 74 (none: 54.3 / 57.1).
 int row_threads(long long rows, int V, int ve, int top_k) {
   const long long vecs = V / (128 * ve);   // a thread's, of 128
-  return top_k * vecs <= 320 && (rows > 5 * kNumSMs || vecs <= 8) ? 128 : kLpThreads;
+  return top_k * vecs <= 320 && (vecs <= 8 || (rows > 5 * kNumSMs && V <= 40960)) ? 128 : kLpThreads;
 }
 
 template <typename T>
