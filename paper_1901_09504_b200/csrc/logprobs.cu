@@ -3,6 +3,9 @@
 //     ln p_v = (l_v - m) * inv_temperature - ln s,   entropy = ln s - ln 2 * w / s,
 // so one pass over the logits with running sums gives everything, and the likeliest tokens come from a threshold found among
 // the threads' maxima.
+#include <cmath>
+#include <type_traits>
+
 #include "elem.cuh"
 #include "ptx.cuh"
 
@@ -34,6 +37,13 @@ __device__ __forceinline__ float ex2(float x) {                // 2^x, relative 
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
   return r;
 }
+// Stand-in for masked tokens (-infinity, or a finite value below it) in the sums: so low that 2^d is zero, and near enough
+// to zero that its product with c rounds by no more than one, like that of every logit that the sums can take (sums_hold()
+// says which).  `two`: in both halves of a word, in the logits' type.
+struct Low {
+  float v;
+  uint32_t two;
+};
 // 32 bytes of a row
 template <typename T>
 struct Vec {
@@ -44,21 +54,17 @@ struct Vec {
                  : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7]) : "l"(p));
   }
   __device__ __forceinline__ void floats(float* f) const;      // the elements as fp32
-  __device__ __forceinline__ void floored(float* f) const;     // ... none below lowest<T>()
+  __device__ __forceinline__ void floored(float* f, const Low& low) const;   // ... none below low
   __device__ __forceinline__ float max_all() const;            // the largest; NaN if any element is
 };
-// Stand-in for a masked token's -infinity in the sums: finite, so that 0 * d stays 0, and so low that 2^d is zero
-// (sums_hold() says when that is so).
-template <typename T> __device__ __forceinline__ constexpr float lowest() { return -0x1p100f; }
-template <> __device__ __forceinline__ constexpr float lowest<__half>() { return -65504.0f; }
 
 template <> __device__ __forceinline__ void Vec<float>::floats(float* f) const {
 #pragma unroll
   for (int i = 0; i < 8; ++i) f[i] = __uint_as_float(w[i]);
 }
-template <> __device__ __forceinline__ void Vec<float>::floored(float* f) const {
+template <> __device__ __forceinline__ void Vec<float>::floored(float* f, const Low& low) const {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) f[i] = fmaxf(__uint_as_float(w[i]), lowest<float>());
+  for (int i = 0; i < 8; ++i) f[i] = fmaxf(__uint_as_float(w[i]), low.v);
 }
 template <> __device__ __forceinline__ float Vec<float>::max_all() const {
   float m[4];
@@ -90,20 +96,18 @@ template <> __device__ __forceinline__ void Vec<__nv_bfloat16>::floats(float* f)
 #pragma unroll
   for (int i = 0; i < 8; ++i) widen(as_half2<__nv_bfloat162>(w[i]), f + 2 * i);
 }
-template <> __device__ __forceinline__ void Vec<__nv_bfloat16>::floored(float* f) const {
-  const __nv_bfloat162 low = __float2bfloat162_rn(lowest<__nv_bfloat16>());
+template <> __device__ __forceinline__ void Vec<__nv_bfloat16>::floored(float* f, const Low& low) const {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) widen(__hmax2(as_half2<__nv_bfloat162>(w[i]), low), f + 2 * i);
+  for (int i = 0; i < 8; ++i) widen(__hmax2(as_half2<__nv_bfloat162>(w[i]), as_half2<__nv_bfloat162>(low.two)), f + 2 * i);
 }
 template <> __device__ __forceinline__ float Vec<__nv_bfloat16>::max_all() const { return packed_max<__nv_bfloat162>(w); }
 template <> __device__ __forceinline__ void Vec<__half>::floats(float* f) const {
 #pragma unroll
   for (int i = 0; i < 8; ++i) widen(as_half2<__half2>(w[i]), f + 2 * i);
 }
-template <> __device__ __forceinline__ void Vec<__half>::floored(float* f) const {
-  const __half2 low = __float2half2_rn(lowest<__half>());
+template <> __device__ __forceinline__ void Vec<__half>::floored(float* f, const Low& low) const {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) widen(__hmax2(as_half2<__half2>(w[i]), low), f + 2 * i);
+  for (int i = 0; i < 8; ++i) widen(__hmax2(as_half2<__half2>(w[i]), as_half2<__half2>(low.two)), f + 2 * i);
 }
 template <> __device__ __forceinline__ float Vec<__half>::max_all() const { return packed_max<__half2>(w); }
 
@@ -154,12 +158,15 @@ __device__ __forceinline__ void move_max(Stats& t, float m, float c) {   // the 
   shift(t, fmaxf(__fmul_rn(__fsub_rn(t.m, m), c), kFloor));              // -infinity or NaN (nothing summed yet): s = w = 0
   t.m = m;
 }
-// The main loop takes d = fma(l, c, -M) with M = fl(m * c) instead of (l - m) * c: one instruction, one rounding.  That
-// holds while no product overflows and a masked token's stand-in is far enough below the maximum; otherwise (logits
-// around the type's lowest or largest value) the sums are taken once more in the other form.
-template <typename T>
-__device__ __forceinline__ bool sums_hold(float m, float c) {
-  return fabsf(m) < 0x1p90f && c < 0x1p20f && __fmul_rn(__fsub_rn(lowest<T>(), m), c) <= -160.0f;
+// The main loop takes d = fma(l, c, -M) with M = fl(m * c) instead of (l - m) * c: one instruction, one rounding.  M's own
+// rounding stays in d until the sums move to m * c at the end, so it has to be small: up to |m * c| = 2^24 it is at most
+// one, while from 2^31 on it would carry 2^d out of range.  That holds for every M of a row whose maximum and whose
+// stand-in for masked tokens (low) are that near to zero.  The stand-in also has to be far enough below the maximum.
+// Otherwise (a row's largest logit far from zero, or nothing in it above a finite mask value) the sums are taken once more
+// in the other form.
+__device__ __forceinline__ bool sums_hold(float m, float c, float low) {
+  return __fmul_rn(fabsf(m), c) <= 0x1p24f && __fmul_rn(-low, c) <= 0x1p24f && c < 0x1p20f &&
+         __fmul_rn(__fsub_rn(low, m), c) <= -160.0f;
 }
 __device__ __forceinline__ float warp_max(float m) {   // NaN if any lane's is
   float r;
@@ -191,12 +198,12 @@ struct Running {
   int pos;
 };
 template <typename T>
-__device__ __forceinline__ void take(Running& t, const Vec<T>& v, int j, float c) {
+__device__ __forceinline__ void take(Running& t, const Vec<T>& v, int j, float c, const Low& low) {
   constexpr int VE = Vec<T>::VE;
   const float mx = v.max_all();
   if (mx > t.m) t.pos = j;
   t.m = max_nan(t.m, mx);
-  const float to = __fmul_rn(fmaxf(mx, lowest<T>()), c);
+  const float to = __fmul_rn(fmaxf(mx, low.v), c);
   if (to > __fadd_rn(t.M, kLag)) {
     const float d = fmaxf(__fsub_rn(t.M, to), kFloor), r = ex2(d);
 #pragma unroll
@@ -207,7 +214,7 @@ __device__ __forceinline__ void take(Running& t, const Vec<T>& v, int j, float c
     t.M = to;
   }
   float f[VE];
-  v.floored(f);
+  v.floored(f, low);
 #pragma unroll
   for (int i = 0; i < VE; ++i) {
     const float d = fmaf(f[i], c, -t.M), e = ex2(d);
@@ -221,6 +228,7 @@ struct LogprobParams {
   int V, top_k;
   const int32_t* targets;
   float beta, c;
+  Low low;
   float *logprob, *entropy, *top_logprob, *stats;
   int32_t* top_ids;
   int* dev_status;
@@ -389,6 +397,7 @@ __global__ void __launch_bounds__(NT, 5 * 256 / NT) logprobs_kernel(const T* __r
   }
 
   const float c = p.c;
+  const Low low = p.low;
   Running run{-INFINITY, 0.0f, {0.0f, 0.0f}, {0.0f, 0.0f}, lo + tid};
   {
     int j = lo + tid;
@@ -398,23 +407,23 @@ __global__ void __launch_bounds__(NT, 5 * 256 / NT) logprobs_kernel(const T* __r
     const bool some = j < hi;
     if (some) v = row.load(j);
     if (j + NT < end) w.load(src + 32ll * (j + NT));
-    run.M = __fmul_rn(fmaxf(warp_max(some ? v.max_all() : -INFINITY), lowest<T>()), c);
-    if (some) take(run, v, j, c);
+    run.M = __fmul_rn(fmaxf(warp_max(some ? v.max_all() : -INFINITY), low.v), c);
+    if (some) take(run, v, j, c, low);
     if (j + 2 * NT < end) v.load(src + 32ll * (j + 2 * NT));
     for (j += NT; j < end; j += 2 * NT) {
-      take(run, w, j, c);
+      take(run, w, j, c, low);
       if (j + 2 * NT < end) w.load(src + 32ll * (j + 2 * NT));
       if (j + NT >= end) { j += NT; break; }
-      take(run, v, j + NT, c);
+      take(run, v, j + NT, c, low);
       if (j + 3 * NT < end) v.load(src + 32ll * (j + 3 * NT));
     }
     if (j < hi) {   // the row's last vector, hanging over
       v = row.load(j);
-      take(run, v, j, c);
+      take(run, v, j, c, low);
     }
   }
   Stats t{warp_max(run.m), __fadd_rn(run.s[0], run.s[1]), __fadd_rn(run.w[0], run.w[1])};
-  if (t.m > lowest<T>()) {   // from M to m * c
+  if (t.m > low.v) {         // from M to m * c
     const float d = fmaxf(fmaf(-t.m, c, run.M), kFloor), r = ex2(d), moved = fmaf(t.s, d, t.w);
     t.s = __fmul_rn(t.s, r);
     t.w = fabsf(moved) <= 0x1p-22f * fabsf(t.w) ? 0.0f : __fmul_rn(moved, r);   // of equals only rounding would be left
@@ -435,7 +444,7 @@ __global__ void __launch_bounds__(NT, 5 * 256 / NT) logprobs_kernel(const T* __r
   float largest = sm.warp[0].m;
 #pragma unroll
   for (int w = 1; w < kWarps; ++w) largest = max_nan(largest, sm.warp[w].m);
-  if (fabsf(largest) < INFINITY && !sums_hold<T>(largest, c)) {   // the same for the whole CTA
+  if (fabsf(largest) < INFINITY && !sums_hold(largest, c, low.v)) {   // the same for the whole CTA
     __syncthreads();
     t = Stats{largest, 0.0f, 0.0f};
     for (int j = lo + tid; j < hi; j += NT) {
@@ -490,7 +499,7 @@ __global__ void __launch_bounds__(NT, 5 * 256 / NT) logprobs_kernel(const T* __r
   const float ls = bad ? nan : (empty ? 0.0f : logf(t.s));
   if (tid == 0) {
     // (an entropy is not negative; rounding alone could make it so)
-    const float H = bad ? nan : (empty ? 0.0f : fmaxf(__fsub_rn(ls, __fmul_rn(__fdiv_rn(t.w, t.s), 0.693147180559945f)), 0.0f));
+    const float H = bad ? nan : (empty ? 0.0f : max_nan(__fsub_rn(ls, __fmul_rn(__fdiv_rn(t.w, t.s), 0.693147180559945f)), 0.0f));
     if (bad) flag(p.dev_status, OCS_DEV_NONFINITE);
     if (p.entropy) p.entropy[r] = H;
     if (p.stats)
@@ -613,9 +622,29 @@ int row_threads(long long rows, int V, int ve, int top_k) {
   return top_k * vecs <= 320 && (vecs <= 8 || (rows > 5 * kNumSMs && V <= 40960)) ? 128 : kLpThreads;
 }
 
+// Low for logits of type T: the power of two whose product with c lies in (-2^24, -2^23], where the type has it.  It bounds
+// what the sums tell from a masked token, not what a logit may be: in fp16, where it is the type's lowest value up to c =
+// 256, live logits may lie near it, and sums_hold() is what keeps them right.
+template <typename T>
+Low stand_in(float c) {
+  const int k = 23 - std::ilogb(c);
+  float v = -std::ldexp(1.0f, k < 100 ? k : 100);
+  if constexpr (std::is_same<T, __half>::value) {
+    if (v < -65504.0f) v = -65504.0f;
+    const __half h = __float2half_rn(v);
+    uint16_t b;
+    memcpy(&b, &h, 2);
+    return Low{v, b * 0x10001u};
+  }
+  uint32_t b;   // a power of two is its upper half as bf16
+  memcpy(&b, &v, 4);
+  return Low{v, (b >> 16) * 0x10001u};
+}
+
 template <typename T>
 ocs_status launch_logprobs(const void* logits_, LogprobParams p, cudaStream_t stream) {
   const T* logits = static_cast<const T*>(logits_);
+  p.low = stand_in<T>(p.c);
   const int cl = row_ctas(p.rows, p.V, Vec<T>::VE), nt = cl > 1 ? kLpThreads : row_threads(p.rows, p.V, Vec<T>::VE, p.top_k);
   const long long rows = p.rows, step = 1ll << 27;   // rows of one launch (the grid's limit)
   for (long long r0 = 0; r0 < rows; r0 += step) {
@@ -685,7 +714,7 @@ extern "C" ocs_status ocs_token_logprobs(const void* logits, ocs_dtype type, int
   if (st != OCS_OK) return st;
   if (!top_ids && !top_logprob) top_k = 0;
   const float c = (float)((double)inv_temperature * 1.4426950408889634);
-  LogprobParams p{rows, ld, V, top_k, targets, inv_temperature, c, logprob, entropy, top_logprob, stats, top_ids, dev_status};
+  LogprobParams p{rows, ld, V, top_k, targets, inv_temperature, c, Low{}, logprob, entropy, top_logprob, stats, top_ids, dev_status};
   switch (type) {
     case OCS_F16: return launch_logprobs<__half>(logits, p, stream);
     case OCS_BF16: return launch_logprobs<__nv_bfloat16>(logits, p, stream);
