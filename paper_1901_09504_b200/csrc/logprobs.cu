@@ -54,7 +54,7 @@ struct Vec {
                  : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7]) : "l"(p));
   }
   __device__ __forceinline__ void floats(float* f) const;      // the elements as fp32
-  __device__ __forceinline__ void floored(float* f, const Low& low) const;   // ... none below low
+  __device__ __forceinline__ void floored(float* f, const Low& low) const;   // ... in 16 bits none below low (a packed maximum)
   __device__ __forceinline__ float max_all() const;            // the largest; NaN if any element is
 };
 
@@ -62,10 +62,7 @@ template <> __device__ __forceinline__ void Vec<float>::floats(float* f) const {
 #pragma unroll
   for (int i = 0; i < 8; ++i) f[i] = __uint_as_float(w[i]);
 }
-template <> __device__ __forceinline__ void Vec<float>::floored(float* f, const Low& low) const {
-#pragma unroll
-  for (int i = 0; i < 8; ++i) f[i] = fmaxf(__uint_as_float(w[i]), low.v);
-}
+template <> __device__ __forceinline__ void Vec<float>::floored(float* f, const Low&) const { floats(f); }
 template <> __device__ __forceinline__ float Vec<float>::max_all() const {
   float m[4];
 #pragma unroll
@@ -154,8 +151,25 @@ __device__ __forceinline__ void shift(Stats& t, float d) {   // every term's exp
   t.w = __fmul_rn(fmaf(t.s, d, t.w), ex2(d));
   t.s = __fmul_rn(t.s, ex2(d));
 }
-__device__ __forceinline__ void move_max(Stats& t, float m, float c) {   // the same sums relative to another maximum
-  shift(t, fmaxf(__fmul_rn(__fsub_rn(t.m, m), c), kFloor));              // -infinity or NaN (nothing summed yet): s = w = 0
+// c * up = inv_temperature * log2 e; up is 1, or 2 where that product is not finite
+struct Scale {
+  float c, up;
+};
+// (l - m) * c * up, l <= m.  Halves keep the difference finite where logits near both ends of fp32 meet.
+__device__ __forceinline__ float scaled_distance(float l, float m, Scale k) {
+  const bool far = fabsf(m) > 0x1p100f;
+  const float h = far ? 0.5f : 1.0f;
+  return __fmul_rn(__fmul_rn(__fsub_rn(__fmul_rn(l, h), __fmul_rn(m, h)), k.c), far ? __fadd_rn(k.up, k.up) : k.up);
+}
+// The exponent of a logit relative to m in base 2.  ENDS: inverse temperatures outside of [2^-64, 2^64].  Between them a
+// difference that overflows has p = 0 anyway, and c is finite.
+template <bool ENDS>
+__device__ __forceinline__ float exponent(float l, float m, Scale k) {
+  return ENDS ? scaled_distance(l, m, k) : __fmul_rn(__fsub_rn(l, m), k.c);
+}
+template <bool ENDS>
+__device__ __forceinline__ void move_max(Stats& t, float m, Scale k) {   // the same sums relative to another maximum
+  shift(t, fmaxf(exponent<ENDS>(t.m, m, k), kFloor));                    // -infinity or NaN (nothing summed yet): s = w = 0
   t.m = m;
 }
 // The main loop takes d = fma(l, c, -M) with M = fl(m * c) instead of (l - m) * c: one instruction, one rounding.  M's own
@@ -183,8 +197,9 @@ __device__ __forceinline__ void add_lanes(Stats& t) {
   }
 }
 // The eight parts that lanes 0..7 hold (and lanes 8..15, ... again) as one, in every lane.
-__device__ __forceinline__ Stats join_eight(Stats t, float c) {
-  move_max(t, warp_max(t.m), c);
+template <bool ENDS>
+__device__ __forceinline__ Stats join_eight(Stats t, Scale k) {
+  move_max<ENDS>(t, warp_max(t.m), k);
   add_lanes<8>(t);
   return t;
 }
@@ -217,7 +232,9 @@ __device__ __forceinline__ void take(Running& t, const Vec<T>& v, int j, float c
   v.floored(f, low);
 #pragma unroll
   for (int i = 0; i < VE; ++i) {
-    const float d = fmaf(f[i], c, -t.M), e = ex2(d);
+    float d = fmaf(f[i], c, -t.M);
+    if constexpr (sizeof(T) == 4) d = fmaxf(d, kFloor);
+    const float e = ex2(d);
     t.s[i & 1] = __fadd_rn(t.s[i & 1], e);
     t.w[i & 1] = fmaf(e, d, t.w[i & 1]);
   }
@@ -227,7 +244,8 @@ struct LogprobParams {
   long long rows, ld;
   int V, top_k;
   const int32_t* targets;
-  float beta, c;
+  float beta;
+  Scale scale;
   Low low;
   float *logprob, *entropy, *top_logprob, *stats;
   int32_t* top_ids;
@@ -377,7 +395,7 @@ __device__ __forceinline__ void store_peer_f32(uint32_t addr, float v) {
 // exponential (2048 x 50257 bf16, 206 MB: 39.3 us, 5.2 TB/s).  Five alternatives add about 3 us per wave of CTAs: 47.5 us
 // there; 20.5 instead of 17.4 us for 700 rows of 33278 fp32 logits (93 MB), which are one wave.  Few rows are latency:
 // 8 x 131072 bf16 takes 4.2 us, 8.4 with twenty alternatives.
-template <typename T, int NT>
+template <typename T, int NT, bool ENDS>
 __global__ void __launch_bounds__(NT, 5 * 256 / NT) logprobs_kernel(const T* __restrict__ logits, const LogprobParams p) {
   constexpr int VE = Vec<T>::VE, kWarps = NT / 32;
   __shared__ LogprobSmem<NT> sm;
@@ -396,7 +414,7 @@ __global__ void __launch_bounds__(NT, 5 * 256 / NT) logprobs_kernel(const T* __r
     if (y >= 0) ly = to_f32(row.x[y]);
   }
 
-  const float c = p.c;
+  const float c = p.scale.c;
   const Low low = p.low;
   Running run{-INFINITY, 0.0f, {0.0f, 0.0f}, {0.0f, 0.0f}, lo + tid};
   {
@@ -444,7 +462,7 @@ __global__ void __launch_bounds__(NT, 5 * 256 / NT) logprobs_kernel(const T* __r
   float largest = sm.warp[0].m;
 #pragma unroll
   for (int w = 1; w < kWarps; ++w) largest = max_nan(largest, sm.warp[w].m);
-  if (fabsf(largest) < INFINITY && !sums_hold(largest, c, low.v)) {   // the same for the whole CTA
+  if (fabsf(largest) < INFINITY && (ENDS || !sums_hold(largest, c, low.v))) {   // the same for the whole CTA
     __syncthreads();
     t = Stats{largest, 0.0f, 0.0f};
     for (int j = lo + tid; j < hi; j += NT) {
@@ -452,7 +470,7 @@ __global__ void __launch_bounds__(NT, 5 * 256 / NT) logprobs_kernel(const T* __r
       row.load(j).floats(f);
 #pragma unroll
       for (int i = 0; i < VE; ++i) {
-        const float d = fmaxf(__fmul_rn(__fsub_rn(f[i], largest), c), kFloor), e = ex2(d);
+        const float d = fmaxf(exponent<ENDS>(f[i], largest, p.scale), kFloor), e = ex2(d);
         t.s = __fadd_rn(t.s, e);
         t.w = fmaf(e, d, t.w);
       }
@@ -462,7 +480,7 @@ __global__ void __launch_bounds__(NT, 5 * 256 / NT) logprobs_kernel(const T* __r
     __syncthreads();
   }
   if (p.top_k > 0) top_of_segment(row, lo, hi, p.top_k, run.m, run.pos, largest, sm, top);
-  t = join_eight(sm.warp[lane & 7], c);   // this CTA's part of the row, in every thread
+  t = join_eight<ENDS>(sm.warp[lane & 7], p.scale);   // this CTA's part of the row, in every thread
   if (CL > 1) {
     asm volatile("barrier.cluster.wait;" ::: "memory");
     if (rank != 0) {
@@ -483,7 +501,7 @@ __global__ void __launch_bounds__(NT, 5 * 256 / NT) logprobs_kernel(const T* __r
     const Stats own = t;
     const int part = lane & 7;
     t = part == 0 ? own : (part < CL ? sm.part[part] : Stats{-INFINITY, 0.0f, 0.0f});
-    t = join_eight(t, c);
+    t = join_eight<ENDS>(t, p.scale);
     if (p.top_k > 0) {
       for (int i = tid; i < CL * p.top_k; i += NT) {
         const key_t k = sm.top[i];
@@ -505,14 +523,14 @@ __global__ void __launch_bounds__(NT, 5 * 256 / NT) logprobs_kernel(const T* __r
     if (p.stats)
       reinterpret_cast<float4*>(p.stats)[r] = make_float4(bad ? nan : t.m, ls, H, fmaf(t.m, p.beta, ls));
     if (p.logprob)
-      p.logprob[r] = bad ? nan : (y < 0 ? 0.0f : (empty ? -INFINITY : __fsub_rn(__fmul_rn(__fsub_rn(ly, t.m), p.beta), ls)));
+      p.logprob[r] = bad ? nan : (y < 0 ? 0.0f : (empty ? -INFINITY : __fsub_rn(scaled_distance(ly, t.m, Scale{p.beta, 1.0f}), ls)));
   }
   for (int i = tid; i < p.top_k; i += NT) {
     const key_t k = best[i];
     if (p.top_ids) p.top_ids[r * p.top_k + i] = bad ? -1 : key_index(k);
     if (p.top_logprob)
       p.top_logprob[r * p.top_k + i] =
-          bad ? nan : (empty ? -INFINITY : __fsub_rn(__fmul_rn(__fsub_rn(key_value(k), t.m), p.beta), ls));
+          bad ? nan : (empty ? -INFINITY : __fsub_rn(scaled_distance(key_value(k), t.m, Scale{p.beta, 1.0f}), ls));
   }
 }
 
@@ -520,7 +538,8 @@ struct GradParams {
   long long ld, ld_d;
   int V, chunks;
   const int32_t* targets;
-  float beta, c;
+  float beta;
+  Scale scale;
   const float *stats, *g_logprob, *g_entropy;
   int* dev_status;
 };
@@ -535,7 +554,7 @@ constexpr int kGradVecs = 2;   // vectors a thread of the gradient kernel handle
 // independent, so rows are cut into parts of two vectors per thread, all loads of a thread are issued before its first
 // arithmetic, and the grid is as large as the tensor.  Bound by HBM: 2048 x 50257 bf16, 412 MB, 64.3 us, 6.4 TB/s (98 % of the
 // measured copy rate); 700 x 33278 fp32, 186 MB, 29.8 us, 6.3 TB/s.
-template <typename T>
+template <typename T, bool ENDS>
 __global__ void __launch_bounds__(kLpThreads) logprobs_backward_kernel(const T* logits, T* d_logits, const GradParams p) {
   constexpr int VE = Vec<T>::VE;
   const long long r = blockIdx.x / p.chunks;
@@ -559,8 +578,9 @@ __global__ void __launch_bounds__(kLpThreads) logprobs_backward_kernel(const T* 
   const float g = p.g_logprob && y >= 0 ? __ldg(p.g_logprob + r) : 0.0f;
   const bool empty = st.x == -INFINITY;
   const float ls2 = __fmul_rn(st.y, 1.44269504088896f);
-  // d = -beta * p * (g + gh * (ln p + H)) = p * (A + B * log2 p)
-  const float A = -__fmul_rn(p.beta, fmaf(gh, st.z, g)), B = -__fmul_rn(__fmul_rn(gh, 0.693147180559945f), p.beta);
+  // d = -beta * p * (g + gh * (ln p + H)) = p * (A + B * log2 p).  ENDS: beta comes last, so that A is not infinite where p is zero.
+  const float first = ENDS ? 1.0f : p.beta;
+  const float A = -__fmul_rn(first, fmaf(gh, st.z, g)), B = -__fmul_rn(__fmul_rn(gh, 0.693147180559945f), first);
   const bool same = ((reinterpret_cast<uintptr_t>(dst) ^ reinterpret_cast<uintptr_t>(row.x)) & 31) == 0;
 #pragma unroll
   for (int u = 0; u < kGradVecs; ++u) {
@@ -570,14 +590,18 @@ __global__ void __launch_bounds__(kLpThreads) logprobs_backward_kernel(const T* 
     float d[VE];
     v[u].floats(d);
 #pragma unroll
-    for (int i = 0; i < VE; ++i) {
-      const float q = fmaxf(fmaf(__fsub_rn(d[i], st.x), p.c, -ls2), kFloor);   // log2 p; a masked token's p is zero
+    for (int i = 0; i < VE; ++i) {   // by log2 p; a masked token's p is zero
+      const float q = fmaxf(ENDS ? __fsub_rn(exponent<true>(d[i], st.x, p.scale), ls2) : fmaf(__fsub_rn(d[i], st.x), p.scale.c, -ls2), kFloor);
       d[i] = __fmul_rn(ex2(q), fmaf(B, q, A));
     }
     if ((unsigned)(y - e0) < (unsigned)VE && y >= 0 && !empty) {   // the given token is in this vector
 #pragma unroll
       for (int e = 0; e < VE; ++e)
-        if (e0 + e == y) d[e] = fmaf(g, p.beta, d[e]);
+        if (e0 + e == y) d[e] = fmaf(g, first, d[e]);
+    }
+    if (ENDS) {
+#pragma unroll
+      for (int e = 0; e < VE; ++e) d[e] = __fmul_rn(d[e], p.beta);
     }
     if (same && row.whole(j)) {
       uint32_t o[8];
@@ -622,6 +646,12 @@ int row_threads(long long rows, int V, int ve, int top_k) {
   return top_k * vecs <= 320 && (vecs <= 8 || (rows > 5 * kNumSMs && V <= 40960)) ? 128 : kLpThreads;
 }
 
+bool at_ends(float beta) { return beta < 0x1p-64f || beta > 0x1p64f; }
+Scale base2(float beta) {
+  const float up = beta > 0x1p127f ? 2.0f : 1.0f;
+  return Scale{(float)((double)beta * 1.4426950408889634 / up), up};
+}
+
 // Low for logits of type T: the power of two whose product with c lies in (-2^24, -2^23], where the type has it.  It bounds
 // what the sums tell from a masked token, not what a logit may be: in fp16, where it is the type's lowest value up to c =
 // 256, live logits may lie near it, and sums_hold() is what keeps them right.
@@ -644,8 +674,9 @@ Low stand_in(float c) {
 template <typename T>
 ocs_status launch_logprobs(const void* logits_, LogprobParams p, cudaStream_t stream) {
   const T* logits = static_cast<const T*>(logits_);
-  p.low = stand_in<T>(p.c);
-  const int cl = row_ctas(p.rows, p.V, Vec<T>::VE), nt = cl > 1 ? kLpThreads : row_threads(p.rows, p.V, Vec<T>::VE, p.top_k);
+  const bool ends = at_ends(p.beta);
+  p.low = stand_in<T>(p.scale.c);
+  const int cl = row_ctas(p.rows, p.V, Vec<T>::VE), nt = cl > 1 || ends ? kLpThreads : row_threads(p.rows, p.V, Vec<T>::VE, p.top_k);
   const long long rows = p.rows, step = 1ll << 27;   // rows of one launch (the grid's limit)
   for (long long r0 = 0; r0 < rows; r0 += step) {
     const long long n = rows - r0 < step ? rows - r0 : step;
@@ -658,7 +689,7 @@ ocs_status launch_logprobs(const void* logits_, LogprobParams p, cudaStream_t st
     attr[0].val.clusterDim.x = cl; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr; cfg.numAttrs = cl > 1 ? 1 : 0;
     LaunchScope ls("logprobs_kernel", stream);
-    const auto kernel = nt == 128 ? logprobs_kernel<T, 128> : logprobs_kernel<T, kLpThreads>;
+    const auto kernel = ends ? logprobs_kernel<T, kLpThreads, true> : nt == 128 ? logprobs_kernel<T, 128, false> : logprobs_kernel<T, kLpThreads, false>;
     if (cudaLaunchKernelEx(&cfg, kernel, logits + r0 * p.ld, p) != cudaSuccess) return OCS_ERR_CUDA;
     if (p.targets) p.targets += n;
     if (p.logprob) p.logprob += n;
@@ -681,7 +712,8 @@ ocs_status launch_backward(const void* logits_, void* d_logits_, long long rows,
   for (long long r0 = 0; r0 < rows; r0 += step) {
     const long long n = rows - r0 < step ? rows - r0 : step;
     LaunchScope ls("logprobs_backward_kernel", stream);
-    logprobs_backward_kernel<T><<<(unsigned)(n * p.chunks), kLpThreads, 0, stream>>>(logits + r0 * p.ld, d_logits + r0 * p.ld_d, p);
+    const auto kernel = at_ends(p.beta) ? logprobs_backward_kernel<T, true> : logprobs_backward_kernel<T, false>;
+    kernel<<<(unsigned)(n * p.chunks), kLpThreads, 0, stream>>>(logits + r0 * p.ld, d_logits + r0 * p.ld_d, p);
     if (p.targets) p.targets += n;
     if (p.g_logprob) p.g_logprob += n;
     if (p.g_entropy) p.g_entropy += n;
@@ -713,8 +745,7 @@ extern "C" ocs_status ocs_token_logprobs(const void* logits, ocs_dtype type, int
   const ocs_status st = check_device();
   if (st != OCS_OK) return st;
   if (!top_ids && !top_logprob) top_k = 0;
-  const float c = (float)((double)inv_temperature * 1.4426950408889634);
-  LogprobParams p{rows, ld, V, top_k, targets, inv_temperature, c, Low{}, logprob, entropy, top_logprob, stats, top_ids, dev_status};
+  LogprobParams p{rows, ld, V, top_k, targets, inv_temperature, base2(inv_temperature), Low{}, logprob, entropy, top_logprob, stats, top_ids, dev_status};
   switch (type) {
     case OCS_F16: return launch_logprobs<__half>(logits, p, stream);
     case OCS_BF16: return launch_logprobs<__nv_bfloat16>(logits, p, stream);
@@ -738,8 +769,7 @@ extern "C" ocs_status ocs_token_logprobs_backward(const void* logits, ocs_dtype 
     return OCS_ERR_SHAPE;
   const ocs_status st = check_device();
   if (st != OCS_OK) return st;
-  const float c = (float)((double)inv_temperature * 1.4426950408889634);
-  GradParams p{ld, ld_d, V, 0, targets, inv_temperature, c, stats, g_logprob, g_entropy, dev_status};
+  GradParams p{ld, ld_d, V, 0, targets, inv_temperature, base2(inv_temperature), stats, g_logprob, g_entropy, dev_status};
   switch (type) {
     case OCS_F16: return launch_backward<__half>(logits, d_logits, rows, p, stream);
     case OCS_BF16: return launch_backward<__nv_bfloat16>(logits, d_logits, rows, p, stream);

@@ -18,13 +18,14 @@ def check_gradient(x, y, r, ref, beta):
     g, gh = torch.randn(T, generator=_gen(8), device="cuda"), torch.randn(T, generator=_gen(9), device="cuda")
     d = ocs.ocs_token_logprobs_backward(x, y, r.stats, g, gh, inv_temperature=beta)
     want, one = _ref_grad(ref, y, beta, g, gh)
-    if x.dtype == torch.float16:             # what rounds beyond the type's largest value is infinite
-        want = torch.where(want.abs() >= 65520, want.sign() * float("inf"), want)
+    limit = {torch.float16: 65520.0, torch.bfloat16: (2 - 2.0 ** -8) * 2.0 ** 127, torch.float32: (2 - 2.0 ** -24) * 2.0 ** 127}[x.dtype]
+    want = torch.where(want.abs() >= limit, want.sign() * float("inf"), want)   # rounds beyond the type's largest value
     p, ts = ref["p"], (_tol_sum(ref, V) + U * 2 * ref["log_s"].abs())[:, None]
     tol_h = (_tol_sum(ref, V) + U * (2 * ref["E2"] + (6 + 2 * _chain(V)) * ref["E1"] + ref["H"].abs()))[:, None]
-    eps_p = U * (2 * ref["d"].abs() + ref["logp"].abs() + 4) + ts
+    live = lambda t: torch.where(p > 0, t.abs(), torch.zeros_like(t))
+    eps_p = U * (2 * live(ref["d"]) + live(ref["logp"]) + 4) + ts
     G, GH = g.double().abs()[:, None], gh.double().abs()[:, None]
-    lph = torch.where(p > 0, (ref["logp"] + ref["H"][:, None]).abs(), torch.zeros_like(p))
+    lph = live(ref["logp"] + ref["H"][:, None])
     tol = beta * (p * (G + GH * lph) * (eps_p + 4 * U) + GH * p * (eps_p + tol_h) + 2 * U * G * one) + 2 * U * want.abs()
     tol = 1.01 * (tol + (HALF_ULP[x.dtype] * want.abs() if x.dtype != torch.float32 else 0))
     tol = tol + {torch.float16: 2.0 ** -25, torch.float32: 1e-44, torch.bfloat16: 1e-40}[x.dtype]
@@ -109,4 +110,36 @@ def test_large_inverse_temperatures(kind, value, beta):
     y = torch.zeros(12, dtype=torch.int32, device="cuda")
     r, ref = check(x, y, 5, beta)
     assert torch.isfinite(r.entropy).all()
+    check_gradient(x, y, r, ref, beta)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [300, 9001, 70001])
+def test_inverse_temperature_whose_base_2_form_leaves_fp32(kind, V):
+    """1.75 * 2^127 is finite, its product with log2 e is not: equal logits, one above the others, and logits so near to zero
+    that their multiples of it are ordinary numbers."""
+    beta = 1.75 * 2.0 ** 127
+    x = torch.zeros((5, V), device="cuda").to(TYPES[kind])
+    x[1] = 0.5
+    x[2, V // 2] = 1.0
+    x[3] = (torch.randint(-9, 10, (V,), generator=_gen(1), device="cuda").double() * 2.0 ** -126).to(TYPES[kind])
+    x[4] = x[3]
+    x[4, ::3] = -float("inf")
+    y = torch.tensor([0, V - 1, V // 2, 1, 1], dtype=torch.int32, device="cuda")
+    r, ref = check(x, y, 3, beta)
+    check_gradient(x, y, r, ref, beta)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [300, 9001, 70001])
+def test_logits_whose_differences_leave_fp32(kind, V):
+    """Logits up to the ends of fp32 with both signs, at an inverse temperature of 2^-126: their differences overflow, the
+    differences' multiples are ordinary numbers."""
+    beta = 2.0 ** -126
+    x = (3.3e38 * (2 * torch.rand((4, V), generator=_gen(1), device="cuda") - 1)).to(TYPES[kind])
+    x[1, :256] = torch.finfo(TYPES[kind]).min
+    x[2, ::2] = -float("inf")
+    x[3, V // 2:] = torch.finfo(TYPES[kind]).min
+    y = torch.tensor([0, V - 1, 1, V // 2], dtype=torch.int32, device="cuda")
+    r, ref = check(x, y, 3, beta)
     check_gradient(x, y, r, ref, beta)
