@@ -143,3 +143,50 @@ def test_logits_whose_differences_leave_fp32(kind, V):
     y = torch.tensor([0, V - 1, 1, V // 2], dtype=torch.int32, device="cuda")
     r, ref = check(x, y, 3, beta)
     check_gradient(x, y, r, ref, beta)
+
+
+def _device_us(f):
+    """Shortest of several replays of ten calls, in us per call."""
+    f()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        for _ in range(10):
+            f()
+    begin, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+    best = float("inf")
+    for _ in range(8):
+        begin.record()
+        graph.replay()
+        end.record()
+        end.synchronize()
+        best = min(best, begin.elapsed_time(end) * 100)
+    del graph
+    return best
+
+
+@pytest.mark.parametrize("kind,T,V,k", [("bf16", 2000, 8000, 64), ("bf16", 800, 3000, 64), ("f16", 4096, 1116, 40), ("f32", 800, 3000, 64)])
+def test_alternatives_of_equal_logits_take_no_pass_for_each(kind, T, V, k):
+    """Rows of one value, and rows with fewer unmasked tokens than alternatives: the right ids, at a price near that of
+    random rows (a pass over the row for each alternative would be ten to twenty times it)."""
+    x = _logits(T, T, V, kind).contiguous()
+    y = torch.zeros(T, dtype=torch.int32, device="cuda")
+    out = ocs.ocs_token_logprobs(x, y, top_k=k)
+    usual = _device_us(lambda: ocs.ocs_token_logprobs(x, y, top_k=k, out=out))
+    for masked in (float("-inf"), -1e4, 1.0):
+        z = torch.full_like(x, masked)
+        z[:, 7::V // 10] = 1.0
+        check(z, y, k, 1.0)
+        took = _device_us(lambda: ocs.ocs_token_logprobs(z, y, top_k=k, out=out))
+        assert took < 5 * usual + 5, (masked, took, usual)
+
+
+@pytest.mark.parametrize("kind,V", [("bf16", 8000), ("f16", 8190), ("f32", 4090)])
+def test_alternatives_that_few_threads_hold(kind, V):
+    """The largest logits all in the vectors of 63 threads (of 128), far more of them than alternatives."""
+    x = _logits(V, 5, V, kind).contiguous()
+    ve = 8 if kind == "f32" else 16
+    lucky = torch.arange(V, device="cuda") % (128 * ve) < 63 * ve
+    x[:, lucky] += 40
+    y = torch.zeros(5, dtype=torch.int32, device="cuda")
+    for k in (5, 63, 64):
+        check(x, y, k, 1.0)
