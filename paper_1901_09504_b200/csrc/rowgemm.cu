@@ -600,8 +600,9 @@ struct RowPlan {
   int tn, cg, slices;
 };
 
-// Test hook (ocs_selftest_force_row_plan): the plan of the following calls where it is valid for the problem.
-std::atomic<int> g_force_tn{0}, g_force_cg{0}, g_force_slices{0};
+// Test hook (ocs_selftest_force_row_plan): the plan of the following calls where it is valid for the problem, in one word
+// so that a call in another thread sees a whole plan: tn << 8 | cg << 4 | slices, 0 for none.
+std::atomic<int> g_forced_plan{0};
 
 // CTAs resident at once, one per SM, for cluster sizes 1, 2, 4, 8 (a cluster lies inside one GPC)
 int cluster_capacity(int cl) { return cl <= 2 ? 148 : (cl == 4 ? 132 : 120); }
@@ -626,9 +627,8 @@ RowPlan choose_plan(int M, int N, int num_kb, int out_bytes) {
   auto tiles_of = [&](int tn, int cg) {
     return (long long)((M + (long long)tn - 1) / tn) * ((N + (long long)TW * cg - 1) / (TW * cg));
   };
-  const int ft = g_force_tn.load(), fc = g_force_cg.load(), fs = g_force_slices.load();
-  if (ft) {
-    RowPlan r{ft, fc, fs};
+  if (const int forced = g_forced_plan.load()) {
+    RowPlan r{forced >> 8, forced >> 4 & 15, forced & 15};
     while (r.slices > 1 && !split_fits(r.tn, r.cg, r.slices, tiles_of(r.tn, r.cg), stages_of(r.tn, num_kb))) r.slices /= 2;
     return r;
   }
@@ -732,12 +732,11 @@ struct Product {
 };
 
 template <typename T>
-ocs_status launch_product(const Product& g, void* Y_, bool overlap, cudaStream_t stream) {
+ocs_status launch_product(const Product& g, const RowPlan& plan, void* Y_, bool overlap, cudaStream_t stream) {
   RowGemm p{};
   p.M = g.M; p.N = g.N; p.t_signed = g.a_signed;
   p.a_scales = g.a_scales; p.w_scales = g.w_scales; p.bias = g.bias; p.ldy = g.ldy; p.dev_status = g.dev_status;
   const int num_kb = (g.K + KB - 1) / KB;
-  const RowPlan plan = choose_plan(g.M, g.N, num_kb, (int)sizeof(T));
   p.num_kb = stages_of(plan.tn, num_kb);
   T* Y = static_cast<T*>(Y_);
   if (!g.A) {
@@ -756,11 +755,11 @@ ocs_status launch_product(const Product& g, void* Y_, bool overlap, cudaStream_t
   }
 }
 
-ocs_status run_product(const Product& p, void* Y, ocs_dtype y_type, bool overlap, cudaStream_t stream) {
+ocs_status run_product(const Product& p, const RowPlan& plan, void* Y, ocs_dtype y_type, bool overlap, cudaStream_t stream) {
   switch (y_type) {
-    case OCS_F16: return launch_product<__half>(p, Y, overlap, stream);
-    case OCS_BF16: return launch_product<__nv_bfloat16>(p, Y, overlap, stream);
-    default: return launch_product<float>(p, Y, overlap, stream);
+    case OCS_F16: return launch_product<__half>(p, plan, Y, overlap, stream);
+    case OCS_BF16: return launch_product<__nv_bfloat16>(p, plan, Y, overlap, stream);
+    default: return launch_product<float>(p, plan, Y, overlap, stream);
   }
 }
 
@@ -794,28 +793,32 @@ extern "C" ocs_status ocs_qlinear_rows(const void* A_codes, int a_signed, const 
   if ((st = check_device()) != OCS_OK) return st;
   Product p{A_codes, a_scales, W_codes, w_scales, bias, M, N, K, a_signed ? 1 : 0,
             lda, ldw, ldy, dev_status, nullptr, 0, nullptr, OCS_F32, 0, 0, 0.0f};
-  return run_product(p, Y, y_type, false, stream);
+  return run_product(p, choose_plan(M, N, (K + KB - 1) / KB, elem_bytes(y_type)), Y, y_type, false, stream);
 }
 
 namespace {
-// The plan of an ocs_linear_rows call, and the bytes of codes and scales it keeps in the workspace (0: quantized inside
-// the product's kernel).
+// The plan of an ocs_linear_rows call, chosen once (the two forms of the call and their kernels have to agree on it), and the
+// bytes of codes and scales it keeps in the workspace (0: quantized inside the product's kernel).
+struct RowsCall {
+  RowPlan plan;
+  size_t ws_bytes;
+};
 int row_align(const void* X, int M, int64_t ldx, ocs_dtype x_type) {
   const uintptr_t a = reinterpret_cast<uintptr_t>(X) | (M > 1 ? (uintptr_t)(ldx * elem_bytes(x_type)) : 0);
   return a % 16 == 0 ? 16 : (a % 8 == 0 ? 8 : 1);
 }
-size_t linear_rows_plan(const void* X, int M, int C, int64_t ldx, int S, int N, ocs_dtype x_type, ocs_dtype y_type) {
+RowsCall linear_rows_plan(const void* X, int M, int C, int64_t ldx, int S, int N, ocs_dtype x_type, ocs_dtype y_type) {
   const int K = C + S, num_kb = (K + KB - 1) / KB;
   const RowPlan plan = choose_plan(M, N, num_kb, elem_bytes(y_type));
-  if (fuse_tokens(plan, M, N, C, num_kb, elem_bytes(x_type), row_align(X, M, ldx, x_type))) return 0;
-  return align_up((size_t)M * align_up((size_t)K, 16), 256) + align_up((size_t)M * 4, 256);
+  if (fuse_tokens(plan, M, N, C, num_kb, elem_bytes(x_type), row_align(X, M, ldx, x_type))) return {plan, 0};
+  return {plan, align_up((size_t)M * align_up((size_t)K, 16), 256) + align_up((size_t)M * 4, 256)};
 }
 }  // namespace
 
 extern "C" size_t ocs_linear_rows_workspace_bytes(const void* X, ocs_dtype x_type, int M, int C, int64_t ldx, int S, int N,
                                                   ocs_dtype y_type) {
   if (M <= 0 || C <= 0 || S < 0 || N <= 0 || !valid_dtype(x_type) || !valid_dtype(y_type) || (int64_t)C + S >= (1 << 30)) return 0;
-  return linear_rows_plan(X, M, C, ldx, S, N, x_type, y_type);
+  return linear_rows_plan(X, M, C, ldx, S, N, x_type, y_type).ws_bytes;
 }
 
 extern "C" ocs_status ocs_linear_rows(const void* X, ocs_dtype x_type, int M, int C, int64_t ldx, int S,
@@ -831,7 +834,8 @@ extern "C" ocs_status ocs_linear_rows(const void* X, ocs_dtype x_type, int M, in
   if ((int64_t)C + S >= (1 << 30)) return OCS_ERR_UNSUPPORTED;
   const int K = C + S;
   const int64_t lda = (int64_t)align_up((size_t)K, 16);
-  const size_t need = linear_rows_plan(X, M, C, ldx, S, N, x_type, y_type);
+  const RowsCall call = linear_rows_plan(X, M, C, ldx, S, N, x_type, y_type);
+  const size_t need = call.ws_bytes;
   if (need && (!ws || !aligned(ws, 256) || ws_bytes < need)) return OCS_ERR_WORKSPACE;
   ocs_status st = check_product(is_signed, M, K, lda, nullptr, W_codes, N, ldw, bias, Y, y_type, ldy, w_scales);
   if (st != OCS_OK) return st;
@@ -846,7 +850,7 @@ extern "C" ocs_status ocs_linear_rows(const void* X, ocs_dtype x_type, int M, in
     if (st != OCS_OK) return st;
     p.A = codes; p.a_scales = scales;
   }
-  return run_product(p, Y, y_type, true, stream);
+  return run_product(p, call.plan, Y, y_type, true, stream);
 }
 
 // Test hook: the next ocs_qlinear_rows / ocs_linear_rows calls of this process use the given plan; tn = 0 gives the
@@ -855,6 +859,6 @@ extern "C" ocs_status ocs_selftest_force_row_plan(int tn, int cg, int slices) {
   if (tn != 0 && ((tn != 16 && tn != 32 && tn != 64 && tn != 128 && tn != 256) || (cg != 1 && !(cg == 2 && tn == 256)) ||
                   (slices != 1 && slices != 2 && slices != 4 && slices != 8)))
     return OCS_ERR_INVALID_ARG;
-  g_force_tn.store(tn); g_force_cg.store(cg); g_force_slices.store(slices);
+  g_forced_plan.store(tn ? tn << 8 | cg << 4 | slices : 0);
   return OCS_OK;
 }
