@@ -456,7 +456,7 @@ ocs_status ocs_quantize_rows(const void* X, ocs_dtype x_type, int64_t rows, int 
  * A codes [M][K] (uint8 when a_signed = 0 else int8), row stride lda bytes; Wc int8 [N][K], row stride ldw
  * bytes; both 16-byte aligned with strides that are multiples of 16; a_scales fp32 [M], w_scales fp32 [N],
  * bias fp32 [N]; Y [M][N] of y_type, row stride ldy elements.
- * M = 0 is a no-op.  Limits: K * 128 * (a_signed ? 128 : 255) must fit int32, M < 2^30.
+ * M = 0 is a no-op.  Limits: K * 128 * (a_signed ? 128 : 255) must fit int32, M < 2^30, N < 2^31 - 511.
  * Device flag: TIMEOUT. */
 ocs_status ocs_qlinear_rows(const void* A_codes, int a_signed, const float* a_scales, int M, int K, int64_t lda,
                             const int8_t* W_codes, const float* w_scales, int N, int64_t ldw, const float* bias,

@@ -706,7 +706,7 @@ ocs_status launch_tiles(RowGemm p, int slices, const void* A, long long lda, con
 // launch, but each CTA reads the whole rows, so it is for few tokens.
 bool fuse_tokens(const RowPlan& plan, int M, int N, int C, int num_kb, int x_bytes, int x_align) {
   if (plan.tn > 32 || plan.cg != 1 || x_align < 8) return false;
-  const long long m_tiles = (M + plan.tn - 1) / plan.tn, tiles = m_tiles * ((N + TW - 1) / TW);
+  const long long m_tiles = (M + plan.tn - 1) / plan.tn, tiles = m_tiles * ((N + (long long)TW - 1) / TW);
   const int my_kb = (stages_of(plan.tn, num_kb) + plan.slices - 1) / plan.slices * stage_blocks(plan.tn);
   if ((long long)my_kb * plan.tn * KB > kFusedCodes) return false;                                // the codes have to fit
   if (m_tiles > 1 && tiles > cluster_capacity(plan.slices) / plan.slices) return false;           // one token tile per CTA
@@ -769,7 +769,8 @@ ocs_status check_product(int a_signed, int M, int K, int64_t lda, const void* A,
   if (lda < K || lda % 16 != 0 || !aligned(A, 16)) return OCS_ERR_SHAPE;
   if (ldw < K || ldw % 16 != 0 || !aligned(W, 16)) return OCS_ERR_SHAPE;
   if (ldy < N || !aligned(Y, elem_bytes(y_type)) || !aligned(w_scales, 4) || (bias && !aligned(bias, 4))) return OCS_ERR_SHAPE;
-  if ((int64_t)K * 128 * (a_signed ? 128 : 255) > 2147483647ll || M >= (1 << 30)) return OCS_ERR_UNSUPPORTED;
+  if ((int64_t)K * 128 * (a_signed ? 128 : 255) > 2147483647ll || M >= (1 << 30) || N > 0x7fffffff - 512)
+    return OCS_ERR_UNSUPPORTED;
   return OCS_OK;
 }
 
