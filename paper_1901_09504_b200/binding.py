@@ -628,9 +628,10 @@ def _check_vec(t, n: int):
 
 def ocs_quantize_rows(x, bits: int = 8, is_signed: bool = True, idx_map=None, S: int = 0, ld_codes: int | None = None,
                       dev_status=None, out=None):
-    """x fp32 / fp16 / bf16 [rows, C] (row stride = x.stride(0)) -> (codes int8 / uint8 [rows, ld_codes], scales fp32
-    [rows]): one grid per row, the S duplicated channels of idx_map appended at columns C..C+S-1.
-    `out` = (codes, scales)."""
+    """x fp32 / fp16 / bf16 [rows, C] (row stride = x.stride(0)) -> (codes int8 / uint8 [rows, C+S], scales fp32
+    [rows]): one grid per row, the S duplicated channels of idx_map appended at columns C..C+S-1.  The codes' rows are
+    ld_codes bytes apart (default: C+S rounded up to 16, what the product asks for); the bytes between them are not
+    written and not part of what is returned.  `out` = (codes, scales), the codes at least C+S wide."""
     assert x.is_cuda and x.dtype in DTYPES
     ldx = _rows_of(x)
     rows, Cn = x.shape
@@ -641,10 +642,12 @@ def ocs_quantize_rows(x, bits: int = 8, is_signed: bool = True, idx_map=None, S:
         assert codes.is_cuda and codes.element_size() == 1 and codes.shape[0] == rows and codes.shape[1] >= Cn + S
         _check_vec(scales, rows)
         ld_codes = _rows_of(codes)
+        if codes.shape[1] > Cn + S:
+            codes = codes[:, :Cn + S]
     else:
         if ld_codes is None:
             ld_codes = (Cn + S + 15) & ~15
-        codes = torch.empty((rows, ld_codes), dtype=torch.int8 if is_signed else torch.uint8, device=x.device)
+        codes = torch.empty_strided((rows, Cn + S), (ld_codes, 1), dtype=torch.int8 if is_signed else torch.uint8, device=x.device)
         scales = torch.empty(rows, dtype=torch.float32, device=x.device)
     st = lib().ocs_quantize_rows(x.data_ptr(), DTYPES[x.dtype], rows, Cn, ldx, S, _addr(idx_map), int(bits),
                                  1 if is_signed else 0, codes.data_ptr(), ld_codes, scales.data_ptr(),

@@ -98,7 +98,7 @@ def linear_forward(L: QLayer, x, a_signed: bool, a_bits: int = 8, dev_status=Non
 @dataclass
 class RowLayer:
     """A split linear layer quantized with one scale per output channel; its activations get one per row (token)."""
-    codes: torch.Tensor        # int8 [O, ld >= C + S]
+    codes: torch.Tensor        # int8 [O, C + S], rows of whole 16 bytes
     w_scales: torch.Tensor     # fp32 [O]
     idx_map: torch.Tensor      # int32 [C + S]
     bias: torch.Tensor | None  # fp32 [O]

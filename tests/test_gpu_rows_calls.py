@@ -1,0 +1,31 @@
+"""The row-wise calls put together as their signatures suggest, and what their binding refuses."""
+import pytest
+import torch
+
+import paper_1901_09504_b200 as ocs
+
+from test_gpu_rows import _codes, _gen, _idx, _x, check_product
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("M,C,S,N", [(5, 650, 13, 300), (1, 33, 0, 70), (200, 1001, 20, 513), (3, 64, 0, 64)])
+@pytest.mark.parametrize("given", [False, True])
+def test_codes_go_into_the_product_without_a_length(M, C, S, N, given):
+    """Both halves of the layer quantized by ocs_quantize_rows and multiplied without a word about K: the bytes that pad the
+    codes' rows to 16 are not part of them (and are not zero here)."""
+    x, w, idx = _x(M, M, C, "f32"), _x(N, N, C + S, "f32"), _idx(C, C, S)
+    K = C + S
+    def room(rows):
+        buf = torch.full((rows, ocs.round_up(K, 16)), 99, dtype=torch.int8, device="cuda")
+        return (buf, torch.empty(rows, device="cuda")) if given else None
+    if not given:                            # the allocator hands these bytes out again
+        waste = [torch.full((n * ocs.round_up(K, 16),), 99, dtype=torch.int8, device="cuda") for n in (M, N) for _ in range(4)]
+        del waste
+    codes, a_s = ocs.ocs_quantize_rows(x, idx_map=idx, S=S, out=room(M))
+    W, w_s = ocs.ocs_quantize_rows(w, out=room(N))
+    assert codes.shape == (M, K) and W.shape == (N, K)
+    Y = ocs.ocs_qlinear_rows(codes, a_s, W, w_s)
+    check_product(codes, a_s, W, w_s, None, Y)
+    assert torch.equal(Y, ocs.ocs_qlinear_rows(codes, a_s, W, w_s, K=K))
+    assert torch.equal(Y, ocs.ocs_linear_rows(x, W, w_s, idx_map=idx, S=S))
