@@ -639,7 +639,9 @@ def ocs_quantize_rows(x, bits: int = 8, is_signed: bool = True, idx_map=None, S:
     _check_idx(idx_map, Cn, S)
     if out is not None:
         codes, scales = out
-        assert codes.is_cuda and codes.element_size() == 1 and codes.shape[0] == rows and codes.shape[1] >= Cn + S
+        # (the product takes the grid's sign from the type)
+        assert codes.is_cuda and codes.dtype == (torch.int8 if is_signed else torch.uint8)
+        assert codes.shape[0] == rows and codes.shape[1] >= Cn + S
         _check_vec(scales, rows)
         ld_codes = _rows_of(codes)
         if codes.shape[1] > Cn + S:

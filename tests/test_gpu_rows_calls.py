@@ -29,3 +29,11 @@ def test_codes_go_into_the_product_without_a_length(M, C, S, N, given):
     check_product(codes, a_s, W, w_s, None, Y)
     assert torch.equal(Y, ocs.ocs_qlinear_rows(codes, a_s, W, w_s, K=K))
     assert torch.equal(Y, ocs.ocs_linear_rows(x, W, w_s, idx_map=idx, S=S))
+
+
+@pytest.mark.parametrize("is_signed,kind", [(True, torch.uint8), (False, torch.int8), (True, torch.bool)])
+def test_codes_of_the_other_sign_are_refused(is_signed, kind):
+    """The product tells signed from unsigned codes by their type: -1 written as 255 would count as 255."""
+    x = _x(1, 4, 32, "f32")
+    with pytest.raises(AssertionError):
+        ocs.ocs_quantize_rows(x, 8, is_signed, out=(torch.zeros((4, 32), dtype=kind, device="cuda"), torch.empty(4, device="cuda")))
