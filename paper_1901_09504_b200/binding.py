@@ -626,6 +626,11 @@ def _check_vec(t, n: int):
     assert t is None or (t.is_cuda and t.dtype == torch.float32 and t.is_contiguous() and t.numel() >= n)
 
 
+def _check_status(t):
+    """The library cannot tell a host address from a device address: what kernels write to has to be on the device."""
+    assert t is None or (t.is_cuda and t.dtype == torch.int32 and t.numel() >= 1)
+
+
 def ocs_quantize_rows(x, bits: int = 8, is_signed: bool = True, idx_map=None, S: int = 0, ld_codes: int | None = None,
                       dev_status=None, out=None):
     """x fp32 / fp16 / bf16 [rows, C] (row stride = x.stride(0)) -> (codes int8 / uint8 [rows, C+S], scales fp32
@@ -636,12 +641,13 @@ def ocs_quantize_rows(x, bits: int = 8, is_signed: bool = True, idx_map=None, S:
     ldx = _rows_of(x)
     rows, Cn = x.shape
     S = int(S)
-    _check_idx(idx_map, Cn, S)
+    _check_idx(idx_map, Cn, S), _check_status(dev_status)
     if out is not None:
         codes, scales = out
         # (the product takes the grid's sign from the type)
         assert codes.is_cuda and codes.dtype == (torch.int8 if is_signed else torch.uint8)
         assert codes.shape[0] == rows and codes.shape[1] >= Cn + S
+        assert scales is not None
         _check_vec(scales, rows)
         ld_codes = _rows_of(codes)
         if codes.shape[1] > Cn + S:
@@ -669,7 +675,7 @@ def ocs_qlinear_rows(A_codes, a_scales, W_codes, w_scales, K: int | None = None,
         K = min(A_codes.shape[1], W_codes.shape[1])
     assert 0 < K <= A_codes.shape[1] and K <= W_codes.shape[1]
     assert a_scales is not None and w_scales is not None
-    _check_vec(a_scales, M), _check_vec(w_scales, N), _check_vec(bias, N)
+    _check_vec(a_scales, M), _check_vec(w_scales, N), _check_vec(bias, N), _check_status(dev_status)
     if out is None:
         out, ldy = torch.empty((M, N), dtype=out_dtype, device=A_codes.device), N
     else:
@@ -693,7 +699,8 @@ def ocs_linear_rows(x, W_codes, w_scales, idx_map=None, S: int = 0, bits: int = 
     N, S = W_codes.shape[0], int(S)
     _check_idx(idx_map, Cn, S)
     assert W_codes.shape[1] >= Cn + S and w_scales is not None
-    _check_vec(w_scales, N), _check_vec(bias, N)
+    _check_vec(w_scales, N), _check_vec(bias, N), _check_status(dev_status)
+    assert ws is None or (ws.is_cuda and ws.dtype == torch.uint8 and ws.is_contiguous())
     if out is None:
         out = x.new_empty((M, N)) if out_dtype is None else torch.empty((M, N), dtype=out_dtype, device=x.device)
         ldy = N
@@ -739,6 +746,7 @@ def ocs_token_logprobs(logits, targets=None, top_k: int = 0, inv_temperature: fl
     assert targets is None or (targets.is_cuda and targets.dtype == torch.int32 and targets.is_contiguous()
                                and targets.numel() >= rows)
     k = int(top_k)
+    _check_status(dev_status)
     if out is None:
         entropy = torch.empty(rows, dtype=torch.float32, device=logits.device)   # (new_empty takes its type at less cost)
         out = TokenLogprobs(entropy.new_empty(rows) if targets is not None else None, entropy,
@@ -767,7 +775,7 @@ def ocs_token_logprobs_backward(logits, targets, stats, g_logprob=None, g_entrop
     assert targets is None or (targets.is_cuda and targets.dtype == torch.int32 and targets.is_contiguous()
                                and targets.numel() >= rows)
     assert stats is not None
-    _check_vec(stats, 4 * rows), _check_vec(g_logprob, rows), _check_vec(g_entropy, rows)
+    _check_vec(stats, 4 * rows), _check_vec(g_logprob, rows), _check_vec(g_entropy, rows), _check_status(dev_status)
     if out is None:
         out, ld_d = logits.new_empty((rows, V)), V
     else:

@@ -37,3 +37,22 @@ def test_codes_of_the_other_sign_are_refused(is_signed, kind):
     x = _x(1, 4, 32, "f32")
     with pytest.raises(AssertionError):
         ocs.ocs_quantize_rows(x, 8, is_signed, out=(torch.zeros((4, 32), dtype=kind, device="cuda"), torch.empty(4, device="cuda")))
+
+
+def test_workspaces_and_status_words_on_the_host_are_refused():
+    x, W, s = _x(1, 600, 32, "f32"), _codes(2, 5000, 32, True), torch.ones(5000, device="cuda")
+    y, g = torch.zeros(600, dtype=torch.int32, device="cuda"), torch.ones(600, device="cuda")
+    r = ocs.ocs_token_logprobs(x, y, want_stats=True)
+    codes, a_s = ocs.ocs_quantize_rows(x)
+    big = torch.empty(1 << 20, dtype=torch.uint8, device="cuda")
+    for ws in (big.cpu(), big.view(torch.int32), big[::2]):
+        with pytest.raises(AssertionError):
+            ocs.ocs_linear_rows(x, W, s, ws=ws)
+    for st in (torch.zeros(1, dtype=torch.int32), torch.zeros(1, device="cuda"), torch.zeros(0, dtype=torch.int32, device="cuda")):
+        for call in (lambda: ocs.ocs_quantize_rows(x, dev_status=st), lambda: ocs.ocs_qlinear_rows(codes, a_s, W, s, dev_status=st),
+                     lambda: ocs.ocs_linear_rows(x, W, s, dev_status=st), lambda: ocs.ocs_token_logprobs(x, y, dev_status=st),
+                     lambda: ocs.ocs_token_logprobs_backward(x, y, r.stats, g, dev_status=st)):
+            with pytest.raises(AssertionError):
+                call()
+    with pytest.raises(AssertionError):
+        ocs.ocs_quantize_rows(x, out=(codes, None))
