@@ -330,13 +330,16 @@ def lstm_forward(cfg, layers, tokens, a_bits: int = 8, keep: bool = False, dev_s
 
 
 def lstm_score(cfg, layers, tokens, targets, a_bits: int = 8, top_k: int = 0, inv_temperature: float = 1.0,
-               want_stats: bool = False, dev_status=None) -> B.TokenLogprobs:
+               want_stats: bool = False, dev_status=None, keep: bool = False):
     """What the language model says of given tokens: tokens int32 [seq, batch] and the tokens to score after each of them,
     targets int32 [seq, batch] (negative: none) -> TokenLogprobs over the seq * batch positions (ocs_token_logprobs on
-    the decoder's logits).  The model's perplexity (Section 6) is exp(-mean of logprob)."""
+    the decoder's logits).  The model's perplexity (Section 6) is exp(-mean of logprob) over the positions with
+    a given token.  keep: also the logits fp32 [seq * batch, vocab]; with them and want_stats, ocs_token_logprobs_backward
+    gives the scores' gradient."""
     logits = lstm_forward(cfg, layers, tokens, a_bits, dev_status=dev_status)
-    return B.ocs_token_logprobs(logits, targets.reshape(-1), top_k=top_k, inv_temperature=inv_temperature,
-                                want_stats=want_stats, dev_status=dev_status)
+    r = B.ocs_token_logprobs(logits, targets.reshape(-1), top_k=top_k, inv_temperature=inv_temperature,
+                             want_stats=want_stats, dev_status=dev_status)
+    return (r, logits) if keep else r
 
 
 # ------------------------------------------------------------------------------ activation OCS
