@@ -464,7 +464,9 @@ ocs_status ocs_qlinear_rows(const void* A_codes, int a_signed, const float* a_sc
 
 /* ocs_linear_rows ---------------------------------------------------------------------------
  * ocs_quantize_rows on X followed by ocs_qlinear_rows on its codes (K = C + S), in one call, bit-identical to
- * the two.  Few tokens, in rows that are 8-byte aligned, are quantized inside the product's kernel (one launch);
+ * the two.  Few tokens, in rows that are 8-byte aligned, are quantized inside the product's kernel (one launch, which
+ * spares the host 4 us; on the device two are up to 2 us faster where the rows are more than 16 KB, so a caller that
+ * replays graphs may prefer the two calls);
  * otherwise codes and token scales live in the workspace and the product's launch overlaps the quantization.
  * Workspace: ocs_linear_rows_workspace_bytes (of the same X: only its alignment counts); 0 means none is
  * needed and ws may be NULL.  Arguments, limits and device flags of the two calls. */
@@ -490,9 +492,10 @@ ocs_status ocs_selftest_force_row_plan(int tn, int cg, int slices);
  * logits of `type` [rows][V], row stride ld >= V elements, aligned to its element; targets int32 [rows]
  * (NULL: none; a negative entry: this row has no given token and logprob 0); top_k in [0, 64], at most V;
  * logprob (with targets), entropy, top_ids int32 and top_logprob (with top_k > 0) and stats may each be
- * NULL where they are not wanted.  stats fp32 [rows][4], kept for the gradient: max logit, ln of the sum of
- * exp(z - max z), entropy, ln of the sum of exp(z).
- * A logit of -infinity is a masked token: p = 0, no part in the entropy.  A row with nothing but
+ * NULL where they are not wanted.  stats fp32 [rows][4], 16-byte aligned, kept for the gradient: max logit, ln of the
+ * sum of exp(z - max z), entropy, ln of the sum of exp(z).
+ * A logit of -infinity is a masked token: p = 0, no part in the entropy.  Any finite logit is a logit like others, also
+ * a mask value such as -1e9 or the type's lowest.  A row with nothing but
  * -infinity has logprob and top_logprob -infinity, entropy 0.  A row with NaN or +infinity sets NONFINITE;
  * its floats are NaN and its top_ids -1.  A target >= V sets BAD_INDEX (where logprob is wanted) and
  * counts as none.

@@ -428,12 +428,12 @@ __device__ __forceinline__ void store_peer_f32(uint32_t addr, float v) {
 
 // One row per cluster; the CTAs of a cluster take consecutive parts of it and send what they found to the first one.
 // A thread strides over its CTA's part in vectors of 32 bytes, one of them on its way while another is summed; five CTAs of
-// 256 threads per SM, or ten of 128 (48 registers).  Deeper prefetch with fewer CTAs is slower (three and four vectors, four CTAs: 52 us at 2048 rows of
-// 50257 bf16 logits; one vector, six CTAs: 53; this form 50 at the time).  What bounds it: fp32 rows the loads (2048 x 50257:
-// 65 us for 412 MB, 6.3 TB/s, without alternatives); 16-bit rows the instructions, six per element and one of them an
-// exponential (2048 x 50257 bf16, 206 MB: 39.3 us, 5.2 TB/s).  Five alternatives add about 3 us per wave of CTAs: 47.5 us
-// there; 20.5 instead of 17.4 us for 700 rows of 33278 fp32 logits (93 MB), which are one wave.  Few rows are latency:
-// 8 x 131072 bf16 takes 4.2 us, 8.4 with twenty alternatives.
+// 256 threads per SM, or ten of 128 (48 registers).  Deeper prefetch with fewer CTAs is slower (three and four vectors,
+// four CTAs: 52 us at 2048 rows of 50257 bf16 logits; one vector, six CTAs: 53; this form 50 at the time).  What bounds it: fp32
+// rows the loads (2500 x 33278: 53.3 us for 333 MB, 6.2 TB/s, without alternatives); 16-bit rows the instructions, six per
+// element and one of them an exponential (2048 x 50257 bf16, 206 MB: 39.5 us, 5.2 TB/s).  Five alternatives add about 3 us per
+// wave of CTAs: 47.9 us there; 20.6 instead of 17.7 us for 700 rows of 33278 fp32 logits (93 MB), which are one wave.  Few
+// rows are latency: 8 x 131072 bf16 takes 4.5 us, 8.5 with twenty alternatives.
 template <typename T, int NT, bool ENDS>
 __global__ void __launch_bounds__(NT, 5 * 256 / NT) logprobs_kernel(const T* __restrict__ logits, const LogprobParams p) {
   constexpr int VE = Vec<T>::VE, kWarps = NT / 32;
@@ -591,8 +591,8 @@ constexpr int kGradVecs = 2;   // vectors a thread of the gradient kernel handle
 
 // One part of a row per CTA: read, p = 2^((l - m) * c - log2 s), the gradient, write.  The statistics make every element
 // independent, so rows are cut into parts of two vectors per thread, all loads of a thread are issued before its first
-// arithmetic, and the grid is as large as the tensor.  Bound by HBM: 2048 x 50257 bf16, 412 MB, 64.3 us, 6.4 TB/s (98 % of the
-// measured copy rate); 700 x 33278 fp32, 186 MB, 29.8 us, 6.3 TB/s.
+// arithmetic, and the grid is as large as the tensor.  Bound by HBM: 2048 x 50257 bf16, 412 MB, 63.5 us, 6.5 TB/s (99 % of the
+// measured copy rate); 700 x 33278 fp32, 186 MB, 29.7 us, 6.3 TB/s.
 template <typename T, bool ENDS>
 __global__ void __launch_bounds__(kLpThreads) logprobs_backward_kernel(const T* logits, T* d_logits, const GradParams p) {
   constexpr int VE = Vec<T>::VE;
@@ -662,9 +662,9 @@ __global__ void __launch_bounds__(kLpThreads) logprobs_backward_kernel(const T* 
 // CTAs that share a row.  A row alone leaves most SMs idle, so few rows are shared, as long as every thread keeps two
 // vectors; but a CTA's fixed cost (about 3 us of start, join and selection, hidden only by other CTAs of its SM) grows with
 // their number: the more CTAs a row gets, the fewer there may be in all, and never more than the 740 that are resident at
-// once.  Five alternatives, us with 1 / 2 / 4 / 8 CTAs on a row, 16-bit logits unless noted: 1 row of 33278 fp32: 7.8 / 7.0 /
-// 6.4 / 6.0; 8 of 131072: 13.2 / 9.5 / 7.7 / 7.1; 64 of 131072: 13.4 / 9.8 / 9.0 / 10.3; 128 of 128000: 18.6 / 13.7 / 13.5 /
-// 18.2; 370 of 128000: 26.0 / 23.7 / 33 / 44; 450 of 128000: 31.7 / 34.6 / 37 / 51; 2048 of 50257: 47.6 / 67 / 104 / 176.
+// once.  Five alternatives, us with 1 / 2 / 4 / 8 CTAs on a row, 16-bit logits unless noted: 1 row of 33278 fp32: 8.1 / 7.1 /
+// 6.4 / 6.1; 8 of 131072: 12.8 / 9.5 / 7.6 / 7.0; 64 of 131072: 18.8 / 13.2 / 10.8 / 11.3; 128 of 128000: 19.4 / 14.7 / 14.1 /
+// 19.9; 370 of 128000: 26.7 / 24.2 / 34 / 45; 450 of 128000: 32.1 / 34.5 / 38 / 53; 2048 of 50257: 47.9 / 68 / 106 / 179.
 int row_ctas(long long rows, int V, int ve) {
   int cl = 1;
   while (cl < kMaxCluster && rows * 2 * cl <= 5 * kNumSMs && rows * 4 * cl * cl <= 2048 &&
@@ -676,10 +676,10 @@ int row_ctas(long long rows, int V, int ve) {
 // Threads of a CTA that has a row to itself.  With 128 of them ten rows are under way on an SM instead of five, which hides
 // twice as much of the fixed cost; but the alternatives' threads have twice as many vectors each, which are read again, and
 // where all rows are resident at once anyway (740 CTAs of 256) a long row takes its threads' time.  us with 128 / 256 threads
-// (64 threads were ahead only below 2000 logits): five alternatives, bf16 4096 x 1116: 17.5 / 32.4, 4096 x 8200: 28.4 / 43.0,
-// 2500 x 33278: 42.4 / 46.5, 2048 x 50257: 51.4 / 47.5, fp32 2500 x 33278: 65.5 / 66.7, 2048 x 50257: 83.1 / 76.4, 450 x 8200:
-// 7.2 / 7.9, but 450 x 16228: 9.9 / 9.5 and 450 x 33278: 20.3 / 16.2; twenty alternatives: bf16 2500 x 16228: 32.5 / 35.9,
-// 2500 x 33278: 53.3 / 52.0, fp32 2500 x 33278: 83 / 74 (none: 54.3 / 57.1).
+// (64 threads were ahead only below 2000 logits): five alternatives, bf16 4096 x 1116: 18.2 / 34.6, 4096 x 8200: 27.9 / 42.9,
+// 2500 x 33278: 42.9 / 46.3, 2048 x 50257: 51.8 / 47.9, fp32 2500 x 33278: 65.4 / 67.0, 2048 x 50257: 83.3 / 75.2, 450 x 8200
+// even (8.9 / 8.7), but 450 x 16228: 12.6 / 11.0 and 450 x 33278: 20.2 / 16.1; twenty alternatives: bf16 2500 x 16228: 32.2 /
+// 35.8, 2500 x 33278: 53.7 / 52.0, fp32 2500 x 33278: 83 / 75 (none: 53.3 / 57.3).
 int row_threads(long long rows, int V, int ve, int top_k) {
   const long long vecs = V / (128 * ve);   // a thread's, of 128
   return top_k * vecs <= 320 && (vecs <= 8 || (rows > 5 * kNumSMs && V <= 40960)) ? 128 : kLpThreads;

@@ -11,16 +11,18 @@
 // empty one of two accumulators while the other fills.  Few tiles: 2, 4 or 8 CTAs of a cluster split the contraction, send
 // each other their partial sums as 16-byte cells through distributed shared memory, and finish a share of the tokens each.
 //
-// What bounds it (device times; HBM 6.54 TB/s and 3.0 int8 POPS measured on the same card; the floor is the larger of bytes
-// and operations at these rates):
+// What bounds it (device times; the floor is the larger of the bytes at 6.54 TB/s, the measured copy rate, and the operations
+// at 3.35 int8 POPS, twice the measured bf16 rate):
 // M x K x N
-//   8192 x 8192 x 8192, bf16 out   331 us, 3.3 POPS: the tensor pipe (93 % busy at 4096 x 8192 x 8192)
-//   2047 x 4178 x 4096, bf16 out   28.7 us (floor 23.4): the tensor pipe, in two waves of which the second is not full
-//   128 x 25339 x 4096, fp32 out   27.5 us (floor 16.7): HBM latency of 128 CTAs' rings, the exchange and the epilogue
-//   700 x 663 x 33278, fp32 out    36.3 us (floor 17.7): 225 MB of operand tiles from L2 and the stores of the output (93 MB)
-//                                  share the SMs' way to L2; 23.3 us without the stores
-//   1 x 8192 x 8192, quantized here, bf16   16.3 us (floor 10.3): HBM, and 6 us of start, quantization, exchange and end
-//   1 x 16384 x 16384, likewise    46 us: HBM at 5.8 TB/s
+//   8192 x 8192 x 8192, bf16 out   331 us (floor 328): the tensor pipe (93 % busy at 4096 x 8192 x 8192)
+//   2047 x 4178 x 4096, bf16 out   28.7 us (floor 20.9): the tensor pipe, in two waves of which the second is not full
+//   128 x 25339 x 4096, fp32 out   27.5 us (floor 16.7): one wave of 128 CTAs with one tile each, whose start (4 us), exchange
+//                                  (4) and epilogue (1; the plan model's terms) have no other tile's loads beside them
+//   700 x 663 x 33278, fp32 out    36.3 us (floor 17.7): 225 MB of operand tiles from L2 (a token tile again for every channel
+//                                  tile) and the stores of the output (93 MB, straight from registers) share the SMs' way to
+//                                  L2; 23.3 us without the stores
+//   1 x 8192 x 8192, quantized here, bf16   16.5 us (floor 10.3): HBM, and 6 us of start, quantization, exchange and end
+//   1 x 16384 x 16384, bf16        46 us: HBM at 5.8 TB/s (quantized by a launch of its own: its codes do not fit beside the ring)
 #include <atomic>
 
 #include "elem.cuh"
@@ -590,10 +592,13 @@ row_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant_
 }
 
 // ------------------------------------------------------------------------------------------------ host
-// Bytes of unquantized tokens that a CTA may read itself.  Against two launches, us of a graph's time per call / of an eager
-// call's host time: (M, C, N) = (1, 4096, 4096), 8 KB: 8.7 / 15.5 against 8.9 / 22.1; (1, 8192, 8192), 16 KB: 17.1 / 12.1
-// against 17.4 / 16.1; (16, 1024, 4096), 32 KB: 6.7 / 15.4 against 6.1 / 22.5; (20, 650, 2600) in fp32, 50 KB: 8.2 / 15.7
-// against 5.8 / 22.9; but (4, 8192, 8192), 64 KB: 20.6 against 17.5 on the device, more than the launch costs the host.
+// Bytes of a token tile, unquantized, that a CTA may read itself (min(M, tokens per tile) rows).  The host decides here: at
+// these sizes an eager call is bound by it, and one launch takes 12 to 14 us of it, two take 17.  On the device the fused
+// form is even up to 16 KB and slower beyond, since every CTA reads its rows twice before its first product.  us by graph
+// replay, fused against two launches: (M, C, N) = (1, 4096, 4096), 8 KB: 8.7 against 8.6; (1, 8192, 8192), 16 KB: 16.5 against
+// 16.6; (16, 1024, 4096), 32 KB: 6.5 against 5.6; (20, 650, 2600) in fp32, 41.6 KB a tile: 8.0 against 5.9.  At (4, 8192,
+// 8192), 64 KB, the device is the slower side: 20.2 against 17.0.  A caller that replays graphs takes ocs_quantize_rows and
+// ocs_qlinear_rows instead, which give the same bits.
 constexpr long long kFuseBytes = 48 * 1024;
 
 struct RowPlan {
