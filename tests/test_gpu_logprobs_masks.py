@@ -190,3 +190,18 @@ def test_alternatives_that_few_threads_hold(kind, V):
     y = torch.zeros(5, dtype=torch.int32, device="cuda")
     for k in (5, 63, 64):
         check(x, y, k, 1.0)
+
+
+@pytest.mark.parametrize("kind,T,V", [("bf16", 370, 128000), ("f32", 128, 128000)])
+def test_masked_stretches_of_shared_rows_are_read_once(kind, T, V):
+    """Nine tenths of rows that several CTAs share are masked: whatever the mask value, right and at one price."""
+    x = _logits(T, T, V, kind).contiguous()
+    y = torch.randint(0, V // 10, (T,), generator=_gen(7), device="cuda", dtype=torch.int32)
+    took = {}
+    for value in (-1e4, -1e9, -1e30):
+        x[:, V // 10:] = value
+        if T < 200:
+            check(x, y, 0, 1.0)
+        out = ocs.ocs_token_logprobs(x, y)
+        took[value] = _device_us(lambda: ocs.ocs_token_logprobs(x, y, out=out))
+    assert max(took.values()) < 1.25 * took[-1e4], took
