@@ -151,10 +151,11 @@ __device__ __forceinline__ void shift(Stats& t, float d) {   // every term's exp
   t.w = __fmul_rn(fmaf(t.s, d, t.w), ex2(d));
   t.s = __fmul_rn(t.s, ex2(d));
 }
-// c * up = inv_temperature * log2 e; up is 1, or 2 where that product is not finite
+// c * up = inv_temperature * log2 e; up is 1, or 2 where that product may not be finite
 struct Scale {
   float c, up;
 };
+__host__ __device__ __forceinline__ float up_of(float beta) { return beta > 0x1p127f ? 2.0f : 1.0f; }
 // (l - m) * c * up, l <= m.  Halves keep the difference finite where logits near both ends of fp32 meet.
 __device__ __forceinline__ float scaled_distance(float l, float m, Scale k) {
   const bool far = fabsf(m) > 0x1p100f;
@@ -257,12 +258,13 @@ __device__ __forceinline__ void take(Running& t, const Vec<T>& v, int j, float c
   }
 }
 
+// (Every 8 bytes of a kernel's parameters cost the host about 0.3 us of a small call, so what a thread works out in an
+// instruction or two stays out of them.  The stand-in is here because in a register it costs 16-bit rows 1 to 3 %.)
 struct LogprobParams {
-  long long rows, ld;
+  long long ld;
   int V, top_k;
   const int32_t* targets;
-  float beta;
-  Scale scale;
+  float beta, c;
   Low low;
   float *logprob, *entropy, *top_logprob, *stats;
   int32_t* top_ids;
@@ -470,7 +472,8 @@ __global__ void __launch_bounds__(NT, 5 * 256 / NT) logprobs_kernel(const T* __r
     if (y >= 0) ly = to_f32(row.x[y]);
   }
 
-  const float c = p.scale.c;
+  const float c = p.c;
+  const Scale scale{c, up_of(p.beta)};
   const Low low = p.low;
   Running run{-INFINITY, 0.0f, {0.0f, 0.0f}, {0.0f, 0.0f}, lo + tid};
   {
@@ -524,12 +527,12 @@ __global__ void __launch_bounds__(NT, 5 * 256 / NT) logprobs_kernel(const T* __r
   const bool left_out = !ENDS && CL > 1 && largest <= low.v;
   if (fabsf(largest) < INFINITY && !left_out && (ENDS || !sums_hold(largest, c, low.v))) {   // the same for the whole CTA
     __syncthreads();
-    t = sums_of_differences<ENDS, NT>(row, lo, hi, largest, p.scale);
+    t = sums_of_differences<ENDS, NT>(row, lo, hi, largest, scale);
     if (lane == 0) sm.warp[warp] = t;
     __syncthreads();
   }
   if (p.top_k > 0) top_of_segment(row, lo, hi, p.top_k, run.m, run.pos, largest, sm, top);
-  t = join_eight<ENDS>(sm.warp[lane & 7], p.scale);   // this CTA's part of the row, in every thread
+  t = join_eight<ENDS>(sm.warp[lane & 7], scale);   // this CTA's part of the row, in every thread
   if (CL > 1) {
     asm volatile("barrier.cluster.wait;" ::: "memory");
     if (rank != 0) {
@@ -552,14 +555,14 @@ __global__ void __launch_bounds__(NT, 5 * 256 / NT) logprobs_kernel(const T* __r
     t = part == 0 ? own : (part < CL ? sm.part[part] : Stats{-INFINITY, 0.0f, 0.0f});
     if (!ENDS && __any_sync(0xffffffffu, t.s == 0.0f && fabsf(t.m) < INFINITY)) {   // a part without sums; the same in every warp
       const float row_max = warp_max(t.m);
-      if (__any_sync(0xffffffffu, t.s == 0.0f && fabsf(t.m) < INFINITY && exponent<ENDS>(t.m, row_max, p.scale) > -160.0f)) {
-        t = sums_of_differences<ENDS, NT>(row, 0, row.count, row_max, p.scale);   // it counts
+      if (__any_sync(0xffffffffu, t.s == 0.0f && fabsf(t.m) < INFINITY && exponent<ENDS>(t.m, row_max, scale) > -160.0f)) {
+        t = sums_of_differences<ENDS, NT>(row, 0, row.count, row_max, scale);   // it counts
         if (lane == 0) sm.warp[warp] = t;
         __syncthreads();
         t = sm.warp[part];
       }
     }
-    t = join_eight<ENDS>(t, p.scale);
+    t = join_eight<ENDS>(t, scale);
     if (p.top_k > 0) {
       for (int i = tid; i < CL * p.top_k; i += NT) {
         const key_t k = sm.top[i];
@@ -596,8 +599,7 @@ struct GradParams {
   long long ld, ld_d;
   int V, chunks;
   const int32_t* targets;
-  float beta;
-  Scale scale;
+  float beta, c;
   const float *stats, *g_logprob, *g_entropy;
   int* dev_status;
 };
@@ -649,7 +651,7 @@ __global__ void __launch_bounds__(kLpThreads) logprobs_backward_kernel(const T* 
     v[u].floats(d);
 #pragma unroll
     for (int i = 0; i < VE; ++i) {   // by log2 p; a masked token's p is zero
-      const float q = fmaxf(ENDS ? __fsub_rn(exponent<true>(d[i], st.x, p.scale), ls2) : fmaf(__fsub_rn(d[i], st.x), p.scale.c, -ls2), kFloor);
+      const float q = fmaxf(ENDS ? __fsub_rn(exponent<true>(d[i], st.x, Scale{p.c, up_of(p.beta)}), ls2) : fmaf(__fsub_rn(d[i], st.x), p.c, -ls2), kFloor);
       d[i] = __fmul_rn(ex2(q), fmaf(B, q, A));
     }
     if ((unsigned)(y - e0) < (unsigned)VE && y >= 0 && !empty) {   // the given token is in this vector
@@ -705,10 +707,7 @@ int row_threads(long long rows, int V, int ve, int top_k) {
 }
 
 bool at_ends(float beta) { return beta < 0x1p-64f || beta > 0x1p64f; }
-Scale base2(float beta) {
-  const float up = beta > 0x1p127f ? 2.0f : 1.0f;
-  return Scale{(float)((double)beta * 1.4426950408889634 / up), up};
-}
+float base2(float beta) { return (float)((double)beta * 1.4426950408889634 / up_of(beta)); }
 
 // Low for logits of type T: the power of two whose product with c lies in (-2^24, -2^23], where the type has it.  It bounds
 // what the sums tell from a masked token, not what a logit may be: in fp16, where it is the type's lowest value up to c =
@@ -730,12 +729,12 @@ Low stand_in(float c) {
 }
 
 template <typename T>
-ocs_status launch_logprobs(const void* logits_, LogprobParams p, cudaStream_t stream) {
+ocs_status launch_logprobs(const void* logits_, long long rows, LogprobParams p, cudaStream_t stream) {
   const T* logits = static_cast<const T*>(logits_);
   const bool ends = at_ends(p.beta);
-  p.low = stand_in<T>(p.scale.c);
-  const int cl = row_ctas(p.rows, p.V, Vec<T>::VE), nt = cl > 1 || ends ? kLpThreads : row_threads(p.rows, p.V, Vec<T>::VE, p.top_k);
-  const long long rows = p.rows, step = 1ll << 27;   // rows of one launch (the grid's limit)
+  p.low = stand_in<T>(p.c);
+  const int cl = row_ctas(rows, p.V, Vec<T>::VE), nt = cl > 1 || ends ? kLpThreads : row_threads(rows, p.V, Vec<T>::VE, p.top_k);
+  const long long step = 1ll << 27;   // rows of one launch (the grid's limit)
   for (long long r0 = 0; r0 < rows; r0 += step) {
     const long long n = rows - r0 < step ? rows - r0 : step;
     cudaLaunchConfig_t cfg = {};
@@ -803,11 +802,11 @@ extern "C" ocs_status ocs_token_logprobs(const void* logits, ocs_dtype type, int
   const ocs_status st = check_device();
   if (st != OCS_OK) return st;
   if (!top_ids && !top_logprob) top_k = 0;
-  LogprobParams p{rows, ld, V, top_k, targets, inv_temperature, base2(inv_temperature), Low{}, logprob, entropy, top_logprob, stats, top_ids, dev_status};
+  LogprobParams p{ld, V, top_k, targets, inv_temperature, base2(inv_temperature), Low{}, logprob, entropy, top_logprob, stats, top_ids, dev_status};
   switch (type) {
-    case OCS_F16: return launch_logprobs<__half>(logits, p, stream);
-    case OCS_BF16: return launch_logprobs<__nv_bfloat16>(logits, p, stream);
-    default: return launch_logprobs<float>(logits, p, stream);
+    case OCS_F16: return launch_logprobs<__half>(logits, rows, p, stream);
+    case OCS_BF16: return launch_logprobs<__nv_bfloat16>(logits, rows, p, stream);
+    default: return launch_logprobs<float>(logits, rows, p, stream);
   }
 }
 
