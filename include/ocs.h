@@ -483,6 +483,108 @@ ocs_status ocs_linear_rows(const void* X, ocs_dtype x_type, int M, int C, int64_
  * it.  This process-wide hook fixes the choice for the following calls; tn = 0 returns it to the planner.  Host call. */
 ocs_status ocs_selftest_force_row_plan(int tn, int cg, int slices);
 
+/* Block-scaled 4-bit grids ------------------------------------------------------------------
+ * Where one step per row (ocs_quantize_rows) is too coarse: a code is one of the sixteen e2m1 numbers 0, .5, 1, 1.5, 2, 3,
+ * 4, 6 and their negatives, and every block of consecutive channels has a scale of eight bits.
+ *   OCS_GRID_E8M0: blocks of 32, scale s = 2^(floor(log2 max|x|) - 2), stored as its exponent + 127 (at least 0)
+ *   OCS_GRID_E4M3: blocks of 16, scale s = e4m3(max|x| / r / 6), stored as that number's byte, times the row's scale
+ *       r = 2^k (fp32), k the smallest in [-117, 117] with max|x| of the row <= 6 * 448 * r
+ *   code = e2m1(x / (s r)), r = 1 for E8M0; the division of each block's max|x| / r by 6 and, for fp32 x, the quotients are
+ *   rounded to fp32 once, all else in between is exact; e2m1() and e4m3() round to the nearest, ties to even, and saturate.
+ * (OCS_GRID_I8 is ocs_quantize_rows' signed 8-bit grid: int8 codes and one fp32 step; for the cache below.) */
+typedef enum {
+  OCS_GRID_I8 = 0,
+  OCS_GRID_E8M0 = 1,
+  OCS_GRID_E4M3 = 2
+} ocs_grid;
+
+/* ocs_quantize_mx4 --------------------------------------------------------------------------
+ * Rows of X (tokens, or the output channels of split weights [O][C+S]) to a block-scaled grid, the S duplicated channels
+ * of a split layer appended as in ocs_quantize_rows: channel C+s is channel idx_map[C+s].  Blocks run over all K = C + S
+ * channels; a last one that is not full is filled with zeros.
+ * X of x_type [rows][C], row stride ldx >= C elements, aligned to its element; idx_map int32 [C+S] (NULL when S = 0).
+ * codes [rows][(K+1)/2] bytes, channel 2i in the low half of byte i, row stride ld_codes bytes (bytes between rows are
+ * untouched, the last high half of an odd K is zero).
+ * scales: ocs_mx4_scale_bytes(rows, K, grid) bytes, 16-byte aligned, in tiles of 128 rows and four blocks:
+ *   scale of block b of row m: byte ((m/128 * P + b/4) * 32 + m%32) * 16 + m/32%4 * 4 + b%4,  P = ceil(blocks of a row / 4),
+ *   zeros for the blocks between a row's last and the next multiple of four; the bytes of rows that do not exist are left as
+ *   they are and mean nothing.
+ * row_scales fp32 [rows] (E4M3; ignored for E8M0).
+ * rows = 0 is a no-op.  Limits: C + S < 2^30.  Device flags: NONFINITE (that row's outputs are unspecified), BAD_INDEX. */
+int64_t ocs_mx4_scale_bytes(int64_t rows, int K, ocs_grid grid);
+ocs_status ocs_quantize_mx4(const void* X, ocs_dtype x_type, int64_t rows, int C, int64_t ldx, int S,
+                            const int32_t* idx_map, ocs_grid grid, uint8_t* codes, int64_t ld_codes, uint8_t* scales,
+                            float* row_scales, int* dev_status, void* stream);
+
+/* ocs_dequantize_mx4: Y[m][k] = code * s * r, the values that the codes stand for (exact in fp32, rounded to y_type once);
+ * Y [rows][K], row stride ldy elements.  With ocs_quantize_mx4 it simulates the grid on floating-point layers. */
+ocs_status ocs_dequantize_mx4(const uint8_t* codes, int64_t ld_codes, const uint8_t* scales, const float* row_scales,
+                              int64_t rows, int K, ocs_grid grid, void* Y, ocs_dtype y_type, int64_t ldy, void* stream);
+
+/* ocs_qlinear_mx4 ---------------------------------------------------------------------------
+ * The layer on codes and scales as ocs_quantize_mx4 writes them, both operands on the same grid:
+ *     Y[m][n] = a_row[m] * w_row[n] * sum_k (A[m][k] sa[m][k]) (W[n][k] sw[n][k]) + bias[n]     (bias 0 if NULL)
+ * The sums are fp32 (their order, and so their last bits, depend on M, N and K, not on the run); products are exact.
+ * Row scales and bias come last, rounded once, and once more to y_type.
+ * A codes [M], W codes [N] rows of (K+1)/2 bytes, 16-byte aligned, strides lda and ldw multiples of 16; Y [M][N] of y_type,
+ * row stride ldy elements; row scales are ignored for E8M0.
+ * M = 0 is a no-op.  Limits: M, K < 2^30, N < 2^31 - 511.  Device flag: TIMEOUT. */
+ocs_status ocs_qlinear_mx4(const uint8_t* A_codes, const uint8_t* A_scales, const float* a_row_scales, int M, int K,
+                           int64_t lda, const uint8_t* W_codes, const uint8_t* W_scales, const float* w_row_scales, int N,
+                           int64_t ldw, ocs_grid grid, const float* bias, void* Y, ocs_dtype y_type, int64_t ldy,
+                           int* dev_status, void* stream);
+
+/* ocs_linear_mx4: ocs_quantize_mx4 on X, then ocs_qlinear_mx4 on its codes (K = C + S), in one call, bit-identical to the
+ * two; the product's launch overlaps the quantization.  Workspace: ocs_linear_mx4_workspace_bytes, 256-byte aligned.
+ * Arguments, limits and device flags of the two calls. */
+size_t ocs_linear_mx4_workspace_bytes(int M, int C, int S, ocs_grid grid);
+ocs_status ocs_linear_mx4(const void* X, ocs_dtype x_type, int M, int C, int64_t ldx, int S, const int32_t* idx_map,
+                          ocs_grid grid, const uint8_t* W_codes, const uint8_t* W_scales, const float* w_row_scales, int N,
+                          int64_t ldw, const float* bias, void* Y, ocs_dtype y_type, int64_t ldy, void* ws, size_t ws_bytes,
+                          int* dev_status, void* stream);
+
+/* ocs_selftest_force_mx4_plan (for tests): ocs_qlinear_mx4 / ocs_linear_mx4 choose how many tokens a tile has (tn in {16,
+ * 32, 64, 128, 256}; 16 and 32 are raised to the next where M is larger), whether two CTAs share a tile (cg = 2 with 256 tokens, else 1) and how many
+ * split its contraction (slices in {1, 2, 4, 8}, lowered until it fits the problem).  Process-wide; tn = 0 returns the
+ * choice to the planner.  Host call. */
+ocs_status ocs_selftest_force_mx4_plan(int tn, int cg, int slices);
+
+/* A key/value cache that is quantized as it is written ----------------------------------------
+ * Vectors of `dim` numbers (one per token and head) on one of the three grids, each vector a row of its own, in pages of
+ * page_size tokens.  A page is ocs_cache_page_bytes bytes, 16-byte aligned, and holds, with n = page_size * heads and vector
+ * v = (token in the page) * heads + head:
+ *   codes: vector v at byte v * cb, cb = round_up(I8: dim, else (dim+1)/2, 16)
+ *   block scales at round_up(n * cb, 16): vector v at v * sb, block b at + b, sb = round_up(blocks, 4) (I8: none, sb = 0)
+ *   row scales (I8, E4M3) fp32 [n] at the next multiple of 16
+ * Slot s of the cache is token s % page_size of page s / page_size.  dim <= 1024. */
+typedef struct {
+  int n_pages, page_size, heads, dim;
+  ocs_grid grid;
+} ocs_cache;
+int64_t ocs_cache_page_bytes(const ocs_cache* cache);
+
+/* ocs_cache_write: token t's heads x dim vectors of X go to slot slots[t] (int64 [tokens]); a negative slot leaves the token
+ * out.  What else the cache holds is untouched.  Slots of one call are distinct: what a slot that two tokens name holds
+ * afterwards is unspecified.  X of x_type, token t's head h at X + t * ld_token + h * ld_head elements (any strides), aligned
+ * to its element.  pages2 / X2: a second cache of the same shape (values beside keys), written by the same launch; NULL: none.
+ * tokens = 0 is a no-op.  Device flags: BAD_INDEX (a slot beyond the cache: its token is left out), NONFINITE (that vector's
+ * content is unspecified). */
+ocs_status ocs_cache_write(const ocs_cache* cache, void* pages, const void* X, int64_t ld_token, int64_t ld_head, void* pages2,
+                           const void* X2, int64_t ld_token2, int64_t ld_head2, ocs_dtype x_type, int64_t tokens,
+                           const int64_t* slots, int* dev_status, void* stream);
+
+/* ocs_cache_read: the values of B sequences, one after the other: row t of Y, starts[b] <= t < starts[b+1], is token
+ * t - starts[b] of sequence b, which is in page table[b][(t - starts[b]) / page_size].  table int32 [B][table_cols], row
+ * stride ld_table; starts int32 [B+1], ascending; Y [rows][heads][dim] of y_type with the given strides in elements.  Rows
+ * before starts[0] and from starts[B] on are left as they are.  pages2 / Y2: the second cache, by the same launch; NULL: none.
+ * Values are code * s * r (I8: code * step), rounded once (E4M3, E8M0: exact before the rounding to y_type).
+ * rows = 0 and B = 0 are no-ops.  Device flag: BAD_INDEX (a page outside of the cache or a row behind the table's last column:
+ * zeros). */
+ocs_status ocs_cache_read(const ocs_cache* cache, const void* pages, const void* pages2, const int32_t* table,
+                          int64_t ld_table, int table_cols, const int32_t* starts, int B, int64_t rows, void* Y,
+                          int64_t ld_token, int64_t ld_head, void* Y2, int64_t ld_token2, int64_t ld_head2, ocs_dtype y_type,
+                          int* dev_status, void* stream);
+
 /* ocs_token_logprobs ------------------------------------------------------------------------
  * What a language model's logits say about given tokens (Section 6 reports perplexity, the exponential of
  * the mean of -logprob).  With z = inv_temperature * logits[t][:], p = softmax(z):

@@ -22,6 +22,7 @@ STATUS_NAMES = {0: "OCS_OK", 1: "OCS_ERR_INVALID_ARG", 2: "OCS_ERR_SHAPE", 3: "O
                 4: "OCS_ERR_UNSUPPORTED", 5: "OCS_ERR_CUDA"}
 DEV_NONFINITE, DEV_BAD_INDEX, DEV_TIMEOUT, DEV_DEPTH, DEV_OVERFLOW = 1, 2, 4, 8, 16
 CLIP_NONE, CLIP_MSE, CLIP_MSE_EXACT, CLIP_KL, CLIP_ACIQ = 0, 1, 2, 3, 4
+GRID_I8, MX4_E8M0, MX4_E4M3 = 0, 1, 2   # ocs_grid
 
 EXPORTS = [
     "ocs_num_splits", "ocs_poll_status", "ocs_version",
@@ -36,6 +37,8 @@ EXPORTS = [
     "ocs_qlinear_workspace_bytes", "ocs_qlinear", "ocs_transpose_codes", "ocs_selftest_force_gemm_plan",
     "ocs_conv_packed_k", "ocs_pack_conv_weights", "ocs_pack_conv_weights_batch", "ocs_qconv_workspace_bytes", "ocs_qconv",
     "ocs_quantize_rows", "ocs_qlinear_rows", "ocs_linear_rows_workspace_bytes", "ocs_linear_rows", "ocs_selftest_force_row_plan",
+    "ocs_mx4_scale_bytes", "ocs_quantize_mx4", "ocs_dequantize_mx4", "ocs_qlinear_mx4", "ocs_linear_mx4_workspace_bytes", "ocs_linear_mx4",
+    "ocs_selftest_force_mx4_plan", "ocs_cache_page_bytes", "ocs_cache_write", "ocs_cache_read",
     "ocs_token_logprobs", "ocs_token_logprobs_backward",
     "ocs_add_relu", "ocs_maxpool3x3s2", "ocs_global_avgpool", "ocs_nchw_to_nhwc", "ocs_embedding", "ocs_lstm_cell",
 ]
@@ -50,6 +53,15 @@ _ARGTYPES = {
     "ocs_qlinear_rows": [_P, _I, _P, _I, _I, _L, _P, _P, _I, _L, _P, _P, _I, _L, _P, _P],
     "ocs_linear_rows_workspace_bytes": [_P, _I, _I, _I, _L, _I, _I, _I],
     "ocs_linear_rows": [_P, _I, _I, _I, _L, _I, _P, _I, _I, _P, _P, _I, _L, _P, _P, _I, _L, _P, C.c_size_t, _P, _P],
+    "ocs_mx4_scale_bytes": [_L, _I, _I],
+    "ocs_quantize_mx4": [_P, _I, _L, _I, _L, _I, _P, _I, _P, _L, _P, _P, _P, _P],
+    "ocs_dequantize_mx4": [_P, _L, _P, _P, _L, _I, _I, _P, _I, _L, _P],
+    "ocs_qlinear_mx4": [_P, _P, _P, _I, _I, _L, _P, _P, _P, _I, _L, _I, _P, _P, _I, _L, _P, _P],
+    "ocs_linear_mx4_workspace_bytes": [_I, _I, _I, _I],
+    "ocs_linear_mx4": [_P, _I, _I, _I, _L, _I, _P, _I, _P, _P, _P, _I, _L, _P, _P, _I, _L, _P, C.c_size_t, _P, _P],
+    "ocs_cache_page_bytes": [_P],
+    "ocs_cache_write": [_P, _P, _P, _L, _L, _P, _P, _L, _L, _I, _L, _P, _P, _P],
+    "ocs_cache_read": [_P, _P, _P, _P, _L, _I, _P, _I, _L, _P, _L, _L, _P, _L, _L, _I, _P, _P],
     "ocs_token_logprobs": [_P, _I, _L, _I, _L, _P, _F, _I, _P, _P, _P, _P, _P, _P, _P],
     "ocs_token_logprobs_backward": [_P, _I, _L, _I, _L, _P, _F, _P, _P, _P, _P, _L, _P, _P],
 }
@@ -81,6 +93,8 @@ def lib():
         for name, types in _ARGTYPES.items():
             getattr(L, name).argtypes = types
         L.ocs_linear_rows_workspace_bytes.restype = C.c_size_t
+        L.ocs_linear_mx4_workspace_bytes.restype = C.c_size_t
+        L.ocs_mx4_scale_bytes.restype = L.ocs_cache_page_bytes.restype = C.c_int64
         _lib = L
     return _lib
 
@@ -725,6 +739,214 @@ def ocs_selftest_force_row_plan(tn: int = 0, cg: int = 1, slices: int = 1):
     """Fixes tokens per tile / CTAs per tile / K split of the following ocs_qlinear_rows / ocs_linear_rows calls (tn = 0:
     planner)."""
     _check(lib().ocs_selftest_force_row_plan(int(tn), int(cg), int(slices)), "ocs_selftest_force_row_plan")
+
+
+# ------------------------------------------------------------------------- block-scaled 4-bit grids
+class Mx4(NamedTuple):
+    """Rows on a block-scaled 4-bit grid (ocs_quantize_mx4)."""
+    codes: torch.Tensor                # uint8 [rows, (K + 1) // 2], two channels per byte
+    scales: torch.Tensor               # uint8 [ceil(rows / 128), ceil(blocks / 4), 32, 4, 4]: row 128 t + 32 j + i, block 4 p + q at [t, p, i, j, q]
+    row_scales: torch.Tensor | None    # fp32 [rows] (MX4_E4M3)
+    K: int
+    grid: int                          # MX4_E8M0 or MX4_E4M3
+
+
+def _mx4_pieces(K: int, grid: int) -> int:
+    return (K + 127) >> 7 if grid == MX4_E8M0 else (K + 63) >> 6
+
+
+def _check_mx4(q: Mx4):
+    """Checks that q's tensors hold what its K and grid say -> (rows, row stride in bytes)."""
+    codes, scales, rs, K, grid = q
+    assert grid in (MX4_E8M0, MX4_E4M3) and K > 0
+    assert codes.is_cuda and codes.dtype == torch.uint8 and scales.is_cuda and scales.dtype == torch.uint8
+    rows = codes.shape[0]
+    assert codes.shape[1] >= (K + 1) >> 1
+    assert scales.is_contiguous() and scales.numel() >= (rows + 127 >> 7) * _mx4_pieces(K, grid) * 512
+    if grid == MX4_E4M3:
+        assert rs is not None
+        _check_vec(rs, rows)
+    return rows, _rows_of(codes)
+
+
+def ocs_quantize_mx4(x, grid: int = MX4_E4M3, idx_map=None, S: int = 0, out: Mx4 | None = None, dev_status=None) -> Mx4:
+    """x fp32 / fp16 / bf16 [rows, C] (row stride = x.stride(0)) -> Mx4 with K = C + S: e2m1 codes with a scale per 32
+    (MX4_E8M0) or 16 (MX4_E4M3) channels, the S duplicated channels of idx_map appended.  `out`: an Mx4 of that K and
+    grid to write to."""
+    assert x.is_cuda and x.dtype in DTYPES and grid in (MX4_E8M0, MX4_E4M3)
+    ldx = _rows_of(x)
+    rows, Cn = x.shape
+    S = int(S)
+    _check_idx(idx_map, Cn, S), _check_status(dev_status)
+    K = Cn + S
+    if out is None:
+        nb = (K + 1) >> 1
+        codes = torch.empty_strided((rows, nb), ((nb + 15) & ~15, 1), dtype=torch.uint8, device=x.device)
+        out = Mx4(codes, codes.new_empty((rows + 127 >> 7, _mx4_pieces(K, grid), 32, 4, 4)),
+                  torch.empty(rows, dtype=torch.float32, device=x.device) if grid == MX4_E4M3 else None, K, grid)
+        ld = (nb + 15) & ~15
+    else:
+        assert out.K == K and out.grid == grid and out.codes.shape[0] == rows
+        ld = _check_mx4(out)[1]
+    st = lib().ocs_quantize_mx4(x.data_ptr(), DTYPES[x.dtype], rows, Cn, ldx, S, _addr(idx_map), grid, out.codes.data_ptr(), ld,
+                                out.scales.data_ptr(), _addr(out.row_scales), _addr(dev_status), _raw_stream(x))
+    _check(st, "ocs_quantize_mx4")
+    return out
+
+
+def ocs_dequantize_mx4(q: Mx4, out_dtype=torch.float32, out=None):
+    """The values that q's codes stand for, [rows, K] of out_dtype (fp32: exact)."""
+    rows, ld = _check_mx4(q)
+    if out is None:
+        out, ldy = torch.empty((rows, q.K), dtype=out_dtype, device=q.codes.device), q.K
+    else:
+        assert out.is_cuda and out.shape == (rows, q.K)
+        ldy = _rows_of(out)
+    st = lib().ocs_dequantize_mx4(q.codes.data_ptr(), ld, q.scales.data_ptr(), _addr(q.row_scales), rows, q.K, q.grid,
+                                  out.data_ptr(), DTYPES[out.dtype], ldy, _raw_stream(q.codes))
+    _check(st, "ocs_dequantize_mx4")
+    return out
+
+
+def ocs_qlinear_mx4(a: Mx4, w: Mx4, bias=None, out_dtype=torch.float32, out=None, dev_status=None):
+    """Tokens a [M, K] and weights w [N, K] on the same grid -> Y [M, N] of out_dtype (fp32, fp16, bf16), fp32 sums."""
+    M, lda = _check_mx4(a)
+    N, ldw = _check_mx4(w)
+    assert a.K == w.K and a.grid == w.grid
+    _check_vec(bias, N), _check_status(dev_status)
+    if out is None:
+        out, ldy = torch.empty((M, N), dtype=out_dtype, device=a.codes.device), N
+    else:
+        assert out.is_cuda and out.shape == (M, N)
+        ldy = _rows_of(out)
+    assert out.dtype in DTYPES
+    st = lib().ocs_qlinear_mx4(a.codes.data_ptr(), a.scales.data_ptr(), _addr(a.row_scales), M, a.K, lda, w.codes.data_ptr(),
+                               w.scales.data_ptr(), _addr(w.row_scales), N, ldw, a.grid, _addr(bias), out.data_ptr(),
+                               DTYPES[out.dtype], ldy, _addr(dev_status), _raw_stream(a.codes))
+    _check(st, "ocs_qlinear_mx4")
+    return out
+
+
+def ocs_linear_mx4(x, w: Mx4, idx_map=None, S: int = 0, bias=None, out_dtype=None, out=None, ws=None, dev_status=None):
+    """x fp32 / fp16 / bf16 [M, C], weights w [N, K = C + S] -> Y [M, N] (of x's type, or out_dtype): ocs_quantize_mx4 on
+    w's grid and ocs_qlinear_mx4 in one call."""
+    assert x.is_cuda and x.dtype in DTYPES
+    ldx = _rows_of(x)
+    M, Cn = x.shape
+    S = int(S)
+    N, ldw = _check_mx4(w)
+    assert w.K == Cn + S
+    _check_idx(idx_map, Cn, S), _check_vec(bias, N), _check_status(dev_status)
+    assert ws is None or (ws.is_cuda and ws.dtype == torch.uint8 and ws.is_contiguous())
+    if out is None:
+        out = x.new_empty((M, N)) if out_dtype is None else torch.empty((M, N), dtype=out_dtype, device=x.device)
+        ldy = N
+    else:
+        assert out.is_cuda and out.shape == (M, N)
+        ldy = _rows_of(out)
+    assert out.dtype in DTYPES
+    L = lib()
+    if ws is None:
+        ws = torch.empty(L.ocs_linear_mx4_workspace_bytes(M, Cn, S, w.grid), dtype=torch.uint8, device=x.device)
+    st = L.ocs_linear_mx4(x.data_ptr(), DTYPES[x.dtype], M, Cn, ldx, S, _addr(idx_map), w.grid, w.codes.data_ptr(),
+                          w.scales.data_ptr(), _addr(w.row_scales), N, ldw, _addr(bias), out.data_ptr(), DTYPES[out.dtype],
+                          ldy, ws.data_ptr(), ws.numel(), _addr(dev_status), _raw_stream(x))
+    _check(st, "ocs_linear_mx4")
+    return out
+
+
+def ocs_selftest_force_mx4_plan(tn: int = 0, cg: int = 1, slices: int = 1):
+    """Fixes tokens per tile / CTAs per tile / K split of the following ocs_qlinear_mx4 / ocs_linear_mx4 calls (tn = 0:
+    planner)."""
+    _check(lib().ocs_selftest_force_mx4_plan(int(tn), int(cg), int(slices)), "ocs_selftest_force_mx4_plan")
+
+
+# ------------------------------------------------------------------------- quantized key/value cache
+class _CacheDesc(C.Structure):
+    _fields_ = [("n_pages", C.c_int), ("page_size", C.c_int), ("heads", C.c_int), ("dim", C.c_int), ("grid", C.c_int)]
+
+
+class QuantCache(NamedTuple):
+    """A paged cache of keys or values; slot s is token s % page_size of page s // page_size."""
+    pages: torch.Tensor                # uint8 [n_pages, page bytes]
+    page_size: int                     # tokens
+    heads: int
+    dim: int
+    grid: int                          # GRID_I8, MX4_E8M0 or MX4_E4M3
+
+
+def ocs_cache_new(n_pages: int, page_size: int, heads: int, dim: int, grid: int = GRID_I8, device="cuda") -> QuantCache:
+    """An empty cache (all zeros)."""
+    n = lib().ocs_cache_page_bytes(C.byref(_CacheDesc(0, page_size, heads, dim, grid)))
+    if n <= 0:
+        raise OcsError("ocs_cache_new", 2)
+    return QuantCache(torch.zeros((n_pages, n), dtype=torch.uint8, device=device), page_size, heads, dim, grid)
+
+
+def _check_caches(cache: QuantCache, cache2):
+    pages, page_size, heads, dim, grid = cache
+    d = _CacheDesc(pages.shape[0], page_size, heads, dim, grid)
+    assert pages.is_cuda and pages.dtype == torch.uint8 and pages.is_contiguous()
+    assert lib().ocs_cache_page_bytes(C.byref(d)) == pages.shape[1]
+    if cache2 is not None:
+        p2 = cache2.pages
+        assert cache2[1:] == cache[1:] and p2.shape == pages.shape and p2.is_cuda and p2.dtype == torch.uint8 and p2.is_contiguous()
+    return d
+
+
+def _check_vectors(x, rows, cache: QuantCache):
+    """x [rows, heads, dim], vectors dense -> (address, strides of tokens and heads)."""
+    assert x.is_cuda and x.dtype in DTYPES and x.shape == (rows, cache.heads, cache.dim)
+    st = x.stride()
+    assert st[2] == 1 or cache.dim == 1
+    return x.data_ptr(), st[0], st[1]
+
+
+def ocs_cache_write(cache: QuantCache, x, slots, cache2: QuantCache | None = None, x2=None, dev_status=None) -> None:
+    """Quantizes x fp32 / fp16 / bf16 [tokens, heads, dim] into the cache's slots (int64 [tokens], distinct; negative: the
+    token is left out).  cache2, x2: a second cache of the same shape (values beside keys), by the same launch."""
+    d = _check_caches(cache, cache2)
+    n = x.shape[0]
+    assert slots.is_cuda and slots.dtype == torch.int64 and slots.is_contiguous() and slots.numel() >= n
+    assert (cache2 is None) == (x2 is None)
+    _check_status(dev_status)
+    v = _check_vectors(x, n, cache)
+    p2, v2 = None, (None, 0, 0)
+    if x2 is not None:
+        assert x2.dtype == x.dtype
+        p2, v2 = cache2.pages.data_ptr(), _check_vectors(x2, n, cache)
+    st = lib().ocs_cache_write(C.byref(d), cache.pages.data_ptr(), *v, p2, *v2, DTYPES[x.dtype], n, slots.data_ptr(),
+                               _addr(dev_status), _raw_stream(x))
+    _check(st, "ocs_cache_write")
+
+
+def ocs_cache_read(cache: QuantCache, table, starts, rows: int, out_dtype=torch.bfloat16, cache2: QuantCache | None = None,
+                   out=None, out2=None, dev_status=None):
+    """The values of sequences in the cache: table int32 [B, columns] (pages of each sequence, in order), starts int32 [B+1]
+    (on the device; rows starts[b] .. starts[b+1] - 1 are sequence b's tokens from its first on) -> [rows, heads, dim] of
+    out_dtype, with cache2 a pair of them.  Rows from starts[B] on are not written."""
+    d = _check_caches(cache, cache2)
+    assert table.is_cuda and table.dtype == torch.int32 and starts.is_cuda and starts.dtype == torch.int32
+    ld_table = _rows_of(table)
+    B, cols = table.shape
+    assert starts.is_contiguous() and starts.numel() >= B + 1
+    _check_status(dev_status)
+    rows = int(rows)
+    if out is None:
+        out = torch.empty((rows, cache.heads, cache.dim), dtype=out_dtype, device=table.device)
+    v = _check_vectors(out, rows, cache)
+    p2, v2 = None, (None, 0, 0)
+    if cache2 is not None:
+        if out2 is None:
+            out2 = torch.empty_like(out)
+        assert out2.dtype == out.dtype
+        p2, v2 = cache2.pages.data_ptr(), _check_vectors(out2, rows, cache)
+    else:
+        assert out2 is None
+    st = lib().ocs_cache_read(C.byref(d), cache.pages.data_ptr(), p2, table.data_ptr(), ld_table, cols, starts.data_ptr(), B, rows,
+                              *v, *v2, DTYPES[out.dtype], _addr(dev_status), _raw_stream(table))
+    _check(st, "ocs_cache_read")
+    return out if cache2 is None else (out, out2)
 
 
 class TokenLogprobs(NamedTuple):

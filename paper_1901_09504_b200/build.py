@@ -9,11 +9,12 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 _ROOT = os.path.dirname(_HERE)
 CSRC = os.path.join(_HERE, "csrc")
 LIB = os.path.join(_HERE, "libocs_b200.so")
-SOURCES = ["split.cu", "actsel.cu", "quantize.cu", "gemm.cu", "glue.cu", "knapsack.cu", "rows.cu", "rowgemm.cu", "logprobs.cu", "api.cu"]
+SOURCES = ["split.cu", "actsel.cu", "quantize.cu", "gemm.cu", "glue.cu", "knapsack.cu", "rows.cu", "rowgemm.cu", "logprobs.cu", "mx4.cu", "mxgemm.cu", "cache.cu", "api.cu"]
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
     "-fmad=false",                      # every fp operation rounds once, as written
+    "--threads", "0",                   # the sources side by side
     "-Xcompiler", "-fPIC", "-shared", "-cudart", "static",
     "-I", os.path.join(_ROOT, "include"), "-I", CSRC,
 ]
@@ -27,7 +28,7 @@ def needs_build() -> bool:
     if not os.path.exists(LIB):
         return True
     t = os.path.getmtime(LIB)
-    deps = _sources() + [os.path.join(CSRC, "common.cuh"), os.path.join(CSRC, "elem.cuh"), os.path.join(CSRC, "ptx.cuh"), os.path.join(_ROOT, "include", "ocs.h"),
+    deps = _sources() + [os.path.join(CSRC, "common.cuh"), os.path.join(CSRC, "elem.cuh"), os.path.join(CSRC, "ptx.cuh"), os.path.join(CSRC, "mx4.cuh"), os.path.join(_ROOT, "include", "ocs.h"),
                          os.path.abspath(__file__)]
     return any(os.path.getmtime(d) > t for d in deps if os.path.exists(d))
 

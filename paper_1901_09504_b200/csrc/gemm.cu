@@ -962,6 +962,16 @@ bool encode_u8(CUtensorMap* map, const void* base, int rank, const cuuint64_t* d
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+bool encode_mx4_scales(CUtensorMap* map, const void* base, int pieces, int tiles, int box_pieces) {
+  EncodeTiledFn fn = encode_fn();
+  if (!fn) return false;
+  const cuuint64_t dims[3] = {128, (cuuint64_t)pieces, (cuuint64_t)tiles}, strides[2] = {512, (cuuint64_t)pieces * 512};
+  const cuuint32_t box[3] = {128, (cuuint32_t)box_pieces, 1}, estr[3] = {1, 1, 1};
+  return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT32, 3, const_cast<void*>(base), dims, strides, box, estr,
+            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 namespace {
 
 struct GemmPlan {

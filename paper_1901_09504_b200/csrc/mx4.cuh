@@ -1,0 +1,195 @@
+// The block-scaled grids: e2m1 codes (0, .5, 1, 1.5, 2, 3, 4, 6 and their negatives) in halves of bytes, and their scales.
+//   OCS_GRID_E8M0: blocks of 32, scale 2^(floor(log2 max|x|) - 2)                        (one byte: the exponent + 127)
+//   OCS_GRID_E4M3: blocks of 16, scale e4m3(max|x| / r / 6) * r, r a power of two per row  (one byte, and r as fp32)
+// A code is the grid point nearest to x / scale, ties to even, saturating at 6.
+#pragma once
+
+#include <type_traits>
+
+#include "elem.cuh"
+
+namespace ocs {
+
+constexpr int kMxTile = 512;   // scale bytes of 128 rows x 4 blocks, the tensor cores' unit
+
+inline bool mx4_grid(ocs_grid g) { return g == OCS_GRID_E8M0 || g == OCS_GRID_E4M3; }
+__host__ __device__ constexpr int mx4_block(int grid) { return grid == OCS_GRID_E8M0 ? 32 : 16; }
+
+// Byte of block b of row r among the scales of a matrix with `chunks` groups of four blocks: tiles of 128 rows, in them one
+// 512-byte piece per group, in that [row % 32][row / 32 % 4][block % 4] -- what tcgen05.cp moves to tensor memory as it is.
+__host__ __device__ __forceinline__ long long mx4_scale_at(long long r, int b, int chunks) {
+  return ((r >> 7) * chunks + (b >> 2)) * kMxTile + (r & 31) * 16 + ((r >> 5) & 3) * 4 + (b & 3);
+}
+
+// Eight values as codes, the first in the lowest four bits.
+__device__ __forceinline__ uint32_t e2m1_codes(const float* t) {
+  uint32_t r;
+  asm("{\n\t.reg .b8 a, b, c, d;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 c, %6, %5;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n\t"
+      "mov.b32 %0, {a, b, c, d};\n\t}"
+      : "=r"(r) : "f"(t[0]), "f"(t[1]), "f"(t[2]), "f"(t[3]), "f"(t[4]), "f"(t[5]), "f"(t[6]), "f"(t[7]));
+  return r;
+}
+// Four bytes of codes as eight values, in four pairs of halves (exact).
+__device__ __forceinline__ void e2m1_values(uint32_t codes, __half2* v) {
+  uint32_t r[4];
+  asm("{\n\t.reg .b8 a, b, c, d;\n\t"
+      "mov.b32 {a, b, c, d}, %4;\n\t"
+      "cvt.rn.f16x2.e2m1x2 %0, a;\n\t"
+      "cvt.rn.f16x2.e2m1x2 %1, b;\n\t"
+      "cvt.rn.f16x2.e2m1x2 %2, c;\n\t"
+      "cvt.rn.f16x2.e2m1x2 %3, d;\n\t}"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(codes));
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = *reinterpret_cast<__half2*>(&r[i]);
+}
+__device__ __forceinline__ uint32_t e4m3_byte(float v) {
+  uint16_t r;
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(0.0f), "f"(v));
+  return r;
+}
+__device__ __forceinline__ float e4m3_value(uint32_t byte) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"((uint16_t)byte));
+  return __half2float(__ushort_as_half((unsigned short)r));
+}
+// 2^(byte - 127), and its reciprocal for bytes below 255
+__device__ __forceinline__ float e8m0_value(uint32_t byte) {
+  return __uint_as_float(byte == 255 ? 0x7fffffffu : (byte ? byte << 23 : 0x00400000u));
+}
+__device__ __forceinline__ float e8m0_inverse(uint32_t byte) { return __uint_as_float((254u - byte) << 23); }
+
+// Exponent of a row's scale: the smallest k in [-117, 117] with alpha <= 6 * 448 * 2^k (6 * 448 = 1.3125 * 2^11).  Within
+// these bounds a block's unit (2^-9 to 448 times 2^k) and its reciprocal are normal numbers.
+__device__ __forceinline__ int mx4_row_exponent(uint32_t max_bits) {
+  const int k = (int)(max_bits >> 23) - 127 - 11 + ((max_bits & 0x7fffffu) > 0x280000u ? 1 : 0);
+  return max(-117, min(117, k));
+}
+__device__ __forceinline__ float two_to(int k) { return __uint_as_float((uint32_t)(k + 127) << 23); }
+
+// A block's scale from the bits of its largest magnitude: the stored byte, and what takes a value to code units (a factor,
+// `inv`; `unit` is its exact counterpart).  k: the row's exponent (E4M3).
+struct MxScale {
+  uint32_t byte;
+  float unit, inv;
+};
+template <int GRID>
+__device__ __forceinline__ MxScale mx4_scale(uint32_t max_bits, int k) {
+  MxScale s;
+  if constexpr (GRID == OCS_GRID_E8M0) {
+    s.byte = (uint32_t)max((int)(min(max_bits, 0x7f7fffffu) >> 23) - 2, 0);
+    s.unit = e8m0_value(s.byte);
+    s.inv = e8m0_inverse(s.byte);
+  } else {
+    s.byte = e4m3_byte(__fdiv_rn(__fmul_rn(__uint_as_float(max_bits), two_to(-k)), 6.0f));
+    s.unit = __fmul_rn(e4m3_value(s.byte), two_to(k));
+    s.inv = s.byte ? __frcp_rn(s.unit) : 0.0f;
+  }
+  return s;
+}
+
+// x in units of the block's scale, as the rounding to e2m1 needs it.  E8M0: exact.  E4M3 with 16-bit x: a value x / unit is
+// either a border between two codes or at least 2^-13 away from each (x has at most 11 bits, a border times the unit at most
+// 7), so that the product with the rounded reciprocal, rounded to multiples of 2^-14, falls on the right side and borders on
+// themselves: one fused multiply-add and one subtraction instead of a division.  E4M3 with fp32 x: the rounded quotient.
+template <int GRID, typename T>
+__device__ __forceinline__ float mx4_units(float x, const MxScale& s) {
+  if constexpr (GRID == OCS_GRID_E8M0) return __fmul_rn(x, s.inv);
+  else if constexpr (sizeof(T) == 2) return copysignf(__fsub_rn(fmaf(x, s.inv, 768.0f), 768.0f), x);   // (zeros keep x's sign)
+  else return s.byte ? __fdiv_rn(x, s.unit) : copysignf(0.0f, x);
+}
+
+// N consecutive elements of a row in registers.
+template <typename T, int N>
+struct Block {
+  static constexpr int W = N * (int)sizeof(T) / 4;
+  uint32_t w[W];
+  // x aligned to ALIGN bytes (32, 16, or its element)
+  template <int ALIGN>
+  __device__ __forceinline__ void load(const T* x) {
+    if constexpr (ALIGN == 32) {
+#pragma unroll
+      for (int i = 0; i < W; i += 8)
+        asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                     : "=r"(w[i]), "=r"(w[i + 1]), "=r"(w[i + 2]), "=r"(w[i + 3]), "=r"(w[i + 4]), "=r"(w[i + 5]), "=r"(w[i + 6]), "=r"(w[i + 7])
+                     : "l"(reinterpret_cast<const uint32_t*>(x) + i));
+    } else if constexpr (ALIGN == 16) {
+#pragma unroll
+      for (int i = 0; i < W; i += 4) {
+        const uint4 v = __ldg(reinterpret_cast<const uint4*>(x) + i / 4);
+        w[i] = v.x; w[i + 1] = v.y; w[i + 2] = v.z; w[i + 3] = v.w;
+      }
+    } else if constexpr (sizeof(T) == 4) {
+#pragma unroll
+      for (int i = 0; i < W; ++i) w[i] = __ldg(reinterpret_cast<const uint32_t*>(x) + i);
+    } else if (reinterpret_cast<uintptr_t>(x) & 2) {
+      // between two half words the words in the middle are aligned
+      const uint16_t* h = reinterpret_cast<const uint16_t*>(x);
+      uint32_t before = __ldg(h);
+#pragma unroll
+      for (int i = 0; i < W - 1; ++i) {
+        const uint32_t v = __ldg(reinterpret_cast<const uint32_t*>(h + 1) + i);
+        w[i] = __byte_perm(before, v, 0x5410);
+        before = v >> 16;
+      }
+      w[W - 1] = before | (uint32_t)__ldg(h + N - 1) << 16;
+    } else {
+#pragma unroll
+      for (int i = 0; i < W; ++i) w[i] = __ldg(reinterpret_cast<const uint32_t*>(x) + i);
+    }
+  }
+  // Elements c, c + 1, ... of the expanded row: the row's C own, then its duplicated channels up to K, then zeros.
+  __device__ __forceinline__ void gather(const T* x, int c, int C, int K, const int32_t* idx_map, int* dev_status) {
+#pragma unroll
+    for (int i = 0; i < W; ++i) w[i] = 0;
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      int src = c + e;
+      if (src < K) {
+        if (src >= C) {
+          src = __ldg(idx_map + src);
+          if ((unsigned)src >= (unsigned)C) { flag(dev_status, OCS_DEV_BAD_INDEX); src = 0; }
+        }
+        if constexpr (sizeof(T) == 4) w[e] = __ldg(reinterpret_cast<const uint32_t*>(x) + src);
+        else w[e / 2] |= (uint32_t)__ldg(reinterpret_cast<const uint16_t*>(x) + src) << (16 * (e & 1));
+      }
+    }
+  }
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int i = 0; i < W; ++i) w[i] = 0;
+  }
+  __device__ __forceinline__ float operator[](int e) const {
+    if constexpr (sizeof(T) == 4) return __uint_as_float(w[e]);
+    else if constexpr (std::is_same<T, __nv_bfloat16>::value) return __uint_as_float(e & 1 ? w[e / 2] & 0xffff0000u : w[e / 2] << 16);
+    else return __half2float(__ushort_as_half((unsigned short)(e & 1 ? w[e / 2] >> 16 : w[e / 2] & 0xffffu)));
+  }
+  // Bits of the largest magnitude as fp32 (magnitudes order like their bits, and so does what is not finite).
+  __device__ __forceinline__ uint32_t max_bits() const {
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
+      if constexpr (sizeof(T) == 4) m = max(m, w[i] & 0x7fffffffu);
+      else asm("max.u16x2 %0, %0, %1;" : "+r"(m) : "r"(w[i] & 0x7fff7fffu));
+    }
+    if constexpr (sizeof(T) == 4) return m;
+    const uint32_t h = max(m & 0xffffu, m >> 16);
+    if constexpr (std::is_same<T, __nv_bfloat16>::value) return h << 16;
+    else return __float_as_uint(__half2float(__ushort_as_half((unsigned short)h)));
+  }
+  template <int GRID>
+  __device__ __forceinline__ void codes(const MxScale& s, uint32_t* out) const {
+#pragma unroll
+    for (int i = 0; i < N / 8; ++i) {
+      float t[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) t[e] = mx4_units<GRID, T>((*this)[8 * i + e], s);
+      out[i] = e2m1_codes(t);
+    }
+  }
+};
+
+}  // namespace ocs

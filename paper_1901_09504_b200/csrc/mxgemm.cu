@@ -1,0 +1,724 @@
+// ocs_qlinear_mx4 / ocs_linear_mx4: the layer on block-scaled 4-bit codes,
+//     Y[m][n] = a[m] w[n] sum_k (A[m][k] sa[m][k / B]) (W[n][k] sw[n][k / B]) + bias[n],   B = 32 (E8M0) or 16 (E4M3),
+// by tcgen05's block-scaled products: the codes and their scales go to the tensor cores as they are stored, at four times the
+// rate of 16-bit operands, and sums are fp32.  The rows' own scales (E4M3, powers of two) and the bias come in the epilogue.
+//
+// Layout as in the int8 row product: the weights are the rows of the tensor-core tile (128 channels, the lanes of tensor
+// memory), the tokens its columns, so that few tokens cost a narrow tile.  A K-block is 256 contraction indices: 128 bytes of
+// codes a row (one swizzle span, by TMA) and 2 or 4 pieces of 512 scale bytes per 128 rows, which tcgen05.cp spreads over
+// tensor memory ahead of the products that read them (instructions of one thread, executed in order).
+#include <atomic>
+
+#include "mx4.cuh"
+#include "ptx.cuh"
+
+namespace ocs {
+namespace {
+
+constexpr int TW = 128;        // channels of one CTA's tile
+constexpr int KB = 128;        // bytes of a K-block's row: 256 contraction indices
+constexpr int kThreads = 320;  // copy warp, tensor-core warp, 8 epilogue warps
+constexpr int kEpiWarps = 8;
+
+__host__ __device__ constexpr int stage_blocks(int tn) { return tn <= 64 ? 2 : 1; }   // K-blocks of a ring stage
+
+struct MxGemm {
+  int M, N, num_st;              // num_st: stages' worth of contraction
+  int n_tiles, m_tiles, total, slices;
+  const float* a_scales;         // of rows (NULL: 1)
+  const float* w_scales;
+  const float* bias;
+  void* Y;
+  long long ldy;
+  int y_type;
+  int* dev_status;
+};
+
+// Tensor memory columns: two accumulators, then the scales of a K-block.  256 tokens: the accumulators overlap by 48 columns,
+// which leaves 48 for the scales; the epilogue empties those first and says so before it goes on.
+template <int GRID, int TN, int CG>
+struct MxSmem {
+  static constexpr int kTokens = TN / CG;
+  static constexpr int kPieces = GRID == OCS_GRID_E8M0 ? 2 : 4;        // groups of four blocks in a K-block
+  static constexpr int kTiles = TN > 128 ? 2 : 1;                       // 128-token scale tiles
+  static constexpr int kWBytes = TW * KB, kTBytes = kTokens * KB;
+  static constexpr int kSWBytes = kPieces * kMxTile, kSTBytes = kTiles * kPieces * kMxTile;
+  static constexpr int kSub = stage_blocks(TN);
+  static constexpr int kStageBytes = kSub * (kWBytes + kTBytes + kSWBytes + kSTBytes);
+  static constexpr int kAtT = kSub * kWBytes, kAtSW = kAtT + kSub * kTBytes, kAtST = kAtSW + kSub * kSWBytes;
+  static constexpr int kXBytes = TN == 256 ? 0 : TN * TW * 4;           // partial sums of a K split
+  static constexpr bool kXInRing = TN == 128;
+  static constexpr int kXExtra = kXInRing ? 0 : kXBytes;
+  static constexpr int kWarpTokens = TN < 32 ? 16 : TN / 2;
+  static constexpr int kScaleBytes = kEpiWarps * kWarpTokens * 4;
+  static constexpr int kCtrlBytes = 512;
+  static constexpr int kBudget = 227 * 1024 - 1024 - kCtrlBytes - kScaleBytes - kXExtra;
+  static constexpr int kStages = kBudget / kStageBytes < 8 ? kBudget / kStageBytes : 8;
+  static constexpr int kDynBytes = 1024 + kStages * kStageBytes + kXExtra + kScaleBytes + kCtrlBytes;
+  static constexpr bool kOverlap = TN == 256;
+  static constexpr int kAccStride = kOverlap ? 208 : (TN < 32 ? 32 : TN);
+  static constexpr int kSWCol = kOverlap ? 464 : 2 * kAccStride, kSTCol = kSWCol + 4 * kPieces;
+  static constexpr int kUsedCols = kSTCol + 4 * kPieces * kTiles;
+  static constexpr uint32_t kTmemCols = kUsedCols <= 128 ? 128 : (kUsedCols <= 256 ? 256 : 512);
+  static_assert(kStages >= 3 && (!kXInRing || kXBytes <= kStages * kStageBytes) && kStageBytes % 1024 == 0 && kTBytes % 1024 == 0 && kUsedCols <= 512, "tile does not fit");
+};
+
+// Instruction descriptor of the block-scaled 4-bit products: e2m1 operands, K-major, scales e8m0 or e4m3.  sf: which bytes
+// of the scales' 32-bit cells (0, or 2 for the second half where an instruction takes two).
+__host__ __device__ constexpr uint32_t mx_instr_desc(int grid, int m, int n, int sf) {
+  return ((uint32_t)sf << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) |
+         ((uint32_t)(grid == OCS_GRID_E8M0 ? 1 : 0) << 23) | ((uint32_t)(m >> 4) << 24) | ((uint32_t)sf << 29);
+}
+
+template <int GRID, int CG>
+__device__ __forceinline__ void umma_mx4(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sa, uint32_t sb, uint32_t accumulate) {
+#define OCS_MX4_MMA(cg, kind)                                                                             \
+  asm volatile(                                                                                           \
+      "{\n\t.reg .pred p;\n\t"                                                                            \
+      "setp.ne.b32 p, %6, 0;\n\t"                                                                         \
+      "tcgen05.mma.cta_group::" cg "." kind " [%0], %1, %2, %3, [%4], [%5], p;\n\t}"                      \
+      ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(accumulate) : "memory")
+  if constexpr (GRID == OCS_GRID_E8M0) {
+    if constexpr (CG == 1) OCS_MX4_MMA("1", "kind::mxf4.block_scale.scale_vec::2X");
+    else OCS_MX4_MMA("2", "kind::mxf4.block_scale.scale_vec::2X");
+  } else {
+    if constexpr (CG == 1) OCS_MX4_MMA("1", "kind::mxf4nvf4.block_scale.scale_vec::4X");
+    else OCS_MX4_MMA("2", "kind::mxf4nvf4.block_scale.scale_vec::4X");
+  }
+#undef OCS_MX4_MMA
+}
+
+// 512 bytes of scales (32 rows of 16 bytes) to four columns of tensor memory, the same for all four quarters of the lanes;
+// for a pair, of each CTA's own shared memory to its own tensor memory.
+template <int CG>
+__device__ __forceinline__ void copy_scales(uint32_t tmem, uint64_t desc) {
+  if constexpr (CG == 1) asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
+  else asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
+}
+// Shared-memory descriptor of such a piece: no swizzle, groups of eight 16-byte rows 128 bytes apart.
+__device__ __forceinline__ uint64_t scales_desc(uint32_t saddr) {
+  return (uint64_t)((saddr >> 4) & 0x3FFFu) | (uint64_t)(128 >> 4) << 32 | (uint64_t)1 << 46;
+}
+
+template <int CG>
+__device__ __forceinline__ void tma_load_scales(uint32_t dst, const CUtensorMap* map, uint32_t bar, int piece, int tile) {
+  if constexpr (CG == 1)
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
+        ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(0), "r"(piece), "r"(tile) : "memory");
+  else
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%3, %4, %5}], [%2];"
+        ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(0), "r"(piece), "r"(tile) : "memory");
+}
+
+// Tile t of the launch: token tiles in groups of eight, all channel tiles of a group before the next group, so that the tiles
+// in flight at one time share their operand panels in L2.
+__device__ __forceinline__ void tile_of(const MxGemm& p, int t, int* mt, int* nt) {
+  const int per_group = 8 * p.n_tiles;
+  const int g = t / per_group, in = t - g * per_group;
+  const int rows = min(8, p.m_tiles - 8 * g);
+  *nt = in / rows;
+  *mt = 8 * g + in - *nt * rows;
+}
+
+template <typename T> struct Pair;
+template <> struct Pair<__half> { static __device__ __forceinline__ uint32_t pack(float a, float b) { __half2 h = __floats2half2_rn(a, b); return *reinterpret_cast<uint32_t*>(&h); } };
+template <> struct Pair<__nv_bfloat16> { static __device__ __forceinline__ uint32_t pack(float a, float b) { __nv_bfloat162 h = __floats2bfloat162_rn(a, b); return *reinterpret_cast<uint32_t*>(&h); } };
+
+// One output: the sum times two powers of two (exact within fp32's range, the sum first), plus the bias, rounded once.
+__device__ __forceinline__ float one_output(uint32_t acc, float as, float ws, float b) {
+  return fmaf(__fmul_rn(__uint_as_float(acc), as), ws, b);
+}
+
+// CNT consecutive tokens of one channel per lane, rounded to T and stored; the lanes of the warp hold consecutive channels.
+// at: the element offset of the lane's channel of the first token; left: tokens that exist, from the first on.  WHOLE: all
+// CNT tokens and all 32 channels exist.
+template <bool WHOLE, typename T, int CNT>
+__device__ __forceinline__ void finish(T* y, long long ldy, const uint32_t* acc, const float* sc, float ws, float b, int left,
+                                       bool n_ok, bool pairs) {
+  if constexpr (sizeof(T) == 2) {
+    if (pairs) {
+      // neighbouring lanes swap halves, so that a lane stores two channels of one token in 32 bits
+      const int odd = threadIdx.x & 1;
+      T* q = y + (odd ? ldy - 1 : 0);
+#pragma unroll
+      for (int j = 0; j < CNT; j += 2) {
+        const uint32_t mine = Pair<T>::pack(one_output(acc[j], sc[j], ws, b), one_output(acc[j + 1], sc[j + 1], ws, b));
+        const uint32_t other = __shfl_xor_sync(0xffffffffu, mine, 1);
+        const uint32_t out = odd ? __byte_perm(other, mine, 0x7632) : __byte_perm(mine, other, 0x5410);
+        if (WHOLE || (j + odd < left && n_ok)) *reinterpret_cast<uint32_t*>(q) = out;
+        q += 2 * ldy;
+      }
+      return;
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < CNT; ++j) {
+    const float f = one_output(acc[j], sc[j], ws, b);
+    if (WHOLE || (j < left && n_ok)) *y = from_f32<T>(f);
+    y += ldy;
+  }
+}
+template <bool WHOLE, int CNT>
+__device__ __forceinline__ void finish(const MxGemm& p, long long at, const uint32_t* acc, const float* sc, float ws, float b,
+                                       int left, bool n_ok, bool pairs) {
+  if (p.y_type == OCS_F32) finish<WHOLE, float, CNT>(static_cast<float*>(p.Y) + at, p.ldy, acc, sc, ws, b, left, n_ok, pairs);
+  else if (p.y_type == OCS_F16) finish<WHOLE, __half, CNT>(static_cast<__half*>(p.Y) + at, p.ldy, acc, sc, ws, b, left, n_ok, pairs);
+  else finish<WHOLE, __nv_bfloat16, CNT>(static_cast<__nv_bfloat16*>(p.Y) + at, p.ldy, acc, sc, ws, b, left, n_ok, pairs);
+}
+
+template <int GRID, int TN, int CG>
+__global__ void __launch_bounds__(kThreads, 1)
+mx_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtensorMap tm_t,
+               const __grid_constant__ CUtensorMap tm_sw, const __grid_constant__ CUtensorMap tm_st, const MxGemm p) {
+  using L = MxSmem<GRID, TN, CG>;
+  extern __shared__ unsigned char smem_dyn[];
+  const uint32_t raw = smem_u32(smem_dyn);
+  const uint32_t base = (raw + 1023u) & ~1023u;
+  unsigned char* tiles = smem_dyn + (base - raw);
+  unsigned char* after = tiles + L::kStages * L::kStageBytes;
+  unsigned char* xbuf = L::kXInRing ? tiles : after;
+  float* scale_buf = reinterpret_cast<float*>(after + L::kXExtra);
+  uint64_t* bars = reinterpret_cast<uint64_t*>(after + L::kXExtra + L::kScaleBytes);
+  auto full_bar = [&](int s) { return smem_u32(bars + s); };
+  auto empty_bar = [&](int s) { return smem_u32(bars + L::kStages + s); };
+  auto accfull_bar = [&](int a) { return smem_u32(bars + 2 * L::kStages + a); };
+  auto accempty_bar = [&](int a) { return smem_u32(bars + 2 * L::kStages + 2 + a); };
+  const uint32_t xfull_bar = smem_u32(bars + 2 * L::kStages + 4);
+  const uint32_t xready_bar = smem_u32(bars + 2 * L::kStages + 5);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * L::kStages + 6);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  static_assert((2 * L::kStages + 6) * 8 + 8 <= L::kCtrlBytes, "control block");
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int CL = CG * p.slices;
+  const int rank = CL > 1 ? (int)cluster_rank() : 0;
+  const int half = rank % CG, slice = rank / CG;
+  const int cluster = blockIdx.x / CL, n_clusters = gridDim.x / CL;
+  const int my_st = (p.num_st - slice + p.slices - 1) / p.slices;
+
+  // Set-up.  Nobody waits for more than it needs (named barriers: 2 = set up, 3 = barriers stand).  A peer may be written to
+  // once all threads of the cluster have arrived; a pair waits for that at once, the others where they first need it.
+  if (warp == 0) {
+    if (lane == 0) {
+      prefetch_tmap(&tm_w);
+      prefetch_tmap(&tm_t);
+      prefetch_tmap(&tm_sw);
+      prefetch_tmap(&tm_st);
+      for (int s = 0; s < L::kStages; ++s) {
+        mbar_init(full_bar(s), 1);     // the leader's producer announces the bytes of both CTAs
+        mbar_init(empty_bar(s), 1);    // commit of the products that read the stage
+      }
+      for (int a = 0; a < 2; ++a) {
+        mbar_init(accfull_bar(a), 1);
+        mbar_init(accempty_bar(a), CG * kEpiWarps);
+      }
+      mbar_init(xfull_bar, 1);
+      mbar_init(xready_bar, p.slices);
+      *abort_flag = 0;
+      fence_barrier_init();
+      fence_proxy_async_smem();
+      if (L::kXBytes && p.slices > 1) mbar_arrive_expect_tx(xfull_bar, (uint32_t)L::kXBytes);
+    }
+    __syncwarp();
+    asm volatile("bar.arrive 3, 64;" ::: "memory");
+    asm volatile("bar.arrive 2, 320;" ::: "memory");
+    if (CL > 1) cluster_arrive();
+  } else if (warp == 1) {
+    if (CG == 2) tmem_alloc_pair(smem_u32(tmem_slot), L::kTmemCols);
+    else tmem_alloc(smem_u32(tmem_slot), L::kTmemCols);
+    tc_fence_before();
+    asm volatile("bar.arrive 2, 320;" ::: "memory");
+    if (CL > 1) cluster_arrive();
+    asm volatile("bar.sync 3, 64;" ::: "memory");
+  } else {
+    if (CL > 1) cluster_arrive();
+    asm volatile("bar.sync 2, 320;" ::: "memory");
+  }
+  if (CG == 2) cluster_wait();
+  tc_fence_after();
+  const uint32_t tmem_base = warp == 0 ? 0u : *reinterpret_cast<volatile uint32_t*>(tmem_slot);
+
+  if (warp == 0) {
+    // ---------------------------------------------------------------- copies
+    if (lane == 0) {
+      const uint32_t lead = CG == 2 ? (uint32_t)(rank & ~1) : 0;
+      int it = 0;
+      bool ok = true;
+      int ahead = 0, mt, nt;
+      auto bar_of = [&](int s) { return CG == 2 ? peer_addr(full_bar(s), lead) : full_bar(s); };
+      auto load_w = [&](int s, int st) {
+        const uint32_t at = base + s * L::kStageBytes, bar = bar_of(s);
+#pragma unroll
+        for (int u = 0; u < L::kSub; ++u) {
+          const int kb = st * L::kSub + u, row = (nt * CG + half) * TW;
+          if (CG == 2) tma_load_2d_pair(at + u * L::kWBytes, &tm_w, bar, kb * KB, row);
+          else tma_load_2d(at + u * L::kWBytes, &tm_w, bar, kb * KB, row);
+          tma_load_scales<CG>(at + L::kAtSW + u * L::kSWBytes, &tm_sw, bar, kb * L::kPieces, nt * CG + half);
+        }
+      };
+      auto load_t = [&](int s, int st) {
+        const uint32_t at = base + s * L::kStageBytes, bar = bar_of(s);
+#pragma unroll
+        for (int u = 0; u < L::kSub; ++u) {
+          const int kb = st * L::kSub + u, row = mt * TN + half * L::kTokens;
+          if (CG == 2) tma_load_2d_pair(at + L::kAtT + u * L::kTBytes, &tm_t, bar, kb * KB, row);
+          else tma_load_2d(at + L::kAtT + u * L::kTBytes, &tm_t, bar, kb * KB, row);
+#pragma unroll
+          for (int i = 0; i < L::kTiles; ++i)   // (both CTAs of a pair need the scales of all the tile's tokens)
+            tma_load_scales<CG>(at + L::kAtST + u * L::kSTBytes + i * L::kSWBytes, &tm_st, bar, kb * L::kPieces, mt * TN / 128 + i);
+        }
+      };
+      // weights do not depend on the kernel before: the first ring of them is requested before waiting for it
+      if (cluster < p.total) {
+        tile_of(p, cluster, &mt, &nt);
+        ahead = min(L::kStages, my_st);
+        for (int i = 0; i < ahead; ++i) {
+          if (half == 0) mbar_arrive_expect_tx(full_bar(i), CG * L::kStageBytes);
+          load_w(i, slice + i * p.slices);
+        }
+      }
+      grid_wait_previous();
+      for (int t = cluster; ok && t < p.total; t += n_clusters) {
+        tile_of(p, t, &mt, &nt);
+        for (int i = 0; i < my_st; ++i, ++it) {
+          const int s = it % L::kStages;
+          if (it >= ahead) {
+            if (!mbar_wait(empty_bar(s), (uint32_t)((it / L::kStages) & 1) ^ 1u, abort_flag)) { ok = false; break; }
+            if (half == 0) mbar_arrive_expect_tx(full_bar(s), CG * L::kStageBytes);
+            load_w(s, slice + i * p.slices);
+          }
+          load_t(s, slice + i * p.slices);
+        }
+      }
+      // every commit has arrived (also those the other CTA of a pair sends here) before the CTA may leave
+      for (int i = 0; ok && i < L::kStages; ++i, ++it)
+        ok = mbar_wait(empty_bar(it % L::kStages), (uint32_t)((it / L::kStages) & 1) ^ 1u, abort_flag);
+      if (*abort_flag)   // copies that are still in flight land before the CTA's shared memory is released
+        for (int i = 0; i < 2000; ++i) __nanosleep(100);
+    }
+    __syncwarp();
+    if (CL > 1 && CG == 1) cluster_wait();
+  } else if (warp == 1) {
+    // ---------------------------------------------------------------- tensor cores
+    if (lane == 0 && half == 0) {
+      constexpr uint32_t kDescM = TW * CG;
+      const uint16_t mask = (uint16_t)(3u << (rank & ~1));
+      const uint64_t w_desc0 = smem_desc_sw128(base), t_desc0 = smem_desc_sw128(base + L::kAtT);
+      const uint64_t sw_desc0 = scales_desc(base + L::kAtSW), st_desc0 = scales_desc(base + L::kAtST);
+      const uint32_t sw_col = tmem_base + L::kSWCol, st_col = tmem_base + L::kSTCol;
+      int j = 0, s = 0;
+      uint32_t phase = 0;
+      bool ok = true;
+      for (int t = cluster; ok && t < p.total; t += n_clusters, ++j) {
+        int mt, nt;
+        tile_of(p, t, &mt, &nt);
+        const int acc = j & 1;
+        const uint32_t st_use = st_col + (uint32_t)(TN == 64 ? (mt & 1) * 2 : 0);   // the columns of this half of the 128 tokens
+        if (L::kOverlap) {
+          if (j && !mbar_wait_cluster(accempty_bar(0), (uint32_t)(j - 1) & 1u, abort_flag)) break;
+        } else {
+          if (!mbar_wait_cluster(accempty_bar(acc), (((uint32_t)j >> 1) & 1u) ^ 1u, abort_flag)) break;
+        }
+        tc_fence_after();
+        const uint32_t d = tmem_base + (uint32_t)(acc * L::kAccStride);
+        uint32_t more = 0;
+        for (int i = 0; i < my_st; ++i) {
+          if (!mbar_wait(full_bar(s), phase, abort_flag)) { ok = false; break; }
+          tc_fence_after();
+          const uint32_t o = (uint32_t)(s * (L::kStageBytes >> 4));
+#pragma unroll
+          for (int u = 0; u < L::kSub; ++u) {
+#pragma unroll
+            for (int c = 0; c < L::kPieces; ++c) {
+              copy_scales<CG>(sw_col + 4 * c, sw_desc0 + o + u * (L::kSWBytes >> 4) + c * (kMxTile >> 4));
+#pragma unroll
+              for (int k = 0; k < L::kTiles; ++k)
+                copy_scales<CG>(st_col + 4 * (c * L::kTiles + k), st_desc0 + o + u * (L::kSTBytes >> 4) + k * (L::kSWBytes >> 4) + c * (kMxTile >> 4));
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {   // 64 contraction indices: 32 bytes on, 2 in the descriptors' units of 16
+              constexpr int kPer = 4 / L::kPieces;   // products per piece of scales
+              const int c = k / kPer, sf = k % kPer * 2;
+              umma_mx4<GRID, CG>(d, w_desc0 + o + u * (L::kWBytes >> 4) + 2 * k, t_desc0 + o + u * (L::kTBytes >> 4) + 2 * k,
+                                 mx_instr_desc(GRID, kDescM, TN, sf), sw_col + 4 * c, st_use + 4 * c * L::kTiles, u + k == 0 ? more : 1u);
+            }
+          }
+          more = 1;
+          if (CG == 2) umma_commit_pair(empty_bar(s), mask);
+          else umma_commit(empty_bar(s));
+          if (++s == L::kStages) { s = 0; phase ^= 1; }
+        }
+        if (!ok) break;
+        if (CG == 2) umma_commit_pair(accfull_bar(acc), mask);
+        else umma_commit(accfull_bar(acc));
+      }
+    }
+    __syncwarp();
+    if (CL > 1 && CG == 1) cluster_wait();
+  } else {
+    // ---------------------------------------------------------------- epilogue
+    constexpr int EC = 16;                              // accumulator columns (tokens) moved at a time
+    const int ew = warp - 2, q = warp & 3, part = ew >> 2;   // lanes 32q.. of tensor memory; two warps share a quadrant
+    float* sc = scale_buf + ew * L::kWarpTokens;
+    const bool pairs = p.y_type != OCS_F32 && (p.ldy % 2 == 0) && (p.N % 2 == 0) && (reinterpret_cast<uintptr_t>(p.Y) & 3) == 0;
+    grid_wait_previous();
+    if (CL > 1 && CG == 1) cluster_wait();
+    auto token_scale = [&](int m) { return m < p.M ? (p.a_scales ? __ldcg(p.a_scales + m) : 1.0f) : 0.0f; };
+    int j = 0;
+    for (int t = cluster; t < p.total; t += n_clusters, ++j) {
+      int mt, nt;
+      tile_of(p, t, &mt, &nt);
+      const int acc = j & 1;
+      const int n = (nt * CG + half) * TW + q * 32 + lane;
+      const float ws = n < p.N && p.w_scales ? __ldg(p.w_scales + n) : 1.0f;
+      const float b = p.bias && n < p.N ? __ldg(p.bias + n) : 0.0f;
+      if (p.slices > 1) {
+        // K split: owner o of the tile's slices finishes tokens [o * own, (o + 1) * own).  Every CTA sends the columns
+        // another one owns into that one's buffer, cells of 16 bytes [sender][four tokens][channel], counted as
+        // transaction bytes on the owner's barrier; they are added in the order of the senders.
+        if constexpr (L::kXBytes > 0) {
+          const int own = TN / p.slices, groups = own / 4;
+          __syncwarp();
+          for (int i = lane; i < own; i += 32) sc[i] = token_scale(mt * TN + slice * own + i);
+          __syncwarp();
+          if (!mbar_wait(accfull_bar(acc), ((uint32_t)j >> 1) & 1u, abort_flag)) break;
+          tc_fence_after();
+          if (L::kXInRing) {
+            // this CTA's tensor cores are done with its ring: it may be written to; and so are all the others'
+            if (ew == 0 && lane == 0)
+              for (int o = 0; o < p.slices; ++o) mbar_arrive_peer(peer_addr(xready_bar, (uint32_t)o));
+            if (!mbar_wait_cluster(xready_bar, 0u, abort_flag)) break;
+          }
+          const uint32_t mine = smem_u32(xbuf) + (uint32_t)(slice * groups * TW + q * 32 + lane) * 16u;
+          const uint32_t addr = tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(acc * L::kAccStride);
+          uint32_t v[2][16];
+          constexpr int kPieces = TN >= 32 ? TN / 32 : 1;
+          if (part * 16 < TN) {
+            __syncwarp();
+            tmem_ld_async<16>(addr + part * 16, v[0]);
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i) {
+              tmem_wait_ld16(v[i & 1]);
+              if (i + 1 < kPieces) tmem_ld_async<16>(addr + part * 16 + 32 * (i + 1), v[(i + 1) & 1]);
+              const uint32_t* w = v[i & 1];
+#pragma unroll
+              for (int e = 0; e < 16; e += 4) {
+                const int col = part * 16 + 32 * i + e;
+                const int owner = col / own, g = (col - owner * own) / 4;
+                const uint32_t peer = (uint32_t)owner;
+                st_async_v4(peer_addr(mine + (uint32_t)g * (TW * 16u), peer), make_uint4(w[e], w[e + 1], w[e + 2], w[e + 3]),
+                            peer_addr(xfull_bar, peer));
+              }
+            }
+          }
+          if (!mbar_wait_cluster(xfull_bar, 0u, abort_flag)) break;
+          const int m_own = mt * TN + slice * own;
+          const long long y = (long long)m_own * p.ldy + n;
+          const uint32_t slot = (uint32_t)groups * TW * 16u;   // from one sender's cells to the next one's
+          for (int g = part; g < groups; g += 2) {
+            const unsigned char* cell = xbuf + (size_t)(g * TW + q * 32 + lane) * 16;
+            float4 a = *reinterpret_cast<const float4*>(cell);
+#pragma unroll 4
+            for (int sl = 1; sl < p.slices; ++sl) {
+              const float4 b4 = *reinterpret_cast<const float4*>(cell + sl * slot);
+              a.x = __fadd_rn(a.x, b4.x); a.y = __fadd_rn(a.y, b4.y); a.z = __fadd_rn(a.z, b4.z); a.w = __fadd_rn(a.w, b4.w);
+            }
+            const uint32_t av[4] = {__float_as_uint(a.x), __float_as_uint(a.y), __float_as_uint(a.z), __float_as_uint(a.w)};
+            const float4 s4 = *reinterpret_cast<const float4*>(sc + 4 * g);
+            const float sv[4] = {s4.x, s4.y, s4.z, s4.w};
+            finish<false, 4>(p, y + 4 * g * p.ldy, av, sv, ws, b, p.M - m_own - 4 * g, n < p.N, pairs);
+          }
+        }
+        break;   // a K split is used only where every cluster has one tile
+      }
+      // the token scales of this warp's columns: fetched while the main loop runs
+      __syncwarp();
+      for (int i = lane; i < L::kWarpTokens; i += 32) sc[i] = token_scale(mt * TN + (i / EC) * 2 * EC + part * EC + i % EC);
+      __syncwarp();
+      if (!mbar_wait(accfull_bar(acc), ((uint32_t)j >> 1) & 1u, abort_flag)) break;
+      tc_fence_after();
+      // Pieces of EC columns; the next one's way out of tensor memory overlaps this one's arithmetic and stores.  Overlapping
+      // accumulators: from the end that the next tile's products write to (the first one's last columns, the second one's
+      // first); once two pieces per warp are out, the next tile may start.
+      constexpr int kPieces = TN >= 2 * EC ? TN / (2 * EC) : 1;
+      const bool down = L::kOverlap && acc == 0;
+      const uint32_t addr = tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(acc * L::kAccStride + part * EC);
+      const bool n_all = (nt * CG + half) * TW + q * 32 + 32 <= p.N;
+      const int m_first = mt * TN + part * EC;
+      auto emptied = [&](int a) {
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) {
+          if (CG == 2) mbar_arrive_peer(peer_addr(accempty_bar(a), (uint32_t)(rank & ~1)));
+          else mbar_arrive(accempty_bar(a));
+        }
+      };
+      uint32_t v[2][EC];
+      if (part * EC < TN) {
+        auto piece = [&](int i) { return down ? kPieces - 1 - i : i; };
+        tmem_ld_async<EC>(addr + 2 * EC * piece(0), v[0]);
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+          tmem_wait_ld16(v[i & 1]);
+          if (L::kOverlap && i == 1) emptied(0);
+          if (i + 1 < kPieces) tmem_ld_async<EC>(addr + 2 * EC * piece(i + 1), v[(i + 1) & 1]);
+          const int at = 2 * EC * piece(i), left = p.M - m_first - at;   // tokens from this piece's first on
+          if (left <= 0) continue;               // the same for the whole warp
+          float s[EC];
+#pragma unroll
+          for (int e = 0; e < EC; e += 4) {
+            const float4 f = *reinterpret_cast<const float4*>(sc + at / 2 + e);
+            s[e] = f.x; s[e + 1] = f.y; s[e + 2] = f.z; s[e + 3] = f.w;
+          }
+          const long long y = (long long)(m_first + at) * p.ldy + n;
+          if (n_all && left >= EC) finish<true, EC>(p, y, v[i & 1], s, ws, b, left, true, pairs);
+          else finish<false, EC>(p, y, v[i & 1], s, ws, b, left, n < p.N, pairs);
+        }
+      }
+      if (!L::kOverlap) emptied(acc);
+    }
+    tc_fence_before();
+  }
+
+  __syncthreads();
+  if (CL > 1) cluster_sync_all();   // no CTA leaves while a peer may still store into it or arrive on its barriers
+  if (warp == 1) {
+    __syncwarp();
+    tc_fence_after();
+    if (CG == 2) tmem_dealloc_pair(tmem_base, L::kTmemCols);
+    else tmem_dealloc(tmem_base, L::kTmemCols);
+  }
+  if (threadIdx.x == 0 && *abort_flag) flag(p.dev_status, OCS_DEV_TIMEOUT);
+}
+
+// ------------------------------------------------------------------------------------------------ host
+struct MxPlan {
+  int tn, cg, slices;
+};
+
+// Test hook (ocs_selftest_force_mx4_plan), in one word: tn << 8 | cg << 4 | slices, 0 for none.
+std::atomic<int> g_forced_plan{0};
+
+// CTAs resident at once, one per SM, for cluster sizes 1, 2, 4, 8 (a cluster lies inside one GPC)
+int cluster_capacity(int cl) { return cl <= 2 ? 148 : (cl == 4 ? 132 : 120); }
+
+int stages_of(int tn, int num_kb) { return (num_kb + stage_blocks(tn) - 1) / stage_blocks(tn); }
+
+// Scales come in groups of 128 tokens, of which a product takes an aligned half or the first part: tiles of fewer than 64
+// tokens are for calls with no more tokens than that.
+bool tile_fits(int tn, int M) { return tn >= 64 || M <= tn; }
+
+bool split_fits(int tn, int cg, int slices, long long tiles, int stages) {
+  if (slices == 1) return true;
+  return cg == 1 && tn < 256 && tn / slices >= 4 && slices <= stages && tiles * slices <= cluster_capacity(slices);
+}
+
+MxPlan choose_plan(int M, int N, int num_kb, int out_bytes) {
+  struct Form { int tn, cg; double block_us, epilogue_us; };
+  static const Form forms[5] = {{16, 1, 0.18, 0.0}, {32, 1, 0.18, 0.01}, {64, 1, 0.18, 0.27}, {128, 1, 0.23, 0.91}, {256, 2, 0.27, 3.02}};
+  auto tiles_of = [&](int tn, int cg) {
+    return (long long)((M + (long long)tn - 1) / tn) * ((N + (long long)TW * cg - 1) / (TW * cg));
+  };
+  if (const int forced = g_forced_plan.load()) {
+    MxPlan r{forced >> 8, forced >> 4 & 15, forced & 15};
+    while (!tile_fits(r.tn, M)) r.tn *= 2;
+    while (r.slices > 1 && !split_fits(r.tn, r.cg, r.slices, tiles_of(r.tn, r.cg), stages_of(r.tn, num_kb))) r.slices /= 2;
+    return r;
+  }
+  const double K = (double)num_kb * KB;
+  const double bytes_us = ((double)N * K + (double)M * K + (double)M * N * out_bytes) / 6.22e6;
+  MxPlan best{64, 1, 1};
+  double best_us = 1e300;   // squared
+  for (const Form& f : forms) {
+    if (!tile_fits(f.tn, M)) continue;
+    const long long tiles = tiles_of(f.tn, f.cg);
+    for (int s = 1; s <= 8; s *= 2) {
+      if (!split_fits(f.tn, f.cg, s, tiles, stages_of(f.tn, num_kb))) continue;
+      const long long slots = cluster_capacity(f.cg * s) / (f.cg * s);
+      const double waves = (double)((tiles + slots - 1) / slots);
+      const int blocks = (stages_of(f.tn, num_kb) + s - 1) / s * stage_blocks(f.tn);
+      double us = waves * (blocks * f.block_us + f.epilogue_us * (out_bytes == 4 ? 1.2 : 1.0) + 0.29);
+      if (s > 1) us += 3.85 * f.tn / 128.0;
+      us = us * us + bytes_us * bytes_us;
+      if (us < best_us) { best_us = us; best = MxPlan{f.tn, f.cg, s}; }
+    }
+  }
+  return best;
+}
+
+struct Product {
+  const uint8_t* A;
+  const uint8_t* A_scales;
+  const float* a_rows;
+  const uint8_t* W;
+  const uint8_t* W_scales;
+  const float* w_rows;
+  const float* bias;
+  int M, N, K;
+  long long lda, ldw, ldy;
+  ocs_grid grid;
+  void* Y;
+  ocs_dtype y_type;
+  int* dev_status;
+};
+
+template <int GRID, int TN, int CG>
+ocs_status launch_tiles(const Product& g, int slices, bool overlap, cudaStream_t stream) {
+  using L = MxSmem<GRID, TN, CG>;
+  static std::atomic<unsigned long long> ready{0};   // devices whose copy of the kernel has its attribute set
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return OCS_ERR_CUDA;
+  if (dev >= 64 || !(ready.load() >> dev & 1)) {
+    if (cudaFuncSetAttribute(mx_gemm_kernel<GRID, TN, CG>, cudaFuncAttributeMaxDynamicSharedMemorySize, L::kDynBytes) != cudaSuccess)
+      return OCS_ERR_CUDA;
+    if (dev < 64) ready.fetch_or(1ull << dev);
+  }
+  MxGemm p{};
+  p.M = g.M; p.N = g.N; p.num_st = stages_of(TN, (g.K + 2 * KB - 1) / (2 * KB));
+  p.a_scales = g.a_rows; p.w_scales = g.w_rows; p.bias = g.bias; p.Y = g.Y; p.ldy = g.ldy; p.y_type = g.y_type;
+  p.dev_status = g.dev_status;
+  p.n_tiles = (g.N + TW * CG - 1) / (TW * CG);
+  p.m_tiles = (g.M + TN - 1) / TN;
+  const long long total = (long long)p.n_tiles * p.m_tiles;
+  if (total > 0x3fffffff) return OCS_ERR_UNSUPPORTED;
+  p.total = (int)total;
+  p.slices = slices;
+  CUtensorMap tm_w, tm_t, tm_sw, tm_st;
+  const cuuint64_t row = (cuuint64_t)(g.K + 1) / 2;
+  const cuuint64_t wd[2] = {row, (cuuint64_t)g.N}, ws[1] = {(cuuint64_t)g.ldw};
+  const cuuint64_t td[2] = {row, (cuuint64_t)g.M}, ts[1] = {(cuuint64_t)g.lda};
+  const cuuint32_t wb[2] = {KB, TW}, tb[2] = {KB, (cuuint32_t)L::kTokens};
+  if (!encode_u8(&tm_w, g.W, 2, wd, ws, wb) || !encode_u8(&tm_t, g.A, 2, td, ts, tb)) return OCS_ERR_CUDA;
+  const int n = mx4_block(GRID), pieces = ((g.K + n - 1) / n + 3) / 4;
+  if (!encode_mx4_scales(&tm_sw, g.W_scales, pieces, (g.N + 127) / 128, L::kPieces) ||
+      !encode_mx4_scales(&tm_st, g.A_scales, pieces, (g.M + 127) / 128, L::kPieces))
+    return OCS_ERR_CUDA;
+  const int cl = CG * slices;
+  const long long slots = cluster_capacity(cl) / cl;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)((total < slots ? total : slots) * cl), 1, 1);
+  cfg.blockDim = dim3(kThreads, 1, 1);
+  cfg.dynamicSmemBytes = L::kDynBytes;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[2];
+  int n_attr = 0;
+  if (cl > 1) {
+    attr[n_attr].id = cudaLaunchAttributeClusterDimension;
+    attr[n_attr].val.clusterDim.x = cl; attr[n_attr].val.clusterDim.y = 1; attr[n_attr].val.clusterDim.z = 1;
+    ++n_attr;
+  }
+  if (overlap) {
+    attr[n_attr].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[n_attr].val.programmaticStreamSerializationAllowed = 1;
+    ++n_attr;
+  }
+  cfg.attrs = attr; cfg.numAttrs = n_attr;
+  LaunchScope scope("mx_gemm_kernel", stream);
+  if (cudaLaunchKernelEx(&cfg, mx_gemm_kernel<GRID, TN, CG>, tm_w, tm_t, tm_sw, tm_st, p) != cudaSuccess) return OCS_ERR_CUDA;
+  return launch_status();
+}
+
+template <int GRID>
+ocs_status run_product(const Product& g, const MxPlan& plan, bool overlap, cudaStream_t stream) {
+  switch (plan.tn) {
+    case 16: return launch_tiles<GRID, 16, 1>(g, plan.slices, overlap, stream);
+    case 32: return launch_tiles<GRID, 32, 1>(g, plan.slices, overlap, stream);
+    case 64: return launch_tiles<GRID, 64, 1>(g, plan.slices, overlap, stream);
+    case 128: return launch_tiles<GRID, 128, 1>(g, plan.slices, overlap, stream);
+    default: return launch_tiles<GRID, 256, 2>(g, plan.slices, overlap, stream);
+  }
+}
+ocs_status run_product(const Product& g, const MxPlan& plan, bool overlap, cudaStream_t stream) {
+  return g.grid == OCS_GRID_E8M0 ? run_product<OCS_GRID_E8M0>(g, plan, overlap, stream)
+                                 : run_product<OCS_GRID_E4M3>(g, plan, overlap, stream);
+}
+
+// Everything but the tokens, which ocs_linear_mx4 has in another form.
+ocs_status check_product(const Product& g) {
+  if (!g.W || !g.W_scales || !g.Y || (g.grid == OCS_GRID_E4M3 && !g.w_rows)) return OCS_ERR_INVALID_ARG;
+  if (g.M >= (1 << 30) || g.K >= (1 << 30) || g.N > 0x7fffffff - 512) return OCS_ERR_UNSUPPORTED;
+  if (g.ldw < (g.K + 1) / 2 || g.ldw % 16 != 0 || !aligned(g.W, 16) || !aligned(g.W_scales, 16)) return OCS_ERR_SHAPE;
+  if (g.ldy < g.N || !aligned(g.Y, elem_bytes(g.y_type)) || !aligned(g.w_rows, 4) || !aligned(g.bias, 4)) return OCS_ERR_SHAPE;
+  return OCS_OK;
+}
+
+}  // namespace
+}  // namespace ocs
+
+using namespace ocs;
+
+extern "C" ocs_status ocs_qlinear_mx4(const uint8_t* A_codes, const uint8_t* A_scales, const float* a_row_scales, int M, int K,
+                                      int64_t lda, const uint8_t* W_codes, const uint8_t* W_scales, const float* w_row_scales,
+                                      int N, int64_t ldw, ocs_grid grid, const float* bias, void* Y, ocs_dtype y_type,
+                                      int64_t ldy, int* dev_status, void* stream_) {
+  cudaStream_t stream = reinterpret_cast<cudaStream_t>(stream_);
+  if (!valid_dtype(y_type) || !mx4_grid(grid)) return OCS_ERR_INVALID_ARG;
+  if (M < 0 || K <= 0 || N <= 0) return OCS_ERR_SHAPE;
+  if (M == 0) return OCS_OK;
+  if (!A_codes || !A_scales || (grid == OCS_GRID_E4M3 && !a_row_scales)) return OCS_ERR_INVALID_ARG;
+  const bool rows = grid == OCS_GRID_E4M3;
+  const Product g{A_codes, A_scales, rows ? a_row_scales : nullptr, W_codes, W_scales, rows ? w_row_scales : nullptr, bias,
+                  M, N, K, lda, ldw, ldy, grid, Y, y_type, dev_status};
+  ocs_status st = check_product(g);
+  if (st != OCS_OK) return st;
+  if (lda < (K + 1) / 2 || lda % 16 != 0 || !aligned(A_codes, 16) || !aligned(A_scales, 16) || !aligned(g.a_rows, 4)) return OCS_ERR_SHAPE;
+  if ((st = check_device()) != OCS_OK) return st;
+  return run_product(g, choose_plan(M, N, (K + 2 * KB - 1) / (2 * KB), elem_bytes(y_type)), false, stream);
+}
+
+namespace {
+// Where ocs_linear_mx4 keeps the tokens' codes, scales and row scales in its workspace.
+struct TokenSpace {
+  int64_t lda;
+  size_t scales, rows, bytes;
+};
+TokenSpace token_space(int M, int K, ocs_grid grid) {
+  TokenSpace t;
+  t.lda = (int64_t)align_up((size_t)(K + 1) / 2, 16);
+  t.scales = align_up((size_t)M * t.lda, 256);
+  t.rows = t.scales + align_up((size_t)ocs_mx4_scale_bytes(M, K, grid), 256);
+  t.bytes = t.rows + (grid == OCS_GRID_E4M3 ? align_up((size_t)M * 4, 256) : 0);
+  return t;
+}
+}  // namespace
+
+extern "C" size_t ocs_linear_mx4_workspace_bytes(int M, int C, int S, ocs_grid grid) {
+  if (M <= 0 || C <= 0 || S < 0 || !mx4_grid(grid) || (int64_t)C + S >= (1 << 30)) return 0;
+  return token_space(M, C + S, grid).bytes;
+}
+
+extern "C" ocs_status ocs_linear_mx4(const void* X, ocs_dtype x_type, int M, int C, int64_t ldx, int S, const int32_t* idx_map,
+                                     ocs_grid grid, const uint8_t* W_codes, const uint8_t* W_scales, const float* w_row_scales,
+                                     int N, int64_t ldw, const float* bias, void* Y, ocs_dtype y_type, int64_t ldy, void* ws,
+                                     size_t ws_bytes, int* dev_status, void* stream_) {
+  cudaStream_t stream = reinterpret_cast<cudaStream_t>(stream_);
+  if (!valid_dtype(x_type) || !valid_dtype(y_type) || !mx4_grid(grid) || S < 0) return OCS_ERR_INVALID_ARG;
+  if (M < 0 || C <= 0 || N <= 0) return OCS_ERR_SHAPE;
+  if (M == 0) return OCS_OK;
+  if (!X || (S > 0 && !idx_map)) return OCS_ERR_INVALID_ARG;
+  if ((int64_t)C + S >= (1 << 30)) return OCS_ERR_UNSUPPORTED;
+  const int K = C + S;
+  const TokenSpace t = token_space(M, K, grid);
+  if (!ws || !aligned(ws, 256) || ws_bytes < t.bytes) return OCS_ERR_WORKSPACE;
+  uint8_t* codes = static_cast<uint8_t*>(ws);
+  const bool rows = grid == OCS_GRID_E4M3;
+  float* a_rows = rows ? reinterpret_cast<float*>(codes + t.rows) : nullptr;
+  const Product g{codes, codes + t.scales, a_rows, W_codes, W_scales, rows ? w_row_scales : nullptr, bias,
+                  M, N, K, t.lda, ldw, ldy, grid, Y, y_type, dev_status};
+  ocs_status st = check_product(g);
+  if (st != OCS_OK) return st;
+  if ((st = ocs_quantize_mx4(X, x_type, M, C, ldx, S, idx_map, grid, codes, t.lda, codes + t.scales, a_rows, dev_status, stream_)) != OCS_OK)
+    return st;
+  return run_product(g, choose_plan(M, N, (K + 2 * KB - 1) / (2 * KB), elem_bytes(y_type)), true, stream);
+}
+
+// Test hook: the next ocs_qlinear_mx4 / ocs_linear_mx4 calls of this process use the given plan; tn = 0 gives the choice back.
+extern "C" ocs_status ocs_selftest_force_mx4_plan(int tn, int cg, int slices) {
+  if (tn != 0 && ((tn != 16 && tn != 32 && tn != 64 && tn != 128 && tn != 256) || cg != (tn == 256 ? 2 : 1) ||
+                  (slices != 1 && slices != 2 && slices != 4 && slices != 8)))
+    return OCS_ERR_INVALID_ARG;
+  g_forced_plan.store(tn ? tn << 8 | cg << 4 | slices : 0);
+  return OCS_OK;
+}

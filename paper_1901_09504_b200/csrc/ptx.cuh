@@ -281,5 +281,8 @@ __device__ __forceinline__ void grid_wait_previous() { asm volatile("griddepcont
 // dimension.
 bool encode_u8(CUtensorMap* map, const void* base, int rank, const cuuint64_t* dims, const cuuint64_t* strides_bytes,
                const cuuint32_t* box, const cuuint32_t* elem_strides = nullptr);
+// Tensor map over block scales as ocs_quantize_mx4 lays them out ([tiles][pieces][512 bytes]), box_pieces pieces at a time
+// (defined in gemm.cu).
+bool encode_mx4_scales(CUtensorMap* map, const void* base, int pieces, int tiles, int box_pieces);
 
 }  // namespace ocs
