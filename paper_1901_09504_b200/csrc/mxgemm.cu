@@ -5,8 +5,10 @@
 //
 // Layout as in the int8 row product: the weights are the rows of the tensor-core tile (128 channels, the lanes of tensor
 // memory), the tokens its columns, so that few tokens cost a narrow tile.  A K-block is 256 contraction indices: 128 bytes of
-// codes a row (one swizzle span, by TMA) and 2 or 4 pieces of 512 scale bytes per 128 rows, which tcgen05.cp spreads over
-// tensor memory ahead of the products that read them (instructions of one thread, executed in order).
+// codes a row (one swizzle span, by TMA) and 2 or 4 pieces of 512 scale bytes per 128 rows, which have to be spread over tensor
+// memory ahead of the products that read them.  tcgen05.cp does that, in order with the products, and takes the tensor cores'
+// time for it: some 32 cycles a piece.  Narrow tiles wait for memory anyway; in the form of 256 tokens (12 pieces for 512
+// cycles of products) four more warps move the pieces through registers while the products before them run.
 #include <atomic>
 
 #include "mx4.cuh"
@@ -17,7 +19,6 @@ namespace {
 
 constexpr int TW = 128;        // channels of one CTA's tile
 constexpr int KB = 128;        // bytes of a K-block's row: 256 contraction indices
-constexpr int kThreads = 320;  // copy warp, tensor-core warp, 8 epilogue warps
 constexpr int kEpiWarps = 8;
 
 __host__ __device__ constexpr int stage_blocks(int tn) { return tn <= 64 ? 2 : 1; }   // K-blocks of a ring stage
@@ -34,8 +35,9 @@ struct MxGemm {
   int* dev_status;
 };
 
-// Tensor memory columns: two accumulators, then the scales of a K-block.  256 tokens: the accumulators overlap by 48 columns,
-// which leaves 48 for the scales; the epilogue empties those first and says so before it goes on.
+// Tensor memory columns: two accumulators, then the scales of one K-block, or of two where warps of their own bring them
+// (kFeed).  256 tokens: the accumulators overlap by as many columns as the scales need; the epilogue empties those first and
+// says so before it goes on.
 template <int GRID, int TN, int CG>
 struct MxSmem {
   static constexpr int kTokens = TN / CG;
@@ -55,10 +57,15 @@ struct MxSmem {
   static constexpr int kBudget = 227 * 1024 - 1024 - kCtrlBytes - kScaleBytes - kXExtra;
   static constexpr int kStages = kBudget / kStageBytes < 8 ? kBudget / kStageBytes : 8;
   static constexpr int kDynBytes = 1024 + kStages * kStageBytes + kXExtra + kScaleBytes + kCtrlBytes;
-  static constexpr bool kOverlap = TN == 256;
-  static constexpr int kAccStride = kOverlap ? 208 : (TN < 32 ? 32 : TN);
-  static constexpr int kSWCol = kOverlap ? 464 : 2 * kAccStride, kSTCol = kSWCol + 4 * kPieces;
-  static constexpr int kUsedCols = kSTCol + 4 * kPieces * kTiles;
+  static constexpr bool kFeed = TN == 256, kOverlap = kFeed;
+  static constexpr int kThreads = 64 + 32 * kEpiWarps + (kFeed ? 128 : 0);   // copies, tensor cores, epilogue, scales
+  static constexpr int kScaleCols = 4 * kPieces * (1 + kTiles), kBufs = kFeed ? 2 : 1;   // the weights' scales, then the tokens'
+  static constexpr int kAccStride = kOverlap ? 512 - kBufs * kScaleCols - TN : (TN < 32 ? 32 : TN);
+  static constexpr int kShared = kOverlap ? TN - kAccStride : 0;             // columns of both accumulators
+  static constexpr int kScaleCol = kAccStride + (kOverlap ? TN : kAccStride);
+  static constexpr int kUsedCols = kScaleCol + kBufs * kScaleCols;
+  static constexpr uint32_t kFullBytes = kSub * (kWBytes + kTBytes + (kFeed ? 0 : kSWBytes + kSTBytes));   // on a stage's barrier
+  static constexpr uint32_t kFeedBytes = kSub * (kSWBytes + kSTBytes);                                     // on the scales' own
   static constexpr uint32_t kTmemCols = kUsedCols <= 128 ? 128 : (kUsedCols <= 256 ? 256 : 512);
   static_assert(kStages >= 3 && (!kXInRing || kXBytes <= kStages * kStageBytes) && kStageBytes % 1024 == 0 && kTBytes % 1024 == 0 && kUsedCols <= 512, "tile does not fit");
 };
@@ -100,6 +107,19 @@ __device__ __forceinline__ uint64_t scales_desc(uint32_t saddr) {
   return (uint64_t)((saddr >> 4) & 0x3FFFu) | (uint64_t)(128 >> 4) << 32 | (uint64_t)1 << 46;
 }
 
+// The same by a warp, for its quarter of the lanes: N columns, each lane's 4-byte cells of 16-byte rows.
+template <int N>
+__device__ __forceinline__ void tmem_store(uint32_t taddr, const uint32_t* v) {
+  static_assert(N == 8 || N == 16, "columns");
+  if constexpr (N == 8)
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                 ::"r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]) : "memory");
+  else
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+                 ::"r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]),
+                   "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]) : "memory");
+}
+
 template <int CG>
 __device__ __forceinline__ void tma_load_scales(uint32_t dst, const CUtensorMap* map, uint32_t bar, int piece, int tile) {
   if constexpr (CG == 1)
@@ -110,6 +130,14 @@ __device__ __forceinline__ void tma_load_scales(uint32_t dst, const CUtensorMap*
     asm volatile(
         "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%3, %4, %5}], [%2];"
         ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(0), "r"(piece), "r"(tile) : "memory");
+}
+
+// The bounded waits for a whole warp: all lanes go on, or all give up.
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
+  return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag));
+}
+__device__ __forceinline__ bool warp_wait_cluster(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
+  return __all_sync(0xffffffffu, mbar_wait_cluster(bar, parity, abort_flag));
 }
 
 // Tile t of the launch: token tiles in groups of eight, all channel tiles of a group before the next group, so that the tiles
@@ -169,7 +197,7 @@ __device__ __forceinline__ void finish(const MxGemm& p, long long at, const uint
 }
 
 template <int GRID, int TN, int CG>
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__(MxSmem<GRID, TN, CG>::kThreads, 1)
 mx_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtensorMap tm_t,
                const __grid_constant__ CUtensorMap tm_sw, const __grid_constant__ CUtensorMap tm_st, const MxGemm p) {
   using L = MxSmem<GRID, TN, CG>;
@@ -187,9 +215,11 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__
   auto accempty_bar = [&](int a) { return smem_u32(bars + 2 * L::kStages + 2 + a); };
   const uint32_t xfull_bar = smem_u32(bars + 2 * L::kStages + 4);
   const uint32_t xready_bar = smem_u32(bars + 2 * L::kStages + 5);
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * L::kStages + 6);
+  auto sfull_bar = [&](int s) { return smem_u32(bars + 2 * L::kStages + 6 + s); };            // kFeed: a stage's scales are here
+  auto sready_bar = [&](int b) { return smem_u32(bars + 3 * L::kStages + 6 + b); };           // ... and in tensor memory
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 3 * L::kStages + 6 + L::kBufs);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
-  static_assert((2 * L::kStages + 6) * 8 + 8 <= L::kCtrlBytes, "control block");
+  static_assert((3 * L::kStages + 6 + L::kBufs) * 8 + 8 <= L::kCtrlBytes, "control block");
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int CL = CG * p.slices;
@@ -209,11 +239,13 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__
       for (int s = 0; s < L::kStages; ++s) {
         mbar_init(full_bar(s), 1);     // the leader's producer announces the bytes of both CTAs
         mbar_init(empty_bar(s), 1);    // commit of the products that read the stage
+        mbar_init(sfull_bar(s), 1);
       }
       for (int a = 0; a < 2; ++a) {
         mbar_init(accfull_bar(a), 1);
         mbar_init(accempty_bar(a), CG * kEpiWarps);
       }
+      for (int b = 0; b < L::kBufs; ++b) mbar_init(sready_bar(b), CG * 4);
       mbar_init(xfull_bar, 1);
       mbar_init(xready_bar, p.slices);
       *abort_flag = 0;
@@ -223,18 +255,18 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__
     }
     __syncwarp();
     asm volatile("bar.arrive 3, 64;" ::: "memory");
-    asm volatile("bar.arrive 2, 320;" ::: "memory");
+    asm volatile("bar.arrive 2, %0;" ::"n"(L::kThreads) : "memory");
     if (CL > 1) cluster_arrive();
   } else if (warp == 1) {
     if (CG == 2) tmem_alloc_pair(smem_u32(tmem_slot), L::kTmemCols);
     else tmem_alloc(smem_u32(tmem_slot), L::kTmemCols);
     tc_fence_before();
-    asm volatile("bar.arrive 2, 320;" ::: "memory");
+    asm volatile("bar.arrive 2, %0;" ::"n"(L::kThreads) : "memory");
     if (CL > 1) cluster_arrive();
     asm volatile("bar.sync 3, 64;" ::: "memory");
   } else {
     if (CL > 1) cluster_arrive();
-    asm volatile("bar.sync 2, 320;" ::: "memory");
+    asm volatile("bar.sync 2, %0;" ::"n"(L::kThreads) : "memory");
   }
   if (CG == 2) cluster_wait();
   tc_fence_after();
@@ -255,7 +287,7 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__
           const int kb = st * L::kSub + u, row = (nt * CG + half) * TW;
           if (CG == 2) tma_load_2d_pair(at + u * L::kWBytes, &tm_w, bar, kb * KB, row);
           else tma_load_2d(at + u * L::kWBytes, &tm_w, bar, kb * KB, row);
-          tma_load_scales<CG>(at + L::kAtSW + u * L::kSWBytes, &tm_sw, bar, kb * L::kPieces, nt * CG + half);
+          tma_load_scales<L::kFeed ? 1 : CG>(at + L::kAtSW + u * L::kSWBytes, &tm_sw, L::kFeed ? sfull_bar(s) : bar, kb * L::kPieces, nt * CG + half);
         }
       };
       auto load_t = [&](int s, int st) {
@@ -267,15 +299,20 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__
           else tma_load_2d(at + L::kAtT + u * L::kTBytes, &tm_t, bar, kb * KB, row);
 #pragma unroll
           for (int i = 0; i < L::kTiles; ++i)   // (both CTAs of a pair need the scales of all the tile's tokens)
-            tma_load_scales<CG>(at + L::kAtST + u * L::kSTBytes + i * L::kSWBytes, &tm_st, bar, kb * L::kPieces, mt * TN / 128 + i);
+            tma_load_scales<L::kFeed ? 1 : CG>(at + L::kAtST + u * L::kSTBytes + i * L::kSWBytes, &tm_st, L::kFeed ? sfull_bar(s) : bar,
+                                               kb * L::kPieces, mt * TN / 128 + i);
         }
+      };
+      auto announce = [&](int s) {
+        if (half == 0) mbar_arrive_expect_tx(full_bar(s), CG * L::kFullBytes);
+        if (L::kFeed) mbar_arrive_expect_tx(sfull_bar(s), L::kFeedBytes);
       };
       // weights do not depend on the kernel before: the first ring of them is requested before waiting for it
       if (cluster < p.total) {
         tile_of(p, cluster, &mt, &nt);
         ahead = min(L::kStages, my_st);
         for (int i = 0; i < ahead; ++i) {
-          if (half == 0) mbar_arrive_expect_tx(full_bar(i), CG * L::kStageBytes);
+          announce(i);
           load_w(i, slice + i * p.slices);
         }
       }
@@ -286,7 +323,7 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__
           const int s = it % L::kStages;
           if (it >= ahead) {
             if (!mbar_wait(empty_bar(s), (uint32_t)((it / L::kStages) & 1) ^ 1u, abort_flag)) { ok = false; break; }
-            if (half == 0) mbar_arrive_expect_tx(full_bar(s), CG * L::kStageBytes);
+            announce(s);
             load_w(s, slice + i * p.slices);
           }
           load_t(s, slice + i * p.slices);
@@ -307,19 +344,19 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__
       const uint16_t mask = (uint16_t)(3u << (rank & ~1));
       const uint64_t w_desc0 = smem_desc_sw128(base), t_desc0 = smem_desc_sw128(base + L::kAtT);
       const uint64_t sw_desc0 = scales_desc(base + L::kAtSW), st_desc0 = scales_desc(base + L::kAtST);
-      const uint32_t sw_col = tmem_base + L::kSWCol, st_col = tmem_base + L::kSTCol;
+      uint32_t sw_col = tmem_base + L::kScaleCol;
       int j = 0, s = 0;
-      uint32_t phase = 0;
+      uint32_t phase = 0, buf = 0, fed = 0;   // kFeed: buffer of scales and the phase of its barrier
       bool ok = true;
       for (int t = cluster; ok && t < p.total; t += n_clusters, ++j) {
         int mt, nt;
         tile_of(p, t, &mt, &nt);
         const int acc = j & 1;
-        const uint32_t st_use = st_col + (uint32_t)(TN == 64 ? (mt & 1) * 2 : 0);   // the columns of this half of the 128 tokens
+        const uint32_t half_col = TN == 64 ? (mt & 1) * 2 : 0;   // the columns of this half of the 128 tokens
         if (L::kOverlap) {
-          if (j && !mbar_wait_cluster(accempty_bar(0), (uint32_t)(j - 1) & 1u, abort_flag)) break;
+          if (j && !mbar_wait_relaxed(accempty_bar(0), (uint32_t)(j - 1) & 1u, abort_flag)) break;
         } else {
-          if (!mbar_wait_cluster(accempty_bar(acc), (((uint32_t)j >> 1) & 1u) ^ 1u, abort_flag)) break;
+          if (!mbar_wait_relaxed(accempty_bar(acc), (((uint32_t)j >> 1) & 1u) ^ 1u, abort_flag)) break;
         }
         tc_fence_after();
         const uint32_t d = tmem_base + (uint32_t)(acc * L::kAccStride);
@@ -330,21 +367,31 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__
           const uint32_t o = (uint32_t)(s * (L::kStageBytes >> 4));
 #pragma unroll
           for (int u = 0; u < L::kSub; ++u) {
+if (L::kFeed) {
+              if (!mbar_wait_relaxed(sready_bar(buf), fed, abort_flag)) { ok = false; break; }
+              tc_fence_after();
+              sw_col = tmem_base + L::kScaleCol + buf * L::kScaleCols;
+              if (++buf == L::kBufs) { buf = 0; fed ^= 1u; }
+            } else {
 #pragma unroll
-            for (int c = 0; c < L::kPieces; ++c) {
-              copy_scales<CG>(sw_col + 4 * c, sw_desc0 + o + u * (L::kSWBytes >> 4) + c * (kMxTile >> 4));
+              for (int c = 0; c < L::kPieces; ++c) {
+                copy_scales<CG>(sw_col + 4 * c, sw_desc0 + o + u * (L::kSWBytes >> 4) + c * (kMxTile >> 4));
 #pragma unroll
-              for (int k = 0; k < L::kTiles; ++k)
-                copy_scales<CG>(st_col + 4 * (c * L::kTiles + k), st_desc0 + o + u * (L::kSTBytes >> 4) + k * (L::kSWBytes >> 4) + c * (kMxTile >> 4));
+                for (int k = 0; k < L::kTiles; ++k)
+                  copy_scales<CG>(sw_col + 4 * (L::kPieces + c * L::kTiles + k),
+                                  st_desc0 + o + u * (L::kSTBytes >> 4) + k * (L::kSWBytes >> 4) + c * (kMxTile >> 4));
+              }
             }
+            const uint32_t st_col = sw_col + 4 * L::kPieces + half_col;
 #pragma unroll
             for (int k = 0; k < 4; ++k) {   // 64 contraction indices: 32 bytes on, 2 in the descriptors' units of 16
               constexpr int kPer = 4 / L::kPieces;   // products per piece of scales
               const int c = k / kPer, sf = k % kPer * 2;
               umma_mx4<GRID, CG>(d, w_desc0 + o + u * (L::kWBytes >> 4) + 2 * k, t_desc0 + o + u * (L::kTBytes >> 4) + 2 * k,
-                                 mx_instr_desc(GRID, kDescM, TN, sf), sw_col + 4 * c, st_use + 4 * c * L::kTiles, u + k == 0 ? more : 1u);
+                                 mx_instr_desc(GRID, kDescM, TN, sf), sw_col + 4 * c, st_col + 4 * c * L::kTiles, u + k == 0 ? more : 1u);
             }
           }
+          if (!ok) break;
           more = 1;
           if (CG == 2) umma_commit_pair(empty_bar(s), mask);
           else umma_commit(empty_bar(s));
@@ -357,6 +404,42 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__
     }
     __syncwarp();
     if (CL > 1 && CG == 1) cluster_wait();
+  } else if (L::kFeed && warp >= 2 + kEpiWarps) {
+    // ---------------------------------------------------------------- scales (of the CTA's own shared memory and lanes)
+    const uint32_t q = warp & 3, lead = (uint32_t)(rank & ~1);
+    const uint32_t lanes = tmem_base + ((q * 32) << 16) + L::kScaleCol;
+    int it = 0, s = 0, buf = 0, s_before = 0;   // s_before: stage of the K-block that had the buffer before
+    uint32_t phase = 0, phase_before = 0;
+    bool ok = true;
+    for (int t = cluster; ok && t < p.total; t += n_clusters) {
+      for (int i = 0; i < my_st; ++i, ++it) {
+        if (!warp_wait(sfull_bar(s), phase, abort_flag)) { ok = false; break; }
+        const unsigned char* st = tiles + s * L::kStageBytes + lane * 16;
+        constexpr int n = L::kPieces * (1 + L::kTiles);
+        uint32_t v[4 * n];
+#pragma unroll
+        for (int e = 0; e < n; ++e) {   // the weights' pieces, then for each group of blocks the tokens' tiles
+          const int c = (e - L::kPieces) / L::kTiles, k = (e - L::kPieces) % L::kTiles;
+          const uint4 w = *reinterpret_cast<const uint4*>(st + (e < L::kPieces ? L::kAtSW + e * kMxTile : L::kAtST + k * L::kSWBytes + c * kMxTile));
+          v[4 * e] = w.x; v[4 * e + 1] = w.y; v[4 * e + 2] = w.z; v[4 * e + 3] = w.w;
+        }
+        if (it >= L::kBufs) {           // the products that read this buffer are done
+          if (!warp_wait(empty_bar(s_before), phase_before, abort_flag)) { ok = false; break; }
+          tc_fence_after();
+          if (++s_before == L::kStages) { s_before = 0; phase_before ^= 1u; }
+        }
+        __syncwarp();
+        const uint32_t col = lanes + (uint32_t)buf * L::kScaleCols;
+#pragma unroll
+        for (int e = 0; e < 4 * n; e += 4 * L::kPieces) tmem_store<4 * L::kPieces>(col + e, v + e);
+        asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_peer_relaxed(peer_addr(sready_bar(buf), lead));
+        if (++buf == L::kBufs) buf = 0;
+        if (++s == L::kStages) { s = 0; phase ^= 1u; }
+      }
+    }
   } else {
     // ---------------------------------------------------------------- epilogue
     constexpr int EC = 16;                              // accumulator columns (tokens) moved at a time
@@ -383,13 +466,13 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__
           __syncwarp();
           for (int i = lane; i < own; i += 32) sc[i] = token_scale(mt * TN + slice * own + i);
           __syncwarp();
-          if (!mbar_wait(accfull_bar(acc), ((uint32_t)j >> 1) & 1u, abort_flag)) break;
+          if (!warp_wait(accfull_bar(acc), ((uint32_t)j >> 1) & 1u, abort_flag)) break;
           tc_fence_after();
           if (L::kXInRing) {
             // this CTA's tensor cores are done with its ring: it may be written to; and so are all the others'
             if (ew == 0 && lane == 0)
               for (int o = 0; o < p.slices; ++o) mbar_arrive_peer(peer_addr(xready_bar, (uint32_t)o));
-            if (!mbar_wait_cluster(xready_bar, 0u, abort_flag)) break;
+            if (!warp_wait_cluster(xready_bar, 0u, abort_flag)) break;
           }
           const uint32_t mine = smem_u32(xbuf) + (uint32_t)(slice * groups * TW + q * 32 + lane) * 16u;
           const uint32_t addr = tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(acc * L::kAccStride);
@@ -413,7 +496,7 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__
               }
             }
           }
-          if (!mbar_wait_cluster(xfull_bar, 0u, abort_flag)) break;
+          if (!warp_wait_cluster(xfull_bar, 0u, abort_flag)) break;
           const int m_own = mt * TN + slice * own;
           const long long y = (long long)m_own * p.ldy + n;
           const uint32_t slot = (uint32_t)groups * TW * 16u;   // from one sender's cells to the next one's
@@ -437,11 +520,11 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__
       __syncwarp();
       for (int i = lane; i < L::kWarpTokens; i += 32) sc[i] = token_scale(mt * TN + (i / EC) * 2 * EC + part * EC + i % EC);
       __syncwarp();
-      if (!mbar_wait(accfull_bar(acc), ((uint32_t)j >> 1) & 1u, abort_flag)) break;
+      if (!warp_wait(accfull_bar(acc), ((uint32_t)j >> 1) & 1u, abort_flag)) break;
       tc_fence_after();
       // Pieces of EC columns; the next one's way out of tensor memory overlaps this one's arithmetic and stores.  Overlapping
       // accumulators: from the end that the next tile's products write to (the first one's last columns, the second one's
-      // first); once two pieces per warp are out, the next tile may start.
+      // first); once those are out, the next tile may start.
       constexpr int kPieces = TN >= 2 * EC ? TN / (2 * EC) : 1;
       const bool down = L::kOverlap && acc == 0;
       const uint32_t addr = tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(acc * L::kAccStride + part * EC);
@@ -451,7 +534,7 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__
         tc_fence_before();
         __syncwarp();
         if (lane == 0) {
-          if (CG == 2) mbar_arrive_peer(peer_addr(accempty_bar(a), (uint32_t)(rank & ~1)));
+          if (CG == 2) mbar_arrive_peer_relaxed(peer_addr(accempty_bar(a), (uint32_t)(rank & ~1)));
           else mbar_arrive(accempty_bar(a));
         }
       };
@@ -462,7 +545,7 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__
 #pragma unroll
         for (int i = 0; i < kPieces; ++i) {
           tmem_wait_ld16(v[i & 1]);
-          if (L::kOverlap && i == 1) emptied(0);
+          if (L::kOverlap && i == (L::kShared + 2 * EC - 1) / (2 * EC) - 1) emptied(0);
           if (i + 1 < kPieces) tmem_ld_async<EC>(addr + 2 * EC * piece(i + 1), v[(i + 1) & 1]);
           const int at = 2 * EC * piece(i), left = p.M - m_first - at;   // tokens from this piece's first on
           if (left <= 0) continue;               // the same for the whole warp
@@ -599,7 +682,7 @@ ocs_status launch_tiles(const Product& g, int slices, bool overlap, cudaStream_t
   const long long slots = cluster_capacity(cl) / cl;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)((total < slots ? total : slots) * cl), 1, 1);
-  cfg.blockDim = dim3(kThreads, 1, 1);
+  cfg.blockDim = dim3(L::kThreads, 1, 1);
   cfg.dynamicSmemBytes = L::kDynBytes;
   cfg.stream = stream;
   cudaLaunchAttribute attr[2];

@@ -122,7 +122,34 @@ def row_linear_forward(L: RowLayer, x, a_signed: bool = True, a_bits: int = 8, o
                              out_dtype=out_dtype, dev_status=dev_status)
 
 
+# ------------------------------------------------------------- linear layers on a block-scaled 4-bit grid
+@dataclass
+class Mx4Layer:
+    """A split linear layer on a block-scaled 4-bit grid; its activations go to the same grid, row by row."""
+    weights: B.Mx4             # [O] rows of C + S channels
+    idx_map: torch.Tensor      # int32 [C + S]
+    bias: torch.Tensor | None  # fp32 [O]
+    C: int
+    O: int
+    S: int
+
+
+def prepare_mx4_layer(W, bias, ratio: float, grid: int = B.MX4_E4M3, qa_bits: int = 0, dev_status=None) -> Mx4Layer:
+    """W fp32 [O, C] on the device -> Mx4Layer (ocs_split, then ocs_quantize_mx4)."""
+    O, Cn = W.shape
+    S = B.ocs_num_splits(Cn, ratio)
+    W_out, idx_map, _, _ = B.ocs_split(W.contiguous(), S, qa_bits=qa_bits, dev_status=dev_status, want_order=False)
+    return Mx4Layer(B.ocs_quantize_mx4(W_out[:, :Cn + S], grid, dev_status=dev_status), idx_map, bias, Cn, O, S)
+
+
+def mx4_linear_forward(L: Mx4Layer, x, out_dtype=None, dev_status=None):
+    """x fp32 / fp16 / bf16 [M, C] -> [M, O] of x's type or out_dtype (ocs_linear_mx4)."""
+    return B.ocs_linear_mx4(x, L.weights, idx_map=L.idx_map, S=L.S, bias=L.bias, out_dtype=out_dtype, dev_status=dev_status)
+
+
 def _any_linear_forward(L, x, a_signed: bool, a_bits: int, dev_status):
+    if isinstance(L, Mx4Layer):
+        return mx4_linear_forward(L, x, dev_status=dev_status)
     if isinstance(L, RowLayer):
         return row_linear_forward(L, x, a_signed, a_bits, dev_status=dev_status)
     return linear_forward(L, x, a_signed, a_bits, dev_status)
@@ -247,14 +274,19 @@ def _side_stream(device, which: int = 0):
     return _SIDE_STREAMS[key]
 
 
-def prepare_lstm(cfg, device, dev_status=None, fold: bool = False, row_scales: bool = False):
+def prepare_lstm(cfg, device, dev_status=None, fold: bool = False, row_scales: bool = False, mx4: int | None = None):
     """cfg from ocs_inputs.configs.config5 -> dict of QLayers and the embedding table.  row_scales: RowLayers instead
-    (a scale per output channel and per token; no clip search)."""
+    (a scale per output channel and per token; no clip search).  mx4 (MX4_E8M0 or MX4_E4M3): Mx4Layers, weights and
+    activations on that 4-bit grid (cfg's bits do not count)."""
     p = cfg["params"]
     mode = B.CLIP_MSE if cfg["clip"] == "mse" else B.CLIP_NONE
-    if row_scales:
-        assert mode == B.CLIP_NONE and not fold
+    if row_scales or mx4 is not None:
+        assert mode == B.CLIP_NONE and not fold and not (row_scales and mx4 is not None)
         names = [(f"{nm}{l}", f"{bn}{l}") for l in range(2) for nm, bn in (("W_ih", "b_ih"), ("W_hh", "b_hh"))] + [("W_dec", "b_dec")]
+        if mx4 is not None:
+            out = {nm: prepare_mx4_layer(torch.from_numpy(p[nm]).to(device), torch.from_numpy(p[bn]).to(device), cfg["ratio"], mx4,
+                                         dev_status=dev_status) for nm, bn in names}
+            return {"emb": torch.from_numpy(p["emb"]).to(device), **out}
         out = {nm: prepare_row_layer(torch.from_numpy(p[nm]).to(device), torch.from_numpy(p[bn]).to(device), cfg["ratio"],
                                      cfg["w_bits"], dev_status=dev_status) for nm, bn in names}
         return {"emb": torch.from_numpy(p["emb"]).to(device), **out}
