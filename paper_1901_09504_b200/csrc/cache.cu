@@ -111,7 +111,7 @@ __global__ void __launch_bounds__(256) cache_write_kernel(const CacheArgs a, int
       const int c = (lane * U + i) * kUnit;
       if (c >= a.dim) break;
       const uint32_t mb = GRID == OCS_GRID_E8M0 ? m : mine[i];
-      const MxScale s = mx4_scale<GRID>(mb, k);
+      const MxScale s = mx4_scale<GRID, T>(mb, k);
       uint32_t w[2];
       v[i].template codes<GRID>(s, w);
       *reinterpret_cast<uint2*>(codes + c / 2) = make_uint2(w[0], w[1]);

@@ -41,30 +41,28 @@ __device__ __forceinline__ void store_block(const MxRows& p, long long r, int b,
 
 // E8M0: blocks know nothing of their row; thread g has block g % nb of row g / nb.
 template <typename T, int ALIGN>
-__global__ void __launch_bounds__(256) mx4_blocks_kernel(const T* __restrict__ X, const MxRows p) {
+__global__ void __launch_bounds__(256, sizeof(T) == 2 ? 4 : 3) mx4_blocks_kernel(const T* __restrict__ X, const MxRows p) {
   grid_launch_dependents();
-  const long long g = (long long)blockIdx.x * 256 + threadIdx.x;
-  const long long r = g / p.nb;
+  const unsigned long long g = (unsigned long long)blockIdx.x * 256 + threadIdx.x;
+  const long long r = g >> 32 ? (long long)(g / (unsigned)p.nb) : (long long)((unsigned)g / (unsigned)p.nb);
   if (r >= p.rows) return;
-  const int b = (int)(g - r * p.nb);
-  const T* x = X + r * p.ldx;
+  const int b = (int)(g - (unsigned long long)r * p.nb);
   Block<T, 32> v;
-  if ((b + 1) * 32 <= p.C) v.template load<ALIGN>(x + b * 32);
-  else v.gather(x, b * 32, p.C, p.K, p.idx_map, p.dev_status);
+  v.template load_block<ALIGN>(X + r * p.ldx, b, p.C, p.K, p.idx_map, p.dev_status);
   const uint32_t m = v.max_bits();
   if (m >= 0x7f800000u) flag(p.dev_status, OCS_DEV_NONFINITE);
-  const MxScale s = mx4_scale<OCS_GRID_E8M0>(m, 0);
+  const MxScale s = mx4_scale<OCS_GRID_E8M0, T>(m, 0);
   uint32_t c[4];
   v.template codes<OCS_GRID_E8M0>(s, c);
   store_block<OCS_GRID_E8M0>(p, r, b, s, c);
 }
 
-constexpr int kMaxThreads = 1024;
+constexpr int kRowThreads = 512;
 
-// E4M3: a row's scale is that of its largest magnitude, so the row waits in registers, blockDim.x threads with NV blocks each;
+// E4M3: a row's scale is that of its largest magnitude, so the row waits in registers: blockDim.x threads with NV blocks each,
 // blockDim.y rows per CTA.
 template <typename T, int ALIGN, int NV>
-__global__ void __launch_bounds__(kMaxThreads) mx4_rows_kernel(const T* __restrict__ X, const MxRows p) {
+__global__ void __launch_bounds__(kRowThreads, NV == 1 || sizeof(T) == 4 ? 2 : 3) mx4_rows_kernel(const T* __restrict__ X, const MxRows p) {
   __shared__ uint32_t s_max[32];
   grid_launch_dependents();
   const int G = blockDim.x, tx = threadIdx.x, lane = tx & 31;
@@ -77,8 +75,7 @@ __global__ void __launch_bounds__(kMaxThreads) mx4_rows_kernel(const T* __restri
   for (int i = 0; i < NV; ++i) {
     const int b = tx + i * G;
     if (b >= p.nb || !live) v[i].clear();
-    else if ((b + 1) * 16 <= p.C) v[i].template load<ALIGN>(x + b * 16);
-    else v[i].gather(x, b * 16, p.C, p.K, p.idx_map, p.dev_status);
+    else v[i].template load_block<ALIGN>(x, b, p.C, p.K, p.idx_map, p.dev_status);
   }
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
@@ -102,7 +99,7 @@ __global__ void __launch_bounds__(kMaxThreads) mx4_rows_kernel(const T* __restri
   for (int i = 0; i < NV; ++i) {
     const int b = tx + i * G;
     if (b >= p.nb) break;
-    const MxScale s = mx4_scale<OCS_GRID_E4M3>(mine[i], k);
+    const MxScale s = mx4_scale<OCS_GRID_E4M3, T>(mine[i], k);
     uint32_t c[2];
     v[i].template codes<OCS_GRID_E4M3>(s, c);
     store_block<OCS_GRID_E4M3>(p, r, b, s, c);
@@ -111,40 +108,38 @@ __global__ void __launch_bounds__(kMaxThreads) mx4_rows_kernel(const T* __restri
 
 // E4M3, rows that no CTA's registers hold: read twice, the second time from L2.
 template <typename T, int ALIGN>
-__global__ void __launch_bounds__(kMaxThreads, 1) mx4_long_rows_kernel(const T* __restrict__ X, const MxRows p) {
-  __shared__ uint32_t s_max[32];
+__global__ void __launch_bounds__(kRowThreads, 2) mx4_long_rows_kernel(const T* __restrict__ X, const MxRows p) {
+  __shared__ uint32_t s_max[2][16];
   grid_launch_dependents();
   const int tx = threadIdx.x, lane = tx & 31;
-  for (long long r = blockIdx.x; r < p.rows; r += gridDim.x) {
+  int odd = 0;
+  for (long long r = blockIdx.x; r < p.rows; r += gridDim.x, odd ^= 1) {
     const T* x = X + r * p.ldx;
-    auto load = [&](Block<T, 16>& v, int b) {
-      if ((b + 1) * 16 <= p.C) v.template load<ALIGN>(x + b * 16);
-      else v.gather(x, b * 16, p.C, p.K, p.idx_map, p.dev_status);
-    };
     uint32_t m = 0;
-    for (int b = tx; b < p.nb; b += kMaxThreads) {
+#pragma unroll 2
+    for (int b = tx; b < p.nb; b += kRowThreads) {
       Block<T, 16> v;
-      load(v, b);
+      v.template load_block<ALIGN>(x, b, p.C, p.K, p.idx_map, p.dev_status);
       m = max(m, v.max_bits());
     }
     m = __reduce_max_sync(0xffffffffu, m);
-    if (lane == 0) s_max[tx >> 5] = m;
+    if (lane == 0) s_max[odd][tx >> 5] = m;
     __syncthreads();
-    m = __reduce_max_sync(0xffffffffu, s_max[lane]);
+    m = __reduce_max_sync(0xffffffffu, s_max[odd][lane & 15]);
     const int k = mx4_row_exponent(m);
     if (tx == 0) {
       p.row_scales[r] = two_to(k);
       if (m >= 0x7f800000u) flag(p.dev_status, OCS_DEV_NONFINITE);
     }
-    for (int b = tx; b < p.nb; b += kMaxThreads) {
+#pragma unroll 2
+    for (int b = tx; b < p.nb; b += kRowThreads) {
       Block<T, 16> v;
-      load(v, b);
-      const MxScale s = mx4_scale<OCS_GRID_E4M3>(v.max_bits(), k);
+      v.template load_block<ALIGN>(x, b, p.C, p.K, p.idx_map, p.dev_status);
+      const MxScale s = mx4_scale<OCS_GRID_E4M3, T>(v.max_bits(), k);
       uint32_t c[2];
       v.template codes<OCS_GRID_E4M3>(s, c);
       store_block<OCS_GRID_E4M3>(p, r, b, s, c);
     }
-    __syncthreads();
   }
 }
 
@@ -158,11 +153,14 @@ ocs_status launch_quantize(const T* X, const MxRows& p, ocs_grid grid, cudaStrea
     return launch_status();
   }
   LaunchScope ls("mx4_rows_kernel", stream);
-  if (p.nb > 2 * kMaxThreads) {
-    mx4_long_rows_kernel<T, ALIGN><<<(unsigned)(p.rows < 2 * kNumSMs ? p.rows : 2 * kNumSMs), kMaxThreads, 0, stream>>>(X, p);
+  if (p.nb > 2 * kRowThreads) {
+    const long long most = 2 * kNumSMs;
+    mx4_long_rows_kernel<T, ALIGN><<<(unsigned)(p.rows < most ? p.rows : most), kRowThreads, 0, stream>>>(X, p);
     return launch_status();
   }
-  const int nv = p.nb > 512 ? 2 : 1, G = ((p.nb + nv - 1) / nv + 31) / 32 * 32, R = G <= 128 ? 256 / G : 1;
+  // few rows: a thread for every block; many: two blocks each
+  const int nv = p.nb > kRowThreads || (p.rows > kNumSMs && p.nb > 32) ? 2 : 1;
+  const int G = ((p.nb + nv - 1) / nv + 31) / 32 * 32, R = G <= 128 && p.rows > kNumSMs ? 256 / G : 1;
   const long long ctas = (p.rows + R - 1) / R;
   if (ctas > 0x7fffffff) return OCS_ERR_UNSUPPORTED;
   if (nv == 1) mx4_rows_kernel<T, ALIGN, 1><<<(unsigned)ctas, dim3(G, R), 0, stream>>>(X, p);
@@ -176,17 +174,18 @@ ocs_status launch_quantize(const void* X_, const MxRows& p, ocs_grid grid, cudaS
   const uintptr_t a = reinterpret_cast<uintptr_t>(X) | (p.rows > 1 ? (uintptr_t)(p.ldx * (int64_t)sizeof(T)) : 0);
   if (a % 32 == 0) return launch_quantize<T, 32>(X, p, grid, stream);
   if (a % 16 == 0) return launch_quantize<T, 16>(X, p, grid, stream);
-  return launch_quantize<T, (int)sizeof(T)>(X, p, grid, stream);
+  return launch_quantize<T, 0>(X, p, grid, stream);
 }
 
-// ---- codes to values: 16 of a row per thread
-template <typename T>
-__global__ void __launch_bounds__(256) mx4_values_kernel(const MxRows p, int grid, T* __restrict__ Y, long long ldy, int wide) {
+// ---- codes to values
+// Rows that start at 16-byte boundaries: 16 values per thread, stored 32 (WIDE) or 16 bytes at a time.
+template <typename T, bool WIDE>
+__global__ void __launch_bounds__(256) mx4_values_kernel(const MxRows p, int grid, T* __restrict__ Y, long long ldy) {
   const int per = (p.K + 15) / 16;
-  const long long g = (long long)blockIdx.x * 256 + threadIdx.x;
-  const long long r = g / per;
+  const unsigned long long g = (unsigned long long)blockIdx.x * 256 + threadIdx.x;
+  const long long r = g >> 32 ? (long long)(g / (unsigned)per) : (long long)((unsigned)g / (unsigned)per);
   if (r >= p.rows) return;
-  const int u = (int)(g - r * per), c0 = u * 16, left = p.K - c0;
+  const int u = (int)(g - (unsigned long long)r * per), c0 = u * 16, left = p.K - c0;
   const uint8_t* src = p.codes + r * p.ld_codes + u * 8;
   uint32_t w[2] = {0, 0};
   if (left >= 15 && p.code_align >= 8) {
@@ -213,9 +212,15 @@ __global__ void __launch_bounds__(256) mx4_values_kernel(const MxRows p, int gri
       out[8 * i + 2 * e + 1] = from_f32<T>(__fmul_rn(f.y, unit));
     }
   }
-  if (wide && left >= 16) {
+  const uint32_t* o = reinterpret_cast<const uint32_t*>(out);
+  if (left >= 16) {
+    if constexpr (WIDE) {
 #pragma unroll
-    for (int i = 0; i < (int)sizeof(T); ++i) reinterpret_cast<uint4*>(y)[i] = reinterpret_cast<uint4*>(out)[i];
+      for (int i = 0; i < 4 * (int)sizeof(T); i += 8) store32(reinterpret_cast<uint32_t*>(y) + i, o + i);
+    } else {
+#pragma unroll
+      for (int i = 0; i < (int)sizeof(T); ++i) reinterpret_cast<uint4*>(y)[i] = make_uint4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+    }
   } else {
 #pragma unroll
     for (int i = 0; i < 16; ++i)
@@ -223,14 +228,51 @@ __global__ void __launch_bounds__(256) mx4_values_kernel(const MxRows p, int gri
   }
 }
 
+// Rows that start anywhere: a warp takes 512 values, two per lane and step, so that its stores are dense whatever their
+// alignment.
+template <typename T>
+__global__ void __launch_bounds__(256) mx4_values_any_kernel(const MxRows p, int grid, T* __restrict__ Y, long long ldy) {
+  const int per = (p.K + 511) / 512, lane = threadIdx.x & 31;
+  const unsigned long long g = (unsigned long long)blockIdx.x * 8 + (threadIdx.x >> 5);
+  const long long r = g >> 32 ? (long long)(g / (unsigned)per) : (long long)((unsigned)g / (unsigned)per);
+  if (r >= p.rows) return;
+  const int c0 = (int)(g - (unsigned long long)r * per) * 512 + 2 * lane;
+  const uint8_t* src = p.codes + r * p.ld_codes + c0 / 2;
+  const float row = grid == OCS_GRID_E8M0 ? 1.0f : __ldg(p.row_scales + r);
+  T* y = Y + r * ldy + c0;
+  const bool pairs = reinterpret_cast<uintptr_t>(y) % (2 * sizeof(T)) == 0;
+  uint32_t code[8], byte[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int c = c0 + 64 * i;
+    code[i] = c < p.K ? __ldg(src + 32 * i) : 0u;
+    byte[i] = c < p.K ? __ldg(p.scales + mx4_scale_at(r, grid == OCS_GRID_E8M0 ? c / 32 : c / 16, p.chunks)) : 0u;
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int c = c0 + 64 * i;
+    const float unit = grid == OCS_GRID_E8M0 ? e8m0_value(byte[i]) : __fmul_rn(e4m3_value(byte[i]), row);
+    const float2 f = e2m1_pair(code[i]);
+    struct alignas(2 * sizeof(T)) Two { T a, b; } v{from_f32<T>(__fmul_rn(f.x, unit)), from_f32<T>(__fmul_rn(f.y, unit))};
+    if (pairs && c + 1 < p.K) *reinterpret_cast<Two*>(y + 64 * i) = v;
+    else {
+      if (c < p.K) y[64 * i] = v.a;
+      if (c + 1 < p.K) y[64 * i + 1] = v.b;
+    }
+  }
+}
+
 template <typename T>
 ocs_status launch_values(const MxRows& p, ocs_grid grid, void* Y_, long long ldy, cudaStream_t stream) {
   T* Y = static_cast<T*>(Y_);
-  const long long ctas = (p.rows * ((p.K + 15) / 16) + 255) / 256;
-  if (ctas > 0x7fffffff) return OCS_ERR_UNSUPPORTED;
   const uintptr_t a = reinterpret_cast<uintptr_t>(Y) | (p.rows > 1 ? (uintptr_t)(ldy * (int64_t)sizeof(T)) : 0);
+  const bool any = a % 16 != 0;
+  const long long ctas = any ? (p.rows * ((p.K + 511) / 512) + 7) / 8 : (p.rows * ((p.K + 15) / 16) + 255) / 256;
+  if (ctas > 0x7fffffff) return OCS_ERR_UNSUPPORTED;
   LaunchScope ls("mx4_values_kernel", stream);
-  mx4_values_kernel<T><<<(unsigned)ctas, 256, 0, stream>>>(p, grid, Y, ldy, a % 16 == 0);
+  if (any) mx4_values_any_kernel<T><<<(unsigned)ctas, 256, 0, stream>>>(p, grid, Y, ldy);
+  else if (a % 32 == 0) mx4_values_kernel<T, true><<<(unsigned)ctas, 256, 0, stream>>>(p, grid, Y, ldy);
+  else mx4_values_kernel<T, false><<<(unsigned)ctas, 256, 0, stream>>>(p, grid, Y, ldy);
   return launch_status();
 }
 

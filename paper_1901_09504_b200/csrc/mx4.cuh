@@ -46,6 +46,13 @@ __device__ __forceinline__ void e2m1_values(uint32_t codes, __half2* v) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) v[i] = *reinterpret_cast<__half2*>(&r[i]);
 }
+// One byte of codes as two values.  (The conversion instruction gave zeros here, on a byte that comes straight from a load:
+// the upper bytes of the halves are picked from a table instead.)
+__device__ __forceinline__ float2 e2m1_pair(uint32_t code) {
+  const uint32_t magnitude = __byte_perm(0x3E3C3800u, 0x46444240u, (code & 7u) << 4 | (code & 0x70u) << 8);
+  const uint32_t h = magnitude | (code & 8u) << 12 | (code & 0x80u) << 24;
+  return __half22float2(*reinterpret_cast<const __half2*>(&h));
+}
 __device__ __forceinline__ uint32_t e4m3_byte(float v) {
   uint16_t r;
   asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(0.0f), "f"(v));
@@ -70,36 +77,51 @@ __device__ __forceinline__ int mx4_row_exponent(uint32_t max_bits) {
 }
 __device__ __forceinline__ float two_to(int k) { return __uint_as_float((uint32_t)(k + 127) << 23); }
 
-// A block's scale from the bits of its largest magnitude: the stored byte, and what takes a value to code units (a factor,
-// `inv`; `unit` is its exact counterpart).  k: the row's exponent (E4M3).
+// A block's scale from the bits of its largest magnitude: the stored byte, and what takes a value to code units: the factor
+// inv; E4M3 with fp32 values: the exact factor `down` to the row's units, the scale u there and its reciprocal.
+// k: the row's exponent (E4M3).
 struct MxScale {
   uint32_t byte;
-  float unit, inv;
+  float inv, down, u;
 };
-template <int GRID>
+template <int GRID, typename T>
 __device__ __forceinline__ MxScale mx4_scale(uint32_t max_bits, int k) {
   MxScale s;
   if constexpr (GRID == OCS_GRID_E8M0) {
     s.byte = (uint32_t)max((int)(min(max_bits, 0x7f7fffffu) >> 23) - 2, 0);
-    s.unit = e8m0_value(s.byte);
     s.inv = e8m0_inverse(s.byte);
   } else {
-    s.byte = e4m3_byte(__fdiv_rn(__fmul_rn(__uint_as_float(max_bits), two_to(-k)), 6.0f));
-    s.unit = __fmul_rn(e4m3_value(s.byte), two_to(k));
-    s.inv = s.byte ? __frcp_rn(s.unit) : 0.0f;
+    s.down = two_to(-k);
+    s.byte = e4m3_byte(__fdiv_rn(__fmul_rn(__uint_as_float(max_bits), s.down), 6.0f));
+    s.u = e4m3_value(s.byte);
+    s.inv = s.byte ? __frcp_rn(s.u) : 0.0f;
+    if (sizeof(T) == 2) s.inv = __fmul_rn(s.inv, s.down);   // (exact: within 2^-126 and 2^126)
   }
   return s;
 }
 
-// x in units of the block's scale, as the rounding to e2m1 needs it.  E8M0: exact.  E4M3 with 16-bit x: a value x / unit is
-// either a border between two codes or at least 2^-13 away from each (x has at most 11 bits, a border times the unit at most
-// 7), so that the product with the rounded reciprocal, rounded to multiples of 2^-14, falls on the right side and borders on
-// themselves: one fused multiply-add and one subtraction instead of a division.  E4M3 with fp32 x: the rounded quotient.
+// x in units of the block's scale, as the rounding to e2m1 needs it.  E8M0: exact.
+// E4M3 with 16-bit x: a value x / unit is either a border between two codes or at least 2^-13 away from each (x has at most
+// 11 bits, a border times the unit at most 7), so that the product with the rounded reciprocal, rounded to multiples of
+// 2^-14, falls on the right side and borders on themselves: one fused multiply-add and one subtraction instead of a division.
+// E4M3 with fp32 x: the rounded quotient, by Markstein's correction.  With z = x / r (exact), u = unit / r (an e4m3 number: 4
+// bits), y = rn(1 / u) and t = rn(z y), which is within two units of the quotient, z - t u has at most 6 bits and one
+// fused multiply-add finds it exactly; t + (z - t u) y is then the quotient up to 2^-22 units in the last place, and rounds
+// as the quotient does, since that (24 bits over 4) is never within 1/30 unit of the middle between two numbers unless it is
+// one of them.  (Values z below 2^-100 may lose bits on the way; their code is 0 either way.)
 template <int GRID, typename T>
 __device__ __forceinline__ float mx4_units(float x, const MxScale& s) {
   if constexpr (GRID == OCS_GRID_E8M0) return __fmul_rn(x, s.inv);
   else if constexpr (sizeof(T) == 2) return copysignf(__fsub_rn(fmaf(x, s.inv, 768.0f), 768.0f), x);   // (zeros keep x's sign)
-  else return s.byte ? __fdiv_rn(x, s.unit) : copysignf(0.0f, x);
+  else {
+    const float z = __fmul_rn(x, s.down), t = __fmul_rn(z, s.inv);
+    return copysignf(fmaf(fmaf(-t, s.u, z), s.inv, t), x);
+  }
+}
+
+__device__ __forceinline__ void store32(uint32_t* dst, const uint32_t* v) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+               ::"l"(dst), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]) : "memory");
 }
 
 // N consecutive elements of a row in registers.
@@ -107,7 +129,8 @@ template <typename T, int N>
 struct Block {
   static constexpr int W = N * (int)sizeof(T) / 4;
   uint32_t w[W];
-  // x aligned to ALIGN bytes (32, 16, or its element)
+  // x aligned to ALIGN bytes: 32, 16, or (0) its element.  The last reads the 16-byte pieces around the block and shifts it
+  // out of them: up to 15 bytes before x and 16 behind the block have to belong to the row.
   template <int ALIGN>
   __device__ __forceinline__ void load(const T* x) {
     if constexpr (ALIGN == 32) {
@@ -122,41 +145,68 @@ struct Block {
         const uint4 v = __ldg(reinterpret_cast<const uint4*>(x) + i / 4);
         w[i] = v.x; w[i + 1] = v.y; w[i + 2] = v.z; w[i + 3] = v.w;
       }
-    } else if constexpr (sizeof(T) == 4) {
-#pragma unroll
-      for (int i = 0; i < W; ++i) w[i] = __ldg(reinterpret_cast<const uint32_t*>(x) + i);
-    } else if (reinterpret_cast<uintptr_t>(x) & 2) {
-      // between two half words the words in the middle are aligned
-      const uint16_t* h = reinterpret_cast<const uint16_t*>(x);
-      uint32_t before = __ldg(h);
-#pragma unroll
-      for (int i = 0; i < W - 1; ++i) {
-        const uint32_t v = __ldg(reinterpret_cast<const uint32_t*>(h + 1) + i);
-        w[i] = __byte_perm(before, v, 0x5410);
-        before = v >> 16;
-      }
-      w[W - 1] = before | (uint32_t)__ldg(h + N - 1) << 16;
     } else {
+      const uintptr_t at = reinterpret_cast<uintptr_t>(x);
+      const uint4* c = reinterpret_cast<const uint4*>(at & ~(uintptr_t)15);
+      uint32_t u[W + 4];
 #pragma unroll
-      for (int i = 0; i < W; ++i) w[i] = __ldg(reinterpret_cast<const uint32_t*>(x) + i);
+      for (int i = 0; i < W + 4; i += 4) {
+        const uint4 v = __ldg(c + i / 4);
+        u[i] = v.x; u[i + 1] = v.y; u[i + 2] = v.z; u[i + 3] = v.w;
+      }
+      if (at & 8) {
+#pragma unroll
+        for (int i = 0; i < W + 2; ++i) u[i] = u[i + 2];
+      }
+      if (at & 4) {
+#pragma unroll
+        for (int i = 0; i < W + 1; ++i) u[i] = u[i + 1];
+      }
+      const uint32_t sel = sizeof(T) == 2 && (at & 2) ? 0x5432u : 0x3210u;
+#pragma unroll
+      for (int i = 0; i < W; ++i) w[i] = sizeof(T) == 2 ? __byte_perm(u[i], u[i + 1], sel) : u[i];
     }
   }
-  // Elements c, c + 1, ... of the expanded row: the row's C own, then its duplicated channels up to K, then zeros.
+  // Elements c, c + 1, ... of the expanded row: the row's C own, then its duplicated channels up to K, then zeros.  All
+  // indices are asked for before the first value, and all values before the first is used.
   __device__ __forceinline__ void gather(const T* x, int c, int C, int K, const int32_t* idx_map, int* dev_status) {
+    constexpr int R = 16;
 #pragma unroll
-    for (int i = 0; i < W; ++i) w[i] = 0;
+    for (int h = 0; h < N; h += R) {
+      int src[R];
 #pragma unroll
-    for (int e = 0; e < N; ++e) {
-      int src = c + e;
-      if (src < K) {
-        if (src >= C) {
-          src = __ldg(idx_map + src);
-          if ((unsigned)src >= (unsigned)C) { flag(dev_status, OCS_DEV_BAD_INDEX); src = 0; }
-        }
-        if constexpr (sizeof(T) == 4) w[e] = __ldg(reinterpret_cast<const uint32_t*>(x) + src);
-        else w[e / 2] |= (uint32_t)__ldg(reinterpret_cast<const uint16_t*>(x) + src) << (16 * (e & 1));
+      for (int e = 0; e < R; ++e) {
+        const int i = c + h + e;
+        src[e] = i;
+        if (i >= C && i < K) src[e] = __ldg(idx_map + i);
       }
+      bool bad = false;
+#pragma unroll
+      for (int e = 0; e < R; ++e)
+        if (c + h + e < K && (unsigned)src[e] >= (unsigned)C) { bad = true; src[e] = 0; }
+      uint32_t v[R];
+#pragma unroll
+      for (int e = 0; e < R; ++e) {
+        v[e] = 0;
+        if (c + h + e < K) {
+          if constexpr (sizeof(T) == 4) v[e] = __ldg(reinterpret_cast<const uint32_t*>(x) + src[e]);
+          else v[e] = __ldg(reinterpret_cast<const uint16_t*>(x) + src[e]);
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < R; ++e) {
+        if constexpr (sizeof(T) == 4) w[h + e] = v[e];
+        else if (e & 1) w[(h + e) / 2] = v[e - 1] | v[e] << 16;
+      }
+      if (bad) flag(dev_status, OCS_DEV_BAD_INDEX);
     }
+  }
+  // Block b of an expanded row: whole ones by load, the rest, and where rows start anywhere the first and last, by gather.
+  template <int ALIGN>
+  __device__ __forceinline__ void load_block(const T* x, int b, int C, int K, const int32_t* idx_map, int* dev_status) {
+    const bool whole = ALIGN ? (b + 1) * N <= C : b > 0 && (b + 2) * N <= C;
+    if (whole) load<ALIGN>(x + b * N);
+    else gather(x, b * N, C, K, idx_map, dev_status);
   }
   __device__ __forceinline__ void clear() {
 #pragma unroll
