@@ -39,87 +39,223 @@ __device__ __forceinline__ void store_block(const MxRows& p, long long r, int b,
   }
 }
 
-// E8M0: blocks know nothing of their row; thread g has block g % nb of row g / nb.
-template <typename T, int ALIGN>
-__global__ void __launch_bounds__(256, sizeof(T) == 2 ? 4 : 3) mx4_blocks_kernel(const T* __restrict__ X, const MxRows p) {
-  grid_launch_dependents();
-  const unsigned long long g = (unsigned long long)blockIdx.x * 256 + threadIdx.x;
-  const long long r = g >> 32 ? (long long)(g / (unsigned)p.nb) : (long long)((unsigned)g / (unsigned)p.nb);
-  if (r >= p.rows) return;
-  const int b = (int)(g - (unsigned long long)r * p.nb);
-  Block<T, 32> v;
-  v.template load_block<ALIGN>(X + r * p.ldx, b, p.C, p.K, p.idx_map, p.dev_status);
-  const uint32_t m = v.max_bits();
-  if (m >= 0x7f800000u) flag(p.dev_status, OCS_DEV_NONFINITE);
-  const MxScale s = mx4_scale<OCS_GRID_E8M0, T>(m, 0);
-  uint32_t c[4];
-  v.template codes<OCS_GRID_E8M0>(s, c);
-  store_block<OCS_GRID_E8M0>(p, r, b, s, c);
+// Whether block b of row r can be read by Block::load: all its elements are the row's own, and where rows start anywhere
+// (ALIGN 0), what it reads around them lies in the matrix too (in neighbouring rows, or between them).
+template <int N, int ALIGN>
+__device__ __forceinline__ bool whole_block(const MxRows& p, long long r, int b) {
+  if ((b + 1) * N > p.C) return false;
+  return ALIGN || ((r > 0 || b > 0) && (r + 1 < p.rows || (b + 2) * N <= p.C));
+}
+
+// The row's tail, elements [first, last) of the expanded row from the first block on that is not all its own, into shared
+// memory by G threads, zeros up to a block's end: a thread per element, so that the indices come in one load and the values
+// in another.
+constexpr int kTailBytes = 8192;
+template <typename T, int N>
+__device__ __forceinline__ void stage_tail(const MxRows& p, const T* x, int first, int blocks, T* s, int tx, int G) {
+  for (int e = tx; e < blocks * N; e += G) {
+    int src = first + e;
+    T v = from_f32<T>(0.0f);
+    if (src < p.K) {
+      if (src >= p.C) {
+        src = __ldg(p.idx_map + src);
+        if ((unsigned)src >= (unsigned)p.C) { flag(p.dev_status, OCS_DEV_BAD_INDEX); src = 0; }
+      }
+      v = x[src];
+    }
+    s[e] = v;
+  }
 }
 
 constexpr int kRowThreads = 512;
 
-// E4M3: a row's scale is that of its largest magnitude, so the row waits in registers: blockDim.x threads with NV blocks each,
-// blockDim.y rows per CTA.
-template <typename T, int ALIGN, int NV>
-__global__ void __launch_bounds__(kRowThreads, NV == 1 || sizeof(T) == 4 ? 2 : 3) mx4_rows_kernel(const T* __restrict__ X, const MxRows p) {
-  __shared__ uint32_t s_max[32];
+// G = blockDim.x threads (a power of two below 32, or whole warps) and NV blocks each for one row, or (E8M0, whose blocks need
+// nothing of their row) a part of one: blockIdx.y.  blockDim.y rows per CTA.  E4M3: a row's scale is that of its largest
+// magnitude, so the row waits in registers for it.
+template <typename T, int GRID, int ALIGN, int NV>
+__global__ void __launch_bounds__(kRowThreads, NV * Block<T, mx4_block(GRID)>::W > 16 ? 2 : 3)
+mx4_rows_kernel(const T* __restrict__ X, const MxRows p, int tail_room) {
+  constexpr int N = mx4_block(GRID);
+  __shared__ uint32_t s_max[16];
+  __shared__ __align__(16) unsigned char s_tail[kTailBytes];
   grid_launch_dependents();
-  const int G = blockDim.x, tx = threadIdx.x, lane = tx & 31;
+  const int G = blockDim.x, tx = threadIdx.x, lane = (threadIdx.y * G + tx) & 31;
   const long long r = (long long)blockIdx.x * blockDim.y + threadIdx.y;
   const bool live = r < p.rows;
   const T* x = X + (live ? r : 0) * p.ldx;
-  Block<T, 16> v[NV];
-  uint32_t mine[NV], m = 0;
+  const int lo = GRID == OCS_GRID_E8M0 ? (int)blockIdx.y * G * NV : 0, hi = min(lo + G * NV, p.nb);
+  const int t0 = max(p.C / N, lo), tail = hi - t0;            // the tail's blocks in this part
+  const bool staged = tail > 0 && tail <= tail_room;
+  T* my_tail = reinterpret_cast<T*>(s_tail) + threadIdx.y * tail_room * N;
+  Block<T, N> v[NV];
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
-    const int b = tx + i * G;
-    if (b >= p.nb || !live) v[i].clear();
-    else v[i].template load_block<ALIGN>(x, b, p.C, p.K, p.idx_map, p.dev_status);
+    const int b = lo + tx + i * G;
+    if (b >= hi || !live) v[i].clear();
+    else if (whole_block<N, ALIGN>(p, r, b)) v[i].template load<ALIGN>(x + b * N);
+    else if (!staged || b < t0) v[i].gather(x, b * N, p.C, p.K, p.idx_map, p.dev_status);
   }
+  if (staged) {
+    if (live) stage_tail<T, N>(p, x, t0 * N, tail, my_tail, tx, G);
+    if (G > 32) __syncthreads();
+    else __syncwarp();
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int b = lo + tx + i * G;
+      if (b >= t0 && b < hi && live) v[i].from_shared(my_tail + (b - t0) * N);
+    }
+  }
+  uint32_t mine[NV], m = 0;
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
     mine[i] = v[i].max_bits();
     m = max(m, mine[i]);
   }
-  m = __reduce_max_sync(0xffffffffu, m);
-  if (G > 32) {
-    const int per = G >> 5, first = threadIdx.y * per;
-    if (lane == 0) s_max[first + (tx >> 5)] = m;
-    __syncthreads();
-    m = __reduce_max_sync(0xffffffffu, lane < per ? s_max[first + lane] : 0u);
+  int k = 0;
+  if constexpr (GRID == OCS_GRID_E4M3) {
+    if (G >= 32) m = __reduce_max_sync(0xffffffffu, m);
+    else
+      for (int o = 1; o < G; o <<= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
+    if (G > 32) {
+      const int per = G >> 5, first = threadIdx.y * per;
+      if (lane == 0) s_max[first + (tx >> 5)] = m;
+      __syncthreads();
+      m = __reduce_max_sync(0xffffffffu, lane < per ? s_max[first + lane] : 0u);
+    }
+    k = mx4_row_exponent(m);
+    if (tx == 0 && live) p.row_scales[r] = two_to(k);
   }
   if (!live) return;
-  const int k = mx4_row_exponent(m);
-  if (tx == 0) {
-    p.row_scales[r] = two_to(k);
-    if (m >= 0x7f800000u) flag(p.dev_status, OCS_DEV_NONFINITE);
-  }
+  if (m >= 0x7f800000u && (GRID == OCS_GRID_E8M0 || tx == 0)) flag(p.dev_status, OCS_DEV_NONFINITE);
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
-    const int b = tx + i * G;
-    if (b >= p.nb) break;
-    const MxScale s = mx4_scale<OCS_GRID_E4M3, T>(mine[i], k);
-    uint32_t c[2];
-    v[i].template codes<OCS_GRID_E4M3>(s, c);
-    store_block<OCS_GRID_E4M3>(p, r, b, s, c);
+    const int b = lo + tx + i * G;
+    if (b >= hi) break;
+    const MxScale s = mx4_scale<GRID, T>(mine[i], k);
+    uint32_t c[N / 8];
+    v[i].template codes<GRID>(s, c);
+    store_block<GRID>(p, r, b, s, c);
   }
 }
 
-// E4M3, rows that no CTA's registers hold: read twice, the second time from L2.
+// E4M3, many long rows that start at 16-byte boundaries: one CTA per SM walks over them.  A row comes by one bulk copy into
+// a ring of shared-memory buffers, moves into registers (which frees its buffer), and is quantized from there while the next
+// rows are on their way.
+constexpr int kStagedThreads = 1024, kStagedRing = 4;
+constexpr size_t kStagedBytes = 224 * 1024;
+template <typename T>
+__global__ void __launch_bounds__(kStagedThreads, 1) mx4_staged_rows_kernel(const T* __restrict__ X, const MxRows p, int ring) {
+  constexpr int N = 16, NV = 2;
+  extern __shared__ __align__(128) unsigned char smem[];   // [ring] rows
+  __shared__ __align__(8) uint64_t bars[kStagedRing];
+  __shared__ uint32_t s_max[2][32];
+  __shared__ int abort_flag;
+  const int tx = threadIdx.x, lane = tx & 31;
+  const uint32_t row_bytes = (uint32_t)p.C * (uint32_t)sizeof(T);
+  grid_launch_dependents();
+  auto request = [&](long long r, int slot) {   // one thread
+    const uint32_t bar = smem_u32(bars + slot);
+    mbar_arrive_expect_tx(bar, row_bytes);
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                 ::"r"(smem_u32(smem) + (uint32_t)slot * row_bytes), "l"(X + r * p.ldx), "r"(row_bytes), "r"(bar) : "memory");
+  };
+  if (tx == 0) {
+    for (int i = 0; i < ring; ++i) mbar_init(smem_u32(bars + i), 1);
+    abort_flag = 0;
+    fence_barrier_init();
+    fence_proxy_async_smem();
+    for (int i = 0; i < ring; ++i)
+      if (blockIdx.x + (long long)i * gridDim.x < p.rows) request(blockIdx.x + (long long)i * gridDim.x, i);
+  }
+  __syncthreads();
+  int it = 0, slot = 0;
+  uint32_t phase = 0;
+  for (long long r = blockIdx.x; r < p.rows; r += gridDim.x, ++it) {
+    const bool ok = mbar_wait(smem_u32(bars + slot), phase, &abort_flag);
+    const T* row = reinterpret_cast<const T*>(smem + (size_t)slot * row_bytes);
+    Block<T, N> v[NV];
+    uint32_t mine[NV], m = 0;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int b = tx + i * kStagedThreads;
+      if ((b + 1) * N <= p.C) v[i].from_shared(row + b * N);
+      else {
+        v[i].clear();
+        if (b < p.nb)
+#pragma unroll
+          for (int e = 0; e < N; ++e) {
+            int src = b * N + e;
+            if (src < p.K) {
+              if (src >= p.C) {
+                src = __ldg(p.idx_map + src);
+                if ((unsigned)src >= (unsigned)p.C) { flag(p.dev_status, OCS_DEV_BAD_INDEX); src = 0; }
+              }
+              if constexpr (sizeof(T) == 4) v[i].w[e] = reinterpret_cast<const uint32_t*>(row)[src];
+              else v[i].w[e / 2] |= (uint32_t)reinterpret_cast<const uint16_t*>(row)[src] << (16 * (e & 1));
+            }
+          }
+      }
+      mine[i] = v[i].max_bits();
+      m = max(m, mine[i]);
+    }
+    m = __reduce_max_sync(0xffffffffu, m);
+    if (lane == 0) s_max[it & 1][tx >> 5] = m;
+    if (!__syncthreads_and(ok)) break;          // the row is in registers
+    const long long next = r + (long long)ring * gridDim.x;
+    if (tx == 0 && next < p.rows) request(next, slot);
+    m = __reduce_max_sync(0xffffffffu, s_max[it & 1][lane]);
+    const int k = mx4_row_exponent(m);
+    if (tx == 0) {
+      p.row_scales[r] = two_to(k);
+      if (m >= 0x7f800000u) flag(p.dev_status, OCS_DEV_NONFINITE);
+    }
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int b = tx + i * kStagedThreads;
+      if (b >= p.nb) break;
+      const MxScale s = mx4_scale<OCS_GRID_E4M3, T>(mine[i], k);
+      uint32_t c[2];
+      v[i].template codes<OCS_GRID_E4M3>(s, c);
+      store_block<OCS_GRID_E4M3>(p, r, b, s, c);
+    }
+    if (++slot == ring) { slot = 0; phase ^= 1u; }
+  }
+  if (abort_flag && tx == 0) {
+    for (int i = 0; i < 2000; ++i) __nanosleep(100);   // copies still in flight land before the CTA leaves
+    flag(p.dev_status, OCS_DEV_TIMEOUT);
+  }
+  __syncthreads();
+}
+
+// E4M3, other rows that no CTA's registers hold: read twice, the second time from L2.
 template <typename T, int ALIGN>
 __global__ void __launch_bounds__(kRowThreads, 2) mx4_long_rows_kernel(const T* __restrict__ X, const MxRows p) {
+  constexpr int N = 16;
   __shared__ uint32_t s_max[2][16];
+  __shared__ __align__(16) unsigned char s_tail[kTailBytes];
   grid_launch_dependents();
   const int tx = threadIdx.x, lane = tx & 31;
+  const int t0 = p.C / N, tail = p.nb - t0;
+  const bool staged = tail * N * (int)sizeof(T) <= kTailBytes;
+  T* my_tail = reinterpret_cast<T*>(s_tail);
   int odd = 0;
   for (long long r = blockIdx.x; r < p.rows; r += gridDim.x, odd ^= 1) {
     const T* x = X + r * p.ldx;
+    if (staged) {
+      __syncthreads();
+      stage_tail<T, N>(p, x, t0 * N, tail, my_tail, tx, kRowThreads);
+      __syncthreads();
+    }
+    auto load = [&](Block<T, N>& v, int b) {
+      if (whole_block<N, ALIGN>(p, r, b)) v.template load<ALIGN>(x + b * N);
+      else if (staged && b >= t0) v.from_shared(my_tail + (b - t0) * N);
+      else v.gather(x, b * N, p.C, p.K, p.idx_map, p.dev_status);
+    };
     uint32_t m = 0;
 #pragma unroll 2
     for (int b = tx; b < p.nb; b += kRowThreads) {
-      Block<T, 16> v;
-      v.template load_block<ALIGN>(x, b, p.C, p.K, p.idx_map, p.dev_status);
+      Block<T, N> v;
+      load(v, b);
       m = max(m, v.max_bits());
     }
     m = __reduce_max_sync(0xffffffffu, m);
@@ -133,8 +269,8 @@ __global__ void __launch_bounds__(kRowThreads, 2) mx4_long_rows_kernel(const T* 
     }
 #pragma unroll 2
     for (int b = tx; b < p.nb; b += kRowThreads) {
-      Block<T, 16> v;
-      v.template load_block<ALIGN>(x, b, p.C, p.K, p.idx_map, p.dev_status);
+      Block<T, N> v;
+      load(v, b);
       const MxScale s = mx4_scale<OCS_GRID_E4M3, T>(v.max_bits(), k);
       uint32_t c[2];
       v.template codes<OCS_GRID_E4M3>(s, c);
@@ -143,29 +279,44 @@ __global__ void __launch_bounds__(kRowThreads, 2) mx4_long_rows_kernel(const T* 
   }
 }
 
-template <typename T, int ALIGN>
-ocs_status launch_quantize(const T* X, const MxRows& p, ocs_grid grid, cudaStream_t stream) {
-  if (grid == OCS_GRID_E8M0) {
-    const long long ctas = (p.rows * p.nb + 255) / 256;
-    if (ctas > 0x7fffffff) return OCS_ERR_UNSUPPORTED;
-    LaunchScope ls("mx4_blocks_kernel", stream);
-    mx4_blocks_kernel<T, ALIGN><<<(unsigned)ctas, 256, 0, stream>>>(X, p);
-    return launch_status();
-  }
-  LaunchScope ls("mx4_rows_kernel", stream);
-  if (p.nb > 2 * kRowThreads) {
+template <typename T, int GRID, int ALIGN>
+ocs_status launch_rows(const T* X, const MxRows& p, cudaStream_t stream) {
+  constexpr int N = mx4_block(GRID);
+  if (GRID == OCS_GRID_E4M3 && p.nb > 2 * kRowThreads) {
+    const size_t row_bytes = (size_t)p.C * sizeof(T);
+    if (ALIGN && p.rows >= 2 * kNumSMs && p.nb <= 2 * kStagedThreads && row_bytes % 16 == 0 && 2 * row_bytes <= kStagedBytes) {
+      const int ring = (int)(kStagedBytes / row_bytes < kStagedRing ? kStagedBytes / row_bytes : kStagedRing);
+      if (cudaFuncSetAttribute(mx4_staged_rows_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kStagedBytes) != cudaSuccess)
+        return OCS_ERR_CUDA;
+      LaunchScope ls("mx4_staged_rows_kernel", stream);
+      mx4_staged_rows_kernel<T><<<kNumSMs, kStagedThreads, ring * row_bytes, stream>>>(X, p, ring);
+      return launch_status();
+    }
     const long long most = 2 * kNumSMs;
+    LaunchScope ls("mx4_long_rows_kernel", stream);
     mx4_long_rows_kernel<T, ALIGN><<<(unsigned)(p.rows < most ? p.rows : most), kRowThreads, 0, stream>>>(X, p);
     return launch_status();
   }
-  // few rows: a thread for every block; many: two blocks each
-  const int nv = p.nb > kRowThreads || (p.rows > kNumSMs && p.nb > 32) ? 2 : 1;
-  const int G = ((p.nb + nv - 1) / nv + 31) / 32 * 32, R = G <= 128 && p.rows > kNumSMs ? 256 / G : 1;
+  // few rows: a thread for every block; many: two blocks each (E8M0: one, of twice the size)
+  const int nv = GRID == OCS_GRID_E4M3 && (p.nb > kRowThreads || (p.rows > kNumSMs && p.nb > 32)) ? 2 : 1;
+  const int part = (p.nb + nv - 1) / nv;   // blocks per thread column
+  int G = 4;
+  while (G < part && G < 32) G *= 2;
+  if (part > 32) G = part < kRowThreads ? (part + 31) / 32 * 32 : kRowThreads;
+  const int y = GRID == OCS_GRID_E8M0 ? (p.nb + G - 1) / G : 1;
+  const int R = G <= 128 && p.rows * G > 32 * kNumSMs ? 256 / G : (G < 32 ? 32 / G : 1);
   const long long ctas = (p.rows + R - 1) / R;
-  if (ctas > 0x7fffffff) return OCS_ERR_UNSUPPORTED;
-  if (nv == 1) mx4_rows_kernel<T, ALIGN, 1><<<(unsigned)ctas, dim3(G, R), 0, stream>>>(X, p);
-  else mx4_rows_kernel<T, ALIGN, 2><<<(unsigned)ctas, dim3(G, R), 0, stream>>>(X, p);
+  if (ctas > 0x7fffffff || y > 65535) return OCS_ERR_UNSUPPORTED;
+  const dim3 grid((unsigned)ctas, (unsigned)y), block(G, R);
+  const int room = kTailBytes / (R * N * (int)sizeof(T));
+  LaunchScope ls("mx4_rows_kernel", stream);
+  if (nv == 1) mx4_rows_kernel<T, GRID, ALIGN, 1><<<grid, block, 0, stream>>>(X, p, room);
+  else if constexpr (GRID == OCS_GRID_E4M3) mx4_rows_kernel<T, GRID, ALIGN, 2><<<grid, block, 0, stream>>>(X, p, room);
   return launch_status();
+}
+template <typename T, int ALIGN>
+ocs_status launch_quantize(const T* X, const MxRows& p, ocs_grid grid, cudaStream_t stream) {
+  return grid == OCS_GRID_E8M0 ? launch_rows<T, OCS_GRID_E8M0, ALIGN>(X, p, stream) : launch_rows<T, OCS_GRID_E4M3, ALIGN>(X, p, stream);
 }
 
 template <typename T>
@@ -177,101 +328,77 @@ ocs_status launch_quantize(const void* X_, const MxRows& p, ocs_grid grid, cudaS
   return launch_quantize<T, 0>(X, p, grid, stream);
 }
 
-// ---- codes to values
-// Rows that start at 16-byte boundaries: 16 values per thread, stored 32 (WIDE) or 16 bytes at a time.
-template <typename T, bool WIDE>
+// ---- codes to values: a thread stores 32 aligned bytes of a row.  SHIFTED: rows start anywhere, so its elements are
+// `ahead` behind a multiple of their number: their codes are shifted out of the words around them, and they may have two scales.
+template <typename T, bool SHIFTED>
 __global__ void __launch_bounds__(256) mx4_values_kernel(const MxRows p, int grid, T* __restrict__ Y, long long ldy) {
-  const int per = (p.K + 15) / 16;
+  constexpr int E = 32 / (int)sizeof(T);
+  const int per = (p.K + (SHIFTED ? E - 1 : 0) + E - 1) / E;
   const unsigned long long g = (unsigned long long)blockIdx.x * 256 + threadIdx.x;
   const long long r = g >> 32 ? (long long)(g / (unsigned)per) : (long long)((unsigned)g / (unsigned)per);
   if (r >= p.rows) return;
-  const int u = (int)(g - (unsigned long long)r * per), c0 = u * 16, left = p.K - c0;
-  const uint8_t* src = p.codes + r * p.ld_codes + u * 8;
-  uint32_t w[2] = {0, 0};
-  if (left >= 15 && p.code_align >= 8) {
-    const uint2 v = __ldg(reinterpret_cast<const uint2*>(src));
-    w[0] = v.x; w[1] = v.y;
-  } else {
+  T* y = Y + r * ldy;
+  const int ahead = SHIFTED ? (int)((reinterpret_cast<uintptr_t>(y) & 31) / sizeof(T)) : 0;
+  const int c0 = (int)(g - (unsigned long long)r * per) * E - ahead;    // (negative: from the row's first element on)
+  if (c0 >= p.K) return;
+  y += c0;
+  const uint8_t* src = p.codes + r * p.ld_codes;
+  constexpr int NW = E / 8;
+  uint32_t w[NW + 1];
+  const int w0 = c0 >> 3, bytes = (p.K + 1) / 2;
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (2 * i < left) w[i / 4] |= (uint32_t)__ldg(src + i) << (8 * (i & 3));
+  for (int i = 0; i < NW + (SHIFTED ? 1 : 0); ++i) {
+    const int at = 4 * (w0 + i);
+    w[i] = 0;
+    if (at < 0) continue;
+    if (p.code_align >= 4 && at + 4 <= bytes) w[i] = __ldg(reinterpret_cast<const uint32_t*>(src + at));
+    else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (at + j < bytes) w[i] |= (uint32_t)__ldg(src + at + j) << (8 * j);
+    }
   }
-  float unit;
-  if (grid == OCS_GRID_E8M0) unit = e8m0_value(__ldg(p.scales + mx4_scale_at(r, u / 2, p.chunks)));
-  else unit = __fmul_rn(e4m3_value(__ldg(p.scales + mx4_scale_at(r, u, p.chunks))), __ldg(p.row_scales + r));
-  T* y = Y + r * ldy + c0;
-  T out[16];
+  if (SHIFTED) {
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < NW; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], (c0 & 7) * 4);
+  }
+  const int shift = grid == OCS_GRID_E8M0 ? 5 : 4, first = max(c0, 0) >> shift, last = min(c0 + E, p.K) - 1;
+  auto unit_of = [&](int b) {
+    const uint32_t byte = __ldg(p.scales + mx4_scale_at(r, b, p.chunks));
+    return grid == OCS_GRID_E8M0 ? e8m0_value(byte) : __fmul_rn(e4m3_value(byte), __ldg(p.row_scales + r));
+  };
+  const float u0 = unit_of(first), u1 = SHIFTED ? unit_of(last >> shift) : u0;
+  const int split = SHIFTED ? ((first + 1) << shift) - c0 : E;            // elements from here on have the second scale
+  T out[E];
+#pragma unroll
+  for (int i = 0; i < NW; ++i) {
     __half2 h[4];
     e2m1_values(w[i], h);
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const float2 f = __half22float2(h[e]);
-      out[8 * i + 2 * e] = from_f32<T>(__fmul_rn(f.x, unit));
-      out[8 * i + 2 * e + 1] = from_f32<T>(__fmul_rn(f.y, unit));
+      out[8 * i + 2 * e] = from_f32<T>(__fmul_rn(f.x, 8 * i + 2 * e < split ? u0 : u1));
+      out[8 * i + 2 * e + 1] = from_f32<T>(__fmul_rn(f.y, 8 * i + 2 * e + 1 < split ? u0 : u1));
     }
   }
-  const uint32_t* o = reinterpret_cast<const uint32_t*>(out);
-  if (left >= 16) {
-    if constexpr (WIDE) {
+  if (c0 >= 0 && c0 + E <= p.K) store32(reinterpret_cast<uint32_t*>(y), reinterpret_cast<const uint32_t*>(out));
+  else {
 #pragma unroll
-      for (int i = 0; i < 4 * (int)sizeof(T); i += 8) store32(reinterpret_cast<uint32_t*>(y) + i, o + i);
-    } else {
-#pragma unroll
-      for (int i = 0; i < (int)sizeof(T); ++i) reinterpret_cast<uint4*>(y)[i] = make_uint4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 16; ++i)
-      if (i < left) y[i] = out[i];
-  }
-}
-
-// Rows that start anywhere: a warp takes 512 values, two per lane and step, so that its stores are dense whatever their
-// alignment.
-template <typename T>
-__global__ void __launch_bounds__(256) mx4_values_any_kernel(const MxRows p, int grid, T* __restrict__ Y, long long ldy) {
-  const int per = (p.K + 511) / 512, lane = threadIdx.x & 31;
-  const unsigned long long g = (unsigned long long)blockIdx.x * 8 + (threadIdx.x >> 5);
-  const long long r = g >> 32 ? (long long)(g / (unsigned)per) : (long long)((unsigned)g / (unsigned)per);
-  if (r >= p.rows) return;
-  const int c0 = (int)(g - (unsigned long long)r * per) * 512 + 2 * lane;
-  const uint8_t* src = p.codes + r * p.ld_codes + c0 / 2;
-  const float row = grid == OCS_GRID_E8M0 ? 1.0f : __ldg(p.row_scales + r);
-  T* y = Y + r * ldy + c0;
-  const bool pairs = reinterpret_cast<uintptr_t>(y) % (2 * sizeof(T)) == 0;
-  uint32_t code[8], byte[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int c = c0 + 64 * i;
-    code[i] = c < p.K ? __ldg(src + 32 * i) : 0u;
-    byte[i] = c < p.K ? __ldg(p.scales + mx4_scale_at(r, grid == OCS_GRID_E8M0 ? c / 32 : c / 16, p.chunks)) : 0u;
-  }
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int c = c0 + 64 * i;
-    const float unit = grid == OCS_GRID_E8M0 ? e8m0_value(byte[i]) : __fmul_rn(e4m3_value(byte[i]), row);
-    const float2 f = e2m1_pair(code[i]);
-    struct alignas(2 * sizeof(T)) Two { T a, b; } v{from_f32<T>(__fmul_rn(f.x, unit)), from_f32<T>(__fmul_rn(f.y, unit))};
-    if (pairs && c + 1 < p.K) *reinterpret_cast<Two*>(y + 64 * i) = v;
-    else {
-      if (c < p.K) y[64 * i] = v.a;
-      if (c + 1 < p.K) y[64 * i + 1] = v.b;
-    }
+    for (int i = 0; i < E; ++i)
+      if (c0 + i >= 0 && c0 + i < p.K) y[i] = out[i];
   }
 }
 
 template <typename T>
 ocs_status launch_values(const MxRows& p, ocs_grid grid, void* Y_, long long ldy, cudaStream_t stream) {
+  constexpr int E = 32 / (int)sizeof(T);
   T* Y = static_cast<T*>(Y_);
   const uintptr_t a = reinterpret_cast<uintptr_t>(Y) | (p.rows > 1 ? (uintptr_t)(ldy * (int64_t)sizeof(T)) : 0);
-  const bool any = a % 16 != 0;
-  const long long ctas = any ? (p.rows * ((p.K + 511) / 512) + 7) / 8 : (p.rows * ((p.K + 15) / 16) + 255) / 256;
+  const bool shifted = a % 32 != 0;
+  const long long ctas = (p.rows * ((p.K + (shifted ? E - 1 : 0) + E - 1) / E) + 255) / 256;
   if (ctas > 0x7fffffff) return OCS_ERR_UNSUPPORTED;
   LaunchScope ls("mx4_values_kernel", stream);
-  if (any) mx4_values_any_kernel<T><<<(unsigned)ctas, 256, 0, stream>>>(p, grid, Y, ldy);
-  else if (a % 32 == 0) mx4_values_kernel<T, true><<<(unsigned)ctas, 256, 0, stream>>>(p, grid, Y, ldy);
+  if (shifted) mx4_values_kernel<T, true><<<(unsigned)ctas, 256, 0, stream>>>(p, grid, Y, ldy);
   else mx4_values_kernel<T, false><<<(unsigned)ctas, 256, 0, stream>>>(p, grid, Y, ldy);
   return launch_status();
 }

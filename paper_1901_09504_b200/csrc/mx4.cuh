@@ -46,13 +46,6 @@ __device__ __forceinline__ void e2m1_values(uint32_t codes, __half2* v) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) v[i] = *reinterpret_cast<__half2*>(&r[i]);
 }
-// One byte of codes as two values.  (The conversion instruction gave zeros here, on a byte that comes straight from a load:
-// the upper bytes of the halves are picked from a table instead.)
-__device__ __forceinline__ float2 e2m1_pair(uint32_t code) {
-  const uint32_t magnitude = __byte_perm(0x3E3C3800u, 0x46444240u, (code & 7u) << 4 | (code & 0x70u) << 8);
-  const uint32_t h = magnitude | (code & 8u) << 12 | (code & 0x80u) << 24;
-  return __half22float2(*reinterpret_cast<const __half2*>(&h));
-}
 __device__ __forceinline__ uint32_t e4m3_byte(float v) {
   uint16_t r;
   asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(0.0f), "f"(v));
@@ -130,7 +123,7 @@ struct Block {
   static constexpr int W = N * (int)sizeof(T) / 4;
   uint32_t w[W];
   // x aligned to ALIGN bytes: 32, 16, or (0) its element.  The last reads the 16-byte pieces around the block and shifts it
-  // out of them: up to 15 bytes before x and 16 behind the block have to belong to the row.
+  // out of them: up to 15 bytes before x and 16 behind the block have to be readable.
   template <int ALIGN>
   __device__ __forceinline__ void load(const T* x) {
     if constexpr (ALIGN == 32) {
@@ -201,12 +194,13 @@ struct Block {
       if (bad) flag(dev_status, OCS_DEV_BAD_INDEX);
     }
   }
-  // Block b of an expanded row: whole ones by load, the rest, and where rows start anywhere the first and last, by gather.
-  template <int ALIGN>
-  __device__ __forceinline__ void load_block(const T* x, int b, int C, int K, const int32_t* idx_map, int* dev_status) {
-    const bool whole = ALIGN ? (b + 1) * N <= C : b > 0 && (b + 2) * N <= C;
-    if (whole) load<ALIGN>(x + b * N);
-    else gather(x, b * N, C, K, idx_map, dev_status);
+  // N elements from shared memory.
+  __device__ __forceinline__ void from_shared(const T* s) {
+#pragma unroll
+    for (int i = 0; i < W; i += 4) {
+      const uint4 v = *(reinterpret_cast<const uint4*>(s) + i / 4);
+      w[i] = v.x; w[i + 1] = v.y; w[i + 2] = v.z; w[i + 3] = v.w;
+    }
   }
   __device__ __forceinline__ void clear() {
 #pragma unroll
