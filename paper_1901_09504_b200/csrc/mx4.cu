@@ -328,79 +328,105 @@ ocs_status launch_quantize(const void* X_, const MxRows& p, ocs_grid grid, cudaS
   return launch_quantize<T, 0>(X, p, grid, stream);
 }
 
-// ---- codes to values: a thread stores 32 aligned bytes of a row.  SHIFTED: rows start anywhere, so its elements are
-// `ahead` behind a multiple of their number: their codes are shifted out of the words around them, and they may have two scales.
-template <typename T, bool SHIFTED>
-__global__ void __launch_bounds__(256) mx4_values_kernel(const MxRows p, int grid, T* __restrict__ Y, long long ldy) {
-  constexpr int E = 32 / (int)sizeof(T);
-  const int per = (p.K + (SHIFTED ? E - 1 : 0) + E - 1) / E;
-  const unsigned long long g = (unsigned long long)blockIdx.x * 256 + threadIdx.x;
-  const long long r = g >> 32 ? (long long)(g / (unsigned)per) : (long long)((unsigned)g / (unsigned)per);
+// ---- codes to values: a thread stores NS times 32 aligned bytes of a row; blockDim.x threads and gridDim.y CTAs per row,
+// blockDim.y rows per CTA.  SHIFTED: rows start anywhere, so a thread's elements are `ahead` behind a multiple of their number:
+// their codes are shifted out of the words around them, and each 32 bytes of them may have two scales.
+template <typename T, int GRID, bool SHIFTED, int NS>
+__global__ void __launch_bounds__(256) mx4_values_kernel(const MxRows p, T* __restrict__ Y, long long ldy) {
+  constexpr int E = 32 / (int)sizeof(T), SHIFT = GRID == OCS_GRID_E8M0 ? 5 : 4, NW = NS * E / 8;
+  const long long r = (long long)blockIdx.x * blockDim.y + threadIdx.y;
   if (r >= p.rows) return;
   T* y = Y + r * ldy;
   const int ahead = SHIFTED ? (int)((reinterpret_cast<uintptr_t>(y) & 31) / sizeof(T)) : 0;
-  const int c0 = (int)(g - (unsigned long long)r * per) * E - ahead;    // (negative: from the row's first element on)
+  const int c0 = (int)(blockIdx.y * blockDim.x + threadIdx.x) * (E * NS) - ahead;    // (negative: from the first element on)
   if (c0 >= p.K) return;
-  y += c0;
   const uint8_t* src = p.codes + r * p.ld_codes;
-  constexpr int NW = E / 8;
+  const uint8_t* scales = p.scales + mx4_scale_at(r, 0, p.chunks);
+  const float row = GRID == OCS_GRID_E4M3 ? __ldg(p.row_scales + r) : 1.0f;
+  y += c0;
   uint32_t w[NW + 1];
   const int w0 = c0 >> 3, bytes = (p.K + 1) / 2;
+  const bool inside = c0 >= 0 && c0 + NS * E <= p.K;
+  if (!SHIFTED && inside && p.code_align >= 4 * NW) {
+    if constexpr (NW == 4) { const uint4 v = __ldg(reinterpret_cast<const uint4*>(src + 4 * w0)); w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w; }
+    else if constexpr (NW == 2) { const uint2 v = __ldg(reinterpret_cast<const uint2*>(src + 4 * w0)); w[0] = v.x; w[1] = v.y; }
+    else w[0] = __ldg(reinterpret_cast<const uint32_t*>(src + 4 * w0));
+  } else {
 #pragma unroll
-  for (int i = 0; i < NW + (SHIFTED ? 1 : 0); ++i) {
-    const int at = 4 * (w0 + i);
-    w[i] = 0;
-    if (at < 0) continue;
-    if (p.code_align >= 4 && at + 4 <= bytes) w[i] = __ldg(reinterpret_cast<const uint32_t*>(src + at));
+    for (int i = 0; i < NW + (SHIFTED ? 1 : 0); ++i) {
+      const int at = 4 * (w0 + i);
+      w[i] = 0;
+      if (at < 0) continue;
+      if (p.code_align >= 4 && at + 4 <= bytes) w[i] = __ldg(reinterpret_cast<const uint32_t*>(src + at));
+      else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (at + j < bytes) w[i] |= (uint32_t)__ldg(src + at + j) << (8 * j);
+      }
+    }
+    if (SHIFTED) {
+#pragma unroll
+      for (int i = 0; i < NW; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], (c0 & 7) * 4);
+    }
+  }
+  auto unit_of = [&](int b) {
+    const uint32_t byte = __ldg(scales + (b >> 2) * kMxTile + (b & 3));
+    return GRID == OCS_GRID_E8M0 ? e8m0_value(byte) : __fmul_rn(e4m3_value(byte), row);
+  };
+#pragma unroll
+  for (int n = 0; n < NS; ++n) {
+    const int c = c0 + n * E;
+    if (n && c >= p.K) break;
+    const int first = max(c, 0) >> SHIFT;
+    const float u0 = unit_of(first), u1 = SHIFTED ? unit_of((min(c + E, p.K) - 1) >> SHIFT) : u0;
+    const int split = SHIFTED ? ((first + 1) << SHIFT) - c : E;            // elements from here on have the second scale
+    const unsigned long long u00 = pack_f32x2(u0, u0);
+    T out[E];
+#pragma unroll
+    for (int i = 0; i < E / 8; ++i) {
+      __half2 h[4];
+      e2m1_values(w[n * (E / 8) + i], h);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float2 f = __half22float2(h[e]);
+        const int at = 8 * i + 2 * e;
+        float v0, v1;
+        if (SHIFTED) { v0 = __fmul_rn(f.x, at < split ? u0 : u1); v1 = __fmul_rn(f.y, at + 1 < split ? u0 : u1); }
+        else unpack_f32x2(mul_f32x2(pack_f32x2(f.x, f.y), u00), v0, v1);
+        out[at] = from_f32<T>(v0);
+        out[at + 1] = from_f32<T>(v1);
+      }
+    }
+    if (inside || (c >= 0 && c + E <= p.K)) store32(reinterpret_cast<uint32_t*>(y + n * E), reinterpret_cast<const uint32_t*>(out));
     else {
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
-        if (at + j < bytes) w[i] |= (uint32_t)__ldg(src + at + j) << (8 * j);
+      for (int i = 0; i < E; ++i)
+        if (c + i >= 0 && c + i < p.K) y[n * E + i] = out[i];
     }
-  }
-  if (SHIFTED) {
-#pragma unroll
-    for (int i = 0; i < NW; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], (c0 & 7) * 4);
-  }
-  const int shift = grid == OCS_GRID_E8M0 ? 5 : 4, first = max(c0, 0) >> shift, last = min(c0 + E, p.K) - 1;
-  auto unit_of = [&](int b) {
-    const uint32_t byte = __ldg(p.scales + mx4_scale_at(r, b, p.chunks));
-    return grid == OCS_GRID_E8M0 ? e8m0_value(byte) : __fmul_rn(e4m3_value(byte), __ldg(p.row_scales + r));
-  };
-  const float u0 = unit_of(first), u1 = SHIFTED ? unit_of(last >> shift) : u0;
-  const int split = SHIFTED ? ((first + 1) << shift) - c0 : E;            // elements from here on have the second scale
-  T out[E];
-#pragma unroll
-  for (int i = 0; i < NW; ++i) {
-    __half2 h[4];
-    e2m1_values(w[i], h);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const float2 f = __half22float2(h[e]);
-      out[8 * i + 2 * e] = from_f32<T>(__fmul_rn(f.x, 8 * i + 2 * e < split ? u0 : u1));
-      out[8 * i + 2 * e + 1] = from_f32<T>(__fmul_rn(f.y, 8 * i + 2 * e + 1 < split ? u0 : u1));
-    }
-  }
-  if (c0 >= 0 && c0 + E <= p.K) store32(reinterpret_cast<uint32_t*>(y), reinterpret_cast<const uint32_t*>(out));
-  else {
-#pragma unroll
-    for (int i = 0; i < E; ++i)
-      if (c0 + i >= 0 && c0 + i < p.K) y[i] = out[i];
   }
 }
 
+template <typename T, int GRID, bool SHIFTED>
+ocs_status launch_values(const MxRows& p, T* Y, long long ldy, cudaStream_t stream) {
+  constexpr int NS = 2, E = 32 / (int)sizeof(T) * NS;
+  const int per = (p.K + (SHIFTED ? E - 1 : 0) + E - 1) / E;   // threads that a row may need
+  int G = 4;
+  while (G < per && G < 32) G *= 2;
+  if (per > 32) G = per < 256 ? (per + 31) / 32 * 32 : 256;
+  const int R = 256 / G;
+  const long long ctas = (p.rows + R - 1) / R, y = (per + G - 1) / G;
+  if (ctas > 0x7fffffff || y > 65535) return OCS_ERR_UNSUPPORTED;
+  LaunchScope ls("mx4_values_kernel", stream);
+  mx4_values_kernel<T, GRID, SHIFTED, NS><<<dim3((unsigned)ctas, (unsigned)y), dim3(G, R), 0, stream>>>(p, Y, ldy);
+  return launch_status();
+}
 template <typename T>
 ocs_status launch_values(const MxRows& p, ocs_grid grid, void* Y_, long long ldy, cudaStream_t stream) {
-  constexpr int E = 32 / (int)sizeof(T);
   T* Y = static_cast<T*>(Y_);
   const uintptr_t a = reinterpret_cast<uintptr_t>(Y) | (p.rows > 1 ? (uintptr_t)(ldy * (int64_t)sizeof(T)) : 0);
-  const bool shifted = a % 32 != 0;
-  const long long ctas = (p.rows * ((p.K + (shifted ? E - 1 : 0) + E - 1) / E) + 255) / 256;
-  if (ctas > 0x7fffffff) return OCS_ERR_UNSUPPORTED;
-  LaunchScope ls("mx4_values_kernel", stream);
-  if (shifted) mx4_values_kernel<T, true><<<(unsigned)ctas, 256, 0, stream>>>(p, grid, Y, ldy);
-  else mx4_values_kernel<T, false><<<(unsigned)ctas, 256, 0, stream>>>(p, grid, Y, ldy);
-  return launch_status();
+  if (grid == OCS_GRID_E8M0)
+    return a % 32 ? launch_values<T, OCS_GRID_E8M0, true>(p, Y, ldy, stream) : launch_values<T, OCS_GRID_E8M0, false>(p, Y, ldy, stream);
+  return a % 32 ? launch_values<T, OCS_GRID_E4M3, true>(p, Y, ldy, stream) : launch_values<T, OCS_GRID_E4M3, false>(p, Y, ldy, stream);
 }
 
 int align_of(const void* base, int64_t rows, int64_t ld) {

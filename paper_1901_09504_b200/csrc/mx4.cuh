@@ -7,6 +7,7 @@
 #include <type_traits>
 
 #include "elem.cuh"
+#include "ptx.cuh"
 
 namespace ocs {
 
@@ -85,30 +86,52 @@ __device__ __forceinline__ MxScale mx4_scale(uint32_t max_bits, int k) {
     s.inv = e8m0_inverse(s.byte);
   } else {
     s.down = two_to(-k);
-    s.byte = e4m3_byte(__fdiv_rn(__fmul_rn(__uint_as_float(max_bits), s.down), 6.0f));
+    // the quotient by 6, rounded once (by the correction that is explained below)
+    const float a = __fmul_rn(__uint_as_float(max_bits), s.down), sixth = 1.0f / 6.0f, t = __fmul_rn(a, sixth);
+    s.byte = e4m3_byte(fmaf(fmaf(-t, 6.0f, a), sixth, t));
     s.u = e4m3_value(s.byte);
-    s.inv = s.byte ? __frcp_rn(s.u) : 0.0f;
-    if (sizeof(T) == 2) s.inv = __fmul_rn(s.inv, s.down);   // (exact: within 2^-126 and 2^126)
+    if constexpr (sizeof(T) == 2) {
+      float y;   // (an approximation will do)
+      asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(s.u));
+      s.inv = s.byte ? __fmul_rn(y, s.down) : 0.0f;
+    } else {
+      s.inv = s.byte ? __frcp_rn(s.u) : 0.0f;
+    }
   }
   return s;
 }
 
-// x in units of the block's scale, as the rounding to e2m1 needs it.  E8M0: exact.
+__device__ __forceinline__ unsigned long long mul_f32x2(unsigned long long a, unsigned long long b) {
+  unsigned long long r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+// Two values in units of the block's scale, as the rounding to e2m1 needs them.  E8M0: exact.
 // E4M3 with 16-bit x: a value x / unit is either a border between two codes or at least 2^-13 away from each (x has at most
-// 11 bits, a border times the unit at most 7), so that the product with the rounded reciprocal, rounded to multiples of
-// 2^-14, falls on the right side and borders on themselves: one fused multiply-add and one subtraction instead of a division.
+// 11 bits, a border times the unit at most 7), so that the product with the approximate reciprocal, rounded to multiples of
+// 2^-14, falls on the right side and borders on themselves: a fused multiply-add and a subtraction instead of a division.
 // E4M3 with fp32 x: the rounded quotient, by Markstein's correction.  With z = x / r (exact), u = unit / r (an e4m3 number: 4
 // bits), y = rn(1 / u) and t = rn(z y), which is within two units of the quotient, z - t u has at most 6 bits and one
 // fused multiply-add finds it exactly; t + (z - t u) y is then the quotient up to 2^-22 units in the last place, and rounds
 // as the quotient does, since that (24 bits over 4) is never within 1/30 unit of the middle between two numbers unless it is
 // one of them.  (Values z below 2^-100 may lose bits on the way; their code is 0 either way.)
+// Zeros keep x's sign.
 template <int GRID, typename T>
-__device__ __forceinline__ float mx4_units(float x, const MxScale& s) {
-  if constexpr (GRID == OCS_GRID_E8M0) return __fmul_rn(x, s.inv);
-  else if constexpr (sizeof(T) == 2) return copysignf(__fsub_rn(fmaf(x, s.inv, 768.0f), 768.0f), x);   // (zeros keep x's sign)
-  else {
-    const float z = __fmul_rn(x, s.down), t = __fmul_rn(z, s.inv);
-    return copysignf(fmaf(fmaf(-t, s.u, z), s.inv, t), x);
+__device__ __forceinline__ void mx4_units(float x0, float x1, const MxScale& s, float* t) {
+  const unsigned long long x = pack_f32x2(x0, x1), inv = pack_f32x2(s.inv, s.inv);
+  if constexpr (GRID == OCS_GRID_E8M0) {
+    unpack_f32x2(mul_f32x2(x, inv), t[0], t[1]);
+  } else {
+    if constexpr (sizeof(T) == 2) {
+      const unsigned long long c = pack_f32x2(768.0f, 768.0f);
+      unpack_f32x2(sub_f32x2(fma_f32x2(x, inv, c), c), t[0], t[1]);
+    } else {
+      const unsigned long long z = mul_f32x2(x, pack_f32x2(s.down, s.down)), q = mul_f32x2(z, inv);
+      const unsigned long long rest = fma_f32x2(q, pack_f32x2(-s.u, -s.u), z);
+      unpack_f32x2(fma_f32x2(rest, inv, q), t[0], t[1]);
+    }
+    t[0] = copysignf(t[0], x0);
+    t[1] = copysignf(t[1], x1);
   }
 }
 
@@ -230,7 +253,7 @@ struct Block {
     for (int i = 0; i < N / 8; ++i) {
       float t[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) t[e] = mx4_units<GRID, T>((*this)[8 * i + e], s);
+      for (int e = 0; e < 8; e += 2) mx4_units<GRID, T>((*this)[8 * i + e], (*this)[8 * i + e + 1], s, t + e);
       out[i] = e2m1_codes(t);
     }
   }
