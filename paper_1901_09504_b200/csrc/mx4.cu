@@ -1,5 +1,5 @@
 // ocs_quantize_mx4 / ocs_dequantize_mx4: rows to block-scaled 4-bit codes, the duplicated channels of a split layer appended,
-// and back.  A thread has one block of a row: its scale needs no one else.
+// and back.
 #include "mx4.cuh"
 #include "ptx.cuh"
 
@@ -17,43 +17,60 @@ struct MxRows {
   int* dev_status;
 };
 
-template <int GRID>
-__device__ __forceinline__ void store_block(const MxRows& p, long long r, int b, const MxScale& s, const uint32_t* c) {
-  constexpr int N = mx4_block(GRID), BYTES = N / 2;
-  uint8_t* at = p.scales + mx4_scale_at(r, b, p.chunks);
-  *at = (uint8_t)s.byte;
-  if (b == p.nb - 1)
-    for (int i = b + 1; i & 3; ++i) at[i - b] = 0;     // the group's blocks past the row's end
-  uint8_t* dst = p.codes + r * p.ld_codes + (long long)b * BYTES;
-  const int left = (p.K + 1) / 2 - b * BYTES;          // bytes of the row from here on
-  if (left >= BYTES && p.code_align >= BYTES) {
-    if constexpr (BYTES == 16) *reinterpret_cast<uint4*>(dst) = make_uint4(c[0], c[1], c[2], c[3]);
-    else *reinterpret_cast<uint2*>(dst) = make_uint2(c[0], c[1]);
-  } else if (left >= BYTES && p.code_align >= 4) {
+// A thread's unit of work: a piece of 32 (E4M3) or 64 bytes (E8M0) of a row, which is a block or half of one (kLanes
+// neighbouring threads have the block).
+template <typename T, int GRID>
+struct Piece {
+  static constexpr int N = (GRID == OCS_GRID_E8M0 ? 64 : 32) / (int)sizeof(T), kLanes = mx4_block(GRID) / N, BYTES = N / 2;
+  static_assert(kLanes >= 1, "a block is at least a piece");
+};
+
+// Bits of the largest magnitude of the block that a thread's piece belongs to.
+template <typename T, int GRID>
+__device__ __forceinline__ uint32_t block_max(uint32_t m) {
 #pragma unroll
-    for (int i = 0; i < BYTES / 4; ++i) reinterpret_cast<uint32_t*>(dst)[i] = c[i];
+  for (int o = 1; o < Piece<T, GRID>::kLanes; o <<= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
+  return m;
+}
+
+// Piece j of row r: codes, and by the block's first thread its scale.
+template <typename T, int GRID>
+__device__ __forceinline__ void store_piece(const MxRows& p, uint8_t* codes, uint8_t* scales, int j, const MxScale& s, const uint32_t* c) {
+  using P = Piece<T, GRID>;
+  if (j % P::kLanes == 0) {
+    const int b = j / P::kLanes;
+    uint8_t* at = scales + (b >> 2) * kMxTile + (b & 3);
+    *at = (uint8_t)s.byte;
+    if (b == p.nb - 1)
+      for (int i = b + 1; i & 3; ++i) at[i - b] = 0;     // the group's blocks past the row's end
+  }
+  uint8_t* dst = codes + j * P::BYTES;
+  const int left = (p.K + 1) / 2 - j * P::BYTES;          // bytes of the row from here on
+  if (left >= P::BYTES && p.code_align >= P::BYTES) {
+    if constexpr (P::BYTES == 16) *reinterpret_cast<uint4*>(dst) = make_uint4(c[0], c[1], c[2], c[3]);
+    else if constexpr (P::BYTES == 8) *reinterpret_cast<uint2*>(dst) = make_uint2(c[0], c[1]);
+    else *reinterpret_cast<uint32_t*>(dst) = c[0];
   } else {
 #pragma unroll
-    for (int i = 0; i < BYTES; ++i)
+    for (int i = 0; i < P::BYTES; ++i)
       if (i < left) dst[i] = (uint8_t)(c[i / 4] >> (8 * (i & 3)));
   }
 }
 
-// Whether block b of row r can be read by Block::load: all its elements are the row's own, and where rows start anywhere
+// Whether piece j of row r can be read by Block::load: all its elements are the row's own, and where rows start anywhere
 // (ALIGN 0), what it reads around them lies in the matrix too (in neighbouring rows, or between them).
 template <int N, int ALIGN>
-__device__ __forceinline__ bool whole_block(const MxRows& p, long long r, int b) {
-  if ((b + 1) * N > p.C) return false;
-  return ALIGN || ((r > 0 || b > 0) && (r + 1 < p.rows || (b + 2) * N <= p.C));
+__device__ __forceinline__ bool whole_piece(const MxRows& p, long long r, int j) {
+  if ((j + 1) * N > p.C) return false;
+  return ALIGN || ((r > 0 || j > 0) && (r + 1 < p.rows || (j + 2) * N <= p.C));
 }
 
-// The row's tail, elements [first, last) of the expanded row from the first block on that is not all its own, into shared
-// memory by G threads, zeros up to a block's end: a thread per element, so that the indices come in one load and the values
-// in another.
+// The row's tail, from the first piece on that is not all its own, into shared memory by G threads, zeros up to the last
+// piece's end: a thread per element, so that the indices come in one load and the values in another.
 constexpr int kTailBytes = 8192;
 template <typename T, int N>
-__device__ __forceinline__ void stage_tail(const MxRows& p, const T* x, int first, int blocks, T* s, int tx, int G) {
-  for (int e = tx; e < blocks * N; e += G) {
+__device__ __forceinline__ void stage_tail(const MxRows& p, const T* x, int first, int pieces, T* s, int tx, int G) {
+  for (int e = tx; e < pieces * N; e += G) {
     int src = first + e;
     T v = from_f32<T>(0.0f);
     if (src < p.K) {
@@ -68,14 +85,14 @@ __device__ __forceinline__ void stage_tail(const MxRows& p, const T* x, int firs
 }
 
 constexpr int kRowThreads = 512;
+constexpr int kRowPieces = 4;       // most pieces per thread
 
-// G = blockDim.x threads (a power of two below 32, or whole warps) and NV blocks each for one row, or (E8M0, whose blocks need
+// G = blockDim.x threads (a power of two below 32, or whole warps) and NV pieces each for one row, or (E8M0, whose blocks need
 // nothing of their row) a part of one: blockIdx.y.  blockDim.y rows per CTA.  E4M3: a row's scale is that of its largest
 // magnitude, so the row waits in registers for it.
 template <typename T, int GRID, int ALIGN, int NV>
-__global__ void __launch_bounds__(kRowThreads, NV * Block<T, mx4_block(GRID)>::W > 16 ? 2 : 3)
-mx4_rows_kernel(const T* __restrict__ X, const MxRows p, int tail_room) {
-  constexpr int N = mx4_block(GRID);
+__global__ void __launch_bounds__(kRowThreads, NV * Block<T, Piece<T, GRID>::N>::W > 16 ? 2 : 3) mx4_rows_kernel(const T* __restrict__ X, const MxRows p, int tail_room) {
+  constexpr int N = Piece<T, GRID>::N;
   __shared__ uint32_t s_max[16];
   __shared__ __align__(16) unsigned char s_tail[kTailBytes];
   grid_launch_dependents();
@@ -83,17 +100,17 @@ mx4_rows_kernel(const T* __restrict__ X, const MxRows p, int tail_room) {
   const long long r = (long long)blockIdx.x * blockDim.y + threadIdx.y;
   const bool live = r < p.rows;
   const T* x = X + (live ? r : 0) * p.ldx;
-  const int lo = GRID == OCS_GRID_E8M0 ? (int)blockIdx.y * G * NV : 0, hi = min(lo + G * NV, p.nb);
-  const int t0 = max(p.C / N, lo), tail = hi - t0;            // the tail's blocks in this part
+  const int lo = GRID == OCS_GRID_E8M0 ? (int)blockIdx.y * G * NV : 0, hi = min(lo + G * NV, p.nb * Piece<T, GRID>::kLanes);
+  const int t0 = max(p.C / N, lo), tail = hi - t0;            // the tail's pieces in this part
   const bool staged = tail > 0 && tail <= tail_room;
   T* my_tail = reinterpret_cast<T*>(s_tail) + threadIdx.y * tail_room * N;
   Block<T, N> v[NV];
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
-    const int b = lo + tx + i * G;
-    if (b >= hi || !live) v[i].clear();
-    else if (whole_block<N, ALIGN>(p, r, b)) v[i].template load<ALIGN>(x + b * N);
-    else if (!staged || b < t0) v[i].gather(x, b * N, p.C, p.K, p.idx_map, p.dev_status);
+    const int j = lo + tx + i * G;
+    if (j >= hi || !live) v[i].clear();
+    else if (whole_piece<N, ALIGN>(p, r, j)) v[i].template load<ALIGN>(x + j * N);
+    else if (!staged || j < t0) v[i].gather(x, j * N, p.C, p.K, p.idx_map, p.dev_status);
   }
   if (staged) {
     if (live) stage_tail<T, N>(p, x, t0 * N, tail, my_tail, tx, G);
@@ -101,14 +118,14 @@ mx4_rows_kernel(const T* __restrict__ X, const MxRows p, int tail_room) {
     else __syncwarp();
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int b = lo + tx + i * G;
-      if (b >= t0 && b < hi && live) v[i].from_shared(my_tail + (b - t0) * N);
+      const int j = lo + tx + i * G;
+      if (j >= t0 && j < hi && live) v[i].from_shared(my_tail + (j - t0) * N);
     }
   }
   uint32_t mine[NV], m = 0;
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
-    mine[i] = v[i].max_bits();
+    mine[i] = block_max<T, GRID>(v[i].max_bits());
     m = max(m, mine[i]);
   }
   int k = 0;
@@ -127,14 +144,16 @@ mx4_rows_kernel(const T* __restrict__ X, const MxRows p, int tail_room) {
   }
   if (!live) return;
   if (m >= 0x7f800000u && (GRID == OCS_GRID_E8M0 || tx == 0)) flag(p.dev_status, OCS_DEV_NONFINITE);
+  uint8_t* codes = p.codes + r * p.ld_codes;
+  uint8_t* scales = p.scales + mx4_scale_at(r, 0, p.chunks);
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
-    const int b = lo + tx + i * G;
-    if (b >= hi) break;
+    const int j = lo + tx + i * G;
+    if (j >= hi) break;
     const MxScale s = mx4_scale<GRID, T>(mine[i], k);
     uint32_t c[N / 8];
     v[i].template codes<GRID>(s, c);
-    store_block<GRID>(p, r, b, s, c);
+    store_piece<T, GRID>(p, codes, scales, j, s, c);
   }
 }
 
@@ -145,12 +164,12 @@ constexpr int kStagedThreads = 1024, kStagedRing = 4;
 constexpr size_t kStagedBytes = 224 * 1024;
 template <typename T>
 __global__ void __launch_bounds__(kStagedThreads, 1) mx4_staged_rows_kernel(const T* __restrict__ X, const MxRows p, int ring) {
-  constexpr int N = 16, NV = 2;
+  constexpr int GRID = OCS_GRID_E4M3, N = Piece<T, GRID>::N, NV = kRowPieces;
   extern __shared__ __align__(128) unsigned char smem[];   // [ring] rows
   __shared__ __align__(8) uint64_t bars[kStagedRing];
   __shared__ uint32_t s_max[2][32];
   __shared__ int abort_flag;
-  const int tx = threadIdx.x, lane = tx & 31;
+  const int tx = threadIdx.x, lane = tx & 31, pieces = p.nb * Piece<T, GRID>::kLanes;
   const uint32_t row_bytes = (uint32_t)p.C * (uint32_t)sizeof(T);
   grid_launch_dependents();
   auto request = [&](long long r, int slot) {   // one thread
@@ -177,14 +196,14 @@ __global__ void __launch_bounds__(kStagedThreads, 1) mx4_staged_rows_kernel(cons
     uint32_t mine[NV], m = 0;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int b = tx + i * kStagedThreads;
-      if ((b + 1) * N <= p.C) v[i].from_shared(row + b * N);
+      const int j = tx + i * kStagedThreads;
+      if ((j + 1) * N <= p.C) v[i].from_shared(row + j * N);
       else {
         v[i].clear();
-        if (b < p.nb)
+        if (j < pieces)
 #pragma unroll
           for (int e = 0; e < N; ++e) {
-            int src = b * N + e;
+            int src = j * N + e;
             if (src < p.K) {
               if (src >= p.C) {
                 src = __ldg(p.idx_map + src);
@@ -196,6 +215,10 @@ __global__ void __launch_bounds__(kStagedThreads, 1) mx4_staged_rows_kernel(cons
           }
       }
       mine[i] = v[i].max_bits();
+    }
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      mine[i] = block_max<T, GRID>(mine[i]);
       m = max(m, mine[i]);
     }
     m = __reduce_max_sync(0xffffffffu, m);
@@ -209,14 +232,16 @@ __global__ void __launch_bounds__(kStagedThreads, 1) mx4_staged_rows_kernel(cons
       p.row_scales[r] = two_to(k);
       if (m >= 0x7f800000u) flag(p.dev_status, OCS_DEV_NONFINITE);
     }
+    uint8_t* codes = p.codes + r * p.ld_codes;
+    uint8_t* scales = p.scales + mx4_scale_at(r, 0, p.chunks);
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int b = tx + i * kStagedThreads;
-      if (b >= p.nb) break;
-      const MxScale s = mx4_scale<OCS_GRID_E4M3, T>(mine[i], k);
-      uint32_t c[2];
-      v[i].template codes<OCS_GRID_E4M3>(s, c);
-      store_block<OCS_GRID_E4M3>(p, r, b, s, c);
+      const int j = tx + i * kStagedThreads;
+      if (j >= pieces) break;
+      const MxScale s = mx4_scale<GRID, T>(mine[i], k);
+      uint32_t c[N / 8];
+      v[i].template codes<GRID>(s, c);
+      store_piece<T, GRID>(p, codes, scales, j, s, c);
     }
     if (++slot == ring) { slot = 0; phase ^= 1u; }
   }
@@ -229,13 +254,13 @@ __global__ void __launch_bounds__(kStagedThreads, 1) mx4_staged_rows_kernel(cons
 
 // E4M3, other rows that no CTA's registers hold: read twice, the second time from L2.
 template <typename T, int ALIGN>
-__global__ void __launch_bounds__(kRowThreads, 2) mx4_long_rows_kernel(const T* __restrict__ X, const MxRows p) {
-  constexpr int N = 16;
+__global__ void __launch_bounds__(kRowThreads, 3) mx4_long_rows_kernel(const T* __restrict__ X, const MxRows p) {
+  constexpr int GRID = OCS_GRID_E4M3, N = Piece<T, GRID>::N;
   __shared__ uint32_t s_max[2][16];
   __shared__ __align__(16) unsigned char s_tail[kTailBytes];
   grid_launch_dependents();
   const int tx = threadIdx.x, lane = tx & 31;
-  const int t0 = p.C / N, tail = p.nb - t0;
+  const int pieces = p.nb * Piece<T, GRID>::kLanes, t0 = p.C / N, tail = pieces - t0;
   const bool staged = tail * N * (int)sizeof(T) <= kTailBytes;
   T* my_tail = reinterpret_cast<T*>(s_tail);
   int odd = 0;
@@ -246,16 +271,16 @@ __global__ void __launch_bounds__(kRowThreads, 2) mx4_long_rows_kernel(const T* 
       stage_tail<T, N>(p, x, t0 * N, tail, my_tail, tx, kRowThreads);
       __syncthreads();
     }
-    auto load = [&](Block<T, N>& v, int b) {
-      if (whole_block<N, ALIGN>(p, r, b)) v.template load<ALIGN>(x + b * N);
-      else if (staged && b >= t0) v.from_shared(my_tail + (b - t0) * N);
-      else v.gather(x, b * N, p.C, p.K, p.idx_map, p.dev_status);
+    auto load = [&](Block<T, N>& v, int j) {
+      if (whole_piece<N, ALIGN>(p, r, j)) v.template load<ALIGN>(x + j * N);
+      else if (staged && j >= t0) v.from_shared(my_tail + (j - t0) * N);
+      else v.gather(x, j * N, p.C, p.K, p.idx_map, p.dev_status);
     };
     uint32_t m = 0;
-#pragma unroll 2
-    for (int b = tx; b < p.nb; b += kRowThreads) {
+#pragma unroll 4
+    for (int j = tx; j < pieces; j += kRowThreads) {
       Block<T, N> v;
-      load(v, b);
+      load(v, j);
       m = max(m, v.max_bits());
     }
     m = __reduce_max_sync(0xffffffffu, m);
@@ -267,24 +292,29 @@ __global__ void __launch_bounds__(kRowThreads, 2) mx4_long_rows_kernel(const T* 
       p.row_scales[r] = two_to(k);
       if (m >= 0x7f800000u) flag(p.dev_status, OCS_DEV_NONFINITE);
     }
+    uint8_t* codes = p.codes + r * p.ld_codes;
+    uint8_t* scales = p.scales + mx4_scale_at(r, 0, p.chunks);
 #pragma unroll 2
-    for (int b = tx; b < p.nb; b += kRowThreads) {
+    for (int j0 = 0; j0 < pieces; j0 += kRowThreads) {   // (whole warps stay: they share blocks)
+      const int j = j0 + tx;
       Block<T, N> v;
-      load(v, b);
-      const MxScale s = mx4_scale<OCS_GRID_E4M3, T>(v.max_bits(), k);
-      uint32_t c[2];
-      v.template codes<OCS_GRID_E4M3>(s, c);
-      store_block<OCS_GRID_E4M3>(p, r, b, s, c);
+      v.clear();
+      if (j < pieces) load(v, j);
+      const MxScale s = mx4_scale<GRID, T>(block_max<T, GRID>(v.max_bits()), k);
+      uint32_t c[N / 8];
+      v.template codes<GRID>(s, c);
+      if (j < pieces) store_piece<T, GRID>(p, codes, scales, j, s, c);
     }
   }
 }
 
 template <typename T, int GRID, int ALIGN>
 ocs_status launch_rows(const T* X, const MxRows& p, cudaStream_t stream) {
-  constexpr int N = mx4_block(GRID);
-  if (GRID == OCS_GRID_E4M3 && p.nb > 2 * kRowThreads) {
+  constexpr int N = Piece<T, GRID>::N;
+  const int pieces = p.nb * Piece<T, GRID>::kLanes;
+  if (GRID == OCS_GRID_E4M3 && pieces > kRowPieces * kRowThreads) {
     const size_t row_bytes = (size_t)p.C * sizeof(T);
-    if (ALIGN && p.rows >= 2 * kNumSMs && p.nb <= 2 * kStagedThreads && row_bytes % 16 == 0 && 2 * row_bytes <= kStagedBytes) {
+    if (ALIGN && p.rows >= 2 * kNumSMs && pieces <= kRowPieces * kStagedThreads && row_bytes % 16 == 0 && 2 * row_bytes <= kStagedBytes) {
       const int ring = (int)(kStagedBytes / row_bytes < kStagedRing ? kStagedBytes / row_bytes : kStagedRing);
       if (cudaFuncSetAttribute(mx4_staged_rows_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kStagedBytes) != cudaSuccess)
         return OCS_ERR_CUDA;
@@ -292,18 +322,20 @@ ocs_status launch_rows(const T* X, const MxRows& p, cudaStream_t stream) {
       mx4_staged_rows_kernel<T><<<kNumSMs, kStagedThreads, ring * row_bytes, stream>>>(X, p, ring);
       return launch_status();
     }
-    const long long most = 2 * kNumSMs;
+    const long long most = 3 * kNumSMs;
     LaunchScope ls("mx4_long_rows_kernel", stream);
     mx4_long_rows_kernel<T, ALIGN><<<(unsigned)(p.rows < most ? p.rows : most), kRowThreads, 0, stream>>>(X, p);
     return launch_status();
   }
-  // few rows: a thread for every block; many: two blocks each (E8M0: one, of twice the size)
-  const int nv = GRID == OCS_GRID_E4M3 && (p.nb > kRowThreads || (p.rows > kNumSMs && p.nb > 32)) ? 2 : 1;
-  const int part = (p.nb + nv - 1) / nv;   // blocks per thread column
+  // few rows: a thread for every piece, as far as a CTA has them; many: two pieces each, or four (E8M0: one, twice the size)
+  int nv = GRID == OCS_GRID_E4M3 && p.rows > kNumSMs && pieces > 32 ? 2 : 1;
+  if (GRID == OCS_GRID_E4M3)
+    while (pieces > nv * kRowThreads) nv *= 2;
+  const int part = (pieces + nv - 1) / nv;
   int G = 4;
   while (G < part && G < 32) G *= 2;
   if (part > 32) G = part < kRowThreads ? (part + 31) / 32 * 32 : kRowThreads;
-  const int y = GRID == OCS_GRID_E8M0 ? (p.nb + G - 1) / G : 1;
+  const int y = GRID == OCS_GRID_E8M0 ? (part + G - 1) / G : 1;
   const int R = G <= 128 && p.rows * G > 32 * kNumSMs ? 256 / G : (G < 32 ? 32 / G : 1);
   const long long ctas = (p.rows + R - 1) / R;
   if (ctas > 0x7fffffff || y > 65535) return OCS_ERR_UNSUPPORTED;
@@ -311,7 +343,10 @@ ocs_status launch_rows(const T* X, const MxRows& p, cudaStream_t stream) {
   const int room = kTailBytes / (R * N * (int)sizeof(T));
   LaunchScope ls("mx4_rows_kernel", stream);
   if (nv == 1) mx4_rows_kernel<T, GRID, ALIGN, 1><<<grid, block, 0, stream>>>(X, p, room);
-  else if constexpr (GRID == OCS_GRID_E4M3) mx4_rows_kernel<T, GRID, ALIGN, 2><<<grid, block, 0, stream>>>(X, p, room);
+  else if constexpr (GRID == OCS_GRID_E4M3) {
+    if (nv == 2) mx4_rows_kernel<T, GRID, ALIGN, 2><<<grid, block, 0, stream>>>(X, p, room);
+    else mx4_rows_kernel<T, GRID, ALIGN, 4><<<grid, block, 0, stream>>>(X, p, room);
+  }
   return launch_status();
 }
 template <typename T, int ALIGN>

@@ -186,7 +186,7 @@ struct Block {
   // Elements c, c + 1, ... of the expanded row: the row's C own, then its duplicated channels up to K, then zeros.  All
   // indices are asked for before the first value, and all values before the first is used.
   __device__ __forceinline__ void gather(const T* x, int c, int C, int K, const int32_t* idx_map, int* dev_status) {
-    constexpr int R = 16;
+    constexpr int R = N < 16 ? N : 16;
 #pragma unroll
     for (int h = 0; h < N; h += R) {
       int src[R];
