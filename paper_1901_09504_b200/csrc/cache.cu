@@ -1,7 +1,8 @@
 // ocs_cache_write / ocs_cache_read: a paged cache of keys and values that is quantized as it is written.
 // A page holds page_size tokens x heads vectors: first all their codes, then their block scales, then their row scales, so
-// that every section is dense and a page moves as one run of bytes.  Four lanes' worth of arithmetic per 64 bytes: memory
-// bounds both directions.
+// that every section is dense and a page moves as one run of bytes.  A thread has 32 numbers of a vector (16 where fp32 is read): a
+// block of E8M0, two of E4M3.  Memory is what should bound them; what a thread does besides its numbers (finding its vector, its
+// slot or page) has to stay small against them.
 #include "mx4.cuh"
 
 namespace ocs {
@@ -38,48 +39,41 @@ struct CacheArgs {
   int table_cols, B;
 };
 
-constexpr int kUnit = 16;           // elements of a vector that a lane has at a time
+constexpr int kUnit = 32;           // elements of a vector that a thread has
 constexpr int kMaxDim = 1024;
 
-// N = 16 elements at x, of which `left` exist (zeros behind them)
-template <typename T>
-__device__ __forceinline__ void load_unit(Block<T, kUnit>& v, const T* x, int left, bool wide) {
-  if (wide && left >= kUnit) v.template load<16>(x);
-  else v.gather(x, 0, min(left, kUnit), min(left, kUnit), nullptr, nullptr);
-}
-
-// A group of GS lanes (a power of two, at least 2) per vector, U units of 16 elements per lane, consecutive.
-template <typename T, int GRID, int U>
-__global__ void __launch_bounds__(256) cache_write_kernel(const CacheArgs a, int gs_log2, int wide) {
-  const long long g = (long long)blockIdx.x * 256 + threadIdx.x;
-  const int lane = (int)(g & ((1 << gs_log2) - 1)), which = blockIdx.y;
-  const long long vec = g >> gs_log2, t = vec / a.heads;
-  const int h = (int)(vec - t * a.heads);
+// A group of 2^gs_log2 lanes per vector.  ALIGN: what all vectors are aligned to (32, 16, or 0: their element).
+template <typename T, int GRID, int ALIGN>
+__global__ void __launch_bounds__(256) cache_write_kernel(const CacheArgs a, int gs_log2) {
+  const unsigned long long g = (unsigned long long)blockIdx.x * 256 + threadIdx.x, vec = g >> gs_log2;
+  const int lane = (int)g & ((1 << gs_log2) - 1), which = blockIdx.y;
+  const long long t = vec >> 32 ? (long long)(vec / (unsigned)a.heads) : (long long)((unsigned)vec / (unsigned)a.heads);
+  const int h = (int)(vec - (unsigned long long)t * a.heads);
+  const int c = lane * kUnit, left = a.dim - c;      // (left <= 0: a lane of the group beyond the vector)
   long long slot = -1;
   if (t < a.rows) {
     slot = __ldg(a.slots + t);
     if (slot >= a.n_slots) { if (lane == 0) flag(a.dev_status, OCS_DEV_BAD_INDEX); slot = -1; }
   }
-  Block<T, kUnit> v[U];
-  uint32_t mine[U], m = 0;
+  Block<T, kUnit> v;
+  if (slot < 0 || left <= 0) v.clear();
+  else {
+    const T* x = static_cast<const T*>(a.x[which]) + t * a.ld_row[which] + h * a.ld_head[which] + c;
+    if (ALIGN && left >= kUnit) v.template load<ALIGN ? ALIGN : 16>(x);
+    else if (ALIGN && left == kUnit / 2) {   // dim is an odd multiple of 16
+      Block<T, kUnit / 2> b;
+      b.template load<16>(x);
+      v.clear();
 #pragma unroll
-  for (int i = 0; i < U; ++i) {
-    const int c = (lane * U + i) * kUnit;
-    if (slot >= 0 && c < a.dim)
-      load_unit<T>(v[i], static_cast<const T*>(a.x[which]) + t * a.ld_row[which] + h * a.ld_head[which] + c, a.dim - c, wide);
-    else v[i].clear();
-    mine[i] = v[i].max_bits();
-    m = max(m, mine[i]);
+      for (int j = 0; j < b.W; ++j) v.w[j] = b.w[j];
+    } else v.gather(x, 0, min(left, kUnit), min(left, kUnit), nullptr, nullptr);
   }
-  if (GRID == OCS_GRID_E8M0) {
-    // blocks of two units: a lane's own two, or a pair of lanes
-    if (U == 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
-  } else {
+  uint32_t m = v.max_bits();
+  if (GRID != OCS_GRID_E8M0)
     for (int o = 1; o < (1 << gs_log2); o <<= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
-  }
-  if (slot < 0) return;
+  if (slot < 0 || left <= 0) return;
   if (m >= 0x7f800000u) flag(a.dev_status, OCS_DEV_NONFINITE);
-  const long long page = slot / a.page_size;
+  const long long page = (unsigned long long)slot >> 32 ? slot / a.page_size : (long long)((unsigned)slot / (unsigned)a.page_size);
   const long long at = (slot - page * a.page_size) * a.heads + h;
   uint8_t* base = a.pages[which] + page * a.g.bytes;
   float* row_scale = reinterpret_cast<float*>(base + a.g.at_r) + at;
@@ -89,35 +83,40 @@ __global__ void __launch_bounds__(256) cache_write_kernel(const CacheArgs a, int
     const float alpha = __uint_as_float(m);
     const RowGrid grid = row_grid(alpha, 127.0f);
     if (lane == 0) *row_scale = __fdiv_rn(alpha, 127.0f);
+    uint32_t w[8];
 #pragma unroll
-    for (int i = 0; i < U; ++i) {
-      const int c = (lane * U + i) * kUnit;
-      if (c >= a.dim) break;
-      uint32_t w[4];
+    for (int j = 0; j < 8; ++j) {
+      int q[4];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        int q[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) q[e] = row_code<true>(__fmul_rn(v[i][4 * j + e], grid.up), grid.inv);
-        w[j] = pack4(q[0], q[1], q[2], q[3]);
-      }
-      *reinterpret_cast<uint4*>(codes + c) = make_uint4(w[0], w[1], w[2], w[3]);
+      for (int e = 0; e < 4; ++e) q[e] = row_code<true>(__fmul_rn(v[4 * j + e], grid.up), grid.inv);
+      w[j] = pack4(q[0], q[1], q[2], q[3]);
     }
+    *reinterpret_cast<uint4*>(codes + c) = make_uint4(w[0], w[1], w[2], w[3]);
+    if (left > 16) *reinterpret_cast<uint4*>(codes + c + 16) = make_uint4(w[4], w[5], w[6], w[7]);
   } else {
-    const int k = GRID == OCS_GRID_E4M3 ? mx4_row_exponent(m) : 0;
-    if (GRID == OCS_GRID_E4M3 && lane == 0) *row_scale = two_to(k);
+    uint32_t w[4];
+    if constexpr (GRID == OCS_GRID_E8M0) {
+      const MxScale s = mx4_scale<GRID, T>(m, 0);
+      v.template codes<GRID>(s, w);
+      scales[lane] = (uint8_t)s.byte;
+    } else {
+      const int k = mx4_row_exponent(m);
+      if (lane == 0) *row_scale = two_to(k);
+      uint32_t byte[2];
 #pragma unroll
-    for (int i = 0; i < U; ++i) {
-      const int c = (lane * U + i) * kUnit;
-      if (c >= a.dim) break;
-      const uint32_t mb = GRID == OCS_GRID_E8M0 ? m : mine[i];
-      const MxScale s = mx4_scale<GRID, T>(mb, k);
-      uint32_t w[2];
-      v[i].template codes<GRID>(s, w);
-      *reinterpret_cast<uint2*>(codes + c / 2) = make_uint2(w[0], w[1]);
-      if (GRID == OCS_GRID_E4M3) scales[c / 16] = (uint8_t)s.byte;
-      else if (c % 32 == 0) scales[c / 32] = (uint8_t)s.byte;
+      for (int i = 0; i < 2; ++i) {
+        Block<T, 16> b;
+#pragma unroll
+        for (int j = 0; j < Block<T, 16>::W; ++j) b.w[j] = v.w[i * Block<T, 16>::W + j];
+        const MxScale s = mx4_scale<GRID, T>(b.max_bits(), k);
+        b.template codes<GRID>(s, w + 2 * i);
+        byte[i] = s.byte;
+      }
+      if (left > 16) *reinterpret_cast<uint16_t*>(scales + 2 * lane) = (uint16_t)(byte[0] | byte[1] << 8);
+      else scales[2 * lane] = (uint8_t)byte[0];
     }
+    if (left > 16) *reinterpret_cast<uint4*>(codes + c / 2) = make_uint4(w[0], w[1], w[2], w[3]);
+    else *reinterpret_cast<uint2*>(codes + c / 2) = make_uint2(w[0], w[1]);
   }
 }
 
@@ -133,119 +132,179 @@ __device__ __forceinline__ int sequence_of(const int32_t* starts, int B, long lo
   return lo;
 }
 
-constexpr int kReadTokens = 16;     // output rows of a CTA
+constexpr int kReadTokens = 32;     // most output rows of a CTA
 
-template <typename T, int GRID>
-__global__ void __launch_bounds__(256) cache_read_kernel(const CacheArgs a, int units, int wide) {
-  __shared__ long long s_page[kReadTokens], s_at[kReadTokens];   // page (-1: no such row, -2: a bad page), vector in it
-  const long long t0 = (long long)blockIdx.x * kReadTokens;
+// Where a token's vectors are in its page (codes NULL: no such row; rows NULL: a bad page).
+struct TokenAt {
+  const uint8_t* codes;
+  const uint8_t* scales;
+  const float* rows;
+};
+
+template <typename T> constexpr int kReadUnit = 64 / (int)sizeof(T);
+
+// `tokens` output rows per CTA; per = heads * units threads' worth of work each, units = ceil(dim / U), divided by as
+// floor(x * inv_units / 2^32) where they are more than one (exact: x below 2^26, units at most 64).  A thread has U numbers of a
+// vector: 64 bytes of output.
+template <typename T, int GRID, int ALIGN>
+__global__ void __launch_bounds__(256) cache_read_kernel(const CacheArgs a, int tokens, int units, uint32_t inv_units) {
+  constexpr int U = kReadUnit<T>;
+  __shared__ TokenAt s_at[kReadTokens];
+  const long long t0 = (long long)blockIdx.x * tokens;
   const int which = blockIdx.y;
-  if (threadIdx.x < kReadTokens) {
+  if (threadIdx.x < tokens) {
     const long long t = t0 + threadIdx.x;
-    long long page = -1, at = 0;
+    TokenAt w{nullptr, nullptr, nullptr};
     const int b = t < a.rows ? sequence_of(a.starts, a.B, t) : -1;
     if (b >= 0) {
-      const long long pos = t - __ldg(a.starts + b), col = pos / a.page_size;
-      page = col < a.table_cols ? __ldg(a.table + b * a.ld_table + col) : -2;
-      if (page < 0 || page >= a.n_pages) { flag(a.dev_status, OCS_DEV_BAD_INDEX); page = -2; }
-      at = (pos - col * a.page_size) * a.heads;
+      const int pos = (int)t - __ldg(a.starts + b), col = (unsigned)pos / (unsigned)a.page_size;
+      const int page = col < a.table_cols ? __ldg(a.table + b * a.ld_table + col) : -1;
+      const uint8_t* base = a.pages[which];
+      w.codes = base;
+      if ((unsigned)page >= (unsigned)a.n_pages) flag(a.dev_status, OCS_DEV_BAD_INDEX);
+      else {
+        const long long at = (long long)(pos - col * a.page_size) * a.heads;
+        base += page * a.g.bytes;
+        w.codes = base + at * a.g.cb;
+        w.scales = base + a.g.at_s + at * a.g.sb;
+        w.rows = reinterpret_cast<const float*>(base + a.g.at_r) + at;
+      }
     }
-    s_page[threadIdx.x] = page;
-    s_at[threadIdx.x] = at;
+    s_at[threadIdx.x] = w;
   }
   __syncthreads();
-  const int per = a.heads * units, total = kReadTokens * per;
-  for (int i = threadIdx.x; i < total; i += 256) {
-    const int tok = i / per, in = i - tok * per, h = in / units, u = in - h * units;
-    const long long page = s_page[tok];
-    if (page == -1) continue;
-    const int c = u * kUnit, left = a.dim - c;
-    T out[kUnit];
-    if (page < 0) {
+  const int per = a.heads * units;
+  const int step_tok = 256 / per, step_in = 256 - step_tok * per;
+  int tok = (int)threadIdx.x / per, in = (int)threadIdx.x - tok * per;
+  T* y0 = static_cast<T*>(a.x[which]) + t0 * a.ld_row[which];
+#pragma unroll 2
+  for (; tok < tokens; ) {
+    const TokenAt w = s_at[tok];
+    const int h = units == 1 ? in : (int)__umulhi((uint32_t)in, inv_units), u = in - h * units, c = u * U, left = a.dim - c;
+    T* y = y0 + tok * a.ld_row[which] + h * a.ld_head[which] + c;
+    tok += step_tok;
+    in += step_in;
+    if (in >= per) { in -= per; ++tok; }
+    if (!w.codes) continue;
+    T out[U];
+    if (!w.rows) {
 #pragma unroll
-      for (int e = 0; e < kUnit; ++e) out[e] = from_f32<T>(0.0f);
+      for (int e = 0; e < U; ++e) out[e] = from_f32<T>(0.0f);
+    } else if constexpr (GRID == OCS_GRID_I8) {
+      const float step = __ldg(w.rows + h);
+      const uint8_t* codes = w.codes + h * a.g.cb + c;
+      const uint4 q0 = __ldg(reinterpret_cast<const uint4*>(codes));
+      const uint4 q1 = U > 16 && left > 16 ? __ldg(reinterpret_cast<const uint4*>(codes) + 1) : make_uint4(0, 0, 0, 0);
+      const uint32_t q[8] = {q0.x, q0.y, q0.z, q0.w, q1.x, q1.y, q1.z, q1.w};
+#pragma unroll
+      for (int e = 0; e < U; ++e) out[e] = from_f32<T>(__fmul_rn((float)(int8_t)(q[e / 4] >> (8 * (e & 3))), step));
     } else {
-      const uint8_t* base = a.pages[which] + page * a.g.bytes;
-      const long long at = s_at[tok] + h;
-      const uint8_t* codes = base + at * a.g.cb;
-      if constexpr (GRID == OCS_GRID_I8) {
-        const float step = __ldg(reinterpret_cast<const float*>(base + a.g.at_r) + at);
-        const uint4 q = __ldg(reinterpret_cast<const uint4*>(codes + c));
-        const uint32_t w[4] = {q.x, q.y, q.z, q.w};
-#pragma unroll
-        for (int e = 0; e < kUnit; ++e) out[e] = from_f32<T>(__fmul_rn((float)(int8_t)(w[e / 4] >> (8 * (e & 3))), step));
+      const uint8_t* scales = w.scales + h * a.g.sb;
+      const uint8_t* codes = w.codes + h * a.g.cb + c / 2;
+      float unit[2];
+      if (GRID == OCS_GRID_E8M0) unit[0] = unit[1] = e8m0_value(__ldg(scales + c / 32));
+      else {
+        const uint32_t s = U == 16 ? __ldg(scales + u) : __ldg(reinterpret_cast<const uint16_t*>(scales) + u);
+        const float r = __ldg(w.rows + h);
+        unit[0] = __fmul_rn(e4m3_value(s & 255u), r);
+        unit[1] = __fmul_rn(e4m3_value(s >> 8), r);
+      }
+      uint32_t q[U / 8];
+      if constexpr (U == 32) {
+        const uint4 q4 = __ldg(reinterpret_cast<const uint4*>(codes));
+        q[0] = q4.x; q[1] = q4.y; q[2] = q4.z; q[3] = q4.w;
       } else {
-        const uint8_t* scales = base + a.g.at_s + at * a.g.sb;
-        float unit;
-        if (GRID == OCS_GRID_E8M0) unit = e8m0_value(__ldg(scales + c / 32));
-        else unit = __fmul_rn(e4m3_value(__ldg(scales + c / 16)), __ldg(reinterpret_cast<const float*>(base + a.g.at_r) + at));
-        const uint2 q = __ldg(reinterpret_cast<const uint2*>(codes + c / 2));
-        const uint32_t w[2] = {q.x, q.y};
+        const uint2 q2 = __ldg(reinterpret_cast<const uint2*>(codes));
+        q[0] = q2.x; q[1] = q2.y;
+      }
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          __half2 v[4];
-          e2m1_values(w[j], v);
+      for (int j = 0; j < U / 8; ++j) {
+        __half2 v[4];
+        e2m1_values(q[j], v);
+        const unsigned long long uu = pack_f32x2(unit[j / 2], unit[j / 2]);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float2 f = __half22float2(v[e]);
-            out[8 * j + 2 * e] = from_f32<T>(__fmul_rn(f.x, unit));
-            out[8 * j + 2 * e + 1] = from_f32<T>(__fmul_rn(f.y, unit));
-          }
+        for (int e = 0; e < 4; ++e) {
+          const float2 f = __half22float2(v[e]);
+          float v0, v1;
+          unpack_f32x2(mul_f32x2(pack_f32x2(f.x, f.y), uu), v0, v1);
+          out[8 * j + 2 * e] = from_f32<T>(v0);
+          out[8 * j + 2 * e + 1] = from_f32<T>(v1);
         }
       }
     }
-    T* y = static_cast<T*>(a.x[which]) + (t0 + tok) * a.ld_row[which] + h * a.ld_head[which] + c;
-    if (wide && left >= kUnit) {
+    const uint32_t* o = reinterpret_cast<const uint32_t*>(out);
+    if (ALIGN && left >= U) {
+      if constexpr (ALIGN == 32) {
 #pragma unroll
-      for (int j = 0; j < (int)sizeof(T); ++j) reinterpret_cast<uint4*>(y)[j] = reinterpret_cast<uint4*>(out)[j];
+        for (int j = 0; j < U * (int)sizeof(T) / 4; j += 8) store32(reinterpret_cast<uint32_t*>(y) + j, o + j);
+      } else {
+#pragma unroll
+        for (int j = 0; j < U * (int)sizeof(T) / 16; ++j) reinterpret_cast<uint4*>(y)[j] = make_uint4(o[4 * j], o[4 * j + 1], o[4 * j + 2], o[4 * j + 3]);
+      }
+    } else if (ALIGN && U == 32 && left == 16) {   // half a unit: dim is an odd multiple of 16
+#pragma unroll
+      for (int j = 0; j < (int)sizeof(T); ++j) reinterpret_cast<uint4*>(y)[j] = make_uint4(o[4 * j], o[4 * j + 1], o[4 * j + 2], o[4 * j + 3]);
     } else {
 #pragma unroll
-      for (int e = 0; e < kUnit; ++e)
+      for (int e = 0; e < U; ++e)
         if (e < left) y[e] = out[e];
     }
   }
 }
 
-template <typename T, int GRID>
-ocs_status launch_write(const CacheArgs& a, int caches, int wide, cudaStream_t stream) {
-  const int units = (a.dim + kUnit - 1) / kUnit, U = units > 32 ? 2 : 1, lanes = (units + U - 1) / U;
-  int gs = 1;
-  while ((1 << gs) < lanes) ++gs;
+template <typename T, int GRID, int ALIGN>
+ocs_status launch_write(const CacheArgs& a, int caches, cudaStream_t stream) {
+  const int units = (a.dim + kUnit - 1) / kUnit;
+  int gs = 0;
+  while ((1 << gs) < units) ++gs;
   const long long ctas = (((a.rows * a.heads) << gs) + 255) / 256;
   if (ctas > 0x7fffffff) return OCS_ERR_UNSUPPORTED;
   LaunchScope ls("cache_write_kernel", stream);
-  if (U == 1) cache_write_kernel<T, GRID, 1><<<dim3((unsigned)ctas, caches), 256, 0, stream>>>(a, gs, wide);
-  else cache_write_kernel<T, GRID, 2><<<dim3((unsigned)ctas, caches), 256, 0, stream>>>(a, gs, wide);
+  cache_write_kernel<T, GRID, ALIGN><<<dim3((unsigned)ctas, caches), 256, 0, stream>>>(a, gs);
   return launch_status();
 }
 
-template <typename T, int GRID>
-ocs_status launch_read(const CacheArgs& a, int caches, int wide, cudaStream_t stream) {
-  const long long ctas = (a.rows + kReadTokens - 1) / kReadTokens;
+template <typename T, int GRID, int ALIGN>
+ocs_status launch_read(const CacheArgs& a, int caches, cudaStream_t stream) {
+  constexpr int U = kReadUnit<T>;
+  const int units = (a.dim + U - 1) / U, per = a.heads * units;
+  // about four units per thread, while there are CTAs for all SMs
+  int tokens = per < 1024 ? (1024 + per - 1) / per : 1;
+  if (tokens > kReadTokens) tokens = kReadTokens;
+  while (tokens > 1 && (a.rows + tokens - 1) / tokens * caches < 4 * kNumSMs) tokens = (tokens + 1) / 2;
+  const long long ctas = (a.rows + tokens - 1) / tokens;
   if (ctas > 0x7fffffff) return OCS_ERR_UNSUPPORTED;
   LaunchScope ls("cache_read_kernel", stream);
-  cache_read_kernel<T, GRID><<<dim3((unsigned)ctas, caches), 256, 0, stream>>>(a, (a.dim + kUnit - 1) / kUnit, wide);
+  cache_read_kernel<T, GRID, ALIGN><<<dim3((unsigned)ctas, caches), 256, 0, stream>>>(a, tokens, units, units > 1 ? (uint32_t)((0xffffffffull + units) / units) : 0u);
   return launch_status();
 }
 
+template <bool WRITE, typename T, int GRID>
+ocs_status dispatch_align(const CacheArgs& a, int align, int caches, cudaStream_t s) {
+  switch (align) {
+    case 32: return WRITE ? launch_write<T, GRID, 32>(a, caches, s) : launch_read<T, GRID, 32>(a, caches, s);
+    case 16: return WRITE ? launch_write<T, GRID, 16>(a, caches, s) : launch_read<T, GRID, 16>(a, caches, s);
+    default: return WRITE ? launch_write<T, GRID, 0>(a, caches, s) : launch_read<T, GRID, 0>(a, caches, s);
+  }
+}
 template <bool WRITE, typename T>
-ocs_status dispatch_grid(const CacheArgs& a, ocs_grid grid, int caches, int wide, cudaStream_t s) {
+ocs_status dispatch_grid(const CacheArgs& a, ocs_grid grid, int align, int caches, cudaStream_t s) {
   switch (grid) {
-    case OCS_GRID_I8: return WRITE ? launch_write<T, OCS_GRID_I8>(a, caches, wide, s) : launch_read<T, OCS_GRID_I8>(a, caches, wide, s);
-    case OCS_GRID_E8M0: return WRITE ? launch_write<T, OCS_GRID_E8M0>(a, caches, wide, s) : launch_read<T, OCS_GRID_E8M0>(a, caches, wide, s);
-    default: return WRITE ? launch_write<T, OCS_GRID_E4M3>(a, caches, wide, s) : launch_read<T, OCS_GRID_E4M3>(a, caches, wide, s);
+    case OCS_GRID_I8: return dispatch_align<WRITE, T, OCS_GRID_I8>(a, align, caches, s);
+    case OCS_GRID_E8M0: return dispatch_align<WRITE, T, OCS_GRID_E8M0>(a, align, caches, s);
+    default: return dispatch_align<WRITE, T, OCS_GRID_E4M3>(a, align, caches, s);
   }
 }
 template <bool WRITE>
 ocs_status dispatch(const CacheArgs& a, ocs_grid grid, ocs_dtype type, int caches, cudaStream_t s) {
   uintptr_t al = 0;   // of every vector
   for (int i = 0; i < caches; ++i)
-    al |= reinterpret_cast<uintptr_t>(a.x[i]) | (uintptr_t)((a.ld_row[i] | a.ld_head[i]) * elem_bytes(type));
-  const int wide = al % 16 == 0;
+    al |= reinterpret_cast<uintptr_t>(a.x[i]) | (uintptr_t)(((a.rows > 1 ? a.ld_row[i] : 0) | (a.heads > 1 ? a.ld_head[i] : 0)) * elem_bytes(type));
+  const int align = al % 32 == 0 ? 32 : (al % 16 == 0 ? 16 : 0);
   switch (type) {
-    case OCS_F16: return dispatch_grid<WRITE, __half>(a, grid, caches, wide, s);
-    case OCS_BF16: return dispatch_grid<WRITE, __nv_bfloat16>(a, grid, caches, wide, s);
-    default: return dispatch_grid<WRITE, float>(a, grid, caches, wide, s);
+    case OCS_F16: return dispatch_grid<WRITE, __half>(a, grid, align, caches, s);
+    case OCS_BF16: return dispatch_grid<WRITE, __nv_bfloat16>(a, grid, align, caches, s);
+    default: return dispatch_grid<WRITE, float>(a, grid, align, caches, s);
   }
 }
 
