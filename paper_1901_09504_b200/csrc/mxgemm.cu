@@ -6,9 +6,9 @@
 // Layout as in the int8 row product: the weights are the rows of the tensor-core tile (128 channels, the lanes of tensor
 // memory), the tokens its columns, so that few tokens cost a narrow tile.  A K-block is 256 contraction indices: 128 bytes of
 // codes a row (one swizzle span, by TMA) and 2 or 4 pieces of 512 scale bytes per 128 rows, which have to be spread over tensor
-// memory ahead of the products that read them.  tcgen05.cp does that, in order with the products, and takes the tensor cores'
-// time for it: some 32 cycles a piece.  Narrow tiles wait for memory anyway; in the form of 256 tokens (12 pieces for 512
-// cycles of products) four more warps move the pieces through registers while the products before them run.
+// memory ahead of the products that read them.  tcgen05.cp would do that, in order with the products and in the tensor cores'
+// time: some 45 cycles a piece, 12 pieces (E4M3, 256 tokens) for 512 cycles of products.  Four warps move them through
+// registers instead, while the products before them run.
 #include <atomic>
 
 #include "mx4.cuh"
@@ -20,6 +20,7 @@ namespace {
 constexpr int TW = 128;        // channels of one CTA's tile
 constexpr int KB = 128;        // bytes of a K-block's row: 256 contraction indices
 constexpr int kEpiWarps = 8;
+constexpr int kThreads = 64 + 32 * kEpiWarps + 128;   // copy warp, tensor-core warp, epilogue warps, scale warps
 
 __host__ __device__ constexpr int stage_blocks(int tn) { return tn <= 64 ? 2 : 1; }   // K-blocks of a ring stage
 
@@ -35,9 +36,8 @@ struct MxGemm {
   int* dev_status;
 };
 
-// Tensor memory columns: two accumulators, then the scales of one K-block, or of two where warps of their own bring them
-// (kFeed).  256 tokens: the accumulators overlap by as many columns as the scales need; the epilogue empties those first and
-// says so before it goes on.
+// Tensor memory columns: two accumulators, then the scales of two stages.  256 tokens: the accumulators overlap by as many
+// columns as the scales need; the epilogue empties those first and says so before it goes on.
 template <int GRID, int TN, int CG>
 struct MxSmem {
   static constexpr int kTokens = TN / CG;
@@ -57,15 +57,13 @@ struct MxSmem {
   static constexpr int kBudget = 227 * 1024 - 1024 - kCtrlBytes - kScaleBytes - kXExtra;
   static constexpr int kStages = kBudget / kStageBytes < 8 ? kBudget / kStageBytes : 8;
   static constexpr int kDynBytes = 1024 + kStages * kStageBytes + kXExtra + kScaleBytes + kCtrlBytes;
-  static constexpr bool kFeed = TN == 256, kOverlap = kFeed;
-  static constexpr int kThreads = 64 + 32 * kEpiWarps + (kFeed ? 128 : 0);   // copies, tensor cores, epilogue, scales
-  static constexpr int kScaleCols = 4 * kPieces * (1 + kTiles), kBufs = kFeed ? 2 : 1;   // the weights' scales, then the tokens'
-  static constexpr int kAccStride = kOverlap ? 512 - kBufs * kScaleCols - TN : (TN < 32 ? 32 : TN);
+  static constexpr bool kOverlap = TN == 256;
+  static constexpr int kScaleCols = 4 * kPieces * (1 + kTiles), kStageCols = kSub * kScaleCols;   // the weights' scales, then the tokens'
+  static constexpr int kAccStride = kOverlap ? 512 - 2 * kStageCols - TN : (TN < 32 ? 32 : TN);
   static constexpr int kShared = kOverlap ? TN - kAccStride : 0;             // columns of both accumulators
   static constexpr int kScaleCol = kAccStride + (kOverlap ? TN : kAccStride);
-  static constexpr int kUsedCols = kScaleCol + kBufs * kScaleCols;
-  static constexpr uint32_t kFullBytes = kSub * (kWBytes + kTBytes + (kFeed ? 0 : kSWBytes + kSTBytes));   // on a stage's barrier
-  static constexpr uint32_t kFeedBytes = kSub * (kSWBytes + kSTBytes);                                     // on the scales' own
+  static constexpr int kUsedCols = kScaleCol + 2 * kStageCols;
+  static constexpr uint32_t kFullBytes = kSub * (kWBytes + kTBytes), kScaleBytes512 = kSub * (kSWBytes + kSTBytes);   // of a stage
   static constexpr uint32_t kTmemCols = kUsedCols <= 128 ? 128 : (kUsedCols <= 256 ? 256 : 512);
   static_assert(kStages >= 3 && (!kXInRing || kXBytes <= kStages * kStageBytes) && kStageBytes % 1024 == 0 && kTBytes % 1024 == 0 && kUsedCols <= 512, "tile does not fit");
 };
@@ -95,19 +93,7 @@ __device__ __forceinline__ void umma_mx4(uint32_t d, uint64_t a, uint64_t b, uin
 #undef OCS_MX4_MMA
 }
 
-// 512 bytes of scales (32 rows of 16 bytes) to four columns of tensor memory, the same for all four quarters of the lanes;
-// for a pair, of each CTA's own shared memory to its own tensor memory.
-template <int CG>
-__device__ __forceinline__ void copy_scales(uint32_t tmem, uint64_t desc) {
-  if constexpr (CG == 1) asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
-  else asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
-}
-// Shared-memory descriptor of such a piece: no swizzle, groups of eight 16-byte rows 128 bytes apart.
-__device__ __forceinline__ uint64_t scales_desc(uint32_t saddr) {
-  return (uint64_t)((saddr >> 4) & 0x3FFFu) | (uint64_t)(128 >> 4) << 32 | (uint64_t)1 << 46;
-}
-
-// The same by a warp, for its quarter of the lanes: N columns, each lane's 4-byte cells of 16-byte rows.
+// N columns of a warp's quarter of the lanes.
 template <int N>
 __device__ __forceinline__ void tmem_store(uint32_t taddr, const uint32_t* v) {
   static_assert(N == 8 || N == 16, "columns");
@@ -120,16 +106,10 @@ __device__ __forceinline__ void tmem_store(uint32_t taddr, const uint32_t* v) {
                    "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]) : "memory");
 }
 
-template <int CG>
 __device__ __forceinline__ void tma_load_scales(uint32_t dst, const CUtensorMap* map, uint32_t bar, int piece, int tile) {
-  if constexpr (CG == 1)
-    asm volatile(
-        "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
-        ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(0), "r"(piece), "r"(tile) : "memory");
-  else
-    asm volatile(
-        "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%3, %4, %5}], [%2];"
-        ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(0), "r"(piece), "r"(tile) : "memory");
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
+      ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(0), "r"(piece), "r"(tile) : "memory");
 }
 
 // The bounded waits for a whole warp: all lanes go on, or all give up.
@@ -197,7 +177,7 @@ __device__ __forceinline__ void finish(const MxGemm& p, long long at, const uint
 }
 
 template <int GRID, int TN, int CG>
-__global__ void __launch_bounds__(MxSmem<GRID, TN, CG>::kThreads, 1)
+__global__ void __launch_bounds__(kThreads, 1)
 mx_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtensorMap tm_t,
                const __grid_constant__ CUtensorMap tm_sw, const __grid_constant__ CUtensorMap tm_st, const MxGemm p) {
   using L = MxSmem<GRID, TN, CG>;
@@ -215,11 +195,11 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__
   auto accempty_bar = [&](int a) { return smem_u32(bars + 2 * L::kStages + 2 + a); };
   const uint32_t xfull_bar = smem_u32(bars + 2 * L::kStages + 4);
   const uint32_t xready_bar = smem_u32(bars + 2 * L::kStages + 5);
-  auto sfull_bar = [&](int s) { return smem_u32(bars + 2 * L::kStages + 6 + s); };            // kFeed: a stage's scales are here
+  auto sfull_bar = [&](int s) { return smem_u32(bars + 2 * L::kStages + 6 + s); };            // a stage's scales are here
   auto sready_bar = [&](int b) { return smem_u32(bars + 3 * L::kStages + 6 + b); };           // ... and in tensor memory
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 3 * L::kStages + 6 + L::kBufs);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 3 * L::kStages + 8);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
-  static_assert((3 * L::kStages + 6 + L::kBufs) * 8 + 8 <= L::kCtrlBytes, "control block");
+  static_assert((3 * L::kStages + 8) * 8 + 8 <= L::kCtrlBytes, "control block");
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int CL = CG * p.slices;
@@ -244,8 +224,8 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__
       for (int a = 0; a < 2; ++a) {
         mbar_init(accfull_bar(a), 1);
         mbar_init(accempty_bar(a), CG * kEpiWarps);
+        mbar_init(sready_bar(a), CG * 4);
       }
-      for (int b = 0; b < L::kBufs; ++b) mbar_init(sready_bar(b), CG * 4);
       mbar_init(xfull_bar, 1);
       mbar_init(xready_bar, p.slices);
       *abort_flag = 0;
@@ -255,18 +235,18 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__
     }
     __syncwarp();
     asm volatile("bar.arrive 3, 64;" ::: "memory");
-    asm volatile("bar.arrive 2, %0;" ::"n"(L::kThreads) : "memory");
+    asm volatile("bar.arrive 2, %0;" ::"n"(kThreads) : "memory");
     if (CL > 1) cluster_arrive();
   } else if (warp == 1) {
     if (CG == 2) tmem_alloc_pair(smem_u32(tmem_slot), L::kTmemCols);
     else tmem_alloc(smem_u32(tmem_slot), L::kTmemCols);
     tc_fence_before();
-    asm volatile("bar.arrive 2, %0;" ::"n"(L::kThreads) : "memory");
+    asm volatile("bar.arrive 2, %0;" ::"n"(kThreads) : "memory");
     if (CL > 1) cluster_arrive();
     asm volatile("bar.sync 3, 64;" ::: "memory");
   } else {
     if (CL > 1) cluster_arrive();
-    asm volatile("bar.sync 2, %0;" ::"n"(L::kThreads) : "memory");
+    asm volatile("bar.sync 2, %0;" ::"n"(kThreads) : "memory");
   }
   if (CG == 2) cluster_wait();
   tc_fence_after();
@@ -287,7 +267,7 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__
           const int kb = st * L::kSub + u, row = (nt * CG + half) * TW;
           if (CG == 2) tma_load_2d_pair(at + u * L::kWBytes, &tm_w, bar, kb * KB, row);
           else tma_load_2d(at + u * L::kWBytes, &tm_w, bar, kb * KB, row);
-          tma_load_scales<L::kFeed ? 1 : CG>(at + L::kAtSW + u * L::kSWBytes, &tm_sw, L::kFeed ? sfull_bar(s) : bar, kb * L::kPieces, nt * CG + half);
+          tma_load_scales(at + L::kAtSW + u * L::kSWBytes, &tm_sw, sfull_bar(s), kb * L::kPieces, nt * CG + half);
         }
       };
       auto load_t = [&](int s, int st) {
@@ -299,13 +279,12 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__
           else tma_load_2d(at + L::kAtT + u * L::kTBytes, &tm_t, bar, kb * KB, row);
 #pragma unroll
           for (int i = 0; i < L::kTiles; ++i)   // (both CTAs of a pair need the scales of all the tile's tokens)
-            tma_load_scales<L::kFeed ? 1 : CG>(at + L::kAtST + u * L::kSTBytes + i * L::kSWBytes, &tm_st, L::kFeed ? sfull_bar(s) : bar,
-                                               kb * L::kPieces, mt * TN / 128 + i);
+            tma_load_scales(at + L::kAtST + u * L::kSTBytes + i * L::kSWBytes, &tm_st, sfull_bar(s), kb * L::kPieces, mt * TN / 128 + i);
         }
       };
       auto announce = [&](int s) {
         if (half == 0) mbar_arrive_expect_tx(full_bar(s), CG * L::kFullBytes);
-        if (L::kFeed) mbar_arrive_expect_tx(sfull_bar(s), L::kFeedBytes);
+        mbar_arrive_expect_tx(sfull_bar(s), L::kScaleBytes512);
       };
       // weights do not depend on the kernel before: the first ring of them is requested before waiting for it
       if (cluster < p.total) {
@@ -343,10 +322,8 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__
       constexpr uint32_t kDescM = TW * CG;
       const uint16_t mask = (uint16_t)(3u << (rank & ~1));
       const uint64_t w_desc0 = smem_desc_sw128(base), t_desc0 = smem_desc_sw128(base + L::kAtT);
-      const uint64_t sw_desc0 = scales_desc(base + L::kAtSW), st_desc0 = scales_desc(base + L::kAtST);
-      uint32_t sw_col = tmem_base + L::kScaleCol;
       int j = 0, s = 0;
-      uint32_t phase = 0, buf = 0, fed = 0;   // kFeed: buffer of scales and the phase of its barrier
+      uint32_t phase = 0, n = 0;   // n: stages so far
       bool ok = true;
       for (int t = cluster; ok && t < p.total; t += n_clusters, ++j) {
         int mt, nt;
@@ -362,26 +339,12 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__
         const uint32_t d = tmem_base + (uint32_t)(acc * L::kAccStride);
         uint32_t more = 0;
         for (int i = 0; i < my_st; ++i) {
-          if (!mbar_wait(full_bar(s), phase, abort_flag)) { ok = false; break; }
+          if (!mbar_wait(full_bar(s), phase, abort_flag) || !mbar_wait_relaxed(sready_bar(n & 1), (n >> 1) & 1u, abort_flag)) { ok = false; break; }
           tc_fence_after();
           const uint32_t o = (uint32_t)(s * (L::kStageBytes >> 4));
 #pragma unroll
           for (int u = 0; u < L::kSub; ++u) {
-if (L::kFeed) {
-              if (!mbar_wait_relaxed(sready_bar(buf), fed, abort_flag)) { ok = false; break; }
-              tc_fence_after();
-              sw_col = tmem_base + L::kScaleCol + buf * L::kScaleCols;
-              if (++buf == L::kBufs) { buf = 0; fed ^= 1u; }
-            } else {
-#pragma unroll
-              for (int c = 0; c < L::kPieces; ++c) {
-                copy_scales<CG>(sw_col + 4 * c, sw_desc0 + o + u * (L::kSWBytes >> 4) + c * (kMxTile >> 4));
-#pragma unroll
-                for (int k = 0; k < L::kTiles; ++k)
-                  copy_scales<CG>(sw_col + 4 * (L::kPieces + c * L::kTiles + k),
-                                  st_desc0 + o + u * (L::kSTBytes >> 4) + k * (L::kSWBytes >> 4) + c * (kMxTile >> 4));
-              }
-            }
+            const uint32_t sw_col = tmem_base + L::kScaleCol + (n & 1) * L::kStageCols + u * L::kScaleCols;
             const uint32_t st_col = sw_col + 4 * L::kPieces + half_col;
 #pragma unroll
             for (int k = 0; k < 4; ++k) {   // 64 contraction indices: 32 bytes on, 2 in the descriptors' units of 16
@@ -391,8 +354,8 @@ if (L::kFeed) {
                                  mx_instr_desc(GRID, kDescM, TN, sf), sw_col + 4 * c, st_col + 4 * c * L::kTiles, u + k == 0 ? more : 1u);
             }
           }
-          if (!ok) break;
           more = 1;
+          ++n;
           if (CG == 2) umma_commit_pair(empty_bar(s), mask);
           else umma_commit(empty_bar(s));
           if (++s == L::kStages) { s = 0; phase ^= 1; }
@@ -404,42 +367,51 @@ if (L::kFeed) {
     }
     __syncwarp();
     if (CL > 1 && CG == 1) cluster_wait();
-  } else if (L::kFeed && warp >= 2 + kEpiWarps) {
+  } else if (warp >= 2 + kEpiWarps) {
     // ---------------------------------------------------------------- scales (of the CTA's own shared memory and lanes)
-    const uint32_t q = warp & 3, lead = (uint32_t)(rank & ~1);
+    const uint32_t q = warp & 3, lead = (uint32_t)(rank & ~(CG - 1));
     const uint32_t lanes = tmem_base + ((q * 32) << 16) + L::kScaleCol;
-    int it = 0, s = 0, buf = 0, s_before = 0;   // s_before: stage of the K-block that had the buffer before
-    uint32_t phase = 0, phase_before = 0;
+    int s = 0, s_before = 0;               // s_before: the stage before the last one
+    uint32_t phase = 0, phase_before = 0, n = 0;
     bool ok = true;
     for (int t = cluster; ok && t < p.total; t += n_clusters) {
-      for (int i = 0; i < my_st; ++i, ++it) {
+      for (int i = 0; i < my_st; ++i, ++n) {
         if (!warp_wait(sfull_bar(s), phase, abort_flag)) { ok = false; break; }
         const unsigned char* st = tiles + s * L::kStageBytes + lane * 16;
-        constexpr int n = L::kPieces * (1 + L::kTiles);
-        uint32_t v[4 * n];
+        constexpr int kAll = L::kPieces * (1 + L::kTiles);
+        uint32_t v[L::kSub][4 * kAll];
 #pragma unroll
-        for (int e = 0; e < n; ++e) {   // the weights' pieces, then for each group of blocks the tokens' tiles
-          const int c = (e - L::kPieces) / L::kTiles, k = (e - L::kPieces) % L::kTiles;
-          const uint4 w = *reinterpret_cast<const uint4*>(st + (e < L::kPieces ? L::kAtSW + e * kMxTile : L::kAtST + k * L::kSWBytes + c * kMxTile));
-          v[4 * e] = w.x; v[4 * e + 1] = w.y; v[4 * e + 2] = w.z; v[4 * e + 3] = w.w;
-        }
-        if (it >= L::kBufs) {           // the products that read this buffer are done
+        for (int u = 0; u < L::kSub; ++u)
+#pragma unroll
+          for (int e = 0; e < kAll; ++e) {   // the weights' pieces, then for each group of blocks the tokens' tiles
+            const int c = (e - L::kPieces) / L::kTiles, k = (e - L::kPieces) % L::kTiles;
+            const uint4 w = *reinterpret_cast<const uint4*>(
+                st + (e < L::kPieces ? L::kAtSW + u * L::kSWBytes + e * kMxTile : L::kAtST + u * L::kSTBytes + k * L::kSWBytes + c * kMxTile));
+            v[u][4 * e] = w.x; v[u][4 * e + 1] = w.y; v[u][4 * e + 2] = w.z; v[u][4 * e + 3] = w.w;
+          }
+        if (n >= 2) {                      // the products that read this buffer are done
           if (!warp_wait(empty_bar(s_before), phase_before, abort_flag)) { ok = false; break; }
           tc_fence_after();
           if (++s_before == L::kStages) { s_before = 0; phase_before ^= 1u; }
         }
         __syncwarp();
-        const uint32_t col = lanes + (uint32_t)buf * L::kScaleCols;
 #pragma unroll
-        for (int e = 0; e < 4 * n; e += 4 * L::kPieces) tmem_store<4 * L::kPieces>(col + e, v + e);
+        for (int u = 0; u < L::kSub; ++u)
+#pragma unroll
+          for (int e = 0; e < 4 * kAll; e += 4 * L::kPieces)
+            tmem_store<4 * L::kPieces>(lanes + (n & 1) * L::kStageCols + u * L::kScaleCols + e, v[u] + e);
         asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive_peer_relaxed(peer_addr(sready_bar(buf), lead));
-        if (++buf == L::kBufs) buf = 0;
+        if (lane == 0) {
+          if (CG == 2) mbar_arrive_peer_relaxed(peer_addr(sready_bar(n & 1), lead));
+          else mbar_arrive(sready_bar(n & 1));
+        }
         if (++s == L::kStages) { s = 0; phase ^= 1u; }
       }
     }
+    __syncwarp();
+    if (CL > 1 && CG == 1) cluster_wait();
   } else {
     // ---------------------------------------------------------------- epilogue
     constexpr int EC = 16;                              // accumulator columns (tokens) moved at a time
@@ -682,7 +654,7 @@ ocs_status launch_tiles(const Product& g, int slices, bool overlap, cudaStream_t
   const long long slots = cluster_capacity(cl) / cl;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)((total < slots ? total : slots) * cl), 1, 1);
-  cfg.blockDim = dim3(L::kThreads, 1, 1);
+  cfg.blockDim = dim3(kThreads, 1, 1);
   cfg.dynamicSmemBytes = L::kDynBytes;
   cfg.stream = stream;
   cudaLaunchAttribute attr[2];
