@@ -30,9 +30,7 @@ struct MxGemm {
   const float* a_scales;         // of rows (NULL: 1)
   const float* w_scales;
   const float* bias;
-  void* Y;
   long long ldy;
-  int y_type;
   int* dev_status;
 };
 
@@ -168,18 +166,10 @@ __device__ __forceinline__ void finish(T* y, long long ldy, const uint32_t* acc,
     y += ldy;
   }
 }
-template <bool WHOLE, int CNT>
-__device__ __forceinline__ void finish(const MxGemm& p, long long at, const uint32_t* acc, const float* sc, float ws, float b,
-                                       int left, bool n_ok, bool pairs) {
-  if (p.y_type == OCS_F32) finish<WHOLE, float, CNT>(static_cast<float*>(p.Y) + at, p.ldy, acc, sc, ws, b, left, n_ok, pairs);
-  else if (p.y_type == OCS_F16) finish<WHOLE, __half, CNT>(static_cast<__half*>(p.Y) + at, p.ldy, acc, sc, ws, b, left, n_ok, pairs);
-  else finish<WHOLE, __nv_bfloat16, CNT>(static_cast<__nv_bfloat16*>(p.Y) + at, p.ldy, acc, sc, ws, b, left, n_ok, pairs);
-}
-
-template <int GRID, int TN, int CG>
+template <typename T, int GRID, int TN, int CG>
 __global__ void __launch_bounds__(kThreads, 1)
 mx_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtensorMap tm_t,
-               const __grid_constant__ CUtensorMap tm_sw, const __grid_constant__ CUtensorMap tm_st, const MxGemm p) {
+               const __grid_constant__ CUtensorMap tm_sw, const __grid_constant__ CUtensorMap tm_st, const MxGemm p, T* __restrict__ Y) {
   using L = MxSmem<GRID, TN, CG>;
   extern __shared__ unsigned char smem_dyn[];
   const uint32_t raw = smem_u32(smem_dyn);
@@ -417,7 +407,7 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__
     constexpr int EC = 16;                              // accumulator columns (tokens) moved at a time
     const int ew = warp - 2, q = warp & 3, part = ew >> 2;   // lanes 32q.. of tensor memory; two warps share a quadrant
     float* sc = scale_buf + ew * L::kWarpTokens;
-    const bool pairs = p.y_type != OCS_F32 && (p.ldy % 2 == 0) && (p.N % 2 == 0) && (reinterpret_cast<uintptr_t>(p.Y) & 3) == 0;
+    const bool pairs = sizeof(T) == 2 && (p.ldy % 2 == 0) && (p.N % 2 == 0) && (reinterpret_cast<uintptr_t>(Y) & 3) == 0;
     grid_wait_previous();
     if (CL > 1 && CG == 1) cluster_wait();
     auto token_scale = [&](int m) { return m < p.M ? (p.a_scales ? __ldcg(p.a_scales + m) : 1.0f) : 0.0f; };
@@ -470,7 +460,7 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__
           }
           if (!warp_wait_cluster(xfull_bar, 0u, abort_flag)) break;
           const int m_own = mt * TN + slice * own;
-          const long long y = (long long)m_own * p.ldy + n;
+          T* y = Y + (long long)m_own * p.ldy + n;
           const uint32_t slot = (uint32_t)groups * TW * 16u;   // from one sender's cells to the next one's
           for (int g = part; g < groups; g += 2) {
             const unsigned char* cell = xbuf + (size_t)(g * TW + q * 32 + lane) * 16;
@@ -483,7 +473,7 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__
             const uint32_t av[4] = {__float_as_uint(a.x), __float_as_uint(a.y), __float_as_uint(a.z), __float_as_uint(a.w)};
             const float4 s4 = *reinterpret_cast<const float4*>(sc + 4 * g);
             const float sv[4] = {s4.x, s4.y, s4.z, s4.w};
-            finish<false, 4>(p, y + 4 * g * p.ldy, av, sv, ws, b, p.M - m_own - 4 * g, n < p.N, pairs);
+            finish<false, T, 4>(y + 4 * g * p.ldy, p.ldy, av, sv, ws, b, p.M - m_own - 4 * g, n < p.N, pairs);
           }
         }
         break;   // a K split is used only where every cluster has one tile
@@ -514,8 +504,8 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__
       if (part * EC < TN) {
         auto piece = [&](int i) { return down ? kPieces - 1 - i : i; };
         tmem_ld_async<EC>(addr + 2 * EC * piece(0), v[0]);
-#pragma unroll
-        for (int i = 0; i < kPieces; ++i) {
+#pragma unroll 2
+        for (int i = 0; i < kPieces; ++i) {   // (no more than the two buffers ask for: what runs should stay in the instruction cache)
           tmem_wait_ld16(v[i & 1]);
           if (L::kOverlap && i == (L::kShared + 2 * EC - 1) / (2 * EC) - 1) emptied(0);
           if (i + 1 < kPieces) tmem_ld_async<EC>(addr + 2 * EC * piece(i + 1), v[(i + 1) & 1]);
@@ -527,9 +517,9 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__
             const float4 f = *reinterpret_cast<const float4*>(sc + at / 2 + e);
             s[e] = f.x; s[e + 1] = f.y; s[e + 2] = f.z; s[e + 3] = f.w;
           }
-          const long long y = (long long)(m_first + at) * p.ldy + n;
-          if (n_all && left >= EC) finish<true, EC>(p, y, v[i & 1], s, ws, b, left, true, pairs);
-          else finish<false, EC>(p, y, v[i & 1], s, ws, b, left, n < p.N, pairs);
+          T* y = Y + (long long)(m_first + at) * p.ldy + n;
+          if (n_all && left >= EC) finish<true, T, EC>(y, p.ldy, v[i & 1], s, ws, b, left, true, pairs);
+          else finish<false, T, EC>(y, p.ldy, v[i & 1], s, ws, b, left, n < p.N, pairs);
         }
       }
       if (!L::kOverlap) emptied(acc);
@@ -619,20 +609,20 @@ struct Product {
   int* dev_status;
 };
 
-template <int GRID, int TN, int CG>
+template <typename T, int GRID, int TN, int CG>
 ocs_status launch_tiles(const Product& g, int slices, bool overlap, cudaStream_t stream) {
   using L = MxSmem<GRID, TN, CG>;
   static std::atomic<unsigned long long> ready{0};   // devices whose copy of the kernel has its attribute set
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess) return OCS_ERR_CUDA;
   if (dev >= 64 || !(ready.load() >> dev & 1)) {
-    if (cudaFuncSetAttribute(mx_gemm_kernel<GRID, TN, CG>, cudaFuncAttributeMaxDynamicSharedMemorySize, L::kDynBytes) != cudaSuccess)
+    if (cudaFuncSetAttribute(mx_gemm_kernel<T, GRID, TN, CG>, cudaFuncAttributeMaxDynamicSharedMemorySize, L::kDynBytes) != cudaSuccess)
       return OCS_ERR_CUDA;
     if (dev < 64) ready.fetch_or(1ull << dev);
   }
   MxGemm p{};
   p.M = g.M; p.N = g.N; p.num_st = stages_of(TN, (g.K + 2 * KB - 1) / (2 * KB));
-  p.a_scales = g.a_rows; p.w_scales = g.w_rows; p.bias = g.bias; p.Y = g.Y; p.ldy = g.ldy; p.y_type = g.y_type;
+  p.a_scales = g.a_rows; p.w_scales = g.w_rows; p.bias = g.bias; p.ldy = g.ldy;
   p.dev_status = g.dev_status;
   p.n_tiles = (g.N + TW * CG - 1) / (TW * CG);
   p.m_tiles = (g.M + TN - 1) / TN;
@@ -671,23 +661,31 @@ ocs_status launch_tiles(const Product& g, int slices, bool overlap, cudaStream_t
   }
   cfg.attrs = attr; cfg.numAttrs = n_attr;
   LaunchScope scope("mx_gemm_kernel", stream);
-  if (cudaLaunchKernelEx(&cfg, mx_gemm_kernel<GRID, TN, CG>, tm_w, tm_t, tm_sw, tm_st, p) != cudaSuccess) return OCS_ERR_CUDA;
+  if (cudaLaunchKernelEx(&cfg, mx_gemm_kernel<T, GRID, TN, CG>, tm_w, tm_t, tm_sw, tm_st, p, static_cast<T*>(g.Y)) != cudaSuccess) return OCS_ERR_CUDA;
   return launch_status();
 }
 
-template <int GRID>
+template <typename T, int GRID>
 ocs_status run_product(const Product& g, const MxPlan& plan, bool overlap, cudaStream_t stream) {
   switch (plan.tn) {
-    case 16: return launch_tiles<GRID, 16, 1>(g, plan.slices, overlap, stream);
-    case 32: return launch_tiles<GRID, 32, 1>(g, plan.slices, overlap, stream);
-    case 64: return launch_tiles<GRID, 64, 1>(g, plan.slices, overlap, stream);
-    case 128: return launch_tiles<GRID, 128, 1>(g, plan.slices, overlap, stream);
-    default: return launch_tiles<GRID, 256, 2>(g, plan.slices, overlap, stream);
+    case 16: return launch_tiles<T, GRID, 16, 1>(g, plan.slices, overlap, stream);
+    case 32: return launch_tiles<T, GRID, 32, 1>(g, plan.slices, overlap, stream);
+    case 64: return launch_tiles<T, GRID, 64, 1>(g, plan.slices, overlap, stream);
+    case 128: return launch_tiles<T, GRID, 128, 1>(g, plan.slices, overlap, stream);
+    default: return launch_tiles<T, GRID, 256, 2>(g, plan.slices, overlap, stream);
   }
 }
+template <typename T>
 ocs_status run_product(const Product& g, const MxPlan& plan, bool overlap, cudaStream_t stream) {
-  return g.grid == OCS_GRID_E8M0 ? run_product<OCS_GRID_E8M0>(g, plan, overlap, stream)
-                                 : run_product<OCS_GRID_E4M3>(g, plan, overlap, stream);
+  return g.grid == OCS_GRID_E8M0 ? run_product<T, OCS_GRID_E8M0>(g, plan, overlap, stream)
+                                 : run_product<T, OCS_GRID_E4M3>(g, plan, overlap, stream);
+}
+ocs_status run_product(const Product& g, const MxPlan& plan, bool overlap, cudaStream_t stream) {
+  switch (g.y_type) {
+    case OCS_F16: return run_product<__half>(g, plan, overlap, stream);
+    case OCS_BF16: return run_product<__nv_bfloat16>(g, plan, overlap, stream);
+    default: return run_product<float>(g, plan, overlap, stream);
+  }
 }
 
 // Everything but the tokens, which ocs_linear_mx4 has in another form.
