@@ -758,15 +758,22 @@ def _mx4_pieces(K: int, grid: int) -> int:
 def _check_mx4(q: Mx4):
     """Checks that q's tensors hold what its K and grid say -> (rows, row stride in bytes)."""
     codes, scales, rs, K, grid = q
-    assert grid in (MX4_E8M0, MX4_E4M3) and K > 0
-    assert codes.is_cuda and codes.dtype == torch.uint8 and scales.is_cuda and scales.dtype == torch.uint8
-    rows = codes.shape[0]
-    assert codes.shape[1] >= (K + 1) >> 1
+    rows, cols = codes.shape
+    assert (grid == MX4_E4M3 or grid == MX4_E8M0) and K > 0 and cols >= (K + 1) >> 1
+    assert codes.is_cuda and codes.dtype is torch.uint8 and scales.is_cuda and scales.dtype is torch.uint8
     assert scales.is_contiguous() and scales.numel() >= (rows + 127 >> 7) * _mx4_pieces(K, grid) * 512
     if grid == MX4_E4M3:
-        assert rs is not None
-        _check_vec(rs, rows)
-    return rows, _rows_of(codes)
+        assert rs.is_cuda and rs.dtype is torch.float32 and rs.is_contiguous() and rs.numel() >= rows
+    if rows == 1:
+        return 1, (cols + 15) & ~15
+    ld, one = codes.stride()
+    assert (one == 1 or cols <= 1) and (ld >= cols or rows == 0)
+    return rows, ld if ld > cols else cols
+
+
+def _new(size, dtype, like):
+    """An empty tensor on like's device (taking the type from a tensor costs the host less than naming it)."""
+    return like.new_empty(size) if like.dtype is dtype else like.new_empty(size, dtype=dtype)
 
 
 def ocs_quantize_mx4(x, grid: int = MX4_E4M3, idx_map=None, S: int = 0, out: Mx4 | None = None, dev_status=None) -> Mx4:
@@ -781,10 +788,10 @@ def ocs_quantize_mx4(x, grid: int = MX4_E4M3, idx_map=None, S: int = 0, out: Mx4
     K = Cn + S
     if out is None:
         nb = (K + 1) >> 1
-        codes = torch.empty_strided((rows, nb), ((nb + 15) & ~15, 1), dtype=torch.uint8, device=x.device)
-        out = Mx4(codes, codes.new_empty((rows + 127 >> 7, _mx4_pieces(K, grid), 32, 4, 4)),
-                  torch.empty(rows, dtype=torch.float32, device=x.device) if grid == MX4_E4M3 else None, K, grid)
         ld = (nb + 15) & ~15
+        codes = torch.empty_strided((rows, nb), (ld, 1), dtype=torch.uint8, device=x.device)
+        out = Mx4(codes, codes.new_empty((rows + 127 >> 7, _mx4_pieces(K, grid), 32, 4, 4)),
+                  _new(rows, torch.float32, x) if grid == MX4_E4M3 else None, K, grid)
     else:
         assert out.K == K and out.grid == grid and out.codes.shape[0] == rows
         ld = _check_mx4(out)[1]
@@ -798,7 +805,7 @@ def ocs_dequantize_mx4(q: Mx4, out_dtype=torch.float32, out=None):
     """The values that q's codes stand for, [rows, K] of out_dtype (fp32: exact)."""
     rows, ld = _check_mx4(q)
     if out is None:
-        out, ldy = torch.empty((rows, q.K), dtype=out_dtype, device=q.codes.device), q.K
+        out, ldy = q.codes.new_empty((rows, q.K), dtype=out_dtype), q.K
     else:
         assert out.is_cuda and out.shape == (rows, q.K)
         ldy = _rows_of(out)
@@ -815,7 +822,7 @@ def ocs_qlinear_mx4(a: Mx4, w: Mx4, bias=None, out_dtype=torch.float32, out=None
     assert a.K == w.K and a.grid == w.grid
     _check_vec(bias, N), _check_status(dev_status)
     if out is None:
-        out, ldy = torch.empty((M, N), dtype=out_dtype, device=a.codes.device), N
+        out, ldy = _new((M, N), out_dtype, a.codes if bias is None else bias), N
     else:
         assert out.is_cuda and out.shape == (M, N)
         ldy = _rows_of(out)
@@ -839,15 +846,14 @@ def ocs_linear_mx4(x, w: Mx4, idx_map=None, S: int = 0, bias=None, out_dtype=Non
     _check_idx(idx_map, Cn, S), _check_vec(bias, N), _check_status(dev_status)
     assert ws is None or (ws.is_cuda and ws.dtype == torch.uint8 and ws.is_contiguous())
     if out is None:
-        out = x.new_empty((M, N)) if out_dtype is None else torch.empty((M, N), dtype=out_dtype, device=x.device)
-        ldy = N
+        out, ldy = x.new_empty((M, N)) if out_dtype is None else _new((M, N), out_dtype, x), N
     else:
         assert out.is_cuda and out.shape == (M, N)
         ldy = _rows_of(out)
     assert out.dtype in DTYPES
     L = lib()
     if ws is None:
-        ws = torch.empty(L.ocs_linear_mx4_workspace_bytes(M, Cn, S, w.grid), dtype=torch.uint8, device=x.device)
+        ws = w.codes.new_empty(L.ocs_linear_mx4_workspace_bytes(M, Cn, S, w.grid))
     st = L.ocs_linear_mx4(x.data_ptr(), DTYPES[x.dtype], M, Cn, ldx, S, _addr(idx_map), w.grid, w.codes.data_ptr(),
                           w.scales.data_ptr(), _addr(w.row_scales), N, ldw, _addr(bias), out.data_ptr(), DTYPES[out.dtype],
                           ldy, ws.data_ptr(), ws.numel(), _addr(dev_status), _raw_stream(x))
@@ -883,23 +889,32 @@ def ocs_cache_new(n_pages: int, page_size: int, heads: int, dim: int, grid: int 
     return QuantCache(torch.zeros((n_pages, n), dtype=torch.uint8, device=device), page_size, heads, dim, grid)
 
 
+_cache_shapes = {}   # (pages, page_size, heads, dim, grid) -> its description in C, and a page's bytes
+
+
 def _check_caches(cache: QuantCache, cache2):
-    pages, page_size, heads, dim, grid = cache
-    d = _CacheDesc(pages.shape[0], page_size, heads, dim, grid)
-    assert pages.is_cuda and pages.dtype == torch.uint8 and pages.is_contiguous()
-    assert lib().ocs_cache_page_bytes(C.byref(d)) == pages.shape[1]
+    pages = cache.pages
+    n, size = pages.shape
+    key = (n, cache.page_size, cache.heads, cache.dim, cache.grid)
+    known = _cache_shapes.get(key)
+    if known is None:
+        d = _CacheDesc(*key)
+        known = d, C.addressof(d), lib().ocs_cache_page_bytes(C.addressof(d))
+        if len(_cache_shapes) < 4096:
+            _cache_shapes[key] = known
+    assert size == known[2] and pages.is_cuda and pages.dtype is torch.uint8 and pages.is_contiguous()
     if cache2 is not None:
         p2 = cache2.pages
-        assert cache2[1:] == cache[1:] and p2.shape == pages.shape and p2.is_cuda and p2.dtype == torch.uint8 and p2.is_contiguous()
-    return d
+        assert cache2[1:] == cache[1:] and p2.shape == pages.shape and p2.is_cuda and p2.dtype is torch.uint8 and p2.is_contiguous()
+    return known
 
 
 def _check_vectors(x, rows, cache: QuantCache):
     """x [rows, heads, dim], vectors dense -> (address, strides of tokens and heads)."""
     assert x.is_cuda and x.dtype in DTYPES and x.shape == (rows, cache.heads, cache.dim)
-    st = x.stride()
-    assert st[2] == 1 or cache.dim == 1
-    return x.data_ptr(), st[0], st[1]
+    token, head, one = x.stride()
+    assert one == 1 or cache.dim == 1
+    return x.data_ptr(), token, head
 
 
 def ocs_cache_write(cache: QuantCache, x, slots, cache2: QuantCache | None = None, x2=None, dev_status=None) -> None:
@@ -915,7 +930,7 @@ def ocs_cache_write(cache: QuantCache, x, slots, cache2: QuantCache | None = Non
     if x2 is not None:
         assert x2.dtype == x.dtype
         p2, v2 = cache2.pages.data_ptr(), _check_vectors(x2, n, cache)
-    st = lib().ocs_cache_write(C.byref(d), cache.pages.data_ptr(), *v, p2, *v2, DTYPES[x.dtype], n, slots.data_ptr(),
+    st = lib().ocs_cache_write(d[1], cache.pages.data_ptr(), *v, p2, *v2, DTYPES[x.dtype], n, slots.data_ptr(),
                                _addr(dev_status), _raw_stream(x))
     _check(st, "ocs_cache_write")
 
@@ -933,17 +948,19 @@ def ocs_cache_read(cache: QuantCache, table, starts, rows: int, out_dtype=torch.
     _check_status(dev_status)
     rows = int(rows)
     if out is None:
-        out = torch.empty((rows, cache.heads, cache.dim), dtype=out_dtype, device=table.device)
-    v = _check_vectors(out, rows, cache)
+        out = cache.pages.new_empty((rows, cache.heads, cache.dim), dtype=out_dtype)
+        v = out.data_ptr(), cache.heads * cache.dim, cache.dim
+    else:
+        v = _check_vectors(out, rows, cache)
     p2, v2 = None, (None, 0, 0)
     if cache2 is not None:
         if out2 is None:
-            out2 = torch.empty_like(out)
+            out2 = out.new_empty((rows, cache.heads, cache.dim))
         assert out2.dtype == out.dtype
         p2, v2 = cache2.pages.data_ptr(), _check_vectors(out2, rows, cache)
     else:
         assert out2 is None
-    st = lib().ocs_cache_read(C.byref(d), cache.pages.data_ptr(), p2, table.data_ptr(), ld_table, cols, starts.data_ptr(), B, rows,
+    st = lib().ocs_cache_read(d[1], cache.pages.data_ptr(), p2, table.data_ptr(), ld_table, cols, starts.data_ptr(), B, rows,
                               *v, *v2, DTYPES[out.dtype], _addr(dev_status), _raw_stream(table))
     _check(st, "ocs_cache_read")
     return out if cache2 is None else (out, out2)
