@@ -57,7 +57,7 @@ _ARGTYPES = {
     "ocs_quantize_mx4": [_P, _I, _L, _I, _L, _I, _P, _I, _P, _L, _P, _P, _P, _P],
     "ocs_dequantize_mx4": [_P, _L, _P, _P, _L, _I, _I, _P, _I, _L, _P],
     "ocs_qlinear_mx4": [_P, _P, _P, _I, _I, _L, _P, _P, _P, _I, _L, _I, _P, _P, _I, _L, _P, _P],
-    "ocs_linear_mx4_workspace_bytes": [_I, _I, _I, _I],
+    "ocs_linear_mx4_workspace_bytes": [_I, _I, _I, _I, _I, _I],
     "ocs_linear_mx4": [_P, _I, _I, _I, _L, _I, _P, _I, _P, _P, _P, _I, _L, _P, _P, _I, _L, _P, C.c_size_t, _P, _P],
     "ocs_cache_page_bytes": [_P],
     "ocs_cache_write": [_P, _P, _P, _L, _L, _P, _P, _L, _L, _I, _L, _P, _P, _P],
@@ -852,11 +852,14 @@ def ocs_linear_mx4(x, w: Mx4, idx_map=None, S: int = 0, bias=None, out_dtype=Non
         ldy = _rows_of(out)
     assert out.dtype in DTYPES
     L = lib()
+    xt, yt = DTYPES[x.dtype], DTYPES[out.dtype]
     if ws is None:
-        ws = w.codes.new_empty(L.ocs_linear_mx4_workspace_bytes(M, Cn, S, w.grid))
-    st = L.ocs_linear_mx4(x.data_ptr(), DTYPES[x.dtype], M, Cn, ldx, S, _addr(idx_map), w.grid, w.codes.data_ptr(),
-                          w.scales.data_ptr(), _addr(w.row_scales), N, ldw, _addr(bias), out.data_ptr(), DTYPES[out.dtype],
-                          ldy, ws.data_ptr(), ws.numel(), _addr(dev_status), _raw_stream(x))
+        n_ws = L.ocs_linear_mx4_workspace_bytes(M, Cn, S, w.grid, N, yt)
+        if n_ws:
+            ws = w.codes.new_empty(n_ws)
+    st = L.ocs_linear_mx4(x.data_ptr(), xt, M, Cn, ldx, S, _addr(idx_map), w.grid, w.codes.data_ptr(),
+                          w.scales.data_ptr(), _addr(w.row_scales), N, ldw, _addr(bias), out.data_ptr(), yt, ldy,
+                          _addr(ws), 0 if ws is None else ws.numel(), _addr(dev_status), _raw_stream(x))
     _check(st, "ocs_linear_mx4")
     return out
 

@@ -20,6 +20,7 @@ namespace {
 constexpr int TW = 128;        // channels of one CTA's tile
 constexpr int KB = 128;        // bytes of a K-block's row: 256 contraction indices
 constexpr int kEpiWarps = 8;
+constexpr int kFusedBytes = 64 * 1024;             // token codes and scales a CTA can hold beside the ring of weights
 constexpr int kThreads = 64 + 32 * kEpiWarps + 128;   // copy warp, tensor-core warp, epilogue warps, scale warps
 
 __host__ __device__ constexpr int stage_blocks(int tn) { return tn <= 64 ? 2 : 1; }   // K-blocks of a ring stage
@@ -32,17 +33,22 @@ struct MxGemm {
   const float* bias;
   long long ldy;
   int* dev_status;
+  // tokens that are quantized here (FUSED): unquantized rows and what ocs_quantize_mx4 takes
+  const void* X;
+  long long ldx;
+  const int32_t* idx_map;
+  int x_type, C, K;
 };
 
 // Tensor memory columns: two accumulators, then the scales of two stages.  256 tokens: the accumulators overlap by as many
 // columns as the scales need; the epilogue empties those first and says so before it goes on.
-template <int GRID, int TN, int CG>
+template <int GRID, int TN, int CG, bool FUSED>
 struct MxSmem {
   static constexpr int kTokens = TN / CG;
   static constexpr int kPieces = GRID == OCS_GRID_E8M0 ? 2 : 4;        // groups of four blocks in a K-block
   static constexpr int kTiles = TN > 128 ? 2 : 1;                       // 128-token scale tiles
-  static constexpr int kWBytes = TW * KB, kTBytes = kTokens * KB;
-  static constexpr int kSWBytes = kPieces * kMxTile, kSTBytes = kTiles * kPieces * kMxTile;
+  static constexpr int kWBytes = TW * KB, kTBytes = FUSED ? 0 : kTokens * KB;
+  static constexpr int kSWBytes = kPieces * kMxTile, kSTBytes = FUSED ? 0 : kTiles * kPieces * kMxTile;
   static constexpr int kSub = stage_blocks(TN);
   static constexpr int kStageBytes = kSub * (kWBytes + kTBytes + kSWBytes + kSTBytes);
   static constexpr int kAtT = kSub * kWBytes, kAtSW = kAtT + kSub * kTBytes, kAtST = kAtSW + kSub * kSWBytes;
@@ -51,10 +57,14 @@ struct MxSmem {
   static constexpr int kXExtra = kXInRing ? 0 : kXBytes;
   static constexpr int kWarpTokens = TN < 32 ? 16 : TN / 2;
   static constexpr int kScaleBytes = kEpiWarps * kWarpTokens * 4;
+  // FUSED: the codes of all the K-blocks a CTA takes, [K-block][token][128 bytes], their scales, [K-block][32 tokens][16
+  // bytes, one per block], a row's maximum and its scale
+  static constexpr int kFusedBlocks = FUSED ? kFusedBytes / (TN * KB + kMxTile) : 0, kTokenBytes = FUSED ? kFusedBlocks * (TN * KB + kMxTile) : 0;
+  static constexpr int kRowBytes = FUSED ? TN * 8 : 0;
   static constexpr int kCtrlBytes = 512;
-  static constexpr int kBudget = 227 * 1024 - 1024 - kCtrlBytes - kScaleBytes - kXExtra;
+  static constexpr int kBudget = 227 * 1024 - 1024 - kCtrlBytes - kScaleBytes - kXExtra - kTokenBytes - kRowBytes;
   static constexpr int kStages = kBudget / kStageBytes < 8 ? kBudget / kStageBytes : 8;
-  static constexpr int kDynBytes = 1024 + kStages * kStageBytes + kXExtra + kScaleBytes + kCtrlBytes;
+  static constexpr int kDynBytes = 1024 + kStages * kStageBytes + kTokenBytes + kXExtra + kScaleBytes + kRowBytes + kCtrlBytes;
   static constexpr bool kOverlap = TN == 256;
   static constexpr int kScaleCols = 4 * kPieces * (1 + kTiles), kStageCols = kSub * kScaleCols;   // the weights' scales, then the tokens'
   static constexpr int kAccStride = kOverlap ? 512 - 2 * kStageCols - TN : (TN < 32 ? 32 : TN);
@@ -63,7 +73,7 @@ struct MxSmem {
   static constexpr int kUsedCols = kScaleCol + 2 * kStageCols;
   static constexpr uint32_t kFullBytes = kSub * (kWBytes + kTBytes), kScaleBytes512 = kSub * (kSWBytes + kSTBytes);   // of a stage
   static constexpr uint32_t kTmemCols = kUsedCols <= 128 ? 128 : (kUsedCols <= 256 ? 256 : 512);
-  static_assert(kStages >= 3 && (!kXInRing || kXBytes <= kStages * kStageBytes) && kStageBytes % 1024 == 0 && kTBytes % 1024 == 0 && kUsedCols <= 512, "tile does not fit");
+  static_assert(kStages >= 3 && (!kXInRing || kXBytes <= kStages * kStageBytes) && kStageBytes % 1024 == 0 && kTBytes % 1024 == 0 && (TN * KB) % 1024 == 0 && kUsedCols <= 512, "tile does not fit");
 };
 
 // Instruction descriptor of the block-scaled 4-bit products: e2m1 operands, K-major, scales e8m0 or e4m3.  sf: which bytes
@@ -166,19 +176,79 @@ __device__ __forceinline__ void finish(T* y, long long ldy, const uint32_t* acc,
     y += ldy;
   }
 }
-template <typename T, int GRID, int TN, int CG>
+// The epilogue warps quantize the token tile (all of the call's M <= TN tokens) into the operand tiles of stages slice,
+// slice + slices, ...; E4M3: after the rows' maxima.  A thread's unit of work is a block of a row.  This code runs once per CTA,
+// so that fetching the instructions is what it costs besides the loads' latency: nothing is unrolled over units, and both
+// passes go through the same load (20 x 650 in fp32 takes 15.5 us in all, with two or four units at a time 15.8 and 16).
+template <typename X, int GRID, int TN>
+__device__ __forceinline__ void quantize_tokens(const MxGemm& p, int slice, int my_kb, unsigned char* tok, unsigned char* scales,
+                                                uint32_t* max_bits, float* row_scale) {
+  constexpr int N = mx4_block(GRID), PER = 2 * KB / N, kSub = stage_blocks(TN);   // blocks of a K-block
+  const int et = threadIdx.x - 64, nb = (p.K + N - 1) / N;
+  if (et < TN) {
+    max_bits[et] = 0;
+    row_scale[et] = 1.0f;
+  }
+#pragma unroll 1
+  for (int pass = GRID == OCS_GRID_E4M3 ? 0 : 1; pass < 2; ++pass) {
+    if (GRID == OCS_GRID_E4M3) asm volatile("bar.sync 1, 256;" ::: "memory");
+    if (GRID == OCS_GRID_E4M3 && pass && et < p.M) {
+      row_scale[et] = two_to(mx4_row_exponent(max_bits[et]));
+      if (max_bits[et] >= 0x7f800000u) flag(p.dev_status, OCS_DEV_NONFINITE);
+    }
+    const int per_row = pass ? my_kb * PER : (p.C + N - 1) / N, units = p.M * per_row;
+#pragma unroll 1
+    for (int u0 = et & ~31; u0 < units; u0 += 256) {   // (whole warps)
+      const int u = min(u0 + (et & 31), units - 1);   // (the last one more than once: harmless)
+      const int r = u / per_row, at = u - r * per_row, in = at / PER, bb = at % PER;   // this CTA's K-block, block in it
+      const int b = pass ? ((slice + in / kSub * p.slices) * kSub + in % kSub) * PER + bb : at;
+      const X* x = static_cast<const X*>(p.X) + r * p.ldx;
+      Block<X, N> v;
+      // (the load reads up to 16 bytes around the block: within the matrix)
+      if ((b + 1) * N <= p.C && (r > 0 || b > 0) && (r + 1 < p.M || (b + 2) * N <= p.C)) v.template load<0>(x + b * N);
+      else if (b < nb) v.gather(x, b * N, p.C, pass ? p.K : p.C, p.idx_map, p.dev_status);
+      else v.clear();
+      const uint32_t m = v.max_bits();
+      if (GRID == OCS_GRID_E4M3 && !pass) {
+        const int first = __shfl_sync(0xffffffffu, r, 0);
+        if (__all_sync(0xffffffffu, r == first)) {
+          const uint32_t all = __reduce_max_sync(0xffffffffu, m);
+          if ((et & 31) == 0) atomicMax(max_bits + first, all);
+        } else {
+          atomicMax(max_bits + r, m);
+        }
+        continue;
+      }
+      if (GRID == OCS_GRID_E8M0 && m >= 0x7f800000u) flag(p.dev_status, OCS_DEV_NONFINITE);
+      const MxScale s = mx4_scale<GRID, X>(m, GRID == OCS_GRID_E4M3 ? mx4_row_exponent(max_bits[r]) : 0);
+      uint32_t c[N / 8];
+      v.template codes<GRID>(s, c);
+      scales[in * kMxTile + r * 16 + bb] = b < nb ? (unsigned char)s.byte : 0;   // (past the end: anything but NaN)
+      unsigned char* row = tok + (in * TN + r) * KB;
+      if constexpr (N == 32) *reinterpret_cast<uint4*>(row + ((bb ^ (r & 7)) << 4)) = make_uint4(c[0], c[1], c[2], c[3]);
+      else *reinterpret_cast<uint2*>(row + (((bb >> 1) ^ (r & 7)) << 4) + (bb & 1) * 8) = make_uint2(c[0], c[1]);
+    }
+  }
+  fence_proxy_async_smem();   // the tensor cores read what these threads wrote
+}
+
+template <typename T, int GRID, int TN, int CG, bool FUSED>
 __global__ void __launch_bounds__(kThreads, 1)
 mx_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtensorMap tm_t,
                const __grid_constant__ CUtensorMap tm_sw, const __grid_constant__ CUtensorMap tm_st, const MxGemm p, T* __restrict__ Y) {
-  using L = MxSmem<GRID, TN, CG>;
+  using L = MxSmem<GRID, TN, CG, FUSED>;
   extern __shared__ unsigned char smem_dyn[];
   const uint32_t raw = smem_u32(smem_dyn);
   const uint32_t base = (raw + 1023u) & ~1023u;
   unsigned char* tiles = smem_dyn + (base - raw);
-  unsigned char* after = tiles + L::kStages * L::kStageBytes;
+  unsigned char* tokens = tiles + L::kStages * L::kStageBytes;
+  unsigned char* token_scales = tokens + L::kFusedBlocks * TN * KB;
+  unsigned char* after = tokens + L::kTokenBytes;
   unsigned char* xbuf = L::kXInRing ? tiles : after;
   float* scale_buf = reinterpret_cast<float*>(after + L::kXExtra);
-  uint64_t* bars = reinterpret_cast<uint64_t*>(after + L::kXExtra + L::kScaleBytes);
+  uint32_t* row_max = reinterpret_cast<uint32_t*>(after + L::kXExtra + L::kScaleBytes);   // FUSED: [TN] maxima, then scales
+  float* row_scale = reinterpret_cast<float*>(row_max + TN);
+  uint64_t* bars = reinterpret_cast<uint64_t*>(after + L::kXExtra + L::kScaleBytes + L::kRowBytes);
   auto full_bar = [&](int s) { return smem_u32(bars + s); };
   auto empty_bar = [&](int s) { return smem_u32(bars + L::kStages + s); };
   auto accfull_bar = [&](int a) { return smem_u32(bars + 2 * L::kStages + a); };
@@ -198,14 +268,16 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__
   const int cluster = blockIdx.x / CL, n_clusters = gridDim.x / CL;
   const int my_st = (p.num_st - slice + p.slices - 1) / p.slices;
 
-  // Set-up.  Nobody waits for more than it needs (named barriers: 2 = set up, 3 = barriers stand).  A peer may be written to
+  // Set-up.  Nobody waits for more than it needs (named barriers: 2 = set up, 3 = barriers stand, 4 = tokens in place).  A peer may be written to
   // once all threads of the cluster have arrived; a pair waits for that at once, the others where they first need it.
   if (warp == 0) {
     if (lane == 0) {
       prefetch_tmap(&tm_w);
-      prefetch_tmap(&tm_t);
       prefetch_tmap(&tm_sw);
-      prefetch_tmap(&tm_st);
+      if (!FUSED) {
+        prefetch_tmap(&tm_t);
+        prefetch_tmap(&tm_st);
+      }
       for (int s = 0; s < L::kStages; ++s) {
         mbar_init(full_bar(s), 1);     // the leader's producer announces the bytes of both CTAs
         mbar_init(empty_bar(s), 1);    // commit of the products that read the stage
@@ -236,6 +308,13 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__
     asm volatile("bar.sync 3, 64;" ::: "memory");
   } else {
     if (CL > 1) cluster_arrive();
+    if (FUSED && warp < 2 + kEpiWarps) {
+      // they need nothing of the set-up
+      if (p.x_type == OCS_F32) quantize_tokens<float, GRID, TN>(p, slice, my_st * L::kSub, tokens, token_scales, row_max, row_scale);
+      else if (p.x_type == OCS_F16) quantize_tokens<__half, GRID, TN>(p, slice, my_st * L::kSub, tokens, token_scales, row_max, row_scale);
+      else quantize_tokens<__nv_bfloat16, GRID, TN>(p, slice, my_st * L::kSub, tokens, token_scales, row_max, row_scale);
+      asm volatile("bar.arrive 4, %0;" ::"n"(kThreads - 32) : "memory");   // this warp's codes are in place
+    }
     asm volatile("bar.sync 2, %0;" ::"n"(kThreads) : "memory");
   }
   if (CG == 2) cluster_wait();
@@ -285,7 +364,7 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__
           load_w(i, slice + i * p.slices);
         }
       }
-      grid_wait_previous();
+      if (!FUSED) grid_wait_previous();
       for (int t = cluster; ok && t < p.total; t += n_clusters) {
         tile_of(p, t, &mt, &nt);
         for (int i = 0; i < my_st; ++i, ++it) {
@@ -295,7 +374,7 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__
             announce(s);
             load_w(s, slice + i * p.slices);
           }
-          load_t(s, slice + i * p.slices);
+          if (!FUSED) load_t(s, slice + i * p.slices);
         }
       }
       // every commit has arrived (also those the other CTA of a pair sends here) before the CTA may leave
@@ -308,10 +387,11 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__
     if (CL > 1 && CG == 1) cluster_wait();
   } else if (warp == 1) {
     // ---------------------------------------------------------------- tensor cores
+    if (FUSED) asm volatile("bar.sync 4, %0;" ::"n"(kThreads - 32) : "memory");   // the tokens' codes are in place
     if (lane == 0 && half == 0) {
       constexpr uint32_t kDescM = TW * CG;
       const uint16_t mask = (uint16_t)(3u << (rank & ~1));
-      const uint64_t w_desc0 = smem_desc_sw128(base), t_desc0 = smem_desc_sw128(base + L::kAtT);
+      const uint64_t w_desc0 = smem_desc_sw128(base), t_desc0 = smem_desc_sw128(FUSED ? smem_u32(tokens) : base + L::kAtT);
       int j = 0, s = 0;
       uint32_t phase = 0, n = 0;   // n: stages so far
       bool ok = true;
@@ -332,6 +412,7 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__
           if (!mbar_wait(full_bar(s), phase, abort_flag) || !mbar_wait_relaxed(sready_bar(n & 1), (n >> 1) & 1u, abort_flag)) { ok = false; break; }
           tc_fence_after();
           const uint32_t o = (uint32_t)(s * (L::kStageBytes >> 4));
+          const uint64_t t_desc = t_desc0 + (FUSED ? (uint32_t)(i * L::kSub * (TN * KB >> 4)) : o);
 #pragma unroll
           for (int u = 0; u < L::kSub; ++u) {
             const uint32_t sw_col = tmem_base + L::kScaleCol + (n & 1) * L::kStageCols + u * L::kScaleCols;
@@ -340,7 +421,7 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__
             for (int k = 0; k < 4; ++k) {   // 64 contraction indices: 32 bytes on, 2 in the descriptors' units of 16
               constexpr int kPer = 4 / L::kPieces;   // products per piece of scales
               const int c = k / kPer, sf = k % kPer * 2;
-              umma_mx4<GRID, CG>(d, w_desc0 + o + u * (L::kWBytes >> 4) + 2 * k, t_desc0 + o + u * (L::kTBytes >> 4) + 2 * k,
+              umma_mx4<GRID, CG>(d, w_desc0 + o + u * (L::kWBytes >> 4) + 2 * k, t_desc + u * ((FUSED ? TN * KB : L::kTBytes) >> 4) + 2 * k,
                                  mx_instr_desc(GRID, kDescM, TN, sf), sw_col + 4 * c, st_col + 4 * c * L::kTiles, u + k == 0 ? more : 1u);
             }
           }
@@ -361,6 +442,7 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__
     // ---------------------------------------------------------------- scales (of the CTA's own shared memory and lanes)
     const uint32_t q = warp & 3, lead = (uint32_t)(rank & ~(CG - 1));
     const uint32_t lanes = tmem_base + ((q * 32) << 16) + L::kScaleCol;
+    if (FUSED) asm volatile("bar.sync 4, %0;" ::"n"(kThreads - 32) : "memory");   // the tokens' scales are in place
     int s = 0, s_before = 0;               // s_before: the stage before the last one
     uint32_t phase = 0, phase_before = 0, n = 0;
     bool ok = true;
@@ -371,14 +453,21 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__
         constexpr int kAll = L::kPieces * (1 + L::kTiles);
         uint32_t v[L::kSub][4 * kAll];
 #pragma unroll
-        for (int u = 0; u < L::kSub; ++u)
+        for (int u = 0; u < L::kSub; ++u) {
+          if (FUSED) {   // a lane's token: four scales for the first column of each piece
+            const uint4 w = *reinterpret_cast<const uint4*>(token_scales + (i * L::kSub + u) * kMxTile + lane * 16);
+            const uint32_t c[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-          for (int e = 0; e < kAll; ++e) {   // the weights' pieces, then for each group of blocks the tokens' tiles
+            for (int e = 0; e < 4 * L::kPieces; ++e) v[u][4 * L::kPieces + e] = c[e / 4];
+          }
+#pragma unroll
+          for (int e = 0; e < (FUSED ? L::kPieces : kAll); ++e) {   // the weights' pieces, then for each group of blocks the tokens' tiles
             const int c = (e - L::kPieces) / L::kTiles, k = (e - L::kPieces) % L::kTiles;
             const uint4 w = *reinterpret_cast<const uint4*>(
                 st + (e < L::kPieces ? L::kAtSW + u * L::kSWBytes + e * kMxTile : L::kAtST + u * L::kSTBytes + k * L::kSWBytes + c * kMxTile));
             v[u][4 * e] = w.x; v[u][4 * e + 1] = w.y; v[u][4 * e + 2] = w.z; v[u][4 * e + 3] = w.w;
           }
+        }
         if (n >= 2) {                      // the products that read this buffer are done
           if (!warp_wait(empty_bar(s_before), phase_before, abort_flag)) { ok = false; break; }
           tc_fence_after();
@@ -408,9 +497,13 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__
     const int ew = warp - 2, q = warp & 3, part = ew >> 2;   // lanes 32q.. of tensor memory; two warps share a quadrant
     float* sc = scale_buf + ew * L::kWarpTokens;
     const bool pairs = sizeof(T) == 2 && (p.ldy % 2 == 0) && (p.N % 2 == 0) && (reinterpret_cast<uintptr_t>(Y) & 3) == 0;
-    grid_wait_previous();
+    if (!FUSED) grid_wait_previous();
     if (CL > 1 && CG == 1) cluster_wait();
-    auto token_scale = [&](int m) { return m < p.M ? (p.a_scales ? __ldcg(p.a_scales + m) : 1.0f) : 0.0f; };
+    auto token_scale = [&](int m) {
+      if (m >= p.M) return 0.0f;
+      if (FUSED) return row_scale[m];
+      return p.a_scales ? __ldcg(p.a_scales + m) : 1.0f;
+    };
     int j = 0;
     for (int t = cluster; t < p.total; t += n_clusters, ++j) {
       int mt, nt;
@@ -560,9 +653,15 @@ bool split_fits(int tn, int cg, int slices, long long tiles, int stages) {
   return cg == 1 && tn < 256 && tn / slices >= 4 && slices <= stages && tiles * slices <= cluster_capacity(slices);
 }
 
-MxPlan choose_plan(int M, int N, int num_kb, int out_bytes) {
+// The plan by a time model in microseconds, fitted to 1545 measurements (M 1..8192, K 64..25088, N 64..33278, both grids, fp32
+// and 16-bit outputs, every plan that fits): root mean square error 7.4 %; the plan it picks is 0.7 % slower than the best
+// measured one on average, 11 % at worst.  A tile costs its K-blocks and its epilogue; a K split adds the exchange; the bytes
+// take their time at 4.9 TB/s; of the two the longer one counts most (root of the sum of squares); 3.7 us pass before the first
+// and after the last tile.
+MxPlan choose_plan(int M, int N, int K, ocs_grid grid, int out_bytes) {
   struct Form { int tn, cg; double block_us, epilogue_us; };
-  static const Form forms[5] = {{16, 1, 0.18, 0.0}, {32, 1, 0.18, 0.01}, {64, 1, 0.18, 0.27}, {128, 1, 0.23, 0.91}, {256, 2, 0.27, 3.02}};
+  static const Form forms[5] = {{16, 1, 0.256, 0.60}, {32, 1, 0.257, 0.57}, {64, 1, 0.273, 0.63}, {128, 1, 0.331, 1.31}, {256, 2, 0.352, 2.56}};
+  const int num_kb = (K + 2 * KB - 1) / (2 * KB);
   auto tiles_of = [&](int tn, int cg) {
     return (long long)((M + (long long)tn - 1) / tn) * ((N + (long long)TW * cg - 1) / (TW * cg));
   };
@@ -572,8 +671,8 @@ MxPlan choose_plan(int M, int N, int num_kb, int out_bytes) {
     while (r.slices > 1 && !split_fits(r.tn, r.cg, r.slices, tiles_of(r.tn, r.cg), stages_of(r.tn, num_kb))) r.slices /= 2;
     return r;
   }
-  const double K = (double)num_kb * KB;
-  const double bytes_us = ((double)N * K + (double)M * K + (double)M * N * out_bytes) / 6.22e6;
+  const double row = K * (grid == OCS_GRID_E4M3 ? 0.5625 : 0.53125);   // bytes of a row's codes and scales
+  const double bytes_us = (((double)N + M) * row + (double)M * N * out_bytes) / 4.94e6;
   MxPlan best{64, 1, 1};
   double best_us = 1e300;   // squared
   for (const Form& f : forms) {
@@ -584,9 +683,9 @@ MxPlan choose_plan(int M, int N, int num_kb, int out_bytes) {
       const long long slots = cluster_capacity(f.cg * s) / (f.cg * s);
       const double waves = (double)((tiles + slots - 1) / slots);
       const int blocks = (stages_of(f.tn, num_kb) + s - 1) / s * stage_blocks(f.tn);
-      double us = waves * (blocks * f.block_us + f.epilogue_us * (out_bytes == 4 ? 1.2 : 1.0) + 0.29);
-      if (s > 1) us += 3.85 * f.tn / 128.0;
-      us = us * us + bytes_us * bytes_us;
+      double us = waves * (blocks * f.block_us * (grid == OCS_GRID_E4M3 ? 1.034 : 1.0) + f.epilogue_us * (out_bytes == 4 ? 0.87 : 1.0));
+      if (s > 1) us += 3.61 * f.tn / 128.0 + 0.35;
+      us = us * us + bytes_us * bytes_us;   // (its root, plus a constant)
       if (us < best_us) { best_us = us; best = MxPlan{f.tn, f.cg, s}; }
     }
   }
@@ -607,16 +706,36 @@ struct Product {
   void* Y;
   ocs_dtype y_type;
   int* dev_status;
+  // not quantized yet (A = NULL)
+  const void* X = nullptr;
+  long long ldx = 0;
+  const int32_t* idx_map = nullptr;
+  ocs_dtype x_type = OCS_F32;
+  int C = 0;
 };
 
-template <typename T, int GRID, int TN, int CG>
+// Whether ocs_linear_mx4 quantizes inside the product's kernel: every CTA quantizes all tokens itself, those of its share of
+// the contraction.  That saves a launch and the workspace, 4 us of the host's 17, which is what bounds an eager call of this
+// size.  On the device it is even up to two blocks per thread and slower beyond, since the code is cold and few warps run it.  us by
+// graph replay, fused against two launches: E4M3 (M, C, N) = (1, 8192, 8192), 512 blocks: 14.8 against 13.5 to 15.5; (20, 650, 2600)
+// in fp32, 820 blocks: 15.5 against 6.5; (8, 4096, 4096), 2048 blocks: 12 against 7.6; E8M0 (16, 1024, 4096), 512 blocks: 7.1
+// against 6.4; (2, 300, 500): 6.5 against 7.8.
+constexpr long long kFuseBlocks = 512;
+bool fuse_tokens(const MxPlan& plan, int M, int C, int K, ocs_grid grid) {
+  if (plan.tn > 32) return false;
+  const int num_kb = (K + 2 * KB - 1) / (2 * KB), n = mx4_block(grid);
+  const int my_kb = (stages_of(plan.tn, num_kb) + plan.slices - 1) / plan.slices * stage_blocks(plan.tn);
+  return my_kb <= kFusedBytes / (plan.tn * KB + kMxTile) && (long long)M * ((C + n - 1) / n) <= kFuseBlocks;
+}
+
+template <typename T, int GRID, int TN, int CG, bool FUSED = false>
 ocs_status launch_tiles(const Product& g, int slices, bool overlap, cudaStream_t stream) {
-  using L = MxSmem<GRID, TN, CG>;
+  using L = MxSmem<GRID, TN, CG, FUSED>;
   static std::atomic<unsigned long long> ready{0};   // devices whose copy of the kernel has its attribute set
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess) return OCS_ERR_CUDA;
   if (dev >= 64 || !(ready.load() >> dev & 1)) {
-    if (cudaFuncSetAttribute(mx_gemm_kernel<T, GRID, TN, CG>, cudaFuncAttributeMaxDynamicSharedMemorySize, L::kDynBytes) != cudaSuccess)
+    if (cudaFuncSetAttribute(mx_gemm_kernel<T, GRID, TN, CG, FUSED>, cudaFuncAttributeMaxDynamicSharedMemorySize, L::kDynBytes) != cudaSuccess)
       return OCS_ERR_CUDA;
     if (dev < 64) ready.fetch_or(1ull << dev);
   }
@@ -635,11 +754,15 @@ ocs_status launch_tiles(const Product& g, int slices, bool overlap, cudaStream_t
   const cuuint64_t wd[2] = {row, (cuuint64_t)g.N}, ws[1] = {(cuuint64_t)g.ldw};
   const cuuint64_t td[2] = {row, (cuuint64_t)g.M}, ts[1] = {(cuuint64_t)g.lda};
   const cuuint32_t wb[2] = {KB, TW}, tb[2] = {KB, (cuuint32_t)L::kTokens};
-  if (!encode_u8(&tm_w, g.W, 2, wd, ws, wb) || !encode_u8(&tm_t, g.A, 2, td, ts, tb)) return OCS_ERR_CUDA;
+  if (!encode_u8(&tm_w, g.W, 2, wd, ws, wb)) return OCS_ERR_CUDA;
   const int n = mx4_block(GRID), pieces = ((g.K + n - 1) / n + 3) / 4;
-  if (!encode_mx4_scales(&tm_sw, g.W_scales, pieces, (g.N + 127) / 128, L::kPieces) ||
-      !encode_mx4_scales(&tm_st, g.A_scales, pieces, (g.M + 127) / 128, L::kPieces))
+  if (!encode_mx4_scales(&tm_sw, g.W_scales, pieces, (g.N + 127) / 128, L::kPieces)) return OCS_ERR_CUDA;
+  if (FUSED) {
+    tm_t = tm_st = tm_w;   // unused
+    p.X = g.X; p.ldx = g.ldx; p.idx_map = g.idx_map; p.x_type = g.x_type; p.C = g.C; p.K = g.K;
+  } else if (!encode_u8(&tm_t, g.A, 2, td, ts, tb) || !encode_mx4_scales(&tm_st, g.A_scales, pieces, (g.M + 127) / 128, L::kPieces)) {
     return OCS_ERR_CUDA;
+  }
   const int cl = CG * slices;
   const long long slots = cluster_capacity(cl) / cl;
   cudaLaunchConfig_t cfg = {};
@@ -660,13 +783,17 @@ ocs_status launch_tiles(const Product& g, int slices, bool overlap, cudaStream_t
     ++n_attr;
   }
   cfg.attrs = attr; cfg.numAttrs = n_attr;
-  LaunchScope scope("mx_gemm_kernel", stream);
-  if (cudaLaunchKernelEx(&cfg, mx_gemm_kernel<T, GRID, TN, CG>, tm_w, tm_t, tm_sw, tm_st, p, static_cast<T*>(g.Y)) != cudaSuccess) return OCS_ERR_CUDA;
+  LaunchScope scope(FUSED ? "mx_gemm_kernel(fused)" : "mx_gemm_kernel", stream);
+  if (cudaLaunchKernelEx(&cfg, mx_gemm_kernel<T, GRID, TN, CG, FUSED>, tm_w, tm_t, tm_sw, tm_st, p, static_cast<T*>(g.Y)) != cudaSuccess) return OCS_ERR_CUDA;
   return launch_status();
 }
 
 template <typename T, int GRID>
 ocs_status run_product(const Product& g, const MxPlan& plan, bool overlap, cudaStream_t stream) {
+  if (!g.A) {
+    if (plan.tn == 16) return launch_tiles<T, GRID, 16, 1, true>(g, plan.slices, false, stream);
+    return launch_tiles<T, GRID, 32, 1, true>(g, plan.slices, false, stream);
+  }
   switch (plan.tn) {
     case 16: return launch_tiles<T, GRID, 16, 1>(g, plan.slices, overlap, stream);
     case 32: return launch_tiles<T, GRID, 32, 1>(g, plan.slices, overlap, stream);
@@ -718,7 +845,7 @@ extern "C" ocs_status ocs_qlinear_mx4(const uint8_t* A_codes, const uint8_t* A_s
   if (st != OCS_OK) return st;
   if (lda < (K + 1) / 2 || lda % 16 != 0 || !aligned(A_codes, 16) || !aligned(A_scales, 16) || !aligned(g.a_rows, 4)) return OCS_ERR_SHAPE;
   if ((st = check_device()) != OCS_OK) return st;
-  return run_product(g, choose_plan(M, N, (K + 2 * KB - 1) / (2 * KB), elem_bytes(y_type)), false, stream);
+  return run_product(g, choose_plan(M, N, K, grid, elem_bytes(y_type)), false, stream);
 }
 
 namespace {
@@ -735,10 +862,20 @@ TokenSpace token_space(int M, int K, ocs_grid grid) {
   t.bytes = t.rows + (grid == OCS_GRID_E4M3 ? align_up((size_t)M * 4, 256) : 0);
   return t;
 }
+// The plan of an ocs_linear_mx4 call, chosen once, and whether its tokens are quantized inside the product's kernel.
+struct LinearCall {
+  MxPlan plan;
+  bool fused;
+};
+LinearCall linear_plan(int M, int C, int K, int N, ocs_grid grid, ocs_dtype y_type) {
+  const MxPlan plan = choose_plan(M, N, K, grid, elem_bytes(y_type));
+  return {plan, fuse_tokens(plan, M, C, K, grid)};
+}
 }  // namespace
 
-extern "C" size_t ocs_linear_mx4_workspace_bytes(int M, int C, int S, ocs_grid grid) {
-  if (M <= 0 || C <= 0 || S < 0 || !mx4_grid(grid) || (int64_t)C + S >= (1 << 30)) return 0;
+extern "C" size_t ocs_linear_mx4_workspace_bytes(int M, int C, int S, ocs_grid grid, int N, ocs_dtype y_type) {
+  if (M <= 0 || C <= 0 || S < 0 || N <= 0 || !mx4_grid(grid) || !valid_dtype(y_type) || (int64_t)C + S >= (1 << 30)) return 0;
+  if (linear_plan(M, C, C + S, N, grid, y_type).fused) return 0;
   return token_space(M, C + S, grid).bytes;
 }
 
@@ -753,18 +890,24 @@ extern "C" ocs_status ocs_linear_mx4(const void* X, ocs_dtype x_type, int M, int
   if (!X || (S > 0 && !idx_map)) return OCS_ERR_INVALID_ARG;
   if ((int64_t)C + S >= (1 << 30)) return OCS_ERR_UNSUPPORTED;
   const int K = C + S;
+  const LinearCall call = linear_plan(M, C, K, N, grid, y_type);
   const TokenSpace t = token_space(M, K, grid);
-  if (!ws || !aligned(ws, 256) || ws_bytes < t.bytes) return OCS_ERR_WORKSPACE;
-  uint8_t* codes = static_cast<uint8_t*>(ws);
+  if (!call.fused && (!ws || !aligned(ws, 256) || ws_bytes < t.bytes)) return OCS_ERR_WORKSPACE;
   const bool rows = grid == OCS_GRID_E4M3;
-  float* a_rows = rows ? reinterpret_cast<float*>(codes + t.rows) : nullptr;
-  const Product g{codes, codes + t.scales, a_rows, W_codes, W_scales, rows ? w_row_scales : nullptr, bias,
-                  M, N, K, t.lda, ldw, ldy, grid, Y, y_type, dev_status};
+  Product g{nullptr, nullptr, nullptr, W_codes, W_scales, rows ? w_row_scales : nullptr, bias,
+            M, N, K, t.lda, ldw, ldy, grid, Y, y_type, dev_status, X, ldx, idx_map, x_type, C};
   ocs_status st = check_product(g);
   if (st != OCS_OK) return st;
-  if ((st = ocs_quantize_mx4(X, x_type, M, C, ldx, S, idx_map, grid, codes, t.lda, codes + t.scales, a_rows, dev_status, stream_)) != OCS_OK)
-    return st;
-  return run_product(g, choose_plan(M, N, (K + 2 * KB - 1) / (2 * KB), elem_bytes(y_type)), true, stream);
+  if (ldx < C || !aligned(X, elem_bytes(x_type)) || (S > 0 && !aligned(idx_map, 4))) return OCS_ERR_SHAPE;
+  if ((st = check_device()) != OCS_OK) return st;
+  if (!call.fused) {
+    uint8_t* codes = static_cast<uint8_t*>(ws);
+    float* a_rows = rows ? reinterpret_cast<float*>(codes + t.rows) : nullptr;
+    if ((st = ocs_quantize_mx4(X, x_type, M, C, ldx, S, idx_map, grid, codes, t.lda, codes + t.scales, a_rows, dev_status, stream_)) != OCS_OK)
+      return st;
+    g.A = codes; g.A_scales = codes + t.scales; g.a_rows = a_rows;
+  }
+  return run_product(g, call.plan, true, stream);
 }
 
 // Test hook: the next ocs_qlinear_mx4 / ocs_linear_mx4 calls of this process use the given plan; tn = 0 gives the choice back.

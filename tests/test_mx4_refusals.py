@@ -58,9 +58,10 @@ def read(n_pages=4, page=8, heads=2, dim=32, grid=2, pages=P, pages2=None, table
     (qlinear, dict(Y=P + 2), SHAPE), (qlinear, dict(bias=P + 1), SHAPE), (qlinear, dict(w_r=P + 1), SHAPE),
     (qlinear, dict(M=1 << 30), UNSUPPORTED), (qlinear, dict(N=2 ** 31 - 511, ldy=2 ** 31 - 511), UNSUPPORTED),
     (qlinear, dict(K=1 << 30, lda=1 << 29, ldw=1 << 29), UNSUPPORTED),
-    (linear, dict(ws=None), WORKSPACE), (linear, dict(ws_bytes=100), WORKSPACE), (linear, dict(ws=P + 16), WORKSPACE),
+    (linear, dict(M=40, ws=None), WORKSPACE), (linear, dict(M=40, ws_bytes=100), WORKSPACE), (linear, dict(M=40, ws=P + 16), WORKSPACE),
+    (linear, dict(C=30000, ldx=30000, ldw=15008, ws=None), WORKSPACE),
     (linear, dict(x_type=7), INVALID), (linear, dict(grid=0), INVALID), (linear, dict(S=1), INVALID), (linear, dict(X=None), INVALID),
-    (linear, dict(w_r=None), INVALID), (linear, dict(ldx=8), SHAPE), (linear, dict(S=8, idx=P), SHAPE), (linear, dict(M=-2), SHAPE),
+    (linear, dict(w_r=None), INVALID), (linear, dict(M=50, w_r=None), INVALID), (linear, dict(ldx=8), SHAPE), (linear, dict(S=8, idx=P), SHAPE), (linear, dict(M=-2), SHAPE),
     (linear, dict(N=2 ** 31 - 1, ldy=2 ** 31 - 1), UNSUPPORTED),
     (write, dict(grid=3), INVALID), (write, dict(grid=-1), INVALID), (write, dict(x_type=5), INVALID), (write, dict(pages=None), INVALID),
     (write, dict(X=None), INVALID), (write, dict(slots=None), INVALID), (write, dict(pages2=2 * P), INVALID), (write, dict(X2=P), INVALID),
@@ -90,8 +91,13 @@ def test_sizes():
     assert L.ocs_mx4_scale_bytes(1, 1, 1) == 512 and L.ocs_mx4_scale_bytes(129, 129, 1) == 4 * 512
     assert L.ocs_mx4_scale_bytes(128, 64, 2) == 512 and L.ocs_mx4_scale_bytes(128, 65, 2) == 1024
     assert L.ocs_mx4_scale_bytes(1 << 24, 1 << 16, 2) == 1 << 36
-    assert L.ocs_linear_mx4_workspace_bytes(0, 10, 0, 1) == 0 and L.ocs_linear_mx4_workspace_bytes(5, 10, 0, 0) == 0
-    assert L.ocs_linear_mx4_workspace_bytes(1 << 20, 25088, 251, 2) > (1 << 20) * 12669
+
+    def q(M, C, S, N, grid=2, y_type=0):
+        return L.ocs_linear_mx4_workspace_bytes(M, C, S, grid, N, y_type)
+    assert q(0, 10, 0, 10) == 0 and q(50, 10, 0, 10, grid=0) == 0 and q(50, 10, 0, 10, y_type=7) == 0 and q(50, 10, 0, 0) == 0
+    assert q(5, 650, 13, 2600) == 0                               # few tokens: quantized inside the product
+    assert q(50, 650, 13, 2600) >= 50 * (332 + 4) + 11 * 512
+    assert q(1 << 20, 25088, 251, 4096) > (1 << 20) * 12669       # 32-bit products would wrap here
 
     def page(*a):
         return L.ocs_cache_page_bytes(ctypes.byref(_CacheDesc(0, *a)))
