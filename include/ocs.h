@@ -510,14 +510,16 @@ typedef enum {
  *   zeros for the blocks between a row's last and the next multiple of four; the bytes of rows that do not exist are left as
  *   they are and mean nothing.
  * row_scales fp32 [rows] (E4M3; ignored for E8M0).
- * rows = 0 is a no-op.  Limits: C + S < 2^30.  Device flags: NONFINITE (that row's outputs are unspecified), BAD_INDEX. */
+ * rows = 0 is a no-op.  Limits: C + S < 2^27.  Device flags: NONFINITE (that row's outputs are unspecified), BAD_INDEX,
+ * TIMEOUT. */
 int64_t ocs_mx4_scale_bytes(int64_t rows, int K, ocs_grid grid);
 ocs_status ocs_quantize_mx4(const void* X, ocs_dtype x_type, int64_t rows, int C, int64_t ldx, int S,
                             const int32_t* idx_map, ocs_grid grid, uint8_t* codes, int64_t ld_codes, uint8_t* scales,
                             float* row_scales, int* dev_status, void* stream);
 
-/* ocs_dequantize_mx4: Y[m][k] = code * s * r, the values that the codes stand for (exact in fp32, rounded to y_type once);
- * Y [rows][K], row stride ldy elements.  With ocs_quantize_mx4 it simulates the grid on floating-point layers. */
+/* ocs_dequantize_mx4: Y[m][k] = code * s * r, the values that the codes stand for (exact in fp32, rounded to y_type once; the
+ * largest value of a block may lie up to 1/16 above the block's own, beyond fp32 or y_type as infinity);
+ * Y [rows][K], row stride ldy elements, K < 2^27.  With ocs_quantize_mx4 it simulates the grid on floating-point layers. */
 ocs_status ocs_dequantize_mx4(const uint8_t* codes, int64_t ld_codes, const uint8_t* scales, const float* row_scales,
                               int64_t rows, int K, ocs_grid grid, void* Y, ocs_dtype y_type, int64_t ldy, void* stream);
 
@@ -528,7 +530,7 @@ ocs_status ocs_dequantize_mx4(const uint8_t* codes, int64_t ld_codes, const uint
  * Row scales and bias come last, rounded once, and once more to y_type.
  * A codes [M], W codes [N] rows of (K+1)/2 bytes, 16-byte aligned, strides lda and ldw multiples of 16; Y [M][N] of y_type,
  * row stride ldy elements; row scales are ignored for E8M0.
- * M = 0 is a no-op.  Limits: M, K < 2^30, N < 2^31 - 511.  Device flag: TIMEOUT. */
+ * M = 0 is a no-op.  Limits: M < 2^30, K < 2^27, N < 2^31 - 511.  Device flag: TIMEOUT. */
 ocs_status ocs_qlinear_mx4(const uint8_t* A_codes, const uint8_t* A_scales, const float* a_row_scales, int M, int K,
                            int64_t lda, const uint8_t* W_codes, const uint8_t* W_scales, const float* w_row_scales, int N,
                            int64_t ldw, ocs_grid grid, const float* bias, void* Y, ocs_dtype y_type, int64_t ldy,

@@ -488,7 +488,7 @@ extern "C" ocs_status ocs_quantize_mx4(const void* X, ocs_dtype x_type, int64_t 
   if (rows < 0 || C <= 0) return OCS_ERR_SHAPE;
   if (rows == 0) return OCS_OK;
   if (!X || !codes || !scales || (grid == OCS_GRID_E4M3 && !row_scales) || (S > 0 && !idx_map)) return OCS_ERR_INVALID_ARG;
-  if ((int64_t)C + S >= (1 << 30)) return OCS_ERR_UNSUPPORTED;
+  if ((int64_t)C + S >= kMxMaxK) return OCS_ERR_UNSUPPORTED;
   const int K = C + S, n = mx4_block(grid), nb = (K + n - 1) / n;
   if (ldx < C || ld_codes < (K + 1) / 2) return OCS_ERR_SHAPE;
   if (!aligned(X, elem_bytes(x_type)) || !aligned(scales, 16) || !aligned(row_scales, 4) || (S > 0 && !aligned(idx_map, 4)))
@@ -512,7 +512,7 @@ extern "C" ocs_status ocs_dequantize_mx4(const uint8_t* codes, int64_t ld_codes,
   if (rows < 0 || K <= 0) return OCS_ERR_SHAPE;
   if (rows == 0) return OCS_OK;
   if (!codes || !scales || !Y || (grid == OCS_GRID_E4M3 && !row_scales)) return OCS_ERR_INVALID_ARG;
-  if (K >= (1 << 30)) return OCS_ERR_UNSUPPORTED;
+  if (K >= kMxMaxK) return OCS_ERR_UNSUPPORTED;
   if (ld_codes < (K + 1) / 2 || ldy < K) return OCS_ERR_SHAPE;
   if (!aligned(Y, elem_bytes(y_type)) || !aligned(scales, 16) || !aligned(row_scales, 4)) return OCS_ERR_SHAPE;
   const ocs_status st = check_device();

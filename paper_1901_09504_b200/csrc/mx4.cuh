@@ -12,6 +12,7 @@
 namespace ocs {
 
 constexpr int kMxTile = 512;   // scale bytes of 128 rows x 4 blocks, the tensor cores' unit
+constexpr int kMxMaxK = 1 << 27;   // channels of a row (the grids' second dimension ends at 65535)
 
 inline bool mx4_grid(ocs_grid g) { return g == OCS_GRID_E8M0 || g == OCS_GRID_E4M3; }
 __host__ __device__ constexpr int mx4_block(int grid) { return grid == OCS_GRID_E8M0 ? 32 : 16; }

@@ -71,7 +71,7 @@ struct MxSmem {
   static constexpr int kShared = kOverlap ? TN - kAccStride : 0;             // columns of both accumulators
   static constexpr int kScaleCol = kAccStride + (kOverlap ? TN : kAccStride);
   static constexpr int kUsedCols = kScaleCol + 2 * kStageCols;
-  static constexpr uint32_t kFullBytes = kSub * (kWBytes + kTBytes), kScaleBytes512 = kSub * (kSWBytes + kSTBytes);   // of a stage
+  static constexpr uint32_t kFullTx = kSub * (kWBytes + kTBytes), kScaleTx = kSub * (kSWBytes + kSTBytes);   // a stage's bytes on its two barriers
   static constexpr uint32_t kTmemCols = kUsedCols <= 128 ? 128 : (kUsedCols <= 256 ? 256 : 512);
   static_assert(kStages >= 3 && (!kXInRing || kXBytes <= kStages * kStageBytes) && kStageBytes % 1024 == 0 && kTBytes % 1024 == 0 && (TN * KB) % 1024 == 0 && kUsedCols <= 512, "tile does not fit");
 };
@@ -352,8 +352,8 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__
         }
       };
       auto announce = [&](int s) {
-        if (half == 0) mbar_arrive_expect_tx(full_bar(s), CG * L::kFullBytes);
-        mbar_arrive_expect_tx(sfull_bar(s), L::kScaleBytes512);
+        if (half == 0) mbar_arrive_expect_tx(full_bar(s), CG * L::kFullTx);
+        mbar_arrive_expect_tx(sfull_bar(s), L::kScaleTx);
       };
       // weights do not depend on the kernel before: the first ring of them is requested before waiting for it
       if (cluster < p.total) {
@@ -818,7 +818,7 @@ ocs_status run_product(const Product& g, const MxPlan& plan, bool overlap, cudaS
 // Everything but the tokens, which ocs_linear_mx4 has in another form.
 ocs_status check_product(const Product& g) {
   if (!g.W || !g.W_scales || !g.Y || (g.grid == OCS_GRID_E4M3 && !g.w_rows)) return OCS_ERR_INVALID_ARG;
-  if (g.M >= (1 << 30) || g.K >= (1 << 30) || g.N > 0x7fffffff - 512) return OCS_ERR_UNSUPPORTED;
+  if (g.M >= (1 << 30) || g.K >= kMxMaxK || g.N > 0x7fffffff - 512) return OCS_ERR_UNSUPPORTED;
   if (g.ldw < (g.K + 1) / 2 || g.ldw % 16 != 0 || !aligned(g.W, 16) || !aligned(g.W_scales, 16)) return OCS_ERR_SHAPE;
   if (g.ldy < g.N || !aligned(g.Y, elem_bytes(g.y_type)) || !aligned(g.w_rows, 4) || !aligned(g.bias, 4)) return OCS_ERR_SHAPE;
   return OCS_OK;
@@ -874,7 +874,7 @@ LinearCall linear_plan(int M, int C, int K, int N, ocs_grid grid, ocs_dtype y_ty
 }  // namespace
 
 extern "C" size_t ocs_linear_mx4_workspace_bytes(int M, int C, int S, ocs_grid grid, int N, ocs_dtype y_type) {
-  if (M <= 0 || C <= 0 || S < 0 || N <= 0 || !mx4_grid(grid) || !valid_dtype(y_type) || (int64_t)C + S >= (1 << 30)) return 0;
+  if (M <= 0 || C <= 0 || S < 0 || N <= 0 || !mx4_grid(grid) || !valid_dtype(y_type) || (int64_t)C + S >= kMxMaxK) return 0;
   if (linear_plan(M, C, C + S, N, grid, y_type).fused) return 0;
   return token_space(M, C + S, grid).bytes;
 }
@@ -888,7 +888,7 @@ extern "C" ocs_status ocs_linear_mx4(const void* X, ocs_dtype x_type, int M, int
   if (M < 0 || C <= 0 || N <= 0) return OCS_ERR_SHAPE;
   if (M == 0) return OCS_OK;
   if (!X || (S > 0 && !idx_map)) return OCS_ERR_INVALID_ARG;
-  if ((int64_t)C + S >= (1 << 30)) return OCS_ERR_UNSUPPORTED;
+  if ((int64_t)C + S >= kMxMaxK) return OCS_ERR_UNSUPPORTED;
   const int K = C + S;
   const LinearCall call = linear_plan(M, C, K, N, grid, y_type);
   const TokenSpace t = token_space(M, K, grid);

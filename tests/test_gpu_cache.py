@@ -239,3 +239,22 @@ def test_a_decoding_loop_captured_and_replayed():
     assert torch.equal(a.pages, k.pages)
     assert torch.equal(ocs.ocs_cache_read(a, table, starts, B * n), ok)
     assert torch.equal(ocs.ocs_cache_read(v, table, starts, B * n), ov)
+
+
+def test_what_does_not_fit_the_cache_is_refused():
+    c = ocs.ocs_cache_new(4, 8, 2, 32, ocs.MX4_E4M3)
+    x, slots = _vectors(1, 3, 2, 32, "f32"), torch.arange(3, device="cuda")
+    table, starts = torch.zeros((1, 2), dtype=torch.int32, device="cuda"), torch.tensor([0, 3], dtype=torch.int32, device="cuda")
+    for call in (lambda: ocs.ocs_cache_write(c, x[:, :1], slots), lambda: ocs.ocs_cache_write(c, x, slots[:2]),
+                 lambda: ocs.ocs_cache_write(c, x, slots.int()), lambda: ocs.ocs_cache_write(c._replace(dim=48), x, slots),
+                 lambda: ocs.ocs_cache_write(c, x.double(), slots), lambda: ocs.ocs_cache_write(c, x, slots, cache2=c._replace(grid=ocs.MX4_E8M0), x2=x),
+                 lambda: ocs.ocs_cache_write(c, x, slots, x2=x), lambda: ocs.ocs_cache_write(c, x.transpose(1, 2), slots),
+                 lambda: ocs.ocs_cache_read(c, table.long(), starts, 3), lambda: ocs.ocs_cache_read(c, table, starts[:1], 3),
+                 lambda: ocs.ocs_cache_read(c, table, starts, 3, out=x[:2]), lambda: ocs.ocs_cache_read(c, table, starts, 3, out2=x),
+                 lambda: ocs.ocs_cache_read(c, table, starts, 3, cache2=c, out2=x.half()), lambda: ocs.ocs_cache_read(c, table, starts.cpu(), 3)):
+        with pytest.raises(AssertionError):
+            call()
+    with pytest.raises(ocs.OcsError):
+        ocs.ocs_cache_new(1, 8, 2, 2000)
+    with pytest.raises(ocs.OcsError):
+        ocs.ocs_cache_write(c, x, slots, cache2=c, x2=x)          # the same cache twice

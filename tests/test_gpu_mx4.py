@@ -83,6 +83,14 @@ def test_quantize(M, C, S, kind, grid):
     check_quantized(_x(M + C, M, C, kind), _idx(C, C, S), S, grid, ref.up((C + S + 1) // 2, 16))
 
 
+@pytest.mark.parametrize("M,C,S,kind", [(200, 10000, 100, "f32"), (310, 25088, 251, "f32"), (300, 16641, 3, "f32"), (299, 28000, 0, "f32"),
+                                        (297, 33280, 16, "bf16"), (150, 33281, 5, "f16"), (160, 20000, 0, "f16"), (299, 30000, 3000, "f32")])
+@pytest.mark.parametrize("grid", GRIDS)
+def test_quantize_many_long_rows(M, C, S, kind, grid):
+    """Four pieces per thread, rows staged through shared memory, rows read twice, tails that shared memory does not hold."""
+    check_quantized(_x(M + C, M, C, kind), _idx(C, C, S), S, grid, ref.up((C + S + 1) // 2, 16))
+
+
 @pytest.mark.parametrize("M,C,S", [(1, 5, 1), (9, 3, 2), (40, 31, 0), (70, 513, 9), (3, 7279, 145), (2, 70003, 11)])
 @pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
 @pytest.mark.parametrize("first,ld_codes", [(0, 0), (1, 1), (6, 4), (8, 3)])
@@ -201,3 +209,72 @@ def test_product_under_every_plan(M, K, N, plan, grid):
     assert ocs.ocs_poll_status(st) == 0
     check_product(y, a, w, bias, torch.float32)
     assert torch.equal(y, again)
+
+
+@pytest.mark.parametrize("grid", GRIDS)
+@pytest.mark.parametrize("M,K,N,bias,kind", [(1, 8192, 1000, False, "bf16"), (3, 25339, 70, True, "f32"), (130, 25088, 300, False, "f16"), (700, 663, 5001, True, "f32"),
+                                             (2047, 4178, 517, True, "bf16"), (1025, 96, 33, False, "f32"), (64, 31, 20000, True, "f16"), (9000, 130, 257, False, "bf16")])
+def test_product_as_planned(M, K, N, bias, kind, grid):
+    a, w = _operand(M, M, K, grid), _operand(N + 1, N, K, grid)
+    b = torch.randn(N, generator=_gen(3), device="cuda") if bias else None
+    st = ocs.new_status()
+    y = ocs.ocs_qlinear_mx4(a, w, bias=b, out_dtype=TYPES[kind], dev_status=st)
+    assert ocs.ocs_poll_status(st) == 0
+    check_product(y, a, w, b, TYPES[kind])
+    assert torch.equal(y, ocs.ocs_qlinear_mx4(a, w, bias=b, out_dtype=TYPES[kind]))
+
+
+@pytest.mark.parametrize("grid", GRIDS)
+def test_scales_of_rows_that_do_not_exist_mean_nothing(grid):
+    """The bytes of the last tile's missing rows are NaN in both formats here."""
+    a, w = _operand(1, 70, 200, grid), _operand(2, 130, 200, grid)
+    want = ocs.ocs_qlinear_mx4(a, w)
+    for q in (a, w):
+        rows = q.codes.shape[0]
+        flat = q.scales.view(-1)
+        at = torch.from_numpy(ref.scale_index(128 * q.scales.shape[0], 4 * q.scales.shape[1])).cuda()
+        flat[at[rows:].reshape(-1)] = 255
+    assert torch.equal(ocs.ocs_qlinear_mx4(a, w), want)
+
+
+@pytest.mark.parametrize("grid", GRIDS)
+def test_zero_rows_and_extreme_scales(grid):
+    """Rows of zeros, and rows whose scales lie far apart (the sums' scale comes last)."""
+    x, w = _x(1, 5, 300, "f32").clone(), _x(2, 140, 300, "f32").clone()
+    x[1], w[7] = 0, 0
+    x[2] *= 2.0 ** 60
+    x[3] *= 2.0 ** -60
+    w[9] *= 2.0 ** -70
+    a, q = ocs.ocs_quantize_mx4(x, grid), ocs.ocs_quantize_mx4(w, grid)
+    y = ocs.ocs_qlinear_mx4(a, q)
+    check_product(y, a, q, None, torch.float32)
+    assert (y[1] == 0).all() and (y[:, 7] == 0).all()
+
+
+def test_grids_and_lengths_that_do_not_match_are_refused():
+    a, b = _operand(1, 5, 64, ocs.MX4_E4M3), _operand(2, 7, 64, ocs.MX4_E8M0)
+    c = _operand(3, 7, 65, ocs.MX4_E4M3)
+    x = _x(1, 5, 64, "f32")
+    for call in (lambda: ocs.ocs_qlinear_mx4(a, b), lambda: ocs.ocs_qlinear_mx4(a, c), lambda: ocs.ocs_linear_mx4(x, c),
+                 lambda: ocs.ocs_quantize_mx4(x, ocs.GRID_I8), lambda: ocs.ocs_quantize_mx4(x, ocs.MX4_E4M3, out=c),
+                 lambda: ocs.ocs_quantize_mx4(x, ocs.MX4_E4M3, idx_map=None, S=2), lambda: ocs.ocs_qlinear_mx4(a, a._replace(codes=a.codes.cpu())),
+                 lambda: ocs.ocs_dequantize_mx4(a._replace(scales=a.scales[:, :0])), lambda: ocs.ocs_quantize_mx4(x.cpu()),
+                 lambda: ocs.ocs_qlinear_mx4(a, a, dev_status=torch.zeros(1, dtype=torch.int32)),
+                 lambda: ocs.ocs_linear_mx4(x, a, ws=torch.empty(1 << 20, dtype=torch.uint8))):
+        with pytest.raises((AssertionError, AttributeError)):
+            call()
+
+
+def test_two_streams_at_once():
+    """Products that run side by side, each with its own operands."""
+    ops = [(_operand(i, 300, 2048, ocs.MX4_E4M3), _operand(i + 9, 1000, 2048, ocs.MX4_E4M3)) for i in range(4)]
+    want = [ocs.ocs_qlinear_mx4(a, w) for a, w in ops]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in ops]
+    got = []
+    for _ in range(5):
+        for s, (a, w) in zip(streams, ops):
+            with torch.cuda.stream(s):
+                got.append(ocs.ocs_qlinear_mx4(a, w))
+    torch.cuda.synchronize()
+    assert all(torch.equal(g, want[i % 4]) for i, g in enumerate(got))
