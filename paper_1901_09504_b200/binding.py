@@ -771,9 +771,9 @@ def _check_mx4(q: Mx4):
     return rows, ld if ld > cols else cols
 
 
-def _new(size, dtype, like):
-    """An empty tensor on like's device (taking the type from a tensor costs the host less than naming it)."""
-    return like.new_empty(size) if like.dtype is dtype else like.new_empty(size, dtype=dtype)
+def _new_rows(rows: int, cols: int, dtype, like):
+    """An empty [rows, cols] on like's device (naming the strides costs the host least)."""
+    return torch.empty_strided((rows, cols), (cols, 1), dtype=dtype, device=like.device)
 
 
 def ocs_quantize_mx4(x, grid: int = MX4_E4M3, idx_map=None, S: int = 0, out: Mx4 | None = None, dev_status=None) -> Mx4:
@@ -790,8 +790,9 @@ def ocs_quantize_mx4(x, grid: int = MX4_E4M3, idx_map=None, S: int = 0, out: Mx4
         nb = (K + 1) >> 1
         ld = (nb + 15) & ~15
         codes = torch.empty_strided((rows, nb), (ld, 1), dtype=torch.uint8, device=x.device)
-        out = Mx4(codes, codes.new_empty((rows + 127 >> 7, _mx4_pieces(K, grid), 32, 4, 4)),
-                  _new(rows, torch.float32, x) if grid == MX4_E4M3 else None, K, grid)
+        P = _mx4_pieces(K, grid)
+        out = Mx4(codes, codes.new_empty_strided((rows + 127 >> 7, P, 32, 4, 4), (P * 512, 512, 16, 4, 1)),
+                  torch.empty_strided((rows,), (1,), dtype=torch.float32, device=x.device) if grid == MX4_E4M3 else None, K, grid)
     else:
         assert out.K == K and out.grid == grid and out.codes.shape[0] == rows
         ld = _check_mx4(out)[1]
@@ -805,7 +806,7 @@ def ocs_dequantize_mx4(q: Mx4, out_dtype=torch.float32, out=None):
     """The values that q's codes stand for, [rows, K] of out_dtype (fp32: exact)."""
     rows, ld = _check_mx4(q)
     if out is None:
-        out, ldy = q.codes.new_empty((rows, q.K), dtype=out_dtype), q.K
+        out, ldy = _new_rows(rows, q.K, out_dtype, q.codes), q.K
     else:
         assert out.is_cuda and out.shape == (rows, q.K)
         ldy = _rows_of(out)
@@ -822,7 +823,7 @@ def ocs_qlinear_mx4(a: Mx4, w: Mx4, bias=None, out_dtype=torch.float32, out=None
     assert a.K == w.K and a.grid == w.grid
     _check_vec(bias, N), _check_status(dev_status)
     if out is None:
-        out, ldy = _new((M, N), out_dtype, a.codes if bias is None else bias), N
+        out, ldy = _new_rows(M, N, out_dtype, a.codes), N
     else:
         assert out.is_cuda and out.shape == (M, N)
         ldy = _rows_of(out)
@@ -846,7 +847,7 @@ def ocs_linear_mx4(x, w: Mx4, idx_map=None, S: int = 0, bias=None, out_dtype=Non
     _check_idx(idx_map, Cn, S), _check_vec(bias, N), _check_status(dev_status)
     assert ws is None or (ws.is_cuda and ws.dtype == torch.uint8 and ws.is_contiguous())
     if out is None:
-        out, ldy = x.new_empty((M, N)) if out_dtype is None else _new((M, N), out_dtype, x), N
+        out, ldy = _new_rows(M, N, x.dtype if out_dtype is None else out_dtype, x), N
     else:
         assert out.is_cuda and out.shape == (M, N)
         ldy = _rows_of(out)
@@ -951,15 +952,17 @@ def ocs_cache_read(cache: QuantCache, table, starts, rows: int, out_dtype=torch.
     _check_status(dev_status)
     rows = int(rows)
     if out is None:
-        out = cache.pages.new_empty((rows, cache.heads, cache.dim), dtype=out_dtype)
-        v = out.data_ptr(), cache.heads * cache.dim, cache.dim
+        H, D = cache.heads, cache.dim
+        out = torch.empty_strided((rows, H, D), (H * D, D, 1), dtype=out_dtype, device=table.device)
+        v = out.data_ptr(), H * D, D
     else:
         v = _check_vectors(out, rows, cache)
     p2, v2 = None, (None, 0, 0)
     if cache2 is not None:
         if out2 is None:
-            out2 = out.new_empty((rows, cache.heads, cache.dim))
-        assert out2.dtype == out.dtype
+            H, D = cache.heads, cache.dim
+            out2 = torch.empty_strided((rows, H, D), (H * D, D, 1), dtype=out.dtype, device=table.device)
+        assert out2.dtype is out.dtype
         p2, v2 = cache2.pages.data_ptr(), _check_vectors(out2, rows, cache)
     else:
         assert out2 is None
