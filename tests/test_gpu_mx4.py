@@ -195,7 +195,8 @@ PLANS = [(16, 1, 1), (16, 1, 4), (32, 1, 1), (32, 1, 8), (64, 1, 1), (64, 1, 2),
 
 @pytest.mark.parametrize("grid", GRIDS)
 @pytest.mark.parametrize("plan", PLANS)
-@pytest.mark.parametrize("M,K,N", [(1, 1, 1), (5, 64, 130), (16, 300, 128), (31, 1000, 257), (100, 257, 40), (300, 2048, 513), (515, 700, 700)])
+@pytest.mark.parametrize("M,K,N", [(1, 1, 1), (5, 64, 130), (16, 300, 128), (31, 1000, 257), (100, 257, 40), (300, 2048, 513), (515, 700, 700),
+                                   (140, 1280, 30000), (9000, 100, 300), (1290, 513, 4100)])
 def test_product_under_every_plan(M, K, N, plan, grid):
     a, w = _operand(M, M, K, grid), _operand(N + 1, N, K, grid)
     bias = torch.randn(N, generator=_gen(3), device="cuda")
