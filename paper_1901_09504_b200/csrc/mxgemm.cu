@@ -9,6 +9,21 @@
 // memory ahead of the products that read them.  tcgen05.cp would do that, in order with the products and in the tensor cores'
 // time: some 45 cycles a piece, 12 pieces (E4M3, 256 tokens) for 512 cycles of products.  Four warps move them through
 // registers instead, while the products before them run.
+// Forms: 16, 32, 64 or 128 tokens per CTA, or 256 by a pair of CTAs (256 channels, each CTA stages half the tokens); few tiles:
+// 2, 4 or 8 CTAs of a cluster split the contraction and exchange their partial sums through distributed shared memory.
+//
+// What bounds it (device times by graph replay; the floor is the larger of the bytes at 6.54 TB/s, the measured copy rate, and
+// the operations at 6.43 PFLOP/s, four times the measured bf16 rate):
+// M x K x N
+//   8192 x 8192 x 8192, bf16 out   E4M3 227 us, E8M0 213 us (floor 171): operand tiles; a K-block is 38 (35) KB a CTA, and five
+//                                  (six) of them in flight bring 82 GB/s an SM; without any scales 228 and 208 us, and one pair
+//                                  alone takes a K-block in 0.36 (0.34) us where its products alone would be 0.28
+//   2047 x 4178 x 4096, bf16 out   23.0 us (floor 10.9): two waves of tiles, the second three quarters full
+//   128 x 25339 x 4096, fp32 out   21.5 us (floor 9.5): one wave of 128 CTAs with a tile each: start (4 us), exchange and end (4)
+//   700 x 663 x 33278, fp32 out    36 us (floor 16): writing (93 MB in this pattern alone take 23 us, 19 where rows start at
+//                                  32-byte boundaries; 8 warps and 16 stores a piece are enough for that), and the
+//                                  stores and the operand requests share the SM's way out; 20 us without the stores
+//   1 x 8192 x 8192, bf16          12.5 us (floor 5.8): HBM after 3 us of start, the exchange and the end
 #include <atomic>
 
 #include "mx4.cuh"
