@@ -89,7 +89,7 @@ constexpr int kRowPieces = 4;       // most pieces per thread
 
 // What bounds it: instructions beside HBM.  8192 x 8192 bf16 (134 MB in, 38 out, floor 26 us): E4M3 36 us, issue slots 64 % full
 // at 12 instructions an element, E8M0 28 us; 333 x 5000 with 50 duplicated channels 3.1 us.  Rows that start anywhere pay
-// for 48 bytes read where they need 32: 4085 x 7279 bf16 E4M3 26 us (aligned 7296: 15).
+// for 48 bytes read where they need 32: 4085 x 7279 bf16 E4M3 25 us (4085 x 7296: 19).
 // G = blockDim.x threads (a power of two below 32, or whole warps) and NV pieces each for one row, or (E8M0, whose blocks need
 // nothing of their row) a part of one: blockIdx.y.  blockDim.y rows per CTA.  E4M3: a row's scale is that of its largest
 // magnitude, so the row waits in registers for it.
@@ -370,7 +370,8 @@ ocs_status launch_quantize(const void* X_, const MxRows& p, ocs_grid grid, cudaS
 // ---- codes to values: a thread stores NS times 32 aligned bytes of a row; blockDim.x threads and gridDim.y CTAs per row,
 // blockDim.y rows per CTA.  SHIFTED: rows start anywhere, so a thread's elements are `ahead` behind a multiple of their number:
 // their codes are shifted out of the words around them, and each 32 bytes of them may have two scales.  HBM bounds it: 4096 x
-// 25088 to fp32 73 us (6.4 TB/s), 8192 x 8192 to bf16 28 us (6.1); rows that start anywhere take 1.3 times that.
+// 25088 to fp32 73 us (6.4 TB/s), 8192 x 8192 to bf16 28 us (6.1); 4085 x
+// 7279, whose rows start anywhere, 19 (7296: 13).
 template <typename T, int GRID, bool SHIFTED, int NS>
 __global__ void __launch_bounds__(256) mx4_values_kernel(const MxRows p, T* __restrict__ Y, long long ldy) {
   constexpr int E = 32 / (int)sizeof(T), SHIFT = GRID == OCS_GRID_E8M0 ? 5 : 4, NW = NS * E / 8;

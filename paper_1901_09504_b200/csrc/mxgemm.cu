@@ -36,6 +36,7 @@ constexpr int TW = 128;        // channels of one CTA's tile
 constexpr int KB = 128;        // bytes of a K-block's row: 256 contraction indices
 constexpr int kEpiWarps = 8;
 constexpr int kFusedBytes = 64 * 1024;             // token codes and scales a CTA can hold beside the ring of weights
+constexpr int kTailBytes = 8 * 1024;               // ... and what its rows have behind their last whole block
 constexpr int kThreads = 64 + 32 * kEpiWarps + 128;   // copy warp, tensor-core warp, epilogue warps, scale warps
 
 __host__ __device__ constexpr int stage_blocks(int tn) { return tn <= 64 ? 2 : 1; }   // K-blocks of a ring stage
@@ -75,7 +76,7 @@ struct MxSmem {
   // FUSED: the codes of all the K-blocks a CTA takes, [K-block][token][128 bytes], their scales, [K-block][32 tokens][16
   // bytes, one per block], a row's maximum and its scale
   static constexpr int kFusedBlocks = FUSED ? kFusedBytes / (TN * KB + kMxTile) : 0, kTokenBytes = FUSED ? kFusedBlocks * (TN * KB + kMxTile) : 0;
-  static constexpr int kRowBytes = FUSED ? TN * 8 : 0;
+  static constexpr int kRowBytes = FUSED ? TN * 8 + kTailBytes : 0;
   static constexpr int kCtrlBytes = 512;
   static constexpr int kBudget = 227 * 1024 - 1024 - kCtrlBytes - kScaleBytes - kXExtra - kTokenBytes - kRowBytes;
   static constexpr int kStages = kBudget / kStageBytes < 8 ? kBudget / kStageBytes : 8;
@@ -194,15 +195,36 @@ __device__ __forceinline__ void finish(T* y, long long ldy, const uint32_t* acc,
 // The epilogue warps quantize the token tile (all of the call's M <= TN tokens) into the operand tiles of stages slice,
 // slice + slices, ...; E4M3: after the rows' maxima.  A thread's unit of work is a block of a row.  This code runs once per CTA,
 // so that fetching the instructions is what it costs besides the loads' latency: nothing is unrolled over units, and both
-// passes go through the same load (20 x 650 in fp32 takes 15.5 us in all, with two or four units at a time 15.8 and 16).
+// passes go through the same load (20 x 650 in fp32 took 15.5 us in all, with two or four units at a time 15.8 and 16).
 template <typename X, int GRID, int TN>
 __device__ __forceinline__ void quantize_tokens(const MxGemm& p, int slice, int my_kb, unsigned char* tok, unsigned char* scales,
-                                                uint32_t* max_bits, float* row_scale) {
+                                                uint32_t* max_bits, float* row_scale, unsigned char* tails) {
   constexpr int N = mx4_block(GRID), PER = 2 * KB / N, kSub = stage_blocks(TN);   // blocks of a K-block
   const int et = threadIdx.x - 64, nb = (p.K + N - 1) / N;
   if (et < TN) {
     max_bits[et] = 0;
     row_scale[et] = 1.0f;
+  }
+  // what rows have behind their last whole block (its rest and the duplicated channels): a thread per element, so that indices
+  // and values each come in one load.  (Gathered by the threads that have the blocks, they cost every pass 2 us a unit.)
+  const int whole = p.C / N, tail = (nb - whole) * N;
+  const bool staged = tail > 0 && p.M * tail * (int)sizeof(X) <= kTailBytes;
+  X* s_tail = reinterpret_cast<X*>(tails);
+  if (staged) {
+    for (int e = et; e < p.M * tail; e += 256) {
+      const int r = e / tail;
+      int src = whole * N + e - r * tail;
+      X v = from_f32<X>(0.0f);
+      if (src < p.K) {
+        if (src >= p.C) {
+          src = __ldg(p.idx_map + src);
+          if ((unsigned)src >= (unsigned)p.C) { flag(p.dev_status, OCS_DEV_BAD_INDEX); src = 0; }
+        }
+        v = static_cast<const X*>(p.X)[r * p.ldx + src];
+      }
+      s_tail[e] = v;
+    }
+    if (GRID == OCS_GRID_E8M0) asm volatile("bar.sync 1, 256;" ::: "memory");
   }
 #pragma unroll 1
   for (int pass = GRID == OCS_GRID_E4M3 ? 0 : 1; pass < 2; ++pass) {
@@ -211,7 +233,7 @@ __device__ __forceinline__ void quantize_tokens(const MxGemm& p, int slice, int 
       row_scale[et] = two_to(mx4_row_exponent(max_bits[et]));
       if (max_bits[et] >= 0x7f800000u) flag(p.dev_status, OCS_DEV_NONFINITE);
     }
-    const int per_row = pass ? my_kb * PER : (p.C + N - 1) / N, units = p.M * per_row;
+    const int per_row = pass ? my_kb * PER : (staged ? nb : (p.C + N - 1) / N), units = p.M * per_row;
 #pragma unroll 1
     for (int u0 = et & ~31; u0 < units; u0 += 256) {   // (whole warps)
       const int u = min(u0 + (et & 31), units - 1);   // (the last one more than once: harmless)
@@ -221,6 +243,7 @@ __device__ __forceinline__ void quantize_tokens(const MxGemm& p, int slice, int 
       Block<X, N> v;
       // (the load reads up to 16 bytes around the block: within the matrix)
       if ((b + 1) * N <= p.C && (r > 0 || b > 0) && (r + 1 < p.M || (b + 2) * N <= p.C)) v.template load<0>(x + b * N);
+      else if (staged && b >= whole && b < nb) v.from_shared(s_tail + r * tail + (b - whole) * N);
       else if (b < nb) v.gather(x, b * N, p.C, pass ? p.K : p.C, p.idx_map, p.dev_status);
       else v.clear();
       const uint32_t m = v.max_bits();
@@ -263,6 +286,7 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__
   float* scale_buf = reinterpret_cast<float*>(after + L::kXExtra);
   uint32_t* row_max = reinterpret_cast<uint32_t*>(after + L::kXExtra + L::kScaleBytes);   // FUSED: [TN] maxima, then scales
   float* row_scale = reinterpret_cast<float*>(row_max + TN);
+  unsigned char* tails = reinterpret_cast<unsigned char*>(row_scale + TN);
   uint64_t* bars = reinterpret_cast<uint64_t*>(after + L::kXExtra + L::kScaleBytes + L::kRowBytes);
   auto full_bar = [&](int s) { return smem_u32(bars + s); };
   auto empty_bar = [&](int s) { return smem_u32(bars + L::kStages + s); };
@@ -325,9 +349,9 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__
     if (CL > 1) cluster_arrive();
     if (FUSED && warp < 2 + kEpiWarps) {
       // they need nothing of the set-up
-      if (p.x_type == OCS_F32) quantize_tokens<float, GRID, TN>(p, slice, my_st * L::kSub, tokens, token_scales, row_max, row_scale);
-      else if (p.x_type == OCS_F16) quantize_tokens<__half, GRID, TN>(p, slice, my_st * L::kSub, tokens, token_scales, row_max, row_scale);
-      else quantize_tokens<__nv_bfloat16, GRID, TN>(p, slice, my_st * L::kSub, tokens, token_scales, row_max, row_scale);
+      if (p.x_type == OCS_F32) quantize_tokens<float, GRID, TN>(p, slice, my_st * L::kSub, tokens, token_scales, row_max, row_scale, tails);
+      else if (p.x_type == OCS_F16) quantize_tokens<__half, GRID, TN>(p, slice, my_st * L::kSub, tokens, token_scales, row_max, row_scale, tails);
+      else quantize_tokens<__nv_bfloat16, GRID, TN>(p, slice, my_st * L::kSub, tokens, token_scales, row_max, row_scale, tails);
       asm volatile("bar.arrive 4, %0;" ::"n"(kThreads - 32) : "memory");   // this warp's codes are in place
     }
     asm volatile("bar.sync 2, %0;" ::"n"(kThreads) : "memory");
@@ -731,16 +755,16 @@ struct Product {
 
 // Whether ocs_linear_mx4 quantizes inside the product's kernel: every CTA quantizes all tokens itself, those of its share of
 // the contraction.  That saves a launch and the workspace, 4 us of the host's 17, which is what bounds an eager call of this
-// size.  On the device it is even up to two blocks per thread and slower beyond, since the code is cold and few warps run it.  us by
-// graph replay, fused against two launches: E4M3 (M, C, N) = (1, 8192, 8192), 512 blocks: 14.8 against 13.5 to 15.5; (20, 650, 2600)
-// in fp32, 820 blocks: 15.5 against 6.5; (8, 4096, 4096), 2048 blocks: 12 against 7.6; E8M0 (16, 1024, 4096), 512 blocks: 7.1
-// against 6.4; (2, 300, 500): 6.5 against 7.8.
-constexpr long long kFuseBlocks = 512;
+// size.  On the device it is even up to two blocks per thread (four on E8M0, which takes one pass) and slower beyond, since the
+// code is cold and few warps run it.  us by graph replay, fused against two launches: E4M3 (M, C, N) = (1, 8192, 8192), 512
+// blocks: 14.8 against 13.5 to 15.5; (20, 650, 2600) in fp32, 820 blocks: 13.6 against 6.5; (8, 4096, 4096), 2048 blocks: 12.4
+// against 7.6; E8M0 (16, 1024, 4096), 512 blocks: 7.2 against 6.4; (2, 300, 500): 6.3 against 7.8; (24, 2000, 2000), 1512 blocks:
+// 9.1 against 7.3.
 bool fuse_tokens(const MxPlan& plan, int M, int C, int K, ocs_grid grid) {
   if (plan.tn > 32) return false;
   const int num_kb = (K + 2 * KB - 1) / (2 * KB), n = mx4_block(grid);
   const int my_kb = (stages_of(plan.tn, num_kb) + plan.slices - 1) / plan.slices * stage_blocks(plan.tn);
-  return my_kb <= kFusedBytes / (plan.tn * KB + kMxTile) && (long long)M * ((C + n - 1) / n) <= kFuseBlocks;
+  return my_kb <= kFusedBytes / (plan.tn * KB + kMxTile) && (long long)M * ((C + n - 1) / n) <= (grid == OCS_GRID_E4M3 ? 512 : 1024);
 }
 
 template <typename T, int GRID, int TN, int CG, bool FUSED = false>
