@@ -332,7 +332,9 @@ ocs_status launch_rows(const T* X, const MxRows& p, cudaStream_t stream) {
     return launch_status();
   }
   // few rows: a thread for every piece, as far as a CTA has them; many: two pieces each, or four (E8M0: one, twice the size)
-  int nv = GRID == OCS_GRID_E4M3 && p.rows > kNumSMs && pieces > 32 ? 2 : 1;
+  // fewer threads have more of a row's common work: 8192 x 8192 bf16 33.7 us with four pieces, 36 with two; rows that start
+  // anywhere need the registers for loads: 4085 x 7279 29 and 26
+  int nv = GRID == OCS_GRID_E4M3 && p.rows > kNumSMs && pieces > 32 ? (ALIGN == 32 && pieces > 128 ? 4 : 2) : 1;
   if (GRID == OCS_GRID_E4M3)
     while (pieces > nv * kRowThreads) nv *= 2;
   const int part = (pieces + nv - 1) / nv;
