@@ -87,8 +87,8 @@ __device__ __forceinline__ void stage_tail(const MxRows& p, const T* x, int firs
 constexpr int kRowThreads = 512;
 constexpr int kRowPieces = 4;       // most pieces per thread
 
-// What bounds it: instructions beside HBM.  8192 x 8192 bf16 (134 MB in, 38 out, floor 26 us): E4M3 36 us, issue slots 64 % full
-// at 12 instructions an element, E8M0 28 us; 333 x 5000 with 50 duplicated channels 3.1 us.  Rows that start anywhere pay
+// What bounds it: instructions beside HBM.  8192 x 8192 bf16 (134 MB in, 38 out, floor 26 us): E4M3 34 us, issue slots two
+// thirds full at 12 instructions an element, E8M0 28 us; 333 x 5000 with 50 duplicated channels 3.1 us.  Rows that start anywhere pay
 // for 48 bytes read where they need 32: 4085 x 7279 bf16 E4M3 25 us (4085 x 7296: 19).
 // G = blockDim.x threads (a power of two below 32, or whole warps) and NV pieces each for one row, or (E8M0, whose blocks need
 // nothing of their row) a part of one: blockIdx.y.  blockDim.y rows per CTA.  E4M3: a row's scale is that of its largest
