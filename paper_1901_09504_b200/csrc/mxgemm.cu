@@ -38,6 +38,7 @@ constexpr int kEpiWarps = 8;
 constexpr int kFusedBytes = 64 * 1024;             // token codes and scales a CTA can hold beside the ring of weights
 constexpr int kTailBytes = 8 * 1024;               // ... and what its rows have behind their last whole block
 constexpr int kThreads = 64 + 32 * kEpiWarps + 128;   // copy warp, tensor-core warp, epilogue warps, scale warps
+constexpr int kTokenThreads = kThreads - 64;          // that quantize tokens (FUSED): all but the first two
 
 __host__ __device__ constexpr int stage_blocks(int tn) { return tn <= 64 ? 2 : 1; }   // K-blocks of a ring stage
 
@@ -192,7 +193,7 @@ __device__ __forceinline__ void finish(T* y, long long ldy, const uint32_t* acc,
     y += ldy;
   }
 }
-// The epilogue warps quantize the token tile (all of the call's M <= TN tokens) into the operand tiles of stages slice,
+// The epilogue and scale warps quantize the token tile (all of the call's M <= TN tokens) into the operand tiles of stages slice,
 // slice + slices, ...; E4M3: after the rows' maxima.  A thread's unit of work is a block of a row.  This code runs once per CTA,
 // so that fetching the instructions is what it costs besides the loads' latency: nothing is unrolled over units, and both
 // passes go through the same load (20 x 650 in fp32 took 15.5 us in all, with two or four units at a time 15.8 and 16).
@@ -211,7 +212,7 @@ __device__ __forceinline__ void quantize_tokens(const MxGemm& p, int slice, int 
   const bool staged = tail > 0 && p.M * tail * (int)sizeof(X) <= kTailBytes;
   X* s_tail = reinterpret_cast<X*>(tails);
   if (staged) {
-    for (int e = et; e < p.M * tail; e += 256) {
+    for (int e = et; e < p.M * tail; e += kTokenThreads) {
       const int r = e / tail;
       int src = whole * N + e - r * tail;
       X v = from_f32<X>(0.0f);
@@ -224,18 +225,18 @@ __device__ __forceinline__ void quantize_tokens(const MxGemm& p, int slice, int 
       }
       s_tail[e] = v;
     }
-    if (GRID == OCS_GRID_E8M0) asm volatile("bar.sync 1, 256;" ::: "memory");
+    if (GRID == OCS_GRID_E8M0) asm volatile("bar.sync 1, %0;" ::"n"(kTokenThreads) : "memory");
   }
 #pragma unroll 1
   for (int pass = GRID == OCS_GRID_E4M3 ? 0 : 1; pass < 2; ++pass) {
-    if (GRID == OCS_GRID_E4M3) asm volatile("bar.sync 1, 256;" ::: "memory");
+    if (GRID == OCS_GRID_E4M3) asm volatile("bar.sync 1, %0;" ::"n"(kTokenThreads) : "memory");
     if (GRID == OCS_GRID_E4M3 && pass && et < p.M) {
       row_scale[et] = two_to(mx4_row_exponent(max_bits[et]));
       if (max_bits[et] >= 0x7f800000u) flag(p.dev_status, OCS_DEV_NONFINITE);
     }
     const int per_row = pass ? my_kb * PER : (staged ? nb : (p.C + N - 1) / N), units = p.M * per_row;
 #pragma unroll 1
-    for (int u0 = et & ~31; u0 < units; u0 += 256) {   // (whole warps)
+    for (int u0 = et & ~31; u0 < units; u0 += kTokenThreads) {   // (whole warps)
       const int u = min(u0 + (et & 31), units - 1);   // (the last one more than once: harmless)
       const int r = u / per_row, at = u - r * per_row, in = at / PER, bb = at % PER;   // this CTA's K-block, block in it
       const int b = pass ? ((slice + in / kSub * p.slices) * kSub + in % kSub) * PER + bb : at;
@@ -347,12 +348,12 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__
     asm volatile("bar.sync 3, 64;" ::: "memory");
   } else {
     if (CL > 1) cluster_arrive();
-    if (FUSED && warp < 2 + kEpiWarps) {
+    if (FUSED) {
       // they need nothing of the set-up
       if (p.x_type == OCS_F32) quantize_tokens<float, GRID, TN>(p, slice, my_st * L::kSub, tokens, token_scales, row_max, row_scale, tails);
       else if (p.x_type == OCS_F16) quantize_tokens<__half, GRID, TN>(p, slice, my_st * L::kSub, tokens, token_scales, row_max, row_scale, tails);
       else quantize_tokens<__nv_bfloat16, GRID, TN>(p, slice, my_st * L::kSub, tokens, token_scales, row_max, row_scale, tails);
-      asm volatile("bar.arrive 4, %0;" ::"n"(kThreads - 32) : "memory");   // this warp's codes are in place
+      if (warp < 2 + kEpiWarps) asm volatile("bar.arrive 4, %0;" ::"n"(kThreads - 32) : "memory");   // this warp's codes are in place
     }
     asm volatile("bar.sync 2, %0;" ::"n"(kThreads) : "memory");
   }
@@ -754,17 +755,17 @@ struct Product {
 };
 
 // Whether ocs_linear_mx4 quantizes inside the product's kernel: every CTA quantizes all tokens itself, those of its share of
-// the contraction.  That saves a launch and the workspace, 4 us of the host's 17, which is what bounds an eager call of this
-// size.  On the device it is even up to two blocks per thread (four on E8M0, which takes one pass) and slower beyond, since the
-// code is cold and few warps run it.  us by graph replay, fused against two launches: E4M3 (M, C, N) = (1, 8192, 8192), 512
-// blocks: 14.8 against 13.5 to 15.5; (20, 650, 2600) in fp32, 820 blocks: 13.6 against 6.5; (8, 4096, 4096), 2048 blocks: 12.4
-// against 7.6; E8M0 (16, 1024, 4096), 512 blocks: 7.2 against 6.4; (2, 300, 500): 6.3 against 7.8; (24, 2000, 2000), 1512 blocks:
-// 9.1 against 7.3.
+// the contraction.  That saves a launch and the workspace, 4 to 6 us of the host's 17, which is what bounds an eager call of
+// this size.  The host decides here: on the device the fused form is even up to some 500 blocks and slower beyond, since its code
+// is cold and few warps run it.  us by graph replay, fused against two launches: E4M3 (M, C, N) = (1, 8192, 8192), 512 blocks:
+// 14.8 against 13.5 to 15.5; (20, 650, 2600) in fp32, 820 blocks: 12.5 against 6.5; (8, 4096, 4096), 2048 blocks: 11.4 against 7.6;
+// E8M0 (16, 1024, 4096), 512 blocks: 7.3 against 6.4; (2, 300, 500): 6.3 against 7.8; (24, 2000, 2000), 1512 blocks: 8.4
+// against 7.3.  A caller that replays graphs takes ocs_quantize_mx4 and ocs_qlinear_mx4 instead, which give the same bits.
 bool fuse_tokens(const MxPlan& plan, int M, int C, int K, ocs_grid grid) {
   if (plan.tn > 32) return false;
   const int num_kb = (K + 2 * KB - 1) / (2 * KB), n = mx4_block(grid);
   const int my_kb = (stages_of(plan.tn, num_kb) + plan.slices - 1) / plan.slices * stage_blocks(plan.tn);
-  return my_kb <= kFusedBytes / (plan.tn * KB + kMxTile) && (long long)M * ((C + n - 1) / n) <= (grid == OCS_GRID_E4M3 ? 512 : 1024);
+  return my_kb <= kFusedBytes / (plan.tn * KB + kMxTile) && (long long)M * ((C + n - 1) / n) <= (grid == OCS_GRID_E4M3 ? 1024 : 2048);
 }
 
 template <typename T, int GRID, int TN, int CG, bool FUSED = false>
