@@ -810,6 +810,7 @@ def ocs_dequantize_mx4(q: Mx4, out_dtype=torch.float32, out=None):
     else:
         assert out.is_cuda and out.shape == (rows, q.K)
         ldy = _rows_of(out)
+    assert out.dtype in DTYPES
     st = lib().ocs_dequantize_mx4(q.codes.data_ptr(), ld, q.scales.data_ptr(), _addr(q.row_scales), rows, q.K, q.grid,
                                   out.data_ptr(), DTYPES[out.dtype], ldy, _raw_stream(q.codes))
     _check(st, "ocs_dequantize_mx4")

@@ -68,7 +68,8 @@ def check_quantized(x, idx, S, grid, ld=None):
     np.testing.assert_array_equal(rows[:, :(K + 1) // 2], ref.pack(codes))
     assert (rows[:, (K + 1) // 2:] == 0x5a).all() and (got[M * ld:] == 0x5a).all()
     v = ref.values(codes, byte, r, grid)
-    np.testing.assert_array_equal(host(ocs.ocs_dequantize_mx4(q)), v.astype(np.float32))
+    with np.errstate(over="ignore"):                              # (a block's 6 may lie above fp32's largest value)
+        np.testing.assert_array_equal(host(ocs.ocs_dequantize_mx4(q)), v.astype(np.float32))
     return q, v
 
 

@@ -34,7 +34,8 @@ def test_the_layer_in_one_call_is_the_two_calls(M, C, S, N, x_kind, y_kind, grid
 @pytest.mark.parametrize("plan", [(16, 1, 1), (16, 1, 2), (16, 1, 8), (32, 1, 1), (32, 1, 4), (64, 1, 1)])
 @pytest.mark.parametrize("M,C,S,N,kind,ld,first", [(1, 8192, 0, 300, "bf16", 0, 0), (1, 700, 9, 129, "f16", 0, 1), (3, 5000, 50, 70, "bf16", 5001, 3),
                                                    (16, 650, 13, 257, "f32", 651, 1), (20, 577, 0, 130, "f16", 577, 5), (32, 333, 40, 500, "bf16", 0, 0),
-                                                   (2, 31, 1, 16, "f32", 0, 0), (9, 1, 1, 5, "f32", 0, 0)])
+                                                   (2, 31, 1, 16, "f32", 0, 0), (9, 1, 1, 5, "f32", 0, 0),
+                                                   (32, 333, 200, 300, "f32", 0, 0), (32, 500, 500, 140, "bf16", 501, 1)])
 def test_few_tokens_inside_the_product_give_the_two_calls_bits(M, C, S, N, kind, ld, first, plan, grid):
     x, w, idx = _x(M, M, C, kind, ld=ld or None, offset=first), _x(N, N, C + S, "f32", std=0.02), _idx(C, C, S)
     W = ocs.ocs_quantize_mx4(w, grid)
@@ -86,12 +87,14 @@ def test_a_row_that_is_not_finite_stays_alone(grid):
 
 
 @pytest.mark.parametrize("grid", GRIDS)
-def test_calls_captured_with_their_own_workspaces(grid):
-    """Two layers on two streams, captured together and replayed with new inputs."""
-    x = [_x(i, 50, 512, "bf16").clone() for i in range(2)]
+@pytest.mark.parametrize("M", [50, 7])
+def test_calls_captured_with_their_own_workspaces(M, grid):
+    """Two layers on two streams, captured together and replayed with new inputs (with workspaces, and without any)."""
+    x = [_x(i, M, 512, "bf16").clone() for i in range(2)]
     W = [ocs.ocs_quantize_mx4(_x(5 + i, 400, 512, "f32"), grid) for i in range(2)]
-    out = [torch.empty((50, 400), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
-    n = ocs.lib().ocs_linear_mx4_workspace_bytes(50, 512, 0, grid, 400, 2)
+    out = [torch.empty((M, 400), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    n = ocs.lib().ocs_linear_mx4_workspace_bytes(M, 512, 0, grid, 400, 2)
+    assert (n == 0) == (M == 7)
     ws = [torch.empty(n, dtype=torch.uint8, device="cuda") for _ in range(2)]
     side = torch.cuda.Stream()
 
@@ -112,7 +115,7 @@ def test_calls_captured_with_their_own_workspaces(grid):
     torch.cuda.current_stream().wait_stream(s)
     for seed in (11, 12, 13):
         for i in range(2):
-            x[i].copy_(_x(seed + i, 50, 512, "bf16"))
+            x[i].copy_(_x(seed + i, M, 512, "bf16"))
         g.replay()
         for i in range(2):
             assert torch.equal(out[i], ocs.ocs_linear_mx4(x[i], W[i]))
