@@ -780,11 +780,15 @@ def ocs_quantize_mx4(x, grid: int = MX4_E4M3, idx_map=None, S: int = 0, out: Mx4
     """x fp32 / fp16 / bf16 [rows, C] (row stride = x.stride(0)) -> Mx4 with K = C + S: e2m1 codes with a scale per 32
     (MX4_E8M0) or 16 (MX4_E4M3) channels, the S duplicated channels of idx_map appended.  `out`: an Mx4 of that K and
     grid to write to."""
-    assert x.is_cuda and x.dtype in DTYPES and grid in (MX4_E8M0, MX4_E4M3)
+    xt = DTYPES.get(x.dtype)
+    assert x.is_cuda and xt is not None and (grid == MX4_E4M3 or grid == MX4_E8M0)
     ldx = _rows_of(x)
     rows, Cn = x.shape
     S = int(S)
-    _check_idx(idx_map, Cn, S), _check_status(dev_status)
+    if S:
+        _check_idx(idx_map, Cn, S)
+    if dev_status is not None:
+        _check_status(dev_status)
     K = Cn + S
     if out is None:
         nb = (K + 1) >> 1
@@ -796,7 +800,7 @@ def ocs_quantize_mx4(x, grid: int = MX4_E4M3, idx_map=None, S: int = 0, out: Mx4
     else:
         assert out.K == K and out.grid == grid and out.codes.shape[0] == rows
         ld = _check_mx4(out)[1]
-    st = lib().ocs_quantize_mx4(x.data_ptr(), DTYPES[x.dtype], rows, Cn, ldx, S, _addr(idx_map), grid, out.codes.data_ptr(), ld,
+    st = lib().ocs_quantize_mx4(x.data_ptr(), xt, rows, Cn, ldx, S, _addr(idx_map), grid, out.codes.data_ptr(), ld,
                                 out.scales.data_ptr(), _addr(out.row_scales), _addr(dev_status), _raw_stream(x))
     _check(st, "ocs_quantize_mx4")
     return out
@@ -839,29 +843,41 @@ def ocs_qlinear_mx4(a: Mx4, w: Mx4, bias=None, out_dtype=torch.float32, out=None
 def ocs_linear_mx4(x, w: Mx4, idx_map=None, S: int = 0, bias=None, out_dtype=None, out=None, ws=None, dev_status=None):
     """x fp32 / fp16 / bf16 [M, C], weights w [N, K = C + S] -> Y [M, N] (of x's type, or out_dtype): ocs_quantize_mx4 on
     w's grid and ocs_qlinear_mx4 in one call."""
-    assert x.is_cuda and x.dtype in DTYPES
+    xt = DTYPES.get(x.dtype)
+    assert x.is_cuda and xt is not None
     ldx = _rows_of(x)
     M, Cn = x.shape
     S = int(S)
+    codes, scales, row_scales, K, grid = w
     N, ldw = _check_mx4(w)
-    assert w.K == Cn + S
-    _check_idx(idx_map, Cn, S), _check_vec(bias, N), _check_status(dev_status)
-    assert ws is None or (ws.is_cuda and ws.dtype == torch.uint8 and ws.is_contiguous())
+    assert K == Cn + S
+    if S:
+        _check_idx(idx_map, Cn, S)
+    if bias is not None:
+        _check_vec(bias, N)
+    if dev_status is not None:
+        _check_status(dev_status)
     if out is None:
-        out, ldy = _new_rows(M, N, x.dtype if out_dtype is None else out_dtype, x), N
+        if out_dtype is None:
+            out_dtype = x.dtype
+        out, ldy = _new_rows(M, N, out_dtype, x), N
     else:
         assert out.is_cuda and out.shape == (M, N)
-        ldy = _rows_of(out)
-    assert out.dtype in DTYPES
+        out_dtype, ldy = out.dtype, _rows_of(out)
+    yt = DTYPES.get(out_dtype)
+    assert yt is not None
     L = lib()
-    xt, yt = DTYPES[x.dtype], DTYPES[out.dtype]
     if ws is None:
-        n_ws = L.ocs_linear_mx4_workspace_bytes(M, Cn, S, w.grid, N, yt)
+        n_ws, at_ws = L.ocs_linear_mx4_workspace_bytes(M, Cn, S, grid, N, yt), None
         if n_ws:
-            ws = w.codes.new_empty(n_ws)
-    st = L.ocs_linear_mx4(x.data_ptr(), xt, M, Cn, ldx, S, _addr(idx_map), w.grid, w.codes.data_ptr(),
-                          w.scales.data_ptr(), _addr(w.row_scales), N, ldw, _addr(bias), out.data_ptr(), yt, ldy,
-                          _addr(ws), 0 if ws is None else ws.numel(), _addr(dev_status), _raw_stream(x))
+            ws = codes.new_empty(n_ws)
+            at_ws = ws.data_ptr()
+    else:
+        assert ws.is_cuda and ws.dtype == torch.uint8 and ws.is_contiguous()
+        n_ws, at_ws = ws.numel(), ws.data_ptr()
+    st = L.ocs_linear_mx4(x.data_ptr(), xt, M, Cn, ldx, S, _addr(idx_map), grid, codes.data_ptr(), scales.data_ptr(),
+                          _addr(row_scales), N, ldw, _addr(bias), out.data_ptr(), yt, ldy, at_ws, n_ws, _addr(dev_status),
+                          _raw_stream(x))
     _check(st, "ocs_linear_mx4")
     return out
 

@@ -134,7 +134,9 @@ __device__ __forceinline__ int sequence_of(const int32_t* starts, int B, long lo
   return lo;
 }
 
-constexpr int kReadTokens = 32;     // most output rows of a CTA
+// Most output rows of a CTA.  Vectors of few heads need many to occupy it: 150 thousand tokens of 2 x 128 57 us, with at most
+// 32 rows 65; 50 thousand of 1 x 64 (int8) 7.4 and 12.8.
+constexpr int kReadTokens = 128;
 
 // Where a token's vectors are in its page (codes NULL: no such row; rows NULL: a bad page).
 struct TokenAt {
