@@ -161,13 +161,13 @@ __global__ void __launch_bounds__(256) cache_read_kernel(const CacheArgs a, int 
     TokenAt w{nullptr, nullptr, nullptr};
     const int b = t < a.rows ? sequence_of(a.starts, a.B, t) : -1;
     if (b >= 0) {
-      const int pos = (int)t - __ldg(a.starts + b), col = (unsigned)pos / (unsigned)a.page_size;
-      const int page = col < a.table_cols ? __ldg(a.table + b * a.ld_table + col) : -1;
+      const unsigned pos = (unsigned)t - (unsigned)__ldg(a.starts + b), col = pos / (unsigned)a.page_size;   // (starts may be negative)
+      const int page = col < (unsigned)a.table_cols ? __ldg(a.table + b * a.ld_table + col) : -1;
       const uint8_t* base = a.pages[which];
       w.codes = base;
       if ((unsigned)page >= (unsigned)a.n_pages) flag(a.dev_status, OCS_DEV_BAD_INDEX);
       else {
-        const long long at = (long long)(pos - col * a.page_size) * a.heads;
+        const long long at = (long long)(pos - col * (unsigned)a.page_size) * a.heads;
         base += page * a.g.bytes;
         w.codes = base + at * a.g.cb;
         w.scales = base + a.g.at_s + at * a.g.sb;

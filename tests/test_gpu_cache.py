@@ -167,6 +167,22 @@ def test_bad_slots_and_pages_are_flagged():
     assert ocs.ocs_poll_status(st) == ocs.DEV_BAD_INDEX and (out[16:] == 0).all()
 
 
+@pytest.mark.parametrize("P", [1, 4])
+def test_starts_before_the_first_row(P):
+    """A negative first start leaves out a sequence's first tokens; one so low that no table has the column reads zeros."""
+    cache = ocs.ocs_cache_new(12, P, 2, 24, ocs.GRID_I8)
+    x = _vectors(11, 9, 2, 24, "f32")
+    ocs.ocs_cache_write(cache, x, torch.arange(9, device="cuda"))
+    table = torch.arange(12, dtype=torch.int32, device="cuda").view(1, 12)
+    whole = ocs.ocs_cache_read(cache, table, torch.tensor([0, 9], dtype=torch.int32, device="cuda"), 9, torch.float32)
+    st = torch.zeros(1, dtype=torch.int32, device="cuda")
+    rest = ocs.ocs_cache_read(cache, table, torch.tensor([-4, 5], dtype=torch.int32, device="cuda"), 5, torch.float32, dev_status=st)
+    assert torch.equal(rest, whole[4:]) and ocs.ocs_poll_status(st) == 0
+    for first in (-2 ** 31, -2 ** 31 + 3, -10 ** 9):
+        low = ocs.ocs_cache_read(cache, table, torch.tensor([first, 5], dtype=torch.int32, device="cuda"), 5, torch.float32, dev_status=st)
+        assert (low == 0).all() and ocs.ocs_poll_status(st) == ocs.DEV_BAD_INDEX
+
+
 @pytest.mark.parametrize("grid", GRIDS)
 def test_not_finite_is_flagged_and_stays_in_its_vector(grid):
     x = _vectors(1, 4, 3, 64, "f32")
