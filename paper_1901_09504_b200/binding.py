@@ -764,10 +764,11 @@ def _check_mx4(q: Mx4):
     assert scales.is_contiguous() and scales.numel() >= (rows + 127 >> 7) * _mx4_pieces(K, grid) * 512
     if grid == MX4_E4M3:
         assert rs.is_cuda and rs.dtype is torch.float32 and rs.is_contiguous() and rs.numel() >= rows
+    ld, one = codes.stride()
+    assert one == 1 or cols <= 1
     if rows == 1:
         return 1, (cols + 15) & ~15
-    ld, one = codes.stride()
-    assert (one == 1 or cols <= 1) and (ld >= cols or rows == 0)
+    assert ld >= cols or rows == 0
     return rows, ld if ld > cols else cols
 
 
