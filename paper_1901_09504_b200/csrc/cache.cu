@@ -334,6 +334,37 @@ ocs_status fill(CacheArgs& a, const ocs_cache* c, void* pages, void* pages2, int
   return OCS_OK;
 }
 
+// Whether no two of n0 x n1 vectors with these strides share an element: one stride goes over all vectors of the other.
+bool nested(long long dim, long long n0, long long ld0, long long n1, long long ld1) {
+  if ((n0 > 1 && ld0 < dim) || (n1 > 1 && ld1 < dim)) return false;
+  return n0 <= 1 || n1 <= 1 || (ld0 - dim) / (n1 - 1) >= ld1 || (ld1 - dim) / (n0 - 1) >= ld0;
+}
+
+// Whether two outputs of the same strides, each of them nested and the second d elements behind the first, share an element: some
+// |i| < outer count and |j| < inner count have |d - i outer stride - j inner stride| < dim.  Only the multiples of a stride on both
+// sides of a distance come into question, since all inner vectors lie within one outer stride.  (Outputs of different strides
+// are not looked at.)
+bool on_each_other(const CacheArgs& a, long long d) {
+  long long n0 = a.rows, ld0 = a.ld_row[0], n1 = a.heads, ld1 = a.ld_head[0];
+  if ((n0 > 1 && ld0 != a.ld_row[1]) || (n1 > 1 && ld1 != a.ld_head[1])) return false;
+  if (n0 > 1 && n1 > 1 && ld1 > ld0) {   // tokens inside of heads
+    long long t = n0; n0 = n1; n1 = t;
+    t = ld0; ld0 = ld1; ld1 = t;
+  }
+  if (d < 0) d = -d;
+  if (n0 <= 1) ld0 = d + 1;              // (only i = 0 is within the bounds)
+  if (n1 <= 1) ld1 = ld0;
+  for (long long i = d / ld0; i <= d / ld0 + 1 && i < n0; ++i) {
+    long long r = d - i * ld0;
+    if (r < 0) r = -r;
+    for (long long j = r / ld1; j <= r / ld1 + 1 && j < n1; ++j) {
+      const long long off = r - j * ld1;
+      if (off < a.dim && off > -a.dim) return true;
+    }
+  }
+  return false;
+}
+
 }  // namespace
 }  // namespace ocs
 
@@ -376,9 +407,10 @@ extern "C" ocs_status ocs_cache_read(const ocs_cache* c, const void* pages, cons
   CacheArgs a{};
   ocs_status st = fill(a, c, const_cast<void*>(pages), const_cast<void*>(pages2), rows, Y, ld_token, ld_head, Y2, ld_token2, ld_head2, y_type);
   if (st != OCS_OK) return st;
-  // the output's vectors must not overlap
+  if (pages2 && Y2 == Y) return OCS_ERR_INVALID_ARG;
   for (int i = 0; i < (pages2 ? 2 : 1); ++i)
-    if ((c->heads > 1 && a.ld_head[i] < c->dim) || (rows > 1 && a.ld_row[i] < c->dim)) return OCS_ERR_SHAPE;
+    if (!nested(c->dim, rows, a.ld_row[i], c->heads, a.ld_head[i])) return OCS_ERR_SHAPE;
+  if (pages2 && on_each_other(a, (reinterpret_cast<intptr_t>(Y2) - reinterpret_cast<intptr_t>(Y)) / elem_bytes(y_type))) return OCS_ERR_SHAPE;
   if (ld_table < table_cols || !aligned(table, 4) || !aligned(starts, 4)) return OCS_ERR_SHAPE;
   if ((st = check_device()) != OCS_OK) return st;
   a.table = table; a.ld_table = ld_table; a.table_cols = table_cols; a.starts = starts; a.B = B; a.dev_status = dev_status;
