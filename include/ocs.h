@@ -537,10 +537,11 @@ ocs_status ocs_qlinear_mx4(const uint8_t* A_codes, const uint8_t* A_scales, cons
                            int* dev_status, void* stream);
 
 /* ocs_linear_mx4: ocs_quantize_mx4 on X, then ocs_qlinear_mx4 on its codes (K = C + S), in one call, bit-identical to the
- * two.  Few tokens (up to 32, of 1024 blocks in all, E8M0 2048) are quantized inside the product's kernel (one launch, which
- * spares the host 4 us and more; on the device two are up to 6 us faster, so a caller that replays graphs may prefer the two
- * calls); otherwise codes and scales live in the workspace and the product's launch overlaps the quantization.  Workspace:
- * ocs_linear_mx4_workspace_bytes, 256-byte aligned; 0 means none is needed and ws may be NULL.  Arguments, limits and device flags of the two calls. */
+ * two.  Few tokens (up to 32, of 1024 blocks in all, E8M0 2048, duplicated channels among them) are quantized inside the
+ * product's kernel (one launch, which spares the host 4 us and more; on the device two are up to 6 us faster, so a caller that
+ * replays graphs may prefer the two calls); otherwise codes and scales live in the workspace and the product's launch overlaps
+ * the quantization.  Workspace: ocs_linear_mx4_workspace_bytes, 256-byte aligned; 0 means none is needed and ws may be NULL.
+ * Arguments, limits and device flags of the two calls. */
 size_t ocs_linear_mx4_workspace_bytes(int M, int C, int S, ocs_grid grid, int N, ocs_dtype y_type);
 ocs_status ocs_linear_mx4(const void* X, ocs_dtype x_type, int M, int C, int64_t ldx, int S, const int32_t* idx_map,
                           ocs_grid grid, const uint8_t* W_codes, const uint8_t* W_scales, const float* w_row_scales, int N,

@@ -761,11 +761,12 @@ struct Product {
 // 14.8 against 13.5 to 15.5; (20, 650, 2600) in fp32, 820 blocks: 12.5 against 6.5; (8, 4096, 4096), 2048 blocks: 11.4 against 7.6;
 // E8M0 (16, 1024, 4096), 512 blocks: 7.3 against 6.4; (2, 300, 500): 6.3 against 7.8; (24, 2000, 2000), 1512 blocks: 8.4
 // against 7.3.  A caller that replays graphs takes ocs_quantize_mx4 and ocs_qlinear_mx4 instead, which give the same bits.
-bool fuse_tokens(const MxPlan& plan, int M, int C, int K, ocs_grid grid) {
+// Blocks are those of all K channels, duplicated ones too: each is quantized.
+bool fuse_tokens(const MxPlan& plan, int M, int K, ocs_grid grid) {
   if (plan.tn > 32) return false;
   const int num_kb = (K + 2 * KB - 1) / (2 * KB), n = mx4_block(grid);
   const int my_kb = (stages_of(plan.tn, num_kb) + plan.slices - 1) / plan.slices * stage_blocks(plan.tn);
-  return my_kb <= kFusedBytes / (plan.tn * KB + kMxTile) && (long long)M * ((C + n - 1) / n) <= (grid == OCS_GRID_E4M3 ? 1024 : 2048);
+  return my_kb <= kFusedBytes / (plan.tn * KB + kMxTile) && (long long)M * ((K + n - 1) / n) <= (grid == OCS_GRID_E4M3 ? 1024 : 2048);
 }
 
 template <typename T, int GRID, int TN, int CG, bool FUSED = false>
@@ -907,15 +908,15 @@ struct LinearCall {
   MxPlan plan;
   bool fused;
 };
-LinearCall linear_plan(int M, int C, int K, int N, ocs_grid grid, ocs_dtype y_type) {
+LinearCall linear_plan(int M, int K, int N, ocs_grid grid, ocs_dtype y_type) {
   const MxPlan plan = choose_plan(M, N, K, grid, elem_bytes(y_type));
-  return {plan, fuse_tokens(plan, M, C, K, grid)};
+  return {plan, fuse_tokens(plan, M, K, grid)};
 }
 }  // namespace
 
 extern "C" size_t ocs_linear_mx4_workspace_bytes(int M, int C, int S, ocs_grid grid, int N, ocs_dtype y_type) {
   if (M <= 0 || C <= 0 || S < 0 || N <= 0 || !mx4_grid(grid) || !valid_dtype(y_type) || (int64_t)C + S >= kMxMaxK) return 0;
-  if (linear_plan(M, C, C + S, N, grid, y_type).fused) return 0;
+  if (linear_plan(M, C + S, N, grid, y_type).fused) return 0;
   return token_space(M, C + S, grid).bytes;
 }
 
@@ -930,7 +931,7 @@ extern "C" ocs_status ocs_linear_mx4(const void* X, ocs_dtype x_type, int M, int
   if (!X || (S > 0 && !idx_map)) return OCS_ERR_INVALID_ARG;
   if ((int64_t)C + S >= kMxMaxK) return OCS_ERR_UNSUPPORTED;
   const int K = C + S;
-  const LinearCall call = linear_plan(M, C, K, N, grid, y_type);
+  const LinearCall call = linear_plan(M, K, N, grid, y_type);
   const TokenSpace t = token_space(M, K, grid);
   if (!call.fused && (!ws || !aligned(ws, 256) || ws_bytes < t.bytes)) return OCS_ERR_WORKSPACE;
   const bool rows = grid == OCS_GRID_E4M3;
