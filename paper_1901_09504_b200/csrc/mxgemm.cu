@@ -159,10 +159,23 @@ template <typename T> struct Pair;
 template <> struct Pair<__half> { static __device__ __forceinline__ uint32_t pack(float a, float b) { __half2 h = __floats2half2_rn(a, b); return *reinterpret_cast<uint32_t*>(&h); } };
 template <> struct Pair<__nv_bfloat16> { static __device__ __forceinline__ uint32_t pack(float a, float b) { __nv_bfloat162 h = __floats2bfloat162_rn(a, b); return *reinterpret_cast<uint32_t*>(&h); } };
 
-// One output: the sum times two powers of two (exact within fp32's range, the sum first), plus the bias, rounded once.
+// One output: the sum times two powers of two (the token's first), plus the bias, rounded once.  The first product is exact
+// downward: sums are multiples of 2^-20 and scales at least 2^-117, so it is a multiple of 2^-137.  Upward it stays in fp32's
+// range for scales up to kNearScale, as sums are below 2^50 (K < 2^27 products of at most 2688^2); where a warp's tokens have
+// larger ones (E4M3 rows of 2^88 and more), near_sums goes before it.
+constexpr float kNearScale = 0x1p77f;
 __device__ __forceinline__ float one_output(uint32_t acc, float as, float ws, float b) {
   return fmaf(__fmul_rn(__uint_as_float(acc), as), ws, b);
 }
+// The sums times the channel's scale if that makes them smaller (exact, as above), so that the product with the token's is too
+// large for fp32 only where the output is; the scale that is left then: at least 1.  (The smaller scale of the two first in every
+// case costs the 16-bit epilogue 4 to 7 %.)
+template <int CNT>
+__device__ __forceinline__ void near_sums(uint32_t* acc, float ws) {
+#pragma unroll
+  for (int i = 0; i < CNT; ++i) acc[i] = __float_as_uint(__fmul_rn(__uint_as_float(acc[i]), fminf(ws, 1.0f)));
+}
+__device__ __forceinline__ float scale_left(float ws) { return fmaxf(ws, 1.0f); }
 
 // CNT consecutive tokens of one channel per lane, rounded to T and stored; the lanes of the warp hold consecutive channels.
 // at: the element offset of the lane's channel of the first token; left: tokens that exist, from the first on.  WHOLE: all
@@ -544,6 +557,18 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__
       if (FUSED) return row_scale[m];
       return p.a_scales ? __ldcg(p.a_scales + m) : 1.0f;
     };
+    // the scales of this warp's `count` tokens; whether any is beyond kNearScale
+    auto fetch_scales = [&](int count, auto token) {
+      bool far = false;
+      for (int i = lane; i < count; i += 32) {
+        const float f = token_scale(token(i));
+        sc[i] = f;
+        far |= f > kNearScale;
+      }
+      far = GRID == OCS_GRID_E4M3 && __any_sync(0xffffffffu, far);
+      __syncwarp();
+      return far;
+    };
     int j = 0;
     for (int t = cluster; t < p.total; t += n_clusters, ++j) {
       int mt, nt;
@@ -559,8 +584,8 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__
         if constexpr (L::kXBytes > 0) {
           const int own = TN / p.slices, groups = own / 4;
           __syncwarp();
-          for (int i = lane; i < own; i += 32) sc[i] = token_scale(mt * TN + slice * own + i);
-          __syncwarp();
+          const bool far = fetch_scales(own, [&](int i) { return mt * TN + slice * own + i; });
+          const float ws_left = far ? scale_left(ws) : ws;
           if (!warp_wait(accfull_bar(acc), ((uint32_t)j >> 1) & 1u, abort_flag)) break;
           tc_fence_after();
           if (L::kXInRing) {
@@ -603,18 +628,19 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__
               const float4 b4 = *reinterpret_cast<const float4*>(cell + sl * slot);
               a.x = __fadd_rn(a.x, b4.x); a.y = __fadd_rn(a.y, b4.y); a.z = __fadd_rn(a.z, b4.z); a.w = __fadd_rn(a.w, b4.w);
             }
-            const uint32_t av[4] = {__float_as_uint(a.x), __float_as_uint(a.y), __float_as_uint(a.z), __float_as_uint(a.w)};
+            uint32_t av[4] = {__float_as_uint(a.x), __float_as_uint(a.y), __float_as_uint(a.z), __float_as_uint(a.w)};
+            if (far) near_sums<4>(av, ws);
             const float4 s4 = *reinterpret_cast<const float4*>(sc + 4 * g);
             const float sv[4] = {s4.x, s4.y, s4.z, s4.w};
-            finish<false, T, 4>(y + 4 * g * p.ldy, p.ldy, av, sv, ws, b, p.M - m_own - 4 * g, n < p.N, pairs);
+            finish<false, T, 4>(y + 4 * g * p.ldy, p.ldy, av, sv, ws_left, b, p.M - m_own - 4 * g, n < p.N, pairs);
           }
         }
         break;   // a K split is used only where every cluster has one tile
       }
       // the token scales of this warp's columns: fetched while the main loop runs
       __syncwarp();
-      for (int i = lane; i < L::kWarpTokens; i += 32) sc[i] = token_scale(mt * TN + (i / EC) * 2 * EC + part * EC + i % EC);
-      __syncwarp();
+      const bool far = fetch_scales(L::kWarpTokens, [&](int i) { return mt * TN + (i / EC) * 2 * EC + part * EC + i % EC; });
+      const float ws_left = far ? scale_left(ws) : ws;
       if (!warp_wait(accfull_bar(acc), ((uint32_t)j >> 1) & 1u, abort_flag)) break;
       tc_fence_after();
       // Pieces of EC columns; the next one's way out of tensor memory overlaps this one's arithmetic and stores.  Overlapping
@@ -635,6 +661,15 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__
       };
       uint32_t v[2][EC];
       if (part * EC < TN) {
+        if (far)   // in tensor memory, so that the loop below stays as short as it is
+#pragma unroll 1
+          for (int i = 0; i < kPieces; ++i) {
+            tmem_ld_async<EC>(addr + 2 * EC * i, v[0]);
+            tmem_wait_ld16(v[0]);
+            near_sums<EC>(v[0], ws);
+            tmem_store<EC>(addr + 2 * EC * i, v[0]);
+            asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+          }
         auto piece = [&](int i) { return down ? kPieces - 1 - i : i; };
         tmem_ld_async<EC>(addr + 2 * EC * piece(0), v[0]);
 #pragma unroll 2
@@ -651,8 +686,8 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__
             s[e] = f.x; s[e + 1] = f.y; s[e + 2] = f.z; s[e + 3] = f.w;
           }
           T* y = Y + (long long)(m_first + at) * p.ldy + n;
-          if (n_all && left >= EC) finish<true, T, EC>(y, p.ldy, v[i & 1], s, ws, b, left, true, pairs);
-          else finish<false, T, EC>(y, p.ldy, v[i & 1], s, ws, b, left, n < p.N, pairs);
+          if (n_all && left >= EC) finish<true, T, EC>(y, p.ldy, v[i & 1], s, ws_left, b, left, true, pairs);
+          else finish<false, T, EC>(y, p.ldy, v[i & 1], s, ws_left, b, left, n < p.N, pairs);
         }
       }
       if (!L::kOverlap) emptied(acc);
