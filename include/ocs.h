@@ -580,7 +580,7 @@ ocs_status ocs_cache_write(const ocs_cache* cache, void* pages, const void* X, i
 
 /* ocs_cache_read: the values of B sequences, one after the other: row t of Y, starts[b] <= t < starts[b+1], is token
  * t - starts[b] of sequence b, which is in page table[b][(t - starts[b]) / page_size].  table int32 [B][table_cols], row
- * stride ld_table; starts int32 [B+1], ascending (below 0: a sequence's first
+ * stride ld_table, NULL for no columns (sequences without tokens); starts int32 [B+1], ascending (below 0: a sequence's first
  * tokens are left out); Y [rows][heads][dim] of y_type with the given strides in elements, one of them (tokens' or heads')
  * at least as long as all vectors of the other, so that no two vectors overlap.  Rows before starts[0] and from starts[B] on are
  * left as they are.  pages2 / Y2: the second cache, by the same launch; NULL: none.  Y2 does not overlap Y (which is refused where

@@ -403,7 +403,7 @@ extern "C" ocs_status ocs_cache_read(const ocs_cache* c, const void* pages, cons
   if (!c || !valid_dtype(y_type) || c->grid < OCS_GRID_I8 || c->grid > OCS_GRID_E4M3) return OCS_ERR_INVALID_ARG;
   if (!valid_geometry(c) || rows < 0 || B < 0 || table_cols < 0) return OCS_ERR_SHAPE;
   if (rows == 0 || B == 0) return OCS_OK;
-  if (!pages || !table || !starts || !Y || (!pages2) != (!Y2)) return OCS_ERR_INVALID_ARG;
+  if (!pages || (!table && table_cols) || !starts || !Y || (!pages2) != (!Y2)) return OCS_ERR_INVALID_ARG;   // (a table of no columns has no address)
   CacheArgs a{};
   ocs_status st = fill(a, c, const_cast<void*>(pages), const_cast<void*>(pages2), rows, Y, ld_token, ld_head, Y2, ld_token2, ld_head2, y_type);
   if (st != OCS_OK) return st;
