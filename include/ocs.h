@@ -9,6 +9,7 @@
  *    minimum size the matching *_workspace_bytes() query returns (host call, no GPU work).
  *    ws must be 256-byte aligned.  Inputs are never modified and outputs must not alias inputs,
  *    unless an entry says otherwise (ocs_dup_weight_columns and ocs_add_relu work in place).
+ *  - Kernels are launched on the current device, whose memory every pointer of the call is and whose stream `stream` is.
  *  - Every call only enqueues work on `stream` (a cudaStream_t passed as void*) and returns
  *    without synchronising.  Scalar results (scales, thresholds, maxima) are written to
  *    device memory.

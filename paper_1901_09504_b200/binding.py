@@ -614,7 +614,10 @@ def _addr(t):
 
 
 def _raw_stream(t):
-    return torch._C._cuda_getCurrentRawStream(t.get_device())
+    """The current stream of t's device, which has to be the current device: kernels are launched there."""
+    d = t.get_device()
+    assert d == torch._C._cuda_getDevice()
+    return torch._C._cuda_getCurrentRawStream(d)
 
 
 def _rows_of(t):

@@ -49,3 +49,36 @@ def test_rows_that_are_dense_are_taken():
     assert check(rows_of_codes(u8(1, 1), K=2)) == (1, 16)
     assert check(rows_of_codes(u8(8, 1).t()[:, :1], K=2)) == (1, 16)        # one byte: its stride says nothing
     assert check(rows_of_codes(u8(0, 64)))[0] == 0
+
+
+class Elsewhere(OnDevice):
+    def get_device(self):
+        return 1
+
+
+def test_tensors_of_a_device_that_is_not_the_current_one(monkeypatch):
+    """Their stream would be another device's: refused before the library is called."""
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda d: 0)
+
+    class Library:
+        def __getattr__(self, name):
+            if name.endswith("_bytes"):
+                return getattr(real, name)
+
+            def called(*_):
+                raise RuntimeError(f"{name} was called")
+            return called
+    real = ocs.lib()
+    monkeypatch.setattr(binding, "_lib", Library())
+    there = lambda *shape: torch.zeros(shape).as_subclass(Elsewhere)  # noqa: E731
+    bytes_there = lambda *shape: torch.zeros(shape, dtype=torch.uint8).as_subclass(Elsewhere)  # noqa: E731
+    q = ocs.Mx4(bytes_there(4, 64), bytes_there(4096), there(4), 128, ocs.MX4_E4M3)
+    cache = ocs.QuantCache(bytes_there(2, real.ocs_cache_page_bytes(binding.C.byref(binding._CacheDesc(0, 4, 2, 32, 0)))), 4, 2, 32, 0)
+    ints = lambda dtype, *shape: torch.zeros(shape, dtype=dtype).as_subclass(Elsewhere)  # noqa: E731
+    for call in (lambda: ocs.ocs_dequantize_mx4(q, out=there(4, 128)), lambda: ocs.ocs_qlinear_mx4(q, q, out=there(4, 4)),
+                 lambda: ocs.ocs_linear_mx4(there(4, 128), q, out=there(4, 4)), lambda: ocs.ocs_quantize_mx4(there(4, 128), out=q),
+                 lambda: ocs.ocs_cache_write(cache, there(3, 2, 32), ints(torch.int64, 3)),
+                 lambda: ocs.ocs_cache_read(cache, ints(torch.int32, 1, 2), ints(torch.int32, 2), 3, out=there(3, 2, 32))):
+        with pytest.raises(AssertionError):
+            call()
