@@ -113,7 +113,7 @@ __global__ void __launch_bounds__(kRowThreads, NV * Block<T, Piece<T, GRID>::N>:
     const int j = lo + tx + i * G;
     if (j >= hi || !live) v[i].clear();
     else if (whole_piece<N, ALIGN>(p, r, j)) v[i].template load<ALIGN>(x + j * N);
-    else if (!staged || j < t0) v[i].gather(x, j * N, p.C, p.K, p.idx_map, p.dev_status);
+    else if (!staged || j < t0) v[i].template gather<(N > 16 ? 8 : N)>(x, j * N, p.C, p.K, p.idx_map, p.dev_status);
   }
   if (staged) {
     if (live) stage_tail<T, N>(p, x, t0 * N, tail, my_tail, tx, G);

@@ -192,9 +192,11 @@ struct Block {
     }
   }
   // Elements c, c + 1, ... of the expanded row: the row's C own, then its duplicated channels up to K, then zeros.  All
-  // indices are asked for before the first value, and all values before the first is used.
+  // indices of R elements are asked for before the first value, and all values before the first is used.  (Row quantization with its
+  // 40 registers a thread: 16 of 32 elements at a time spill 112 to 128 bytes, 8 of them 16 to 20: 2047 x 4096 with 82 duplicated
+  // channels, bf16 E8M0, 6.1 and 5.7 us.  The cache's writing is 4 to 8 % slower on int8 with 8.)
+  template <int R = (N < 16 ? N : 16)>
   __device__ __forceinline__ void gather(const T* x, int c, int C, int K, const int32_t* idx_map, int* dev_status) {
-    constexpr int R = N < 16 ? N : 16;
 #pragma unroll
     for (int h = 0; h < N; h += R) {
       int src[R];
