@@ -88,8 +88,9 @@ constexpr int kRowThreads = 512;
 constexpr int kRowPieces = 4;       // most pieces per thread
 
 // What bounds it: instructions beside HBM.  8192 x 8192 bf16 (134 MB in, 38 out, floor 26 us): E4M3 34 us, issue slots two
-// thirds full at 12 instructions an element, E8M0 28 us; 333 x 5000 with 50 duplicated channels 3.1 us.  Rows that start anywhere pay
-// for 48 bytes read where they need 32: 4085 x 7279 bf16 E4M3 25 us (4085 x 7296: 19).
+// thirds full at 12 instructions an element, E8M0 28 us; 333 x 5000 with 50 duplicated channels 3.1 us.  Rows that start anywhere
+// read 48 bytes where they need 32 and shift them: 4085 x 7279 bf16 E4M3 23.0 us, E8M0 18.8 (4085 x 7296: 17.3 and 13.5, floor 11.6
+// and 11.5).  40 registers a thread hold all but 4 to 28 bytes (spilled) of the 16-bit forms.
 // G = blockDim.x threads (a power of two below 32, or whole warps) and NV pieces each for one row, or (E8M0, whose blocks need
 // nothing of their row) a part of one: blockIdx.y.  blockDim.y rows per CTA.  E4M3: a row's scale is that of its largest
 // magnitude, so the row waits in registers for it.
@@ -256,7 +257,8 @@ __global__ void __launch_bounds__(kStagedThreads, 1) mx4_staged_rows_kernel(cons
   __syncthreads();
 }
 
-// E4M3, other rows that no CTA's registers hold: read twice, the second time from L2.
+// E4M3, other rows that no CTA's registers hold: read twice, the second time from L2 (2377 x 33001 fp32: 117 us, floor 55;
+// at most 84 bytes a thread are spilled in 16 bits).
 template <typename T, int ALIGN>
 __global__ void __launch_bounds__(kRowThreads, 3) mx4_long_rows_kernel(const T* __restrict__ X, const MxRows p) {
   constexpr int GRID = OCS_GRID_E4M3, N = Piece<T, GRID>::N;
