@@ -492,6 +492,7 @@ ocs_status ocs_selftest_force_row_plan(int tn, int cg, int slices);
  *       r = 2^k (fp32), k the smallest in [-117, 117] with max|x| of the row <= 6 * 448 * r
  *   code = e2m1(x / (s r)), r = 1 for E8M0; the division of each block's max|x| / r by 6 and, for fp32 x, the quotients are
  *   rounded to fp32 once, all else in between is exact; e2m1() and e4m3() round to the nearest, ties to even, and saturate.
+ *   Codes of zero keep x's sign; a block whose scale rounds to zero has no others.
  * (OCS_GRID_I8 is ocs_quantize_rows' signed 8-bit grid: int8 codes and one fp32 step; for the cache below.) */
 typedef enum {
   OCS_GRID_I8 = 0,
